@@ -500,6 +500,151 @@ CAP_API int kv_fp8_quantize(const kv_fp8_seg* segs, uint32_t n_seg, void* stream
  * restore). */
 CAP_API int kv_fp8_dequantize(const kv_fp8_seg* segs, uint32_t n_seg, void* stream);
 
+/* ----------------------------------- block-scaled FP8 KV cache (kvb) ---- */
+/* Full-attention K and V held in E4M3 (the format above) and read in that form:
+ * no bf16 stage, no scale chosen ahead.  A cache is one layer's K and V of one
+ * sequence, cut into blocks of KVB_BLOCK = 64 rows, the chunk of the scans: an
+ * aligned boundary P' is a whole number of blocks.  For each block and KV head,
+ * K and V apart, over the block's rows held (finite values):
+ *   scale  = 2^e, e the smallest integer in [-100, 119] with max |x| <= 448 * 2^e
+ *   code   = E4M3 value nearest to x / scale, ties to even; beyond +-448 and
+ *            +-inf saturate, NaN gives a NaN code
+ *   bounds = lowest and highest code of each channel (K only; a channel that
+ *            holds a NaN has NaN for both)
+ * A power of two costs E4M3 no precision, and code * scale is exact in bf16.
+ * While the last block is not full, its rows are also kept in bf16 ("open"), and
+ * an append encodes the whole block again: the block's bytes are a function of
+ * its rows alone, not of the calls that brought them.
+ *
+ * Buffers of a sequence (device, caller-owned; `rows` a multiple of 64):
+ *   k, v   [rows, kv_heads, d] codes       rows at or beyond n are never written
+ *                                          and what they hold does not matter
+ *   scales [rows / 64, 2, kv_heads] fp32   (K, V); 4-byte aligned
+ *   bounds [rows / 64, 2, kv_heads, d]     codes (lowest, highest), or NULL where
+ *                                          no block is ever selected
+ *   open   [2, 64, kv_heads, d] bf16       (K, V): the rows from 64 * (n / 64) on
+ * All but scales are 16-byte aligned.  In a live set k and v are positional
+ * buffers (row_bytes kv_heads * d), scales a fixed one, bounds a fixed one or,
+ * where kv_heads * d is a multiple of 512, positional with row_bytes
+ * kv_heads * d / 32; `open` belongs to it only where P' is not a multiple of 64.
+ *
+ * One step covers n_seq sequences (at most KVB_MAX_SEQ), each with T new tokens
+ * at positions [n - T, n): n counts the rows held with the new ones, for every
+ * call of the step alike (append first, then select and attend).  Going back to
+ * an earlier n needs the open rows of that n; at a multiple of 64 there are none.
+ * Tokens are packed: sequence 0's T tokens, then sequence 1's, and so on;
+ * strides are in elements between tokens (0: contiguous), multiples of 8.
+ * Sequences with T = 0 are passed over.
+ *
+ * Supported: d in {64, 128, 256}, heads a multiple of kv_heads, bf16 tokens,
+ * rows <= 2^31, 64 * kv_heads * d < 2^31, tokens * heads < 2^31.
+ * Errors: CAP_E_INVAL (null required pointer, counts below their range, T > n,
+ * rows not a multiple of 64, heads not a multiple of kv_heads, an output that
+ * overlaps an input or another output), CAP_E_SIZE (n > rows, workspace too
+ * small), CAP_E_UNSUPPORTED (shape or dtype outside the list, n_seq >
+ * KVB_MAX_SEQ), CAP_E_ALIGN.  A call reads the sequence table before it returns,
+ * and its kernel arguments carry every address, length and position: it can be
+ * recorded in a stream capture and replayed for the same n. */
+#define KVB_BLOCK   64
+#define KVB_MAX_SEQ 64
+
+typedef struct kvb_seq {
+    void*   k;
+    void*   v;
+    float*  scales;
+    void*   bounds;
+    void*   open;
+    int64_t rows;
+    int64_t n;
+    int64_t T;
+} kvb_seq;
+
+/* Append: rows [n - T, n) of each sequence from k, v [sum of T, kv_heads, d] bf16.
+ * One launch.  The caches of one call are disjoint from each other. */
+typedef struct kvb_append_args {
+    const kvb_seq* seqs;       /* HOST array of n_seq */
+    const void*    k;
+    const void*    v;
+    int64_t        k_stride;
+    int64_t        v_stride;
+    int32_t        n_seq;
+    int32_t        kv_heads;
+    int32_t        d;
+    int32_t        in_dtype;   /* CAP_DTYPE_BF16 */
+} kvb_append_args;
+
+CAP_API int kvb_append(const kvb_append_args* args, void* stream);
+
+/* Causal attention of the step's tokens: the token at position t sees rows
+ * [0, t]; query head i belongs to KV head i / (heads / kv_heads).
+ *   q   : [sum of T, heads, d] bf16 (stride q_stride)
+ *   o   : [sum of T, heads, d] bf16, contiguous = softmax(scale * q K^T) V
+ *   lse : [sum of T, heads] fp32 or NULL: log of the sum of exp(scale * q . k)
+ *   idx : NULL, or [sum of T, kv_heads, n_sel] int32 block numbers (device):
+ *         the token sees, of rows [0, t], those of the listed blocks only.  An
+ *         entry below 0 or of a block beyond t's is passed over; a block that is
+ *         listed twice counts twice.
+ * A row that sees nothing has o = 0 and lse = -inf.  Rows that a token does not
+ * see have no part in its result, NaN codes included.  The softmax is held in
+ * fp32; scores take the query rows in full, weights enter the second product as
+ * bf16.  One launch, or two where a sequence is cut along its rows (the parts
+ * lie in the workspace).  Results are reproducible for the same arguments. */
+typedef struct kvb_attend_args {
+    const kvb_seq* seqs;       /* HOST array of n_seq (bounds, open: not read) */
+    const void*    q;
+    void*          o;
+    float*         lse;
+    const int32_t* idx;
+    void*          workspace;  /* kvb_attend_workspace_bytes(args), 16-byte aligned */
+    uint64_t       workspace_bytes;
+    int64_t        q_stride;
+    int32_t        n_seq;
+    int32_t        heads;
+    int32_t        kv_heads;
+    int32_t        d;
+    int32_t        n_sel;      /* entries of a list; 0 when idx is NULL */
+    int32_t        in_dtype;   /* CAP_DTYPE_BF16 */
+    float          scale;      /* finite */
+    int32_t        reserved;   /* 0 */
+} kvb_attend_args;
+
+/* Workspace of a call with these sizes (seqs' n and T, n_seq, heads, kv_heads, d,
+ * and idx NULL or not with n_sel); 0 where the call needs none or is refused. */
+CAP_API uint64_t kvb_attend_workspace_bytes(const kvb_attend_args* args);
+CAP_API int kvb_attend(const kvb_attend_args* args, void* stream);
+
+/* Block selection for kvb_attend: for each token and KV head n_sel blocks of
+ * those up to the token's own, ascending, then -1:
+ *   the first `first` blocks; the token's own block and those before it, `last`
+ *   in all; then those of highest score
+ *     scale_k * max over the group's queries q of sum_c max(q_c lo_c, q_c hi_c),
+ *   which no q . k of a key in the block exceeds; ties go to the lower block.
+ * Scores are computed in 64 bits; one that is NaN counts as infinite.
+ *   q   : as for kvb_attend
+ *   idx : [sum of T, kv_heads, n_sel] int32 (written whole)
+ * 0 <= first, 1 <= last, first + last <= n_sel (CAP_E_INVAL).  Two launches. */
+typedef struct kvb_select_args {
+    const kvb_seq* seqs;       /* HOST array of n_seq (k, v, open: not read) */
+    const void*    q;
+    int32_t*       idx;
+    void*          workspace;  /* kvb_select_workspace_bytes(args), 16-byte aligned */
+    uint64_t       workspace_bytes;
+    int64_t        q_stride;
+    int32_t        n_seq;
+    int32_t        heads;
+    int32_t        kv_heads;
+    int32_t        d;
+    int32_t        n_sel;
+    int32_t        first;
+    int32_t        last;
+    int32_t        in_dtype;   /* CAP_DTYPE_BF16 */
+} kvb_select_args;
+
+/* Workspace of a call with these sizes: 8 bytes for each token, KV head and
+ * block of its sequence, rounded up to 16; 0 where the call is refused. */
+CAP_API uint64_t kvb_select_workspace_bytes(const kvb_select_args* args);
+CAP_API int kvb_select(const kvb_select_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,6 +14,8 @@ from ._native import (  # noqa: F401
     capsule_digest_tokens, capsule_fork, capsule_gather_restore, capsule_info, capsule_layout_bytes,
     capsule_move, capsule_release, capsule_restore, capsule_snapshot, capsule_tier, gdn_chunked_prefill,
     gdn_chunked_prefill_noalloc, GDN_NOALLOC_SCRATCH_BYTES,
+    KVB_BLOCK, KVB_MAX_SEQ, kvb_append, kvb_append_args, kvb_attend, kvb_attend_args, kvb_select, kvb_select_args,
+    kvb_seqs,
     gdn_decode_step, gdn_workspace_bytes, kv_fp8_dequantize, kv_fp8_quantize, linattn_chunked_prefill,
     linattn_decode_step, load,
 )

@@ -67,6 +67,36 @@ class kv_fp8_seg(ct.Structure):
                 ("reserved", ct.c_uint32)]
 
 
+KVB_BLOCK = 64
+KVB_MAX_SEQ = 64
+
+
+class kvb_seq(ct.Structure):
+    _fields_ = [("k", ct.c_void_p), ("v", ct.c_void_p), ("scales", ct.c_void_p), ("bounds", ct.c_void_p),
+                ("open", ct.c_void_p), ("rows", ct.c_int64), ("n", ct.c_int64), ("T", ct.c_int64)]
+
+
+class kvb_append_args(ct.Structure):
+    _fields_ = [("seqs", ct.c_void_p), ("k", ct.c_void_p), ("v", ct.c_void_p), ("k_stride", ct.c_int64),
+                ("v_stride", ct.c_int64), ("n_seq", ct.c_int32), ("kv_heads", ct.c_int32), ("d", ct.c_int32),
+                ("in_dtype", ct.c_int32)]
+
+
+class kvb_attend_args(ct.Structure):
+    _fields_ = [("seqs", ct.c_void_p), ("q", ct.c_void_p), ("o", ct.c_void_p), ("lse", ct.c_void_p),
+                ("idx", ct.c_void_p), ("workspace", ct.c_void_p), ("workspace_bytes", ct.c_uint64),
+                ("q_stride", ct.c_int64), ("n_seq", ct.c_int32), ("heads", ct.c_int32), ("kv_heads", ct.c_int32),
+                ("d", ct.c_int32), ("n_sel", ct.c_int32), ("in_dtype", ct.c_int32), ("scale", ct.c_float),
+                ("reserved", ct.c_int32)]
+
+
+class kvb_select_args(ct.Structure):
+    _fields_ = [("seqs", ct.c_void_p), ("q", ct.c_void_p), ("idx", ct.c_void_p), ("workspace", ct.c_void_p),
+                ("workspace_bytes", ct.c_uint64), ("q_stride", ct.c_int64), ("n_seq", ct.c_int32),
+                ("heads", ct.c_int32), ("kv_heads", ct.c_int32), ("d", ct.c_int32), ("n_sel", ct.c_int32),
+                ("first", ct.c_int32), ("last", ct.c_int32), ("in_dtype", ct.c_int32)]
+
+
 # (name, restype, argtypes) of every exported entry point
 _vp, _u64, _u32, _i32 = ct.c_void_p, ct.c_uint64, ct.c_uint32, ct.c_int32
 SIGNATURES = [
@@ -102,6 +132,11 @@ SIGNATURES = [
     ("gdn_chunked_prefill", ct.c_int, [ct.POINTER(gdn_args), _vp]),
     ("gdn_decode_step", ct.c_int, [ct.POINTER(gdn_args), _vp]),
     ("gdn_chunked_prefill_noalloc", ct.c_int, [ct.POINTER(gdn_args), _vp]),
+    ("kvb_append", ct.c_int, [ct.POINTER(kvb_append_args), _vp]),
+    ("kvb_attend_workspace_bytes", _u64, [ct.POINTER(kvb_attend_args)]),
+    ("kvb_attend", ct.c_int, [ct.POINTER(kvb_attend_args), _vp]),
+    ("kvb_select_workspace_bytes", _u64, [ct.POINTER(kvb_select_args)]),
+    ("kvb_select", ct.c_int, [ct.POINTER(kvb_select_args), _vp]),
 ]
 
 _lib = None
@@ -479,3 +514,97 @@ def kv_fp8_dequantize(segs, stream=None):
     """OCP E4M3 -> bf16 for each (src, dst, n, scale) segment, one launch."""
     arr, n = _fp8_segs(segs)
     return _check("kv_fp8_dequantize", load().kv_fp8_dequantize(arr, n, _stream(stream)))
+
+
+# ------------------------------------------- block-scaled FP8 KV cache ----
+def kvb_seqs(caches):
+    """The sequence table of a step: an int64 array [n_seq, 8], one kvb_seq a row.
+
+    caches: iterable of (k, v, scales, bounds, open, rows, n, T); the first five
+    are tensors, addresses or None.  A program may keep the table and advance the
+    last two columns (n, T) itself; it does not keep the tensors alive."""
+    import numpy as np
+    return np.array([[_addr(x) for x in c[:5]] + [int(x) for x in c[5:]] for c in caches],
+                    dtype=np.int64).reshape(-1, 8)
+
+
+def _kvb_table(fn, seqs):
+    """(address, length) of a sequence table."""
+    a = seqs.__array_interface__
+    if seqs.ndim != 2 or seqs.shape[1] != 8 or a["typestr"] != "<i8" or a["strides"] is not None:
+        raise ValueError("%s: the sequence table is a contiguous int64 array [n_seq, 8]" % fn)
+    return a["data"][0], seqs.shape[0]
+
+
+def _kvb_tokens(fn, name, x, tokens=None):
+    """(elements between tokens, dtype) of a packed tensor [tokens, heads, d]."""
+    import torch
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("%s: %s has dtype %s" % (fn, name, x.dtype))
+    if x.dim() != 3 or (x.numel() and (x.stride(2) != 1 or x.stride(1) != x.shape[2])):
+        raise ValueError("%s: %s is [tokens, heads, d] with contiguous heads" % (fn, name))
+    if tokens is not None and x.shape[0] != tokens:
+        raise ValueError("%s: %s holds %d tokens, the step has %d" % (fn, name, x.shape[0], tokens))
+    return (x.stride(0) if x.shape[0] > 1 else 0), CAP_DTYPE_F32 if x.dtype == torch.float32 else CAP_DTYPE_BF16
+
+
+def _kvb_out(fn, name, x, shape, dtype):
+    """Check a contiguous tensor of a call (None and addresses pass)."""
+    if hasattr(x, "data_ptr") and (tuple(x.shape) != shape or x.dtype != dtype or not x.is_contiguous()):
+        raise ValueError("%s: %s is a contiguous %s of shape %s" % (fn, name, dtype, list(shape)))
+
+
+def _kvb_workspace(workspace, need, like):
+    if workspace is None and need > 0:
+        import torch
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+    return workspace, workspace.numel() * workspace.element_size() if hasattr(workspace, "numel") else need
+
+
+def kvb_append(seqs, k, v, *, stream=None):
+    """Append rows [n - T, n) of each sequence of the table from k, v [sum of T, kv_heads, d]."""
+    at, n_seq = _kvb_table("kvb_append", seqs)
+    tokens = int(seqs[:, 7].sum())
+    ks, dt = _kvb_tokens("kvb_append", "k", k, tokens)
+    vs, dv = _kvb_tokens("kvb_append", "v", v, tokens)
+    if v.shape != k.shape or dv != dt:
+        raise ValueError("kvb_append: k and v have the same shape and dtype")
+    a = kvb_append_args(at, _addr(k), _addr(v), ks, vs, n_seq, k.shape[1], k.shape[2], dt)
+    return _check("kvb_append", load().kvb_append(ct.byref(a), _stream(stream)))
+
+
+def kvb_attend(seqs, q, o, *, kv_heads, scale, lse=None, idx=None, workspace=None, stream=None):
+    """Causal attention of the step's tokens q [sum of T, heads, d] over the caches, whole or (idx
+    [sum of T, kv_heads, n_sel]) the listed blocks.  With no workspace given, one is allocated as a
+    torch tensor for the duration of the call."""
+    import torch
+    at, n_seq = _kvb_table("kvb_attend", seqs)
+    qs, dt = _kvb_tokens("kvb_attend", "q", q, int(seqs[:, 7].sum()))
+    tokens, heads, d = q.shape
+    _kvb_out("kvb_attend", "o", o, (tokens, heads, d), torch.bfloat16)
+    _kvb_out("kvb_attend", "lse", lse, (tokens, heads), torch.float32)
+    n_sel = 0
+    if idx is not None:
+        n_sel = idx.shape[-1]
+        _kvb_out("kvb_attend", "idx", idx, (tokens, kv_heads, n_sel), torch.int32)
+    a = kvb_attend_args(at, _addr(q), _addr(o), _addr(lse), _addr(idx), 0, 0, qs, n_seq, heads, int(kv_heads), d, n_sel,
+                        dt, float(scale), 0)
+    workspace, a.workspace_bytes = _kvb_workspace(
+        workspace, load().kvb_attend_workspace_bytes(ct.byref(a)) if workspace is None else 0, q)
+    a.workspace = _addr(workspace)
+    return _check("kvb_attend", load().kvb_attend(ct.byref(a), _stream(stream)))
+
+
+def kvb_select(seqs, q, idx, *, kv_heads, first=1, last=2, workspace=None, stream=None):
+    """For each token and KV head the idx.shape[-1] blocks that kvb_attend is to read."""
+    import torch
+    at, n_seq = _kvb_table("kvb_select", seqs)
+    qs, dt = _kvb_tokens("kvb_select", "q", q, int(seqs[:, 7].sum()))
+    tokens, heads, d = q.shape
+    _kvb_out("kvb_select", "idx", idx, (tokens, kv_heads, idx.shape[-1]), torch.int32)
+    a = kvb_select_args(at, _addr(q), _addr(idx), 0, 0, qs, n_seq, heads, int(kv_heads), d, idx.shape[-1], int(first),
+                        int(last), dt)
+    workspace, a.workspace_bytes = _kvb_workspace(
+        workspace, load().kvb_select_workspace_bytes(ct.byref(a)) if workspace is None else 0, q)
+    a.workspace = _addr(workspace)
+    return _check("kvb_select", load().kvb_select(ct.byref(a), _stream(stream)))

@@ -1,0 +1,84 @@
+// Internal interface of the block-scaled FP8 KV cache: the host checks and
+// launch plans (kvb_host.cpp) and the kernels (kvb_append.hip, kvb_attend.hip,
+// kvb_select.hip).  Not part of the public ABI.
+#pragma once
+
+#include "internal.h"
+
+namespace cap {
+
+constexpr int kKvbBlock = KVB_BLOCK;
+
+// ---- append ----
+// Workgroup w works on sequence s with first_wg <= w < the next one's, on its
+// block, KV head and side (K or V) number w - first_wg.
+struct KvbAppendSeq {
+    uint64_t k, v, scales, bounds, open;
+    int64_t  n, t0;       // rows held with the new ones; first of the packed tokens
+    int32_t  T;
+    uint32_t first_wg;
+};
+struct KvbAppendParams {
+    const void* k_new;
+    const void* v_new;
+    int64_t  k_stride, v_stride;  // bytes between tokens
+    int32_t  n_seq, kv_heads, d;
+    uint32_t wgs;
+    KvbAppendSeq seq[KVB_MAX_SEQ];
+};
+hipError_t launch_kvb_append(const KvbAppendParams& p, hipStream_t stream);
+
+// ---- attend ----
+// The query rows that share a KV head's K and V are taken in tiles of
+// `tile` rows: row r of a sequence and KV head is token r / G, query head
+// h G + r % G (G = heads / kv_heads); with a block list (sparse) the rows of
+// one token.  The blocks of a tile are cut into nsplit runs of `per` blocks,
+// each a workgroup; with more than one the runs leave (o, m, l) in slots of
+// the workspace and a second launch joins them.
+struct KvbAttendSeq {
+    uint64_t k, v, scales;
+    int64_t  n, t0;
+    int32_t  T;
+    uint32_t first_wg, first_slot;
+    int32_t  per, nsplit;
+    int32_t  pad;
+};
+struct KvbAttendParams {
+    const void*    q;
+    void*          o;
+    float*         lse;        // may be null
+    const int32_t* idx;        // null: every block
+    float*         part_o;     // [slot][tile][d], not divided by l
+    float*         part_ml;    // [slot][tile][2]: highest score (log2 units), sum
+    int64_t        q_stride;   // bytes between tokens
+    int64_t        tokens;
+    int32_t        n_seq, heads, kv_heads, d, n_sel, tile;
+    uint32_t       wgs, slots;
+    float          scale_log2; // scale * log2(e)
+    KvbAttendSeq   seq[KVB_MAX_SEQ];
+};
+
+hipError_t launch_kvb_attend(const KvbAttendParams& p, hipStream_t stream);
+
+// ---- select ----
+struct KvbSelectSeq {
+    uint64_t scales, bounds;
+    int64_t  n, t0;
+    int32_t  T;
+    uint32_t first_wg;
+    uint64_t keys;             // first sort key of the sequence in the workspace
+};
+struct KvbSelectParams {
+    const void* q;
+    int32_t*    idx;
+    uint64_t*   keys;          // [token][kv head][blocks of the sequence]
+    int64_t     q_stride, tokens;
+    int32_t     n_seq, heads, kv_heads, d, n_sel, first, last;
+    uint32_t    wgs;
+    KvbSelectSeq seq[KVB_MAX_SEQ];
+};
+// Blocks that one workgroup of the scoring launch takes.
+constexpr int kKvbScoreBlocks = 32;
+hipError_t launch_kvb_select(const KvbSelectParams& p, hipStream_t stream);
+
+}  // namespace cap

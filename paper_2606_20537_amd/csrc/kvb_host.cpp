@@ -1,0 +1,319 @@
+// Host side of the block-scaled FP8 KV cache: argument checks and launch plans
+// of kvb_append, kvb_attend and kvb_select.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "kvb.h"
+
+namespace {
+
+using cap::kKvbBlock;
+
+struct Range { uint64_t a, b; };
+
+uint64_t addr(const void* p) { return (uint64_t)(uintptr_t)p; }
+Range range(const void* p, uint64_t bytes) { return {addr(p), addr(p) + (p ? bytes : 0)}; }
+bool meet(const Range& x, const Range& y) { return x.a < y.b && y.a < x.b; }
+uint64_t up(uint64_t x, uint64_t m) { return (x + m - 1) / m * m; }
+
+// The sizes that every call shares; `tokens` receives the sum of T.
+int check_sizes(const kvb_seq* seqs, int32_t n_seq, int32_t heads, int32_t kv_heads, int32_t d, int32_t in_dtype,
+                int64_t* tokens) {
+    if (n_seq < 0 || (n_seq > 0 && !seqs) || heads < 1 || kv_heads < 1 || d < 1) return CAP_E_INVAL;
+    if (in_dtype != CAP_DTYPE_BF16 && in_dtype != CAP_DTYPE_F32) return CAP_E_INVAL;
+    if (heads % kv_heads != 0) return CAP_E_INVAL;
+    if (n_seq > KVB_MAX_SEQ || in_dtype != CAP_DTYPE_BF16 || (d != 64 && d != 128 && d != 256)) return CAP_E_UNSUPPORTED;
+    // 32-bit offsets inside a block, and grids
+    if ((int64_t)kKvbBlock * kv_heads * d > 0x7fffffff || (int64_t)heads * d > 0x7fffffff) return CAP_E_UNSUPPORTED;
+    *tokens = 0;
+    for (int32_t i = 0; i < n_seq; ++i) {
+        const kvb_seq& s = seqs[i];
+        if (s.rows < 0 || s.rows % kKvbBlock != 0 || s.n < 0 || s.T < 0 || s.T > s.n) return CAP_E_INVAL;
+        if (s.rows > (int64_t)1 << 31) return CAP_E_UNSUPPORTED;
+        if (s.n > s.rows) return CAP_E_SIZE;
+        *tokens += s.T;
+    }
+    if (*tokens > 0x7fffffff / heads) return CAP_E_UNSUPPORTED;
+    return CAP_OK;
+}
+
+// Elements between tokens of a packed tensor (0: contiguous) as bytes.
+int check_stride(int64_t stride, int64_t width, int64_t* bytes) {
+    if (stride == 0) stride = width;
+    if (stride < width) return CAP_E_INVAL;
+    if (stride > (int64_t)1 << 30) return CAP_E_UNSUPPORTED;
+    if (stride % 8 != 0) return CAP_E_ALIGN;
+    *bytes = stride * 2;
+    return CAP_OK;
+}
+
+uint64_t span(int64_t tokens, int64_t stride_bytes, int64_t width) {
+    return tokens == 0 ? 0 : (uint64_t)((tokens - 1) * stride_bytes + width * 2);
+}
+
+enum { K, V, SCALES, BOUNDS, OPEN, PARTS };
+
+Range part(const kvb_seq& s, int which, int64_t row) {
+    const int64_t nb = s.rows / kKvbBlock;
+    switch (which) {
+        case K: return range(s.k, (uint64_t)(s.rows * row));
+        case V: return range(s.v, (uint64_t)(s.rows * row));
+        case SCALES: return range(s.scales, (uint64_t)(nb * 8) * (uint64_t)row);  // row: kv_heads
+        case BOUNDS: return range(s.bounds, (uint64_t)(nb * 2 * row));
+        default: return range(s.open, (uint64_t)(4 * kKvbBlock * row));
+    }
+}
+Range part(const kvb_seq& s, int which, int32_t kv_heads, int32_t d) {
+    return part(s, which, which == SCALES ? kv_heads : (int64_t)kv_heads * d);
+}
+
+// Pointers of the parts of a sequence that a call uses (bit i of `need`: part i
+// must be there; NULL bounds are allowed where they are not needed).
+int check_parts(const kvb_seq& s, unsigned need) {
+    const void* const ptr[PARTS] = {s.k, s.v, s.scales, s.bounds, s.open};
+    for (int i = 0; i < PARTS; ++i)
+        if ((need >> i & 1) && !ptr[i]) return CAP_E_INVAL;
+    return CAP_OK;
+}
+int check_align(const kvb_seq& s) {
+    return ((addr(s.k) | addr(s.v) | addr(s.bounds) | addr(s.open)) & 15) || (addr(s.scales) & 3) ? CAP_E_ALIGN : CAP_OK;
+}
+
+// Whether an output meets one of the parts `used` of a sequence.
+bool meets_cache(const Range& out, const kvb_seq& s, unsigned used, int32_t kv_heads, int32_t d) {
+    for (int i = 0; i < PARTS; ++i)
+        if ((used >> i & 1) && meet(out, part(s, i, kv_heads, d))) return true;
+    return false;
+}
+
+constexpr unsigned bit(int i) { return 1u << i; }
+
+// ---- attend: the launch plan ----
+// Workgroups wanted: two to a CU.
+constexpr int64_t kWantWgs = 512;
+// Blocks that a run of a cut sequence has at least.
+constexpr int64_t kLeastBlocks = 2;
+
+int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams* p) {
+    int64_t tokens = 0;
+    const int rc = check_sizes(a->seqs, a->n_seq, a->heads, a->kv_heads, a->d, a->in_dtype, &tokens);
+    if (rc != CAP_OK) return rc;
+    if (a->idx ? a->n_sel < 1 : a->n_sel != 0) return CAP_E_INVAL;
+    const int64_t G = a->heads / a->kv_heads;
+    p->heads = a->heads;
+    p->kv_heads = a->kv_heads;
+    p->d = a->d;
+    p->n_sel = a->n_sel;
+    p->tokens = tokens;
+    p->tile = 16;
+    auto items = [&](const kvb_seq& s) {
+        return (a->idx ? s.T * ((G + 15) / 16) : (s.T * G + 15) / 16) * a->kv_heads;
+    };
+    auto blocks = [&](const kvb_seq& s) { return a->idx ? (int64_t)a->n_sel : (s.n + kKvbBlock - 1) / kKvbBlock; };
+    int64_t total = 0;
+    for (int32_t i = 0; i < a->n_seq; ++i) total += items(a->seqs[i]) * blocks(a->seqs[i]);
+    const int64_t per = std::max(kLeastBlocks, (total + kWantWgs - 1) / kWantWgs);
+    int64_t wgs = 0, slots = 0, t0 = 0;
+    int32_t n = 0;
+    for (int32_t i = 0; i < a->n_seq; ++i) {
+        const kvb_seq& s = a->seqs[i];
+        if (s.T == 0) continue;
+        cap::KvbAttendSeq& x = p->seq[n++];
+        x.k = addr(s.k);
+        x.v = addr(s.v);
+        x.scales = addr(s.scales);
+        x.n = s.n;
+        x.t0 = t0;
+        x.T = (int32_t)s.T;
+        x.per = (int32_t)std::min(per, blocks(s));
+        x.nsplit = (int32_t)((blocks(s) + x.per - 1) / x.per);
+        x.first_wg = (uint32_t)wgs;
+        x.first_slot = (uint32_t)slots;
+        wgs += items(s) * x.nsplit;
+        if (x.nsplit > 1) slots += items(s) * x.nsplit;
+        if (wgs > 0x7fffffff) return CAP_E_UNSUPPORTED;
+        t0 += s.T;
+    }
+    p->n_seq = n;
+    p->wgs = (uint32_t)wgs;
+    p->slots = (uint32_t)slots;
+    return CAP_OK;
+}
+
+uint64_t attend_workspace(const cap::KvbAttendParams& p) {
+    return (uint64_t)p.slots * (uint64_t)p.tile * ((uint64_t)p.d + 2) * 4;
+}
+
+// ---- select: the launch plan ----
+int plan_select(const kvb_select_args* a, cap::KvbSelectParams* p, uint64_t* bytes) {
+    int64_t tokens = 0;
+    const int rc = check_sizes(a->seqs, a->n_seq, a->heads, a->kv_heads, a->d, a->in_dtype, &tokens);
+    if (rc != CAP_OK) return rc;
+    if (a->first < 0 || a->last < 1 || a->n_sel < 1 || (int64_t)a->first + a->last > a->n_sel) return CAP_E_INVAL;
+    uint64_t keys = 0;
+    int64_t wgs = 0, t0 = 0;
+    int32_t n = 0;
+    for (int32_t i = 0; i < a->n_seq; ++i) {
+        const kvb_seq& s = a->seqs[i];
+        if (s.T == 0) continue;
+        const int64_t nb = (s.n + kKvbBlock - 1) / kKvbBlock, pairs = s.T * a->kv_heads;
+        cap::KvbSelectSeq& x = p->seq[n++];
+        x.scales = addr(s.scales);
+        x.bounds = addr(s.bounds);
+        x.n = s.n;
+        x.t0 = t0;
+        x.T = (int32_t)s.T;
+        x.first_wg = (uint32_t)wgs;
+        x.keys = keys;
+        keys += (uint64_t)(pairs * nb);
+        wgs += pairs * ((nb + cap::kKvbScoreBlocks - 1) / cap::kKvbScoreBlocks);
+        if (wgs > 0x7fffffff) return CAP_E_UNSUPPORTED;
+        t0 += s.T;
+    }
+    p->tokens = tokens;
+    p->n_seq = n;
+    p->heads = a->heads;
+    p->kv_heads = a->kv_heads;
+    p->d = a->d;
+    p->n_sel = a->n_sel;
+    p->first = a->first;
+    p->last = a->last;
+    p->wgs = (uint32_t)wgs;
+    *bytes = up(keys * 8, 16);
+    return CAP_OK;
+}
+
+int launch_status(hipError_t e) { return e == hipSuccess ? CAP_OK : CAP_E_HIP; }
+
+}  // namespace
+
+extern "C" {
+
+int kvb_append(const kvb_append_args* a, void* stream) {
+    if (!a) return CAP_E_INVAL;
+    int64_t tokens = 0;
+    int rc = check_sizes(a->seqs, a->n_seq, a->kv_heads, a->kv_heads, a->d, a->in_dtype, &tokens);
+    if (rc != CAP_OK) return rc;
+    const int64_t row = (int64_t)a->kv_heads * a->d;
+    cap::KvbAppendParams p{};
+    if ((rc = check_stride(a->k_stride, row, &p.k_stride)) != CAP_OK) return rc;
+    if ((rc = check_stride(a->v_stride, row, &p.v_stride)) != CAP_OK) return rc;
+    if (tokens == 0) return CAP_OK;
+    if (!a->k || !a->v) return CAP_E_INVAL;
+    const Range in[2] = {range(a->k, span(tokens, p.k_stride, row)), range(a->v, span(tokens, p.v_stride, row))};
+    Range out[KVB_MAX_SEQ * PARTS];
+    int n_out = 0, n = 0;
+    int64_t wgs = 0, t0 = 0;
+    for (int32_t i = 0; i < a->n_seq; ++i) {
+        const kvb_seq& s = a->seqs[i];
+        if (s.T == 0) continue;
+        if ((rc = check_parts(s, bit(K) | bit(V) | bit(SCALES) | bit(OPEN))) != CAP_OK) return rc;
+        if ((rc = check_align(s)) != CAP_OK) return rc;
+        for (int j = 0; j < PARTS; ++j) {
+            const Range r = part(s, j, a->kv_heads, a->d);
+            if (r.a == r.b) continue;
+            if (meet(r, in[0]) || meet(r, in[1])) return CAP_E_INVAL;
+            out[n_out++] = r;
+        }
+        cap::KvbAppendSeq& x = p.seq[n++];
+        x = {addr(s.k), addr(s.v), addr(s.scales), addr(s.bounds), addr(s.open), s.n, t0, (int32_t)s.T, (uint32_t)wgs};
+        const int64_t begun = (s.n + kKvbBlock - 1) / kKvbBlock - (s.n - s.T) / kKvbBlock;
+        wgs += begun * a->kv_heads * 2;
+        if (wgs > 0x7fffffff) return CAP_E_UNSUPPORTED;
+        t0 += s.T;
+    }
+    if ((addr(a->k) | addr(a->v)) & 15) return CAP_E_ALIGN;
+    std::sort(out, out + n_out, [](const Range& x, const Range& y) { return x.a < y.a; });
+    for (int i = 1; i < n_out; ++i)
+        if (out[i].a < out[i - 1].b) return CAP_E_INVAL;
+    p.k_new = a->k;
+    p.v_new = a->v;
+    p.n_seq = n;
+    p.kv_heads = a->kv_heads;
+    p.d = a->d;
+    p.wgs = (uint32_t)wgs;
+    return launch_status(cap::launch_kvb_append(p, static_cast<hipStream_t>(stream)));
+}
+
+uint64_t kvb_attend_workspace_bytes(const kvb_attend_args* a) {
+    cap::KvbAttendParams p{};
+    return a && plan_attend(a, &p) == CAP_OK ? attend_workspace(p) : 0;
+}
+
+int kvb_attend(const kvb_attend_args* a, void* stream) {
+    if (!a || a->reserved != 0 || !std::isfinite(a->scale)) return CAP_E_INVAL;
+    cap::KvbAttendParams p{};
+    int rc = plan_attend(a, &p);
+    if (rc != CAP_OK) return rc;
+    const int64_t width = (int64_t)a->heads * a->d;
+    if ((rc = check_stride(a->q_stride, width, &p.q_stride)) != CAP_OK) return rc;
+    if (p.tokens == 0) return CAP_OK;
+    if (!a->q || !a->o) return CAP_E_INVAL;
+    const uint64_t need = attend_workspace(p);
+    if (need && !a->workspace) return CAP_E_INVAL;
+    if (a->workspace_bytes < need) return CAP_E_SIZE;
+    for (int32_t i = 0; i < a->n_seq; ++i) {
+        if (a->seqs[i].T == 0) continue;
+        if ((rc = check_parts(a->seqs[i], bit(K) | bit(V) | bit(SCALES))) != CAP_OK) return rc;
+        if ((rc = check_align(a->seqs[i])) != CAP_OK) return rc;
+    }
+    if (((addr(a->q) | addr(a->o) | (need ? addr(a->workspace) : 0)) & 15) || ((addr(a->lse) | addr(a->idx)) & 3)) return CAP_E_ALIGN;
+    const uint64_t tokens = (uint64_t)p.tokens;
+    const Range in[2] = {range(a->q, span(p.tokens, p.q_stride, width)),
+                         range(a->idx, tokens * (uint64_t)a->kv_heads * (uint64_t)a->n_sel * 4)};
+    const Range out[3] = {range(a->o, tokens * (uint64_t)width * 2), range(a->lse, tokens * (uint64_t)a->heads * 4),
+                          range(need ? a->workspace : nullptr, need)};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j])) return CAP_E_INVAL;
+        if (meet(out[i], in[0]) || meet(out[i], in[1])) return CAP_E_INVAL;
+        for (int32_t j = 0; j < a->n_seq; ++j)
+            if (a->seqs[j].T && meets_cache(out[i], a->seqs[j], bit(K) | bit(V) | bit(SCALES), a->kv_heads, a->d)) return CAP_E_INVAL;
+    }
+    p.q = a->q;
+    p.o = a->o;
+    p.lse = a->lse;
+    p.idx = a->idx;
+    p.part_o = static_cast<float*>(a->workspace);
+    p.part_ml = p.part_o + (uint64_t)p.slots * (uint64_t)p.tile * (uint64_t)p.d;
+    p.scale_log2 = a->scale * 1.4426950408889634f;
+    return launch_status(cap::launch_kvb_attend(p, static_cast<hipStream_t>(stream)));
+}
+
+uint64_t kvb_select_workspace_bytes(const kvb_select_args* a) {
+    cap::KvbSelectParams p{};
+    uint64_t bytes = 0;
+    return a && plan_select(a, &p, &bytes) == CAP_OK ? bytes : 0;
+}
+
+int kvb_select(const kvb_select_args* a, void* stream) {
+    if (!a) return CAP_E_INVAL;
+    cap::KvbSelectParams p{};
+    uint64_t need = 0;
+    int rc = plan_select(a, &p, &need);
+    if (rc != CAP_OK) return rc;
+    const int64_t width = (int64_t)a->heads * a->d;
+    if ((rc = check_stride(a->q_stride, width, &p.q_stride)) != CAP_OK) return rc;
+    if (p.tokens == 0) return CAP_OK;
+    if (!a->q || !a->idx || !a->workspace) return CAP_E_INVAL;
+    if (a->workspace_bytes < need) return CAP_E_SIZE;
+    for (int32_t i = 0; i < a->n_seq; ++i) {
+        if (a->seqs[i].T == 0) continue;
+        if ((rc = check_parts(a->seqs[i], bit(SCALES) | bit(BOUNDS))) != CAP_OK) return rc;
+        if ((rc = check_align(a->seqs[i])) != CAP_OK) return rc;
+    }
+    if (((addr(a->q) | addr(a->workspace)) & 15) || (addr(a->idx) & 3)) return CAP_E_ALIGN;
+    const Range q = range(a->q, span(p.tokens, p.q_stride, width));
+    const Range out[2] = {range(a->idx, (uint64_t)p.tokens * (uint64_t)a->kv_heads * (uint64_t)a->n_sel * 4), range(a->workspace, need)};
+    if (meet(out[0], out[1]) || meet(out[0], q) || meet(out[1], q)) return CAP_E_INVAL;
+    for (int i = 0; i < 2; ++i)
+        for (int32_t j = 0; j < a->n_seq; ++j)
+            if (a->seqs[j].T && meets_cache(out[i], a->seqs[j], bit(SCALES) | bit(BOUNDS), a->kv_heads, a->d)) return CAP_E_INVAL;
+    p.q = a->q;
+    p.idx = a->idx;
+    p.keys = static_cast<uint64_t*>(a->workspace);
+    return launch_status(cap::launch_kvb_select(p, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
