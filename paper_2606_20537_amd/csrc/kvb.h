@@ -58,7 +58,9 @@ struct KvbAttendParams {
     KvbAttendSeq   seq[KVB_MAX_SEQ];
 };
 
+// Tiles of 16 rows (kvb_attend.hip) or of 128 (kvb_prefill.hip, no block list).
 hipError_t launch_kvb_attend(const KvbAttendParams& p, hipStream_t stream);
+hipError_t launch_kvb_prefill(const KvbAttendParams& p, hipStream_t stream);  // its first launch alone
 
 // ---- select ----
 struct KvbSelectSeq {

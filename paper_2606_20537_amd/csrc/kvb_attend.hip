@@ -469,7 +469,7 @@ template <int D>
 hipError_t launch(const KvbAttendParams& p, hipStream_t stream) {
     const void* fn = p.idx ? reinterpret_cast<const void*>(&attend_kernel<D, true>)
                            : reinterpret_cast<const void*>(&attend_kernel<D, false>);
-    const hipError_t e = launch_kernel(fn, dim3(p.wgs), dim3(kThreads), p, stream);
+    const hipError_t e = p.tile == 128 ? launch_kvb_prefill(p, stream) : launch_kernel(fn, dim3(p.wgs), dim3(kThreads), p, stream);
     if (e != hipSuccess || p.slots == 0) return e;
     return launch_kernel(reinterpret_cast<const void*>(&join_kernel<D>), dim3((uint32_t)(p.tokens * p.heads)), dim3(kThreads), p,
                          stream);

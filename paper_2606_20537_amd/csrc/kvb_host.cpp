@@ -106,9 +106,11 @@ int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams* p) {
     p->d = a->d;
     p->n_sel = a->n_sel;
     p->tokens = tokens;
-    p->tile = 16;
+    int64_t most = 0;  // query rows of a KV head
+    for (int32_t i = 0; i < a->n_seq; ++i) most = std::max(most, a->seqs[i].T * G);
+    p->tile = !a->idx && most > 64 ? 128 : 16;
     auto items = [&](const kvb_seq& s) {
-        return (a->idx ? s.T * ((G + 15) / 16) : (s.T * G + 15) / 16) * a->kv_heads;
+        return (a->idx ? s.T * ((G + 15) / 16) : (s.T * G + p->tile - 1) / p->tile) * a->kv_heads;
     };
     auto blocks = [&](const kvb_seq& s) { return a->idx ? (int64_t)a->n_sel : (s.n + kKvbBlock - 1) / kKvbBlock; };
     int64_t total = 0;
