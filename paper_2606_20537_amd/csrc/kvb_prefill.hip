@@ -11,10 +11,17 @@
 //    highest score, rounded up to an integer c in log2 units, w = 2^(x - c + 8) in
 //    (0, 256], and split like Q: w = hi + lo / 16 with a relative error of 2^-8 at
 //    most, that of bf16, or 2^-22 of the block's largest weight where that is more.
-//    2^(c - m), m the running maximum of the c, is the instruction's scale of a
-//    row: an exact power of two, as are all corrections of O and l.
+//    2^(c - m) is the instruction's scale of a row, an exact power of two; m is the
+//    c of the row's first block, raised only where a later one is 2^64 above: O and
+//    l are floating, so their reference need not be the running maximum.
 // Against bf16 operands that is the same matrix time (FP8 runs at twice the rate),
 // half the LDS traffic and no conversion of K and V.
+//
+// One wave to a SIMD has registers for 32 rows of 256 channels, so the wave itself
+// keeps the matrix pipe busy: half of a block's softmax stands between the matrix
+// instructions of K Q^T of the block after it, the other half (the maximum first)
+// between those of V^T P^T of the block before it, in slices that the scheduler
+// must not move.
 //
 // A lane has one query row in both products and S^T's accumulators are P^T's
 // operand: byte 4 j + i of lane half h is key 8 j + 4 h + i.  V's operand has its
@@ -33,6 +40,7 @@ using dev::u32x4;
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -44,7 +52,13 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ inline float bits_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ inline uint32_t f32_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
-__device__ inline float pair_max(float x) { return __builtin_fmaxf(x, __shfl_xor(x, 32)); }
+// The higher of the two lanes that share lane % 32.
+__device__ inline float pair_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(x), f32_bits(x), false, false);
+    return __builtin_fmaxf(bits_f32(r[0]), bits_f32(r[1]));
+}
+template <typename T>
+using global_ptr = const T __attribute__((address_space(1)))*;
 
 // 0x80 in exactly the bytes of w that hold a NaN code (0x7F or 0xFF).
 __device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
@@ -53,8 +67,11 @@ __device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0
 __device__ inline void split4(const float* y, int& hi, int& lo) {
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32((y[2] - b[0]) * 16.0f, (y[3] - b[1]) * 16.0f,
-                                         __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - a[0]) * 16.0f, (y[1] - a[1]) * 16.0f, 0, false), true);
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+    i16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, y[0] - a[0], y[1] - a[1], 0.0625f, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, y[2] - b[0], y[3] - b[1], 0.0625f, true);
+    lo = __builtin_bit_cast(int, r);
 }
 
 __device__ inline f32x16 mma(const i32x8& a, const i32x8& b, const f32x16& c, int sa, int sb) {
@@ -75,8 +92,8 @@ template <int D>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(const KvbAttendParams p) {
     constexpr int NJ = D / 64, NT = D / 32, kUnits = D / 16, kRows = kThreads / kUnits, kLoads = kKvbBlock / kRows;
     __shared__ __attribute__((aligned(1024))) uint8_t k_s[2][kKvbBlock * D];
-    __shared__ __attribute__((aligned(1024))) uint8_t v_s[2][kKvbBlock * D];
-    __shared__ int nan_s[2];
+    __shared__ __attribute__((aligned(1024))) uint8_t v_s[3][kKvbBlock * D];
+    __shared__ int nan_s[3];
 
     int lo = 0, hi = p.n_seq - 1;  // last s with first_wg <= blockIdx.x
     while (lo < hi) {
@@ -96,8 +113,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     const int64_t row0 = tile * 128, wrow0 = row0 + wave * 32, last = total - 1;
     const int64_t row = wrow0 + (lane & 31) < last ? wrow0 + (lane & 31) : last;  // rows past the last repeat it
     const int64_t before = s.n - s.T, token = row / G, pos = before + token;     // the last key that the row sees
-    // the wave's first and last position, and the tile's
-    const int64_t wpos0 = before + (wrow0 < last ? wrow0 : last) / G, wpos1 = before + (wrow0 + 31 < last ? wrow0 + 31 : last) / G;
+    // the wave's first position, the tile's first and last
+    const int64_t wpos0 = before + (wrow0 < last ? wrow0 : last) / G;
     const int64_t tpos0 = before + row0 / G, tpos1 = before + (row0 + 127 < last ? row0 + 127 : last) / G;
 
     i32x8 qh[NJ], ql[NJ];
@@ -119,8 +136,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
         amax = pair_max(amax);
         int e = (int)(f32_bits(amax) >> 23) - 127 - 7;  // amax 2^-e in [128, 256)
         e = e < -100 ? -100 : e;
-        const float mul = bits_f32((uint32_t)(127 - e) << 23);  // an infinity stays one, and becomes NaN
-        f = bits_f32((uint32_t)(127 + e) << 23) * p.scale_log2;
+        // an infinity stays one, and becomes NaN; f is positive
+        const float sign = p.scale_log2 < 0.0f ? -1.0f : p.scale_log2 > 0.0f ? 1.0f : 0.0f;
+        const float mul = bits_f32((uint32_t)(127 - e) << 23) * sign;
+        f = sign == 0.0f ? 1.0f : bits_f32((uint32_t)(127 + e) << 23) * __builtin_fabsf(p.scale_log2);
         #pragma unroll
         for (int j = 0; j < NJ; ++j)
             #pragma unroll
@@ -142,24 +161,27 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     const int rowb = p.kv_heads * D;
     const uint8_t* kb = reinterpret_cast<const uint8_t*>(s.k);
     const uint8_t* vb = reinterpret_cast<const uint8_t*>(s.v);
-    const float* sc = reinterpret_cast<const float*>(s.scales);
+    const global_ptr<uint32_t> sc = (global_ptr<uint32_t>)s.scales;
     const int begin = split * s.per;
     const int nblk = (int)(tpos1 / kKvbBlock) + 1, end = begin + s.per < nblk ? begin + s.per : nblk;
 
-    // staging: thread tid moves unit tid % kUnits of rows tid / kUnits + i kRows
+    // Staging: thread tid moves unit tid % kUnits of rows tid / kUnits + i kRows.
     const int srow = tid / kUnits, sunit = tid % kUnits;
     const int svoff = srow * rowb + h * D + 16 * sunit;
     u32x4 ks[kLoads], vs[kLoads];
-    auto fetch = [&](int b) {
-        const rsrc_t rk = dev::make_rsrc_u32(kb + (int64_t)b * kKvbBlock * rowb, (uint32_t)kKvbBlock * rowb);
-        const rsrc_t rv = dev::make_rsrc_u32(vb + (int64_t)b * kKvbBlock * rowb, (uint32_t)kKvbBlock * rowb);
+    auto fetch = [&](const uint8_t* base, int b, u32x4 (&x)[kLoads]) {
+        const rsrc_t r = dev::make_rsrc_u32(base + (int64_t)b * kKvbBlock * rowb, (uint32_t)kKvbBlock * rowb);
+        #pragma unroll
+        for (int i = 0; i < kLoads; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, svoff, i * kRows * rowb, 0);
+    };
+    auto stage_k = [&](int buf) {
         #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            ks[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, svoff, i * kRows * rowb, 0);
-            vs[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, svoff, i * kRows * rowb, 0);
+            const int key = srow + i * kRows;
+            *reinterpret_cast<u32x4*>(&k_s[buf][key * D + 16 * (sunit ^ swizzle_k<D>(key))]) = ks[i];
         }
     };
-    auto stage = [&](int b, int buf) {
+    auto stage_v = [&](int b, int buf) {
         // Where some row does not see every key, NaN codes of V go (a weight of zero
         // would make them NaN), and are put back after the product.
         if ((int64_t)b * kKvbBlock + kKvbBlock - 1 > tpos0) {
@@ -177,108 +199,231 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
         #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int key = srow + i * kRows;
-            *reinterpret_cast<u32x4*>(&k_s[buf][key * D + 16 * (sunit ^ swizzle_k<D>(key))]) = ks[i];
             *reinterpret_cast<u32x4*>(&v_s[buf][key * D + 16 * (sunit ^ swizzle_v<D>(key))]) = vs[i];
         }
+    };
+    // Exponents of the scales as the instruction takes them, of 64 blocks from e0 on: lane i has block e0 + i.
+    int e0 = begin, k_exps = 0, v_exps = 0;
+    auto load_exponents = [&]() {
+        const int64_t at = (int64_t)((e0 + lane < end ? e0 + lane : end - 1) * 2) * p.kv_heads + h;
+        k_exps = (int)(sc[at] >> 23);
+        v_exps = (int)(sc[at + p.kv_heads] >> 23);
     };
 
     // addresses of a lane's reads; units and rows come in by xor and offset
     const int kaddr = (lane & 31) * D + 16 * (half ^ swizzle_k<D>(lane & 31));
     const int vkey = 4 * half + ((lane & 15) >> 1 & 3) + 8 * ((lane & 15) >> 3);
     const int vaddr = vkey * D + 16 * ((lane >> 4 & 1) ^ swizzle_v<D>(vkey)) + 8 * (lane & 1);
-
-    f32x16 acc[NT];
-    #pragma unroll
-    for (int c = 0; c < NT; ++c)
+    auto read_k = [&](int buf, int t, int j) {  // keys 32 t .. + 31, channels 64 j .. + 63
+        const u32x4 a = *reinterpret_cast<const u32x4*>(&k_s[buf][(kaddr ^ (64 * j)) + t * 32 * D]);
+        const u32x4 b = *reinterpret_cast<const u32x4*>(&k_s[buf][(kaddr ^ (64 * j + 32)) + t * 32 * D]);
+        return (i32x8){(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+    };
+    auto read_v = [&](int buf, int i) {  // channels 32 i .. + 31
+        i32x8 a;
         #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[c][r] = 0.0f;
-    float m = kNegInf, l = 0.0f;
+        for (int k = 0; k < 4; ++k) {
+            const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                (__attribute__((address_space(3))) i32x2*)&v_s[buf][(vaddr ^ (32 * i)) + 16 * k * D]);
+            a[2 * k] = v[0];
+            a[2 * k + 1] = v[1];
+        }
+        return a;
+    };
 
-    if (tid < 2) nan_s[tid] = -1;
-    if (begin < end) fetch(begin);
-    __syncthreads();
-    if (begin < end) stage(begin, 0);
-    for (int b = begin; b < end; ++b) {
-        const int buf = (b - begin) & 1;
-        __syncthreads();
-        if (b + 1 < end) fetch(b + 1);
+    f32x16 acc[NT], x[2], y[2];  // O^T; scores of block b and of block b + 1
+    #pragma unroll
+    for (int i = 0; i < NT; ++i) acc[i] = (f32x16){};
+    float m = kNegInf, l = 0.0f;
+    float c = 0.0f, base = 0.0f, sum = 0.0f;  // of block b's softmax, whose first half is done when its step begins
+    i32x8 ph, pl;
+
+    auto mask = [&](int b, f32x16 (&z)[2]) {
         const int64_t r0 = (int64_t)b * kKvbBlock;
-        if (r0 <= wpos1) {
-            const int k_exp = (int)(f32_bits(sc[(int64_t)(b * 2) * p.kv_heads + h]) >> 23);
-            const int v_exp = (int)(f32_bits(sc[(int64_t)(b * 2 + 1) * p.kv_heads + h]) >> 23);
-            f32x16 x[2];
+        if (r0 + kKvbBlock - 1 <= wpos0) return;  // every row sees every key
+        int sees = (int)(pos - r0 < kKvbBlock ? pos - r0 : kKvbBlock) - 4 * half;  // keys up to here
+        asm volatile("" : "+v"(sees));  // rare: not to be computed ahead of the branch
+        #pragma unroll
+        for (int t = 0; t < 2; ++t)
             #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                #pragma unroll
-                for (int r = 0; r < 16; ++r) x[t][r] = 0.0f;
-                #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const u32x4 a0 = *reinterpret_cast<const u32x4*>(&k_s[buf][(kaddr ^ (64 * j)) + t * 32 * D]);
-                    const u32x4 a1 = *reinterpret_cast<const u32x4*>(&k_s[buf][(kaddr ^ (64 * j + 32)) + t * 32 * D]);
-                    const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
-                    x[t] = mma(a, qh[j], x[t], k_exp, 127);
-                    x[t] = mma(a, ql[j], x[t], k_exp, 123);
-                }
+            for (int r = 0; r < 16; ++r)
+                if (32 * t + 8 * (r / 4) + r % 4 > sees) z[t][r] = kNegInf;
+    };
+    auto weights = [&](int q, const f32x16 (&z)[2], int& hi4, int& lo4) {  // of keys 8 q + 4 half .. + 3
+        float e[4];
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[q / 4][4 * (q % 4) + i], f, -base));
+        sum += (e[0] + e[1]) + (e[2] + e[3]);
+        split4(e, hi4, lo4);
+    };
+    auto highest = [&](const f32x16 (&z)[2], int part) {  // of a quarter of a lane's scores
+        const int t = part / 2, r = 8 * (part % 2);
+        const float u = __builtin_fmaxf(__builtin_fmaxf(z[t][r], z[t][r + 1]), z[t][r + 2]);
+        const float v = __builtin_fmaxf(__builtin_fmaxf(z[t][r + 3], z[t][r + 4]), z[t][r + 5]);
+        return __builtin_fmaxf(__builtin_fmaxf(u, v), __builtin_fmaxf(z[t][r + 6], z[t][r + 7]));
+    };
+    auto reference = [&](float top) {
+        c = __builtin_ceilf(pair_max(top) * f);
+        base = c == kNegInf ? 0.0f : c - 8.0f;
+        sum = 0.0f;
+    };
+
+    // Block b's K lies in buffer (b - begin) & 1, its V in (b - begin) % 3.  The step
+    // of block b reads K of b + 1, then V of b; in its first half K of b + 2 is
+    // written, in its second V of b + 2, each where the block before the last was read.
+    // Blocks past the end repeat the last one.
+    if (tid < 3) nan_s[tid] = -1;
+    auto clamp = [&](int b) { return b < end ? b : end - 1; };
+    int ke = 127, ve = 127;  // exponents of K of b + 1 and V of b
+    if (begin < end) {
+        fetch(kb, begin, ks);
+        fetch(vb, begin, vs);
+        load_exponents();
+        dev::lds_barrier();
+        stage_k(0);
+        stage_v(begin, 0);
+        fetch(kb, clamp(begin + 1), ks);
+        fetch(vb, clamp(begin + 1), vs);
+        ke = __builtin_amdgcn_readlane(k_exps, 0);
+        ve = __builtin_amdgcn_readlane(v_exps, 0);
+        dev::lds_barrier();
+        #pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            x[t] = (f32x16){};
+            #pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const i32x8 a = read_k(0, t, j);
+                x[t] = mma(a, qh[j], x[t], ke, 127);
+                x[t] = mma(a, ql[j], x[t], ke, 123);
             }
-            const bool partial = r0 + kKvbBlock - 1 > wpos0;  // some row does not see every key
-            if (partial) {
-                #pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (r0 + 32 * t + 8 * (r / 4) + 4 * half + r % 4 > pos) x[t][r] = f > 0.0f ? kNegInf : -kNegInf;
-            }
-            // f may be negative: the highest score is then that of the lowest product
-            float top = kNegInf;
+        }
+        ke = __builtin_amdgcn_readlane(k_exps, 1);
+        stage_k(1);
+        stage_v(clamp(begin + 1), 1);
+        fetch(kb, clamp(begin + 2), ks);
+        fetch(vb, clamp(begin + 2), vs);
+        mask(begin, x);
+        reference(__builtin_fmaxf(__builtin_fmaxf(highest(x, 0), highest(x, 1)), __builtin_fmaxf(highest(x, 2), highest(x, 3))));
+        #pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            int a, d;
+            weights(q, x, a, d);
+            ph[q] = a;
+            pl[q] = d;
+        }
+        dev::lds_barrier();
+    }
+    int vbuf = 0;
+    for (int b = begin; b < end; ++b) {
+        const int kbuf = (b - begin) & 1;
+        if constexpr (D == 256) {  // O stays in accumulation registers
             #pragma unroll
-            for (int t = 0; t < 2; ++t)
-                #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    x[t][r] *= f;
-                    top = __builtin_fmaxf(top, x[t][r]);
+            for (int i = 0; i < NT; ++i) asm volatile("" : "+a"(acc[i]));
+        }
+        const int next_ve = __builtin_amdgcn_readlane(v_exps, b + 1 - e0);
+        if (b + 2 - e0 >= 64) {
+            e0 = b + 2;
+            load_exponents();
+        }
+        const int next_ke = __builtin_amdgcn_readlane(k_exps, b + 2 - e0);
+        i32x8 v0, v1;
+        {
+            i32x8 k0 = read_k(kbuf ^ 1, 0, 0), k1 = read_k(kbuf ^ 1, 1, 0);
+            #pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                i32x8 n0, n1;
+                if (j + 1 < NJ) {
+                    n0 = read_k(kbuf ^ 1, 0, j + 1);
+                    n1 = read_k(kbuf ^ 1, 1, j + 1);
+                } else {
+                    v0 = read_v(vbuf, 0);
+                    v1 = read_v(vbuf, 1);
                 }
-            const float c = __builtin_ceilf(pair_max(top)), base = c == kNegInf ? 0.0f : c - 8.0f;
-            const float mn = __builtin_fmaxf(m, c);
-            const float fade = __builtin_amdgcn_exp2f(mn == kNegInf ? 0.0f : m - mn);
-            const float shift = __builtin_fmaxf(c - mn, -127.0f);  // c = mn = -inf: -127, with weights of zero
-            m = mn;
-            float sum = 0.0f;
-            i32x8 ph, pl;
-            #pragma unroll
-            for (int t = 0; t < 2; ++t)
                 #pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    float y[4];
+                for (int i = 0; i < 4; ++i) {
+                    const int step = 4 * j + i, steps = 4 * NJ;
+                    if (step < 2) y[step] = (f32x16){};
+                    y[i & 1] = mma(i & 1 ? k1 : k0, i < 2 ? qh[j] : ql[j], y[i & 1], ke, i < 2 ? 127 : 123);
                     #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        y[i] = __builtin_amdgcn_exp2f(x[t][r + i] - base);
-                        sum += y[i];
+                    for (int q = 4 + step * 4 / steps; q < 4 + (step + 1) * 4 / steps; ++q) {
+                        int a, d;
+                        weights(q, x, a, d);
+                        ph[q] = a;
+                        pl[q] = d;
                     }
-                    int a, d;
-                    split4(y, a, d);
-                    ph[4 * t + r / 4] = a;
-                    pl[4 * t + r / 4] = d;
+                    if (step == steps - 2) stage_k(kbuf);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-            l = l * fade + sum * __builtin_amdgcn_exp2f(shift);
-            if (__any(fade != 1.0f)) {
-                #pragma unroll
-                for (int i = 0; i < NT; ++i) acc[i] *= fade;
+                if (j + 1 < NJ) {
+                    k0 = n0;
+                    k1 = n1;
+                }
             }
-            const int se = 127 + (int)shift, sl = se < 4 ? 0 : se - 4;
+        }
+        // (what is needed late is not to be moved there)
+        asm volatile("" : "+v"(sum), "+v"(ph), "+v"(pl));
+        if constexpr (D == 256) asm volatile("" : "+a"(y[0]), "+a"(y[1]));
+        else asm volatile("" : "+v"(y[0]), "+v"(y[1]));
+        dev::lds_barrier();
+        fetch(kb, clamp(b + 3), ks);
+        if (m == kNegInf) m = c;  // O and l are zero so far
+        float shift = c - m;
+        if (__any(shift > 64.0f)) {
+            float up = shift > 64.0f ? c : m;
+            asm volatile("" : "+v"(up));  // rare: not to be computed ahead of the branch
+            const float fade = __builtin_amdgcn_exp2f(m - up);
             #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                i32x8 a;
-                #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                        (__attribute__((address_space(3))) i32x2*)&v_s[buf][(vaddr ^ (32 * i)) + 16 * k * D]);
-                    a[2 * k] = v[0];
-                    a[2 * k + 1] = v[1];
-                }
-                acc[i] = mma(a, ph, acc[i], v_exp, se);
-                acc[i] = mma(a, pl, acc[i], v_exp, sl);
+            for (int i = 0; i < NT; ++i) acc[i] *= fade;
+            l *= fade;
+            m = up;
+            shift = c - m;
+        }
+        shift = __builtin_fmaxf(shift, -127.0f);  // no score: -127, with weights of zero
+        l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(shift), l);
+        const int se = 127 + (int)shift, sl = se < 4 ? 0 : se - 4;
+        i32x4 nh, nl;
+        float top = kNegInf;
+        #pragma unroll
+        for (int i = 0; i < NT; i += 2) {
+            i32x8 n0, n1;
+            if (i + 2 < NT) {
+                n0 = read_v(vbuf, i + 2);
+                n1 = read_v(vbuf, i + 3);
             }
-            if (partial && nan_s[buf] == b) {
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int step = 2 * i + k, steps = 2 * NT;
+                acc[i + (k & 1)] = mma(k & 1 ? v1 : v0, k < 2 ? ph : pl, acc[i + (k & 1)], ve, k < 2 ? se : sl);
+                if (step == 1) {
+                    x[0] = y[0];
+                    x[1] = y[1];
+                    mask(b + 1, x);
+                    asm volatile("" : "+v"(x[0]), "+v"(x[1]));
+                }
+                // the first half of block b + 1's softmax: the maximum in the first quarter of the steps
+                #pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    if (u * steps / 8 != step) continue;
+                    if (u == 1) top = __builtin_fmaxf(highest(x, 0), highest(x, 1));
+                    if (u == 2) reference(__builtin_fmaxf(top, __builtin_fmaxf(highest(x, 2), highest(x, 3))));
+                    if (u >= 3 && u < 7) {
+                        int a, d;
+                        weights(u - 3, x, a, d);
+                        nh[u - 3] = a;
+                        nl[u - 3] = d;
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (i + 2 < NT) {
+                v0 = n0;
+                v1 = n1;
+            }
+        }
+        asm volatile("" : "+v"(sum), "+v"(nh), "+v"(nl));
+        {
+            const int64_t r0 = (int64_t)b * kKvbBlock;
+            if (r0 + kKvbBlock - 1 > wpos0 && nan_s[vbuf] == b) {
                 for (int t = 0; t < kKvbBlock; ++t) {
                     if (r0 + t >= s.n) break;
                     #pragma unroll
@@ -291,7 +436,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
                 }
             }
         }
-        if (b + 1 < end) stage(b + 1, buf ^ 1);
+        stage_v(clamp(b + 2), vbuf == 0 ? 2 : vbuf - 1);
+        fetch(vb, clamp(b + 3), vs);
+        #pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            ph[q] = nh[q];
+            pl[q] = nl[q];
+        }
+        ke = next_ke;
+        ve = next_ve;
+        vbuf = vbuf == 2 ? 0 : vbuf + 1;
     }
 
     l += __shfl_xor(l, 32);
