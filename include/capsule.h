@@ -539,7 +539,7 @@ CAP_API int kv_fp8_dequantize(const kv_fp8_seg* segs, uint32_t n_seg, void* stre
  * Supported: d in {64, 128, 256}, heads a multiple of kv_heads, bf16 tokens,
  * rows <= 2^31, 64 * kv_heads * d < 2^31, tokens * heads < 2^31.
  * Errors: CAP_E_INVAL (null required pointer, counts below their range, T > n,
- * rows not a multiple of 64, heads not a multiple of kv_heads, an output that
+ * tokens not the sum of T, rows not a multiple of 64, heads not a multiple of kv_heads, an output that
  * overlaps an input or another output), CAP_E_SIZE (n > rows, workspace too
  * small), CAP_E_UNSUPPORTED (shape or dtype outside the list, n_seq >
  * KVB_MAX_SEQ), CAP_E_ALIGN.  A call reads the sequence table before it returns,
@@ -567,6 +567,7 @@ typedef struct kvb_append_args {
     const void*    v;
     int64_t        k_stride;
     int64_t        v_stride;
+    int64_t        tokens;     /* sum of T */
     int32_t        n_seq;
     int32_t        kv_heads;
     int32_t        d;
@@ -598,6 +599,7 @@ typedef struct kvb_attend_args {
     void*          workspace;  /* kvb_attend_workspace_bytes(args), 16-byte aligned */
     uint64_t       workspace_bytes;
     int64_t        q_stride;
+    int64_t        tokens;     /* sum of T */
     int32_t        n_seq;
     int32_t        heads;
     int32_t        kv_heads;
@@ -608,8 +610,8 @@ typedef struct kvb_attend_args {
     int32_t        reserved;   /* 0 */
 } kvb_attend_args;
 
-/* Workspace of a call with these sizes (seqs' n and T, n_seq, heads, kv_heads, d,
- * and idx NULL or not with n_sel); 0 where the call needs none or is refused. */
+/* Workspace of a call with these sizes (seqs' n and T, tokens, n_seq, heads, kv_heads,
+ * d, and idx NULL or not with n_sel); 0 where the call needs none or is refused. */
 CAP_API uint64_t kvb_attend_workspace_bytes(const kvb_attend_args* args);
 CAP_API int kvb_attend(const kvb_attend_args* args, void* stream);
 
@@ -630,6 +632,7 @@ typedef struct kvb_select_args {
     void*          workspace;  /* kvb_select_workspace_bytes(args), 16-byte aligned */
     uint64_t       workspace_bytes;
     int64_t        q_stride;
+    int64_t        tokens;     /* sum of T */
     int32_t        n_seq;
     int32_t        heads;
     int32_t        kv_heads;

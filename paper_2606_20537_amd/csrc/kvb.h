@@ -35,6 +35,7 @@ hipError_t launch_kvb_append(const KvbAppendParams& p, hipStream_t stream);
 // one token.  The blocks of a tile are cut into nsplit runs of `per` blocks,
 // each a workgroup; with more than one the runs leave (o, m, l) in slots of
 // the workspace and a second launch joins them.
+constexpr int kKvbListRun = 64;  // entries of a block list in one run
 struct KvbAttendSeq {
     uint64_t k, v, scales;
     int64_t  n, t0;

@@ -16,7 +16,7 @@
 // brought them, also after a session went back to an earlier row.
 #include <hip/hip_runtime.h>
 
-#include "kvb.h"
+#include "kvb_device.h"
 
 namespace cap {
 namespace {
@@ -52,12 +52,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const KvbAppendParams 
     __shared__ float red[kThreads / 64];
     __shared__ float lo_s[kRows][D + 4], hi_s[kRows][D + 4];
 
-    int lo = 0, hi = p.n_seq - 1;                // last s with first_wg <= blockIdx.x
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.seq[mid].first_wg <= blockIdx.x) lo = mid; else hi = mid - 1;
-    }
-    const KvbAppendSeq& s = p.seq[__builtin_amdgcn_readfirstlane(lo)];
+    const KvbAppendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
     const uint32_t w = blockIdx.x - s.first_wg;
     const int side = (int)(w & 1), h = (int)((w >> 1) % (uint32_t)p.kv_heads);
     const int64_t held = s.n - s.T;              // rows before the append

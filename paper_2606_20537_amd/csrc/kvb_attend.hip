@@ -7,13 +7,13 @@
 // in one pass over K and V with a running m and l.  The query rows of a KV head
 // (tokens x query heads of the group) share its K and V: 16 of them are the
 // columns of the matrix instructions, keys and channels the rows.
-//  * S^T = K Q^T on 16x16x128 FP8 tiles straight from the codes.  A bf16 query
-//    row is split into two E4M3 rows, q 2^-e = hi + lo / 16 (e: the row's largest
-//    value falls in [128, 256)): 4 + 4 bits are bf16's 8, what is lost is below
-//    2^-22 of the row's largest value.
-//  * O^T = V^T P^T on 16x16x32 bf16 tiles: codes times the block's power-of-two
-//    scale are exact in bf16, P is rounded to bf16 (relative 2^-8 at most, as
-//    the output is); l sums the unrounded P in 32 bits.
+//  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 tiles: codes are exact in bf16, also
+//    times the block's power-of-two scale (V); the scale of K multiplies the scores.
+//    The FP8 instructions would spare the conversion of K, but their sums lose what is
+//    2^18 below a product of the same instruction (measured: up to 1.6e-4 of the sum of
+//    the products' magnitudes, bf16 2e-7).
+//  * P is rounded to bf16 (relative 2^-8 at most, as the output is); l sums the
+//    unrounded P in 32 bits.
 // Both products leave a lane with one query row (lane % 16), so maximum, sum and
 // correction need no value of another row, and S^T's accumulators are P^T's
 // operand: lane group g holds keys 4g..4g+3 and 16+4g..16+4g+3 of 32, and loads
@@ -23,7 +23,7 @@
 #include <hip/hip_runtime.h>
 
 #include "device_util.h"
-#include "kvb.h"
+#include "kvb_device.h"
 
 namespace cap {
 namespace {
@@ -33,7 +33,6 @@ using dev::f32x4;
 using dev::rsrc_t;
 using dev::u32x4;
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -52,11 +51,6 @@ __device__ inline float group_max(float x) {
 __device__ inline float group_sum(float x) {
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
-}
-
-// 0x80 in exactly the bytes of w that hold a NaN code (0x7F or 0xFF).
-__device__ inline uint32_t nan_bytes(uint32_t w) {
-    return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
 }
 
 // 4x4 bytes: out[c] = byte c of in[0..3].
@@ -81,85 +75,17 @@ __device__ inline void decode4(uint32_t w, float scale, bf16x8& v, int at) {
     v[at + 3] = b[1];
 }
 
-// A query row's two E4M3 rows in operand order, and the power of two that
-// belongs to them.  A lane holds channels 64 j + 16 g .. + 15 of its row.
+// 16 keys (lane % 16: a key, chunk j of 16 bytes: channels 64 j + 16 g .. + 15) against the
+// query rows, whose channels a lane holds in the same order.
 template <int D>
-struct Query {
-    static constexpr int kSteps = D == 64 ? 1 : D / 128;
-    i32x8 hi[kSteps], lo[D == 64 ? 1 : kSteps];  // D == 64: hi and lo in one operand
-    float scale;
-
-    __device__ void load(const uint8_t* row, int g) {
-        u32x4 x[D / 32];
-        float amax = 0.0f;
-        #pragma unroll
-        for (int j = 0; j < D / 64; ++j)
-            #pragma unroll
-            for (int c = 0; c < 2; ++c)
-                x[2 * j + c] = *reinterpret_cast<const u32x4*>(row + (64 * j + 16 * g + 8 * c) * 2);
-        #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-            #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                amax = __builtin_fmaxf(amax, __builtin_fmaxf(__builtin_fabsf(bits_f32(x[i][k] << 16)),
-                                                             __builtin_fabsf(bits_f32(x[i][k] & 0xFFFF0000u))));
-        amax = group_max(amax);
-        int e = (int)(f32_bits(amax) >> 23) - 127 - 7;  // amax 2^-e in [128, 256)
-        e = e < -100 ? -100 : e;
-        const float mul = bits_f32((uint32_t)(127 - e) << 23);  // an infinity stays one, and becomes NaN below
-        scale = bits_f32((uint32_t)(127 + e) << 23);
-        #pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-            #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                float y[4], z[4];
-                #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t u = x[2 * j + w / 2][2 * (w % 2) + k];
-                    y[2 * k] = bits_f32(u << 16) * mul;
-                    y[2 * k + 1] = bits_f32(u & 0xFFFF0000u) * mul;
-                }
-                const int a = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
-                const f32x2 b0 = __builtin_amdgcn_cvt_pk_f32_fp8(a, false), b1 = __builtin_amdgcn_cvt_pk_f32_fp8(a, true);
-                z[0] = (y[0] - b0[0]) * 16.0f;
-                z[1] = (y[1] - b0[1]) * 16.0f;
-                z[2] = (y[2] - b1[0]) * 16.0f;
-                z[3] = (y[3] - b1[1]) * 16.0f;
-                const int r = __builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false), true);
-                if (D == 64) {
-                    hi[0][w] = a;
-                    hi[0][4 + w] = r;
-                } else {
-                    hi[j / 2][4 * (j % 2) + w] = a;
-                    lo[j / 2][4 * (j % 2) + w] = r;
-                }
-            }
-        }
-    }
-};
-
-// 16 keys (lane % 16: a key, chunk j of 16 bytes: channels 64 j + 16 g ..) against 16 query rows.
-template <int D>
-__device__ inline f32x4 scores(const u32x4* k, const Query<D>& q, int lane) {
+__device__ inline f32x4 scores(const u32x4* k, const bf16x8* q) {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (D == 64) {
-        // channels 0..63 twice: against hi, and against lo with 2^-4 from lane groups 2 and 3, whose
-        // scales belong to the operand's second half
-        i32x8 a;
-        #pragma unroll
-        for (int w = 0; w < 4; ++w) a[w] = a[4 + w] = (int)k[0][w];
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.hi[0], s, 0, 0, 0, 127, 0, lane < 32 ? 127 : 123);
-    }
     #pragma unroll
-    for (int i = 0; i < Query<D>::kSteps; ++i) {
-        i32x8 a;
-        #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            a[w] = (int)k[2 * i][w];
-            a[4 + w] = (int)k[2 * i + 1][w];
-        }
-        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.hi[i], s, 0, 0, 0, 127, 0, 127);
-        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.lo[i], s, 0, 0, 0, 127, 0, 123);
+    for (int j = 0; j < D / 32; ++j) {
+        bf16x8 a;
+        decode4(k[j / 2][2 * (j % 2)], 1.0f, a, 0);
+        decode4(k[j / 2][2 * (j % 2) + 1], 1.0f, a, 4);
+        s = dev::mma(a, q[j], s);
     }
     return s;
 }
@@ -187,16 +113,12 @@ __device__ inline VBytes<VB> load_v(rsrc_t r, int voff, int soff) {
 template <int D, bool SPARSE>
 __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendParams p) {
     constexpr int VB = D / 16, NJ = D / 64;
+    constexpr bool kAhead = D < 256;  // registers for V of two units
     constexpr int kPitch = D + 4;
     __shared__ float o_s[4][16][kPitch];
     __shared__ float ml_s[4][16][2];
 
-    int lo = 0, hi = p.n_seq - 1;  // last s with first_wg <= blockIdx.x
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.seq[mid].first_wg <= blockIdx.x) lo = mid; else hi = mid - 1;
-    }
-    const KvbAttendSeq& s = p.seq[__builtin_amdgcn_readfirstlane(lo)];
+    const KvbAttendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
     const uint32_t w = blockIdx.x - s.first_wg;
     const int G = p.heads / p.kv_heads;
     const uint32_t item = w / (uint32_t)s.nsplit;  // (tile, kv head)
@@ -223,14 +145,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendPara
     const int64_t pos = s.n - s.T + my_token;              // the last key that the row sees
     const int64_t pos0 = s.n - s.T + (SPARSE ? token : r0 / G), pos1 = s.n - s.T + (SPARSE ? token : (r0 + rows - 1) / G);
 
-    Query<D> q;
-    q.load(static_cast<const uint8_t*>(p.q) + (s.t0 + my_token) * p.q_stride + ((int64_t)h * G + row % G) * D * 2, g);
-    const float row_scale = q.scale * p.scale_log2;
-
     const int rowb = p.kv_heads * D;
     const uint8_t* kb = reinterpret_cast<const uint8_t*>(s.k);
     const uint8_t* vb = reinterpret_cast<const uint8_t*>(s.v);
-    const float* sc = reinterpret_cast<const float*>(s.scales);
+    const global_ptr<float> sc = (global_ptr<float>)s.scales;
     const int kvoff = li * rowb + h * D + 16 * g, vvoff = 4 * g * rowb + h * D + li * VB;
     const int32_t* list = SPARSE ? p.idx + ((s.t0 + token) * p.kv_heads + h) * p.n_sel : nullptr;
 
@@ -238,19 +156,22 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendPara
     const int begin = split * s.per, end = begin + s.per < nblk ? begin + s.per : nblk;
     const int units = 2 * (end - begin);
 
+    // the run's list entries, one to a lane (kKvbListRun at most)
+    int entries = -1;
+    if (SPARSE && begin + lane < end) entries = list[begin + lane];
     // first row of unit u (32 rows); -1: nothing there (an entry that names no visible block)
     auto unit_row = [&](int u) -> int64_t {
         if (u >= units) return -1;
         int64_t b = begin + (u >> 1);
         if (SPARSE) {
-            b = __builtin_amdgcn_readfirstlane(list[b]);
+            b = __builtin_amdgcn_readlane(entries, u >> 1);
             if (b < 0 || b * kKvbBlock > pos) return -1;
         }
         const int64_t r = b * kKvbBlock + 32 * (u & 1);
         return r <= pos1 ? r : -1;
     };
     auto load_k = [&](int64_t r, u32x4 (&k)[2][NJ]) {
-        const rsrc_t rk = dev::make_rsrc_u32(kb + r * rowb, 32u * rowb);
+        const rsrc_t rk = dev::make_rsrc_u32(kb + (r < 0 ? 0 : r) * rowb, r < 0 ? 0 : 32u * rowb);  // r < 0: nothing is read
         #pragma unroll
         for (int t = 0; t < 2; ++t)
             #pragma unroll
@@ -263,94 +184,120 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendPara
     for (int c = 0; c < VB; ++c) acc[c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
     float m = kNegInf, l = 0.0f;
 
+    auto load_values = [&](int64_t r, VBytes<VB> (&v)[8]) {
+        const rsrc_t rv = dev::make_rsrc_u32(vb + (r < 0 ? 0 : r) * rowb, r < 0 ? 0 : 32u * rowb);
+        #pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = load_v<VB>(rv, vvoff, (e < 4 ? e : 12 + e) * rowb);
+    };
+    // The scales of a unit are loaded ahead of its K (loads return in order), K once the K
+    // before it is used, V at the start of the step before the unit's own (or of its own).
     u32x4 k[2][NJ];
+    VBytes<VB> v[kAhead ? 2 : 1][8];
+    float scales[2] = {1.0f, 1.0f};
+    auto load_scales = [&](int64_t r) {
+        const int64_t b = r < 0 ? 0 : r / kKvbBlock;
+        scales[0] = sc[(b * 2) * p.kv_heads + h];
+        scales[1] = sc[(b * 2 + 1) * p.kv_heads + h];
+    };
     int64_t r = unit_row(wave);
-    if (r >= 0) load_k(r, k);
-    for (int u = wave; u < units; u += 4) {
+    load_scales(r);
+    load_k(r, k);
+    if (kAhead) load_values(r, v[0]);
+    // the query rows, while the first keys are on their way
+    bf16x8 q[D / 32];
+    {
+        const uint8_t* src = static_cast<const uint8_t*>(p.q) + (s.t0 + my_token) * p.q_stride + ((int64_t)h * G + row % G) * D * 2;
+        #pragma unroll
+        for (int j = 0; j < D / 32; ++j) q[j] = *reinterpret_cast<const bf16x8*>(src + (64 * (j / 2) + 16 * g + 8 * (j % 2)) * 2);
+    }
+
+    auto step = [&](int u, VBytes<VB> (&vc)[8], VBytes<VB> (&vn)[8]) {
         const int64_t next = unit_row(u + 4);
-        if (r >= 0) {
-            VBytes<VB> v[8];
-            const rsrc_t rv = dev::make_rsrc_u32(vb + r * rowb, 32u * rowb);
-            #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = load_v<VB>(rv, vvoff, (e < 4 ? e : 12 + e) * rowb);
-            const int64_t b = r / kKvbBlock;
-            const float k_scale = sc[(b * 2) * p.kv_heads + h], v_scale = sc[(b * 2 + 1) * p.kv_heads + h];
-            const f32x4 s0 = scores<D>(k[0], q, lane), s1 = scores<D>(k[1], q, lane);
-            if (next >= 0) load_k(next, k);
-            float x[8];
-            #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = s0[e] * (row_scale * k_scale);
-                x[4 + e] = s1[e] * (row_scale * k_scale);
-            }
-            const bool partial = r + 31 > pos0;  // some row does not see every key
-            bool nan_seen = false;
-            if (partial) {
-                #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int64_t key = r + 4 * g + (e < 4 ? e : 12 + e);
-                    if (key > pos) x[e] = kNegInf;
-                    // NaN in V times a weight of zero would be NaN: such codes go, and are put back below
-                    #pragma unroll
-                    for (int i = 0; i < VB / 4; ++i) {
-                        const uint32_t bad = nan_bytes(v[e].w[i]);
-                        nan_seen |= bad != 0 && key < s.n;
-                        v[e].w[i] &= ~(bad | (bad - (bad >> 7)));
-                    }
-                }
-            }
-            float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3])),
-                                        __builtin_fmaxf(__builtin_fmaxf(x[4], x[5]), __builtin_fmaxf(x[6], x[7])));
-            top = __builtin_fmaxf(m, group_max(top));
-            const float base = top == kNegInf ? 0.0f : top;
-            const float fade = __builtin_amdgcn_exp2f(m - base);
-            m = top;
-            float sum = 0.0f;
-            bf16x8 pr;
-            #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(x[e] - base), p1 = __builtin_amdgcn_exp2f(x[e + 1] - base);
-                sum += p0 + p1;
-                const bf16x2 pp = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
-                pr[e] = pp[0];
-                pr[e + 1] = pp[1];
-            }
-            l = l * fade + sum;
-            if (__any(fade != 1.0f)) {
-                #pragma unroll
-                for (int c = 0; c < VB; ++c) acc[c] *= fade;
-            }
-            #pragma unroll
-            for (int i = 0; i < VB / 4; ++i) {
-                uint32_t a[4], b4[4];
-                const uint32_t in0[4] = {v[0].w[i], v[1].w[i], v[2].w[i], v[3].w[i]};
-                const uint32_t in1[4] = {v[4].w[i], v[5].w[i], v[6].w[i], v[7].w[i]};
-                transpose4(in0, a);
-                transpose4(in1, b4);
-                #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    bf16x8 vt;
-                    decode4(a[c], v_scale, vt, 0);
-                    decode4(b4[c], v_scale, vt, 4);
-                    acc[4 * i + c] = dev::mma(vt, pr, acc[4 * i + c]);
-                }
-            }
-            if (partial && __any(nan_seen)) {
-                for (int t = 0; t < 32; ++t) {
-                    if (r + t >= s.n) break;
-                    #pragma unroll
-                    for (int c = 0; c < VB; ++c)
-                        #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint8_t code = vb[(r + t) * rowb + h * D + (4 * g + j) * VB + c];
-                            if ((code & 0x7F) == 0x7F && r + t <= pos) acc[c][j] = __builtin_nanf("");
-                        }
-                }
-            }
-        } else if (next >= 0) {
-            load_k(next, k);
-        }
+        if (kAhead) load_values(next, vn); else load_values(r, vc);
+        const f32x4 s0 = scores<D>(k[0], q), s1 = scores<D>(k[1], q);
+        const float k_scale = scales[0], v_scale = scales[1];
+        load_scales(next);
+        load_k(next, k);
+        const int64_t now = r;
         r = next;
+        if (now < 0) return;
+        float x[8];
+        #pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = s0[e] * (p.scale_log2 * k_scale);
+            x[4 + e] = s1[e] * (p.scale_log2 * k_scale);
+        }
+        const bool partial = now + 31 > pos0;  // some row does not see every key
+        uint32_t nan_seen = 0;
+        if (partial) {
+            // of the unit's rows: the last that the query row sees, and how many there are
+            const int sees = (int)(pos - now < 32 ? pos - now : 32), held = (int)(s.n - now < 32 ? s.n - now : 32);
+            #pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int key = 4 * g + (e < 4 ? e : 12 + e);
+                x[e] = key > sees ? kNegInf : x[e];
+                const uint32_t there = key < held ? ~0u : 0u;
+                // NaN in V times a weight of zero would be NaN: such codes go, and are put back below
+                #pragma unroll
+                for (int i = 0; i < VB / 4; ++i) {
+                    const uint32_t bad = nan_bytes(vc[e].w[i]);
+                    nan_seen |= bad & there;
+                    vc[e].w[i] &= ~(bad | (bad - (bad >> 7)));
+                }
+            }
+        }
+        float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3])),
+                                    __builtin_fmaxf(__builtin_fmaxf(x[4], x[5]), __builtin_fmaxf(x[6], x[7])));
+        top = __builtin_fmaxf(m, group_max(top));
+        const float base = top == kNegInf ? 0.0f : top;
+        const float fade = __builtin_amdgcn_exp2f(m - base);
+        m = top;
+        float sum = 0.0f;
+        bf16x8 pr;
+        #pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(x[e] - base), p1 = __builtin_amdgcn_exp2f(x[e + 1] - base);
+            sum += p0 + p1;
+            const bf16x2 pp = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
+            pr[e] = pp[0];
+            pr[e + 1] = pp[1];
+        }
+        l = l * fade + sum;
+        if (__any(fade != 1.0f)) {
+            #pragma unroll
+            for (int c = 0; c < VB; ++c) acc[c] *= fade;
+        }
+        #pragma unroll
+        for (int i = 0; i < VB / 4; ++i) {
+            uint32_t a[4], b4[4];
+            const uint32_t in0[4] = {vc[0].w[i], vc[1].w[i], vc[2].w[i], vc[3].w[i]};
+            const uint32_t in1[4] = {vc[4].w[i], vc[5].w[i], vc[6].w[i], vc[7].w[i]};
+            transpose4(in0, a);
+            transpose4(in1, b4);
+            #pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                bf16x8 vt;
+                decode4(a[c], v_scale, vt, 0);
+                decode4(b4[c], v_scale, vt, 4);
+                acc[4 * i + c] = dev::mma(vt, pr, acc[4 * i + c]);
+            }
+        }
+        if (partial && __any(nan_seen != 0)) {
+            for (int t = 0; t < 32; ++t) {
+                if (now + t >= s.n) break;
+                #pragma unroll
+                for (int c = 0; c < VB; ++c)
+                    #pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint8_t code = vb[(now + t) * rowb + h * D + (4 * g + j) * VB + c];
+                        if ((code & 0x7F) == 0x7F && now + t <= pos) acc[c][j] = __builtin_nanf("");
+                    }
+            }
+        }
+    };
+    for (int u = wave; u < units; u += 8) {
+        step(u, v[0], v[kAhead ? 1 : 0]);
+        if (u + 4 < units) step(u + 4, v[kAhead ? 1 : 0], v[0]);
     }
 
     // join the waves
@@ -411,22 +358,34 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendPara
     }
 }
 
-// Joins the runs of a tile: one workgroup for each output row.
-template <int D>
+// Joins the runs of a tile.  A thread takes 16 bytes of an output row; with WAYS > 1,
+// for many runs, a workgroup has 64 channels of one row and WAYS threads share the
+// runs of each 16 bytes.
+template <int D, int WAYS>
 __global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendParams p) {
-    constexpr int kPer = D / 4, kWays = kThreads / kPer;
-    __shared__ float o_s[kWays][D];
-    const int64_t tok = blockIdx.x / (uint32_t)p.heads;
-    const int head = (int)(blockIdx.x - tok * p.heads);
-    int lo = 0, hi = p.n_seq - 1;  // last s with t0 <= tok
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.seq[mid].t0 <= tok) lo = mid; else hi = mid - 1;
+    constexpr int kPer = WAYS > 1 ? kThreads / WAYS : D / 4, kRows = kThreads / kPer / WAYS, kParts = WAYS > 1 ? D / (4 * kPer) : 1;
+    constexpr int kAhead = 4;  // runs whose loads are in flight
+    static_assert(kPer * kParts == D / 4 && kRows * kPer * WAYS == kThreads, "threads of a row");
+    const int tid = (int)threadIdx.x, way = tid / kPer % WAYS, mine = tid / (kPer * WAYS);
+    const int c = (int)(blockIdx.x % kParts) * 4 * kPer + tid % kPer * 4;
+    const uint32_t all = (uint32_t)(p.tokens * p.heads), out = blockIdx.x / kParts * kRows + (uint32_t)mine;
+    const uint32_t at = out < all ? out : all - 1;  // threads past the last row repeat it
+    const uint32_t tok = at / (uint32_t)p.heads;
+    const int head = (int)(at - tok * (uint32_t)p.heads);
+    int seq = 0;
+    if (WAYS > 1) {
+        seq = KVB_SEQ_OF(p, t0, (int64_t)tok);
+    } else {
+        int hi = p.n_seq - 1;  // last s with t0 <= tok
+        while (seq < hi) {
+            const int mid = (seq + hi + 1) >> 1;
+            if (p.seq[mid].t0 <= (int64_t)tok) seq = mid; else hi = mid - 1;
+        }
     }
-    const KvbAttendSeq& s = p.seq[__builtin_amdgcn_readfirstlane(lo)];
-    if (s.nsplit == 1) return;
+    const KvbAttendSeq& s = p.seq[seq];
+    const int n = s.nsplit;  // 1: written by its workgroup, nothing to do
     const int G = p.heads / p.kv_heads, h = head / G;
-    const int64_t t = tok - s.t0;
+    const int64_t t = (int64_t)tok - s.t0;
     int64_t item;
     int rr;
     if (p.idx) {
@@ -437,32 +396,60 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendParams p)
         item = row / p.tile * p.kv_heads + h;
         rr = (int)(row % p.tile);
     }
-    const int64_t slot = s.first_slot + item * s.nsplit;
-    const float* ml = p.part_ml + (slot * p.tile + rr) * 2;
-    const float* po = p.part_o + (slot * p.tile + rr) * D;
-    float top = kNegInf;
-    for (int i = 0; i < s.nsplit; ++i) top = __builtin_fmaxf(top, ml[(int64_t)i * p.tile * 2]);
-    const float base = top == kNegInf ? 0.0f : top;
-    const int tid = (int)threadIdx.x, way = tid / kPer, c = tid % kPer * 4;
-    float sum = 0.0f;
+    const int64_t slot = s.first_slot + item * n;
+    const global_ptr<f32x2> ml = (global_ptr<f32x2>)(p.part_ml + (slot * p.tile + rr) * 2);
+    const global_ptr<f32x4> po = (global_ptr<f32x4>)(p.part_o + (slot * p.tile + rr) * D + c);
+    const int ml_step = p.tile, po_step = p.tile * D / 4;
+    float top = kNegInf, sum = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i = 0; i < s.nsplit; ++i) {
-        const float f = __builtin_amdgcn_exp2f(ml[(int64_t)i * p.tile * 2] - base);
-        sum += ml[(int64_t)i * p.tile * 2 + 1] * f;
-        if (i % kWays == way) o += *reinterpret_cast<const f32x4*>(po + (int64_t)i * p.tile * D + c) * f;
-    }
-    *reinterpret_cast<f32x4*>(&o_s[way][c]) = o;
-    __syncthreads();
-    if (tid < kPer) {
+    for (int i = way; n > 1 && i < n; i += kAhead * WAYS) {
+        f32x2 a[kAhead];
+        f32x4 x[kAhead];
         #pragma unroll
-        for (int i = 1; i < kWays; ++i) o += *reinterpret_cast<const f32x4*>(&o_s[i][c]);
-        const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-        const bf16x2 a = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
-        const bf16x2 b = __builtin_convertvector((f32x2){o[2] * inv, o[3] * inv}, bf16x2);
-        *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + ((int64_t)tok * p.heads + head) * D + c) =
-            (u32x2){__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-        if (tid == 0 && p.lse) p.lse[tok * p.heads + head] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        for (int k = 0; k < kAhead; ++k) {
+            const int j = i + k * WAYS < n ? i + k * WAYS : i;
+            a[k] = ml[(int64_t)j * ml_step];
+            x[k] = po[(int64_t)j * po_step];
+        }
+        #pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i + k * WAYS >= n) continue;
+            const float up = __builtin_fmaxf(top, a[k][0]), base = up == kNegInf ? 0.0f : up;
+            const float f = __builtin_amdgcn_exp2f(top - base), g = __builtin_amdgcn_exp2f(a[k][0] - base);
+            sum = sum * f + a[k][1] * g;
+            o = o * f + x[k] * g;
+            top = up;
+        }
     }
+    if constexpr (WAYS > 1) {
+        __shared__ float o_s[WAYS - 1][4 * kPer], ml_s[WAYS][2];
+        if (tid % kPer == 0) {
+            ml_s[way][0] = top;
+            ml_s[way][1] = sum;
+        }
+        __syncthreads();
+        float up = kNegInf;
+        #pragma unroll
+        for (int i = 0; i < WAYS; ++i) up = __builtin_fmaxf(up, ml_s[i][0]);
+        const float base = up == kNegInf ? 0.0f : up;
+        sum = 0.0f;
+        #pragma unroll
+        for (int i = 0; i < WAYS; ++i) sum += ml_s[i][1] * __builtin_amdgcn_exp2f(ml_s[i][0] - base);
+        o *= __builtin_amdgcn_exp2f(top - base);
+        top = up;
+        if (way) *reinterpret_cast<f32x4*>(&o_s[way - 1][tid % kPer * 4]) = o;
+        __syncthreads();
+        if (way) return;
+        #pragma unroll
+        for (int i = 1; i < WAYS; ++i) o += *reinterpret_cast<const f32x4*>(&o_s[i - 1][tid % kPer * 4]);
+    }
+    if (n == 1 || out >= all) return;
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const bf16x2 a = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
+    const bf16x2 b = __builtin_convertvector((f32x2){o[2] * inv, o[3] * inv}, bf16x2);
+    *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + (int64_t)out * D + c) =
+        (u32x2){__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+    if (c == 0 && p.lse) p.lse[out] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int D>
@@ -471,8 +458,11 @@ hipError_t launch(const KvbAttendParams& p, hipStream_t stream) {
                            : reinterpret_cast<const void*>(&attend_kernel<D, false>);
     const hipError_t e = p.tile == 128 ? launch_kvb_prefill(p, stream) : launch_kernel(fn, dim3(p.wgs), dim3(kThreads), p, stream);
     if (e != hipSuccess || p.slots == 0) return e;
-    return launch_kernel(reinterpret_cast<const void*>(&join_kernel<D>), dim3((uint32_t)(p.tokens * p.heads)), dim3(kThreads), p,
-                         stream);
+    const uint32_t rows = (uint32_t)(p.tokens * p.heads), per = kThreads / (D / 4);
+    int runs = 0;
+    for (int i = 0; i < p.n_seq; ++i) runs = p.seq[i].nsplit > runs ? p.seq[i].nsplit : runs;
+    return runs > 4 ? launch_kernel(reinterpret_cast<const void*>(&join_kernel<D, 16>), dim3(rows * (D / 64)), dim3(kThreads), p, stream)
+                    : launch_kernel(reinterpret_cast<const void*>(&join_kernel<D, 1>), dim3((rows + per - 1) / per), dim3(kThreads), p, stream);
 }
 
 }  // namespace

@@ -17,25 +17,25 @@ Range range(const void* p, uint64_t bytes) { return {addr(p), addr(p) + (p ? byt
 bool meet(const Range& x, const Range& y) { return x.a < y.b && y.a < x.b; }
 uint64_t up(uint64_t x, uint64_t m) { return (x + m - 1) / m * m; }
 
-// The sizes that every call shares; `tokens` receives the sum of T.
+// The sizes that every call shares.
 int check_sizes(const kvb_seq* seqs, int32_t n_seq, int32_t heads, int32_t kv_heads, int32_t d, int32_t in_dtype,
-                int64_t* tokens) {
+                int64_t tokens) {
     if (n_seq < 0 || (n_seq > 0 && !seqs) || heads < 1 || kv_heads < 1 || d < 1) return CAP_E_INVAL;
     if (in_dtype != CAP_DTYPE_BF16 && in_dtype != CAP_DTYPE_F32) return CAP_E_INVAL;
     if (heads % kv_heads != 0) return CAP_E_INVAL;
     if (n_seq > KVB_MAX_SEQ || in_dtype != CAP_DTYPE_BF16 || (d != 64 && d != 128 && d != 256)) return CAP_E_UNSUPPORTED;
     // 32-bit offsets inside a block, and grids
     if ((int64_t)kKvbBlock * kv_heads * d > 0x7fffffff || (int64_t)heads * d > 0x7fffffff) return CAP_E_UNSUPPORTED;
-    *tokens = 0;
+    int64_t sum = 0;
     for (int32_t i = 0; i < n_seq; ++i) {
         const kvb_seq& s = seqs[i];
         if (s.rows < 0 || s.rows % kKvbBlock != 0 || s.n < 0 || s.T < 0 || s.T > s.n) return CAP_E_INVAL;
         if (s.rows > (int64_t)1 << 31) return CAP_E_UNSUPPORTED;
         if (s.n > s.rows) return CAP_E_SIZE;
-        *tokens += s.T;
+        sum += s.T;
     }
-    if (*tokens > 0x7fffffff / heads) return CAP_E_UNSUPPORTED;
-    return CAP_OK;
+    if (sum != tokens) return CAP_E_INVAL;
+    return tokens > 0x7fffffff / heads ? CAP_E_UNSUPPORTED : CAP_OK;
 }
 
 // Elements between tokens of a packed tensor (0: contiguous) as bytes.
@@ -90,14 +90,21 @@ bool meets_cache(const Range& out, const kvb_seq& s, unsigned used, int32_t kv_h
 constexpr unsigned bit(int i) { return 1u << i; }
 
 // ---- attend: the launch plan ----
-// Workgroups wanted: two to a CU.
-constexpr int64_t kWantWgs = 512;
-// Blocks that a run of a cut sequence has at least.
-constexpr int64_t kLeastBlocks = 2;
+// Blocks that a run of a cut sequence takes, for tiles of 16 rows; `total`: the
+// blocks of all tiles.  A workgroup to a CU while runs stay short, two where they
+// are long enough for one's loads to cover the other's arithmetic.  Measured (us,
+// both launches, 8 query heads on each KV head of 256; runs of): 16385 rows x 4 heads
+// 2: 19.3, 4: 16.4, 6: 15.6, 8: 16.7, 16: 20.8; 131072 + 18561 rows x 4 heads
+// 8: 66, 12: 67, 16: 63, 24: 72; 32 sequences of 816 rows x 1 head 2: 13.2, 4: 14.4,
+// 8: 16.0, whole (13, no second launch) 15.6.
+int64_t run_of_16(int64_t total) {
+    const int64_t one = (total + 255) / 256;
+    return std::max<int64_t>(2, one <= 16 ? one : (total + 511) / 512);
+}
 
 int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams* p) {
-    int64_t tokens = 0;
-    const int rc = check_sizes(a->seqs, a->n_seq, a->heads, a->kv_heads, a->d, a->in_dtype, &tokens);
+    const int64_t tokens = a->tokens;
+    const int rc = check_sizes(a->seqs, a->n_seq, a->heads, a->kv_heads, a->d, a->in_dtype, tokens);
     if (rc != CAP_OK) return rc;
     if (a->idx ? a->n_sel < 1 : a->n_sel != 0) return CAP_E_INVAL;
     const int64_t G = a->heads / a->kv_heads;
@@ -106,16 +113,43 @@ int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams* p) {
     p->d = a->d;
     p->n_sel = a->n_sel;
     p->tokens = tokens;
-    int64_t most = 0;  // query rows of a KV head
-    for (int32_t i = 0; i < a->n_seq; ++i) most = std::max(most, a->seqs[i].T * G);
-    p->tile = !a->idx && most > 64 ? 128 : 16;
-    auto items = [&](const kvb_seq& s) {
-        return (a->idx ? s.T * ((G + 15) / 16) : (s.T * G + p->tile - 1) / p->tile) * a->kv_heads;
-    };
+    int64_t most = 0, longest = 0;  // query rows of a KV head, blocks
     auto blocks = [&](const kvb_seq& s) { return a->idx ? (int64_t)a->n_sel : (s.n + kKvbBlock - 1) / kKvbBlock; };
-    int64_t total = 0;
-    for (int32_t i = 0; i < a->n_seq; ++i) total += items(a->seqs[i]) * blocks(a->seqs[i]);
-    const int64_t per = std::max(kLeastBlocks, (total + kWantWgs - 1) / kWantWgs);
+    for (int32_t i = 0; i < a->n_seq; ++i) {
+        if (a->seqs[i].T == 0) continue;
+        most = std::max(most, a->seqs[i].T * G);
+        longest = std::max(longest, blocks(a->seqs[i]));
+    }
+    p->tile = !a->idx && most > 64 ? 128 : 16;
+    auto tiles = [&](const kvb_seq& s) { return a->idx ? s.T * ((G + 15) / 16) : (s.T * G + p->tile - 1) / p->tile; };
+    int64_t total = 0, rows = 0;
+    for (int32_t i = 0; i < a->n_seq; ++i) {
+        const kvb_seq& s = a->seqs[i];
+        int64_t seen = tiles(s) * blocks(s);
+        if (p->tile == 128) seen -= tiles(s) * (s.T / kKvbBlock) / 2;  // the tiles of a prefill see half of its blocks
+        total += seen * a->kv_heads;
+        rows += s.T * a->heads;
+    }
+    int64_t per = longest;
+    if (p->tile == 16) {
+        per = run_of_16(total);
+        if (a->idx) per = std::min<int64_t>(per, cap::kKvbListRun);
+    } else {
+        // The time in blocks: that of the longest workgroup or of all of them in turn, and that of
+        // writing, reading and joining the parts (3 TB/s and a launch).
+        const int64_t at_once = a->d == 256 ? 256 : 512;
+        const double block_us = a->d == 256 ? 2.0 : a->d == 128 ? 1.3 : 0.9;
+        double best = 1e30;
+        for (int64_t cut = 1; cut <= 32 && cut <= longest; ++cut) {
+            const int64_t run = (longest + cut - 1) / cut;
+            double us = block_us * (double)std::max(run, (total + at_once - 1) / at_once);
+            if (cut > 1) us += 5.0 + (double)(rows * cut * a->d) * 8.0 / 3e6;
+            if (us < best) {
+                best = us;
+                per = run;
+            }
+        }
+    }
     int64_t wgs = 0, slots = 0, t0 = 0;
     int32_t n = 0;
     for (int32_t i = 0; i < a->n_seq; ++i) {
@@ -128,12 +162,13 @@ int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams* p) {
         x.n = s.n;
         x.t0 = t0;
         x.T = (int32_t)s.T;
-        x.per = (int32_t)std::min(per, blocks(s));
-        x.nsplit = (int32_t)((blocks(s) + x.per - 1) / x.per);
+        const int64_t nb = blocks(s), items = tiles(s) * a->kv_heads;
+        x.nsplit = (int32_t)((nb + per - 1) / per);
+        x.per = (int32_t)((nb + x.nsplit - 1) / x.nsplit);  // of even lengths
         x.first_wg = (uint32_t)wgs;
         x.first_slot = (uint32_t)slots;
-        wgs += items(s) * x.nsplit;
-        if (x.nsplit > 1) slots += items(s) * x.nsplit;
+        wgs += items * x.nsplit;
+        if (x.nsplit > 1) slots += items * x.nsplit;
         if (wgs > 0x7fffffff) return CAP_E_UNSUPPORTED;
         t0 += s.T;
     }
@@ -149,8 +184,8 @@ uint64_t attend_workspace(const cap::KvbAttendParams& p) {
 
 // ---- select: the launch plan ----
 int plan_select(const kvb_select_args* a, cap::KvbSelectParams* p, uint64_t* bytes) {
-    int64_t tokens = 0;
-    const int rc = check_sizes(a->seqs, a->n_seq, a->heads, a->kv_heads, a->d, a->in_dtype, &tokens);
+    const int64_t tokens = a->tokens;
+    const int rc = check_sizes(a->seqs, a->n_seq, a->heads, a->kv_heads, a->d, a->in_dtype, tokens);
     if (rc != CAP_OK) return rc;
     if (a->first < 0 || a->last < 1 || a->n_sel < 1 || (int64_t)a->first + a->last > a->n_sel) return CAP_E_INVAL;
     uint64_t keys = 0;
@@ -194,8 +229,8 @@ extern "C" {
 
 int kvb_append(const kvb_append_args* a, void* stream) {
     if (!a) return CAP_E_INVAL;
-    int64_t tokens = 0;
-    int rc = check_sizes(a->seqs, a->n_seq, a->kv_heads, a->kv_heads, a->d, a->in_dtype, &tokens);
+    const int64_t tokens = a->tokens;
+    int rc = check_sizes(a->seqs, a->n_seq, a->kv_heads, a->kv_heads, a->d, a->in_dtype, tokens);
     if (rc != CAP_OK) return rc;
     const int64_t row = (int64_t)a->kv_heads * a->d;
     cap::KvbAppendParams p{};

@@ -30,7 +30,7 @@
 #include <hip/hip_runtime.h>
 
 #include "device_util.h"
-#include "kvb.h"
+#include "kvb_device.h"
 
 namespace cap {
 namespace {
@@ -57,12 +57,6 @@ __device__ inline float pair_max(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(x), f32_bits(x), false, false);
     return __builtin_fmaxf(bits_f32(r[0]), bits_f32(r[1]));
 }
-template <typename T>
-using global_ptr = const T __attribute__((address_space(1)))*;
-
-// 0x80 in exactly the bytes of w that hold a NaN code (0x7F or 0xFF).
-__device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
-
 // Four values to four E4M3 codes, and their remainders times 16 to four more.
 __device__ inline void split4(const float* y, int& hi, int& lo) {
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
@@ -95,12 +89,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     __shared__ __attribute__((aligned(1024))) uint8_t v_s[3][kKvbBlock * D];
     __shared__ int nan_s[3];
 
-    int lo = 0, hi = p.n_seq - 1;  // last s with first_wg <= blockIdx.x
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.seq[mid].first_wg <= blockIdx.x) lo = mid; else hi = mid - 1;
-    }
-    const KvbAttendSeq& s = p.seq[__builtin_amdgcn_readfirstlane(lo)];
+    const KvbAttendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
     const uint32_t w = blockIdx.x - s.first_wg;
     const int G = p.heads / p.kv_heads;
     const uint32_t item = w / (uint32_t)s.nsplit;
@@ -394,7 +383,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
             for (int k = 0; k < 4; ++k) {
                 const int step = 2 * i + k, steps = 2 * NT;
                 acc[i + (k & 1)] = mma(k & 1 ? v1 : v0, k < 2 ? ph : pl, acc[i + (k & 1)], ve, k < 2 ? se : sl);
-                if (step == 1) {
+                if (step == (NT > 2 ? 1 : 0)) {  // ahead of its first use below
                     x[0] = y[0];
                     x[1] = y[1];
                     mask(b + 1, x);

@@ -16,7 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include "device_util.h"
-#include "kvb.h"
+#include "kvb_device.h"
 
 namespace cap {
 namespace {
@@ -40,12 +40,7 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void score_kernel(const KvbSelectParams p) {
     constexpr int kPer = D / 8;  // channels of a thread
     __shared__ float q_s[kHeads][D];
-    int lo = 0, hi = p.n_seq - 1;  // last s with first_wg <= blockIdx.x
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.seq[mid].first_wg <= blockIdx.x) lo = mid; else hi = mid - 1;
-    }
-    const KvbSelectSeq& s = p.seq[__builtin_amdgcn_readfirstlane(lo)];
+    const KvbSelectSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
     const uint32_t nb = (uint32_t)((s.n + kKvbBlock - 1) / kKvbBlock);
     const uint32_t parts = (nb + kKvbScoreBlocks - 1) / kKvbScoreBlocks;
     const uint32_t w = blockIdx.x - s.first_wg, pair = w / parts;
@@ -116,12 +111,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const KvbSelectParams p)
     __shared__ uint32_t bins[256], found[2], waves[kThreads / 64];
     const int64_t tok = blockIdx.x / (uint32_t)p.kv_heads;
     const int h = (int)(blockIdx.x - tok * p.kv_heads);
-    int lo = 0, hi = p.n_seq - 1;  // last s with t0 <= tok
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.seq[mid].t0 <= tok) lo = mid; else hi = mid - 1;
-    }
-    const KvbSelectSeq& s = p.seq[__builtin_amdgcn_readfirstlane(lo)];
+    const KvbSelectSeq& s = p.seq[KVB_SEQ_OF(p, t0, tok)];
     const int64_t t = tok - s.t0;
     const uint32_t nb = (uint32_t)((s.n + kKvbBlock - 1) / kKvbBlock);
     const uint32_t count = (uint32_t)((s.n - s.T + t) / kKvbBlock) + 1;  // blocks that the token sees some of
