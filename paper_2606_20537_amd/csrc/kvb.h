@@ -9,6 +9,11 @@ namespace cap {
 
 constexpr int kKvbBlock = KVB_BLOCK;
 
+// Parameters carry a table of sequences by value, of KVB_MAX_SEQ or of kKvbFew: a launch
+// copies its arguments, and 4 KB of them cost the host about as much as the launch.
+// The table comes last, so that the short form is the beginning of the long one.
+constexpr int kKvbFew = 4;
+
 // ---- append ----
 // Workgroup w works on sequence s with first_wg <= w < the next one's, on its
 // block, KV head and side (K or V) number w - first_wg.
@@ -18,14 +23,16 @@ struct KvbAppendSeq {
     int32_t  T;
     uint32_t first_wg;
 };
-struct KvbAppendParams {
+template <int N>
+struct KvbAppendTable {
     const void* k_new;
     const void* v_new;
     int64_t  k_stride, v_stride;  // bytes between tokens
     int32_t  n_seq, kv_heads, d;
     uint32_t wgs;
-    KvbAppendSeq seq[KVB_MAX_SEQ];
+    KvbAppendSeq seq[N];
 };
+using KvbAppendParams = KvbAppendTable<KVB_MAX_SEQ>;
 hipError_t launch_kvb_append(const KvbAppendParams& p, hipStream_t stream);
 
 // ---- attend ----
@@ -44,7 +51,8 @@ struct KvbAttendSeq {
     int32_t  per, nsplit;
     int32_t  pad;
 };
-struct KvbAttendParams {
+template <int N>
+struct KvbAttendTable {
     const void*    q;
     void*          o;
     float*         lse;        // may be null
@@ -56,8 +64,9 @@ struct KvbAttendParams {
     int32_t        n_seq, heads, kv_heads, d, n_sel, tile;
     uint32_t       wgs, slots;
     float          scale_log2; // scale * log2(e)
-    KvbAttendSeq   seq[KVB_MAX_SEQ];
+    KvbAttendSeq   seq[N];
 };
+using KvbAttendParams = KvbAttendTable<KVB_MAX_SEQ>;
 
 // Tiles of 16 rows (kvb_attend.hip) or of 128 (kvb_prefill.hip, no block list).
 hipError_t launch_kvb_attend(const KvbAttendParams& p, hipStream_t stream);
@@ -71,17 +80,27 @@ struct KvbSelectSeq {
     uint32_t first_wg;
     uint64_t keys;             // first sort key of the sequence in the workspace
 };
-struct KvbSelectParams {
+template <int N>
+struct KvbSelectTable {
     const void* q;
     int32_t*    idx;
     uint64_t*   keys;          // [token][kv head][blocks of the sequence]
     int64_t     q_stride, tokens;
     int32_t     n_seq, heads, kv_heads, d, n_sel, first, last;
     uint32_t    wgs;
-    KvbSelectSeq seq[KVB_MAX_SEQ];
+    KvbSelectSeq seq[N];
 };
+using KvbSelectParams = KvbSelectTable<KVB_MAX_SEQ>;
 // Blocks that one workgroup of the scoring launch takes.
-constexpr int kKvbScoreBlocks = 32;
+constexpr int kKvbScoreBlocks = 16;
 hipError_t launch_kvb_select(const KvbSelectParams& p, hipStream_t stream);
+
+// Launch a kernel over a sequence table, in the form that its length asks for.
+template <template <int> class Table>
+inline hipError_t launch_kvb(const void* few, const void* many, dim3 grid, dim3 block, const Table<KVB_MAX_SEQ>& p,
+                             hipStream_t stream) {
+    void* args[] = {const_cast<Table<KVB_MAX_SEQ>*>(&p)};
+    return hipLaunchKernel(p.n_seq <= kKvbFew ? few : many, grid, block, args, 0, stream);
+}
 
 }  // namespace cap

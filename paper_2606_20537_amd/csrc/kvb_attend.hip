@@ -110,8 +110,8 @@ __device__ inline VBytes<VB> load_v(rsrc_t r, int voff, int soff) {
     return x;
 }
 
-template <int D, bool SPARSE>
-__global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendParams p) {
+template <int D, bool SPARSE, int N>
+__global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTable<N> p) {
     constexpr int VB = D / 16, NJ = D / 64;
     constexpr bool kAhead = D < 256;  // registers for V of two units
     constexpr int kPitch = D + 4;
@@ -361,8 +361,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendPara
 // Joins the runs of a tile.  A thread takes 16 bytes of an output row; with WAYS > 1,
 // for many runs, a workgroup has 64 channels of one row and WAYS threads share the
 // runs of each 16 bytes.
-template <int D, int WAYS>
-__global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendParams p) {
+template <int D, int WAYS, int N>
+__global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendTable<N> p) {
     constexpr int kPer = WAYS > 1 ? kThreads / WAYS : D / 4, kRows = kThreads / kPer / WAYS, kParts = WAYS > 1 ? D / (4 * kPer) : 1;
     constexpr int kAhead = 4;  // runs whose loads are in flight
     static_assert(kPer * kParts == D / 4 && kRows * kPer * WAYS == kThreads, "threads of a row");
@@ -452,17 +452,23 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendParams p)
     if (c == 0 && p.lse) p.lse[out] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
+#define KVB_FORMS(kernel, ...) reinterpret_cast<const void*>(&kernel<__VA_ARGS__, kKvbFew>), reinterpret_cast<const void*>(&kernel<__VA_ARGS__, KVB_MAX_SEQ>)
+
 template <int D>
 hipError_t launch(const KvbAttendParams& p, hipStream_t stream) {
-    const void* fn = p.idx ? reinterpret_cast<const void*>(&attend_kernel<D, true>)
-                           : reinterpret_cast<const void*>(&attend_kernel<D, false>);
-    const hipError_t e = p.tile == 128 ? launch_kvb_prefill(p, stream) : launch_kernel(fn, dim3(p.wgs), dim3(kThreads), p, stream);
+    const dim3 block(kThreads);
+    const hipError_t e = p.tile == 128 ? launch_kvb_prefill(p, stream)
+                         : p.idx ? launch_kvb<KvbAttendTable>(KVB_FORMS(attend_kernel, D, true), dim3(p.wgs), block, p, stream)
+                                 : launch_kvb<KvbAttendTable>(KVB_FORMS(attend_kernel, D, false), dim3(p.wgs), block, p, stream);
     if (e != hipSuccess || p.slots == 0) return e;
+    // Threads side by side on the runs of a row where there are few rows for the chip: 161 tokens x
+    // 32 heads x 256 channels of 8 runs took 30 us with them, 32 heads of one token and 43 runs 10 us without.
     const uint32_t rows = (uint32_t)(p.tokens * p.heads), per = kThreads / (D / 4);
     int runs = 0;
     for (int i = 0; i < p.n_seq; ++i) runs = p.seq[i].nsplit > runs ? p.seq[i].nsplit : runs;
-    return runs > 4 ? launch_kernel(reinterpret_cast<const void*>(&join_kernel<D, 16>), dim3(rows * (D / 64)), dim3(kThreads), p, stream)
-                    : launch_kernel(reinterpret_cast<const void*>(&join_kernel<D, 1>), dim3((rows + per - 1) / per), dim3(kThreads), p, stream);
+    return runs > 4 && rows * (D / 64) <= 4096
+               ? launch_kvb<KvbAttendTable>(KVB_FORMS(join_kernel, D, 16), dim3(rows * (D / 64)), block, p, stream)
+               : launch_kvb<KvbAttendTable>(KVB_FORMS(join_kernel, D, 1), dim3((rows + per - 1) / per), block, p, stream);
 }
 
 }  // namespace

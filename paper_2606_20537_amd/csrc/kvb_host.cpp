@@ -247,12 +247,6 @@ int kvb_append(const kvb_append_args* a, void* stream) {
         if (s.T == 0) continue;
         if ((rc = check_parts(s, bit(K) | bit(V) | bit(SCALES) | bit(OPEN))) != CAP_OK) return rc;
         if ((rc = check_align(s)) != CAP_OK) return rc;
-        for (int j = 0; j < PARTS; ++j) {
-            const Range r = part(s, j, a->kv_heads, a->d);
-            if (r.a == r.b) continue;
-            if (meet(r, in[0]) || meet(r, in[1])) return CAP_E_INVAL;
-            out[n_out++] = r;
-        }
         cap::KvbAppendSeq& x = p.seq[n++];
         x = {addr(s.k), addr(s.v), addr(s.scales), addr(s.bounds), addr(s.open), s.n, t0, (int32_t)s.T, (uint32_t)wgs};
         const int64_t begun = (s.n + kKvbBlock - 1) / kKvbBlock - (s.n - s.T) / kKvbBlock;
@@ -260,8 +254,16 @@ int kvb_append(const kvb_append_args* a, void* stream) {
         if (wgs > 0x7fffffff) return CAP_E_UNSUPPORTED;
         t0 += s.T;
     }
+    for (int j = 0; j < PARTS; ++j)  // in the order in which they mostly lie in memory
+        for (int32_t i = 0; i < a->n_seq; ++i) {
+            const Range r = part(a->seqs[i], j, a->kv_heads, a->d);
+            if (a->seqs[i].T == 0 || r.a == r.b) continue;
+            if (meet(r, in[0]) || meet(r, in[1])) return CAP_E_INVAL;
+            out[n_out++] = r;
+        }
     if ((addr(a->k) | addr(a->v)) & 15) return CAP_E_ALIGN;
-    std::sort(out, out + n_out, [](const Range& x, const Range& y) { return x.a < y.a; });
+    const auto lower = [](const Range& x, const Range& y) { return x.a < y.a; };
+    if (!std::is_sorted(out, out + n_out, lower)) std::sort(out, out + n_out, lower);
     for (int i = 1; i < n_out; ++i)
         if (out[i].a < out[i - 1].b) return CAP_E_INVAL;
     p.k_new = a->k;

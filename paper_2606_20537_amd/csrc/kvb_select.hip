@@ -8,11 +8,13 @@
 // choice does not depend on how a kernel adds.  A score that is NaN counts as
 // infinite, as attention over the block gives NaN.
 //
-// Two launches: scores as ordered 64-bit keys, 32 blocks to a workgroup, eight
-// threads to a block; then one workgroup for each token and KV head finds the
-// n_sel-th highest key by its bytes from the top (a histogram of 256 in LDS for
-// each) and writes the blocks in ascending order.  Blocks that a token has to
-// have carry the highest key, those behind it the lowest.
+// Two launches.  Scores: q+ . hi + q- . lo (q+ and q- the positive and the negative part
+// of q) on 64-bit matrix instructions, 16 query heads against 16 blocks to a workgroup,
+// a quarter of the channels to a wave; written as ordered 64-bit keys.  Choice: one
+// workgroup for each token and KV head finds the n_sel-th highest key by histograms of
+// eight bits, from the highest bit in which the keys differ (above it every key would
+// count into one bin), and writes the blocks in ascending order.  Blocks that a token
+// has to have carry the highest key, those behind it the lowest.
 #include <hip/hip_runtime.h>
 
 #include "device_util.h"
@@ -21,12 +23,11 @@
 namespace cap {
 namespace {
 
-using dev::u32x4;
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kHeads = 8;         // query heads that LDS holds at a time
 constexpr int kKeysLds = 4096;    // keys that LDS holds
 constexpr uint64_t kMust = ~0ull, kNever = 0;
 
@@ -36,10 +37,11 @@ __device__ inline uint64_t order_key(double x) {
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-template <int D>
-__global__ __launch_bounds__(kThreads) void score_kernel(const KvbSelectParams p) {
-    constexpr int kPer = D / 8;  // channels of a thread
-    __shared__ float q_s[kHeads][D];
+template <int D, int N>
+__global__ __launch_bounds__(kThreads) void score_kernel(const KvbSelectTable<N> p) {
+    constexpr int kSteps = D / 16;  // channels of a lane: D / 4 to a wave, a quarter of them to a lane group
+    __shared__ double part_s[4][4][64];
+    __shared__ double best_s[4][16];
     const KvbSelectSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
     const uint32_t nb = (uint32_t)((s.n + kKvbBlock - 1) / kKvbBlock);
     const uint32_t parts = (nb + kKvbScoreBlocks - 1) / kKvbScoreBlocks;
@@ -47,67 +49,77 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const KvbSelectParams p
     const int h = (int)(pair % (uint32_t)p.kv_heads);
     const int64_t t = pair / (uint32_t)p.kv_heads;
     const uint32_t mine = (uint32_t)((s.n - s.T + t) / kKvbBlock);  // the token's own block
-    const int tid = (int)threadIdx.x, part = tid & 7, c0 = part * kPer;
-    const uint32_t b = (w - pair * parts) * kKvbScoreBlocks + (uint32_t)tid / 8;
+    const uint32_t b0 = (w - pair * parts) * kKvbScoreBlocks;
+    const int tid = (int)threadIdx.x, lane = tid & 63, li = lane & 15, wave = tid >> 6;
+    const int c0 = (wave * 4 + (lane >> 4)) * kSteps;  // the lane's channels, in both operands
     const int G = p.heads / p.kv_heads;
 
-    const uint8_t* q = static_cast<const uint8_t*>(p.q) + (s.t0 + t) * p.q_stride + (int64_t)h * G * D * 2;
-    float lof[kPer], hif[kPer];
-    {
-        const uint8_t* base = reinterpret_cast<const uint8_t*>(s.bounds) + ((int64_t)(b < nb ? b : nb - 1) * 2 * p.kv_heads + h) * D + c0;
-        const uint8_t* top = base + (int64_t)p.kv_heads * D;
-        #pragma unroll
-        for (int i = 0; i < kPer / 8; ++i) {
-            const u32x2 a = *reinterpret_cast<const u32x2*>(base + 8 * i), z = *reinterpret_cast<const u32x2*>(top + 8 * i);
-            #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const f32x2 a0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)a[k], false), a1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)a[k], true);
-                const f32x2 z0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)z[k], false), z1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)z[k], true);
-                #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    lof[8 * i + 4 * k + e] = a0[e];
-                    lof[8 * i + 4 * k + 2 + e] = a1[e];
-                    hif[8 * i + 4 * k + e] = z0[e];
-                    hif[8 * i + 4 * k + 2 + e] = z1[e];
-                }
-            }
-        }
+    // blocks past the last repeat it
+    const uint32_t b = b0 + (uint32_t)li < nb ? b0 + (uint32_t)li : nb - 1;
+    const global_ptr<uint8_t> lo = (global_ptr<uint8_t>)s.bounds + ((int64_t)b * 2 * p.kv_heads + h) * D + c0;
+    uint32_t low[kSteps / 4], high[kSteps / 4];
+    #pragma unroll
+    for (int i = 0; i < kSteps / 4; ++i) {
+        low[i] = *(global_ptr<uint32_t>)(lo + 4 * i);
+        high[i] = *(global_ptr<uint32_t>)(lo + (int64_t)p.kv_heads * D + 4 * i);
     }
     double best = -__builtin_inf();
     bool nan = false;
-    for (int g0 = 0; g0 < G; g0 += kHeads) {
-        const int heads = G - g0 < kHeads ? G - g0 : kHeads;
-        __syncthreads();
-        for (int i = tid; i < heads * D / 2; i += kThreads) {
-            const uint32_t u = *reinterpret_cast<const uint32_t*>(q + ((int64_t)g0 * D + 2 * i) * 2);
-            q_s[2 * i / D][2 * i % D] = __builtin_bit_cast(float, u << 16);
-            q_s[2 * i / D][2 * i % D + 1] = __builtin_bit_cast(float, u & 0xFFFF0000u);
+    for (int g0 = 0; g0 < G; g0 += 16) {
+        const int head = g0 + li < G ? g0 + li : G - 1;  // heads past the last repeat it
+        const uint8_t* q = static_cast<const uint8_t*>(p.q) + (s.t0 + t) * p.q_stride + (((int64_t)h * G + head) * D + c0) * 2;
+        uint32_t qs[kSteps / 2];
+        #pragma unroll
+        for (int i = 0; i < kSteps / 4; ++i) {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(q + 8 * i);
+            qs[2 * i] = x[0];
+            qs[2 * i + 1] = x[1];
         }
-        __syncthreads();
-        for (int g = 0; g < heads; ++g) {
-            double sum = 0.0;
+        f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+        #pragma unroll
+        for (int c = 0; c < kSteps; c += 2) {
+            const f32x2 l = c & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)low[c / 4], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)low[c / 4], false);
+            const f32x2 u = c & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)high[c / 4], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)high[c / 4], false);
             #pragma unroll
-            for (int c = 0; c < kPer; ++c) {
-                const float x = q_s[g][c0 + c];
-                sum = __builtin_fma((double)x, (double)(x < 0.0f ? lof[c] : hif[c]), sum);
+            for (int e = 0; e < 2; ++e) {
+                const float x = __builtin_bit_cast(float, e ? qs[c / 2] & 0xFFFF0000u : qs[c / 2] << 16);
+                // (a NaN goes into both parts)
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(x < 0.0f ? 0.0f : x), (double)u[e], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(x > 0.0f ? 0.0f : x), (double)l[e], acc, 0, 0, 0);
             }
-            #pragma unroll
-            for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor(sum, o);
-            nan |= sum != sum;
-            best = sum > best ? sum : best;
         }
+        if (g0) __syncthreads();
+        #pragma unroll
+        for (int r = 0; r < 4; ++r) part_s[wave][r][lane] = acc[r];
+        __syncthreads();
+        // accumulator r of all waves: some heads of block lane % 16; wave r sums it
+        const double sum = (part_s[0][wave][lane] + part_s[1][wave][lane]) + (part_s[2][wave][lane] + part_s[3][wave][lane]);
+        nan |= sum != sum;
+        best = sum > best ? sum : best;
     }
-    if (part == 0 && b < nb) {
-        const float scale = reinterpret_cast<const float*>(s.scales)[(int64_t)b * 2 * p.kv_heads + h];
-        uint64_t key = order_key(nan ? __builtin_inf() : best * (double)scale);
+    if (nan) best = __builtin_inf();
+    #pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+        const double x = __shfl_xor(best, o);
+        best = x > best ? x : best;
+    }
+    if (lane < 16) best_s[wave][li] = best;
+    __syncthreads();
+    if (tid < 16 && b0 + (uint32_t)tid < nb) {
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) best = best_s[i][tid] > best ? best_s[i][tid] : best;
+        const float scale = ((global_ptr<float>)s.scales)[(int64_t)b * 2 * p.kv_heads + h];
+        uint64_t key = order_key(best * (double)scale);
         if (b < (uint32_t)p.first || b + (uint32_t)p.last > mine) key = kMust;
         if (b > mine) key = kNever;
         p.keys[s.keys + pair * (uint64_t)nb + b] = key;
     }
 }
 
-__global__ __launch_bounds__(kThreads) void pick_kernel(const KvbSelectParams p) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void pick_kernel(const KvbSelectTable<N> p) {
     __shared__ uint64_t key_s[kKeysLds];
+    __shared__ uint64_t range_s[kThreads / 64][2];
     __shared__ uint32_t bins[256], found[2], waves[kThreads / 64];
     const int64_t tok = blockIdx.x / (uint32_t)p.kv_heads;
     const int h = (int)(blockIdx.x - tok * p.kv_heads);
@@ -123,19 +135,57 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const KvbSelectParams p)
         return;
     }
     const bool in_lds = count <= kKeysLds;
-    if (in_lds)
-        for (uint32_t i = tid; i < count; i += kThreads) key_s[i] = keys[i];
-    uint64_t prefix = 0;     // the bytes found so far, the rest zero
-    uint32_t need = n_sel;   // how many are still to be taken of the keys with these bytes
-    for (int shift = 56; shift >= 0; shift -= 8) {
+    // the highest and lowest key of those that the token need not have, and how many it has to
+    uint64_t low = ~0ull, high = 0;
+    uint32_t must = 0;
+    for (uint32_t i = tid; i < count; i += kThreads) {
+        const uint64_t k = keys[i];
+        if (in_lds) key_s[i] = k;
+        if (k == kMust) {
+            ++must;
+        } else {
+            low = k < low ? k : low;
+            high = k > high ? k : high;
+        }
+    }
+    #pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const uint64_t l = __shfl_xor(low, o), h64 = __shfl_xor(high, o);
+        low = l < low ? l : low;
+        high = h64 > high ? h64 : high;
+        must += __shfl_xor(must, o);
+    }
+    if ((tid & 63) == 0) {
+        range_s[tid / 64][0] = low;
+        range_s[tid / 64][1] = high;
+        waves[tid / 64] = must;
+    }
+    __syncthreads();
+    must = 0;
+    #pragma unroll
+    for (int i = 0; i < kThreads / 64; ++i) {
+        low = range_s[i][0] < low ? range_s[i][0] : low;
+        high = range_s[i][1] > high ? range_s[i][1] : high;
+        must += waves[i];
+    }
+    uint32_t need = n_sel - must;  // how many are still to be taken of the keys with the bits found so far
+    int open = low == high ? 0 : 64 - __builtin_clzll(low ^ high);  // bits not found yet
+    uint64_t prefix = open == 0 ? low : open == 64 ? 0 : low >> open << open;  // the bits found, the rest zero
+    if (need == 0) {  // those it has to have, and no others
+        prefix = kMust;
+        need = ~0u;
+        open = 0;
+    }
+    while (open > 0) {
+        const int width = open < 8 ? open : 8, shift = open - width;
         bins[tid] = 0;
         __syncthreads();
         for (uint32_t i = tid; i < count; i += kThreads) {
             const uint64_t k = in_lds ? key_s[i] : keys[i];
-            if (shift == 56 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&bins[k >> shift & 255], 1u);
+            if (k != kMust && (open == 64 || (k ^ prefix) >> open == 0)) atomicAdd(&bins[k >> shift & ((1u << width) - 1)], 1u);
         }
         __syncthreads();
-        // the byte d with  #(bytes > d) < need <= #(bytes >= d): thread tid looks at d = 255 - tid
+        // the digit d with  #(digits > d) < need <= #(digits >= d): thread tid looks at d = 255 - tid
         const uint32_t mine = bins[255 - tid];
         uint32_t upto = mine;  // inclusive sum over this thread and those before it
         #pragma unroll
@@ -153,56 +203,61 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const KvbSelectParams p)
         __syncthreads();
         prefix |= (uint64_t)found[0] << shift;
         need = found[1];
-        if (need == bins[found[0]]) {  // all keys with these bytes are taken
+        open = shift;
+        if (need == bins[found[0]]) {  // all keys with these bits are taken
             need = ~0u;
             break;
         }
         __syncthreads();  // the bins are read before they are cleared
     }
-    __syncthreads();
-    // ascending: every key above the bound, of those equal to it the first `need`
-    uint32_t done = 0, ties = 0;
-    for (uint32_t i0 = 0; i0 < count; i0 += kThreads) {
-        const uint32_t i = i0 + tid;
-        const uint64_t k = i < count ? (in_lds ? key_s[i] : keys[i]) : 0;
-        const bool equal = i < count && k == prefix;
-        const uint64_t eq = __ballot(equal);
-        const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(eq >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)eq, 0));
-        if ((tid & 63) == 0) waves[tid / 64] = (uint32_t)__builtin_popcountll(eq);
-        __syncthreads();
-        uint32_t tie = ties + below, all = 0;
-        for (uint32_t j = 0; j < kThreads / 64; ++j) {
-            if (j < tid / 64) tie += waves[j];
-            all += waves[j];
+    // ascending: every key above the bound, of those equal to it the first `need`; a thread
+    // takes a run of blocks
+    auto before = [&](uint32_t v) {  // the sum over the threads before this one
+        uint32_t upto = v;
+        #pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t x = __shfl_up(upto, o);
+            if ((int)(tid & 63) >= o) upto += x;
         }
-        ties += all;
-        const bool take = i < count && (k > prefix || (equal && tie < need));
-        const uint64_t tk = __ballot(take);
-        const uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(tk >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)tk, 0));
+        __syncthreads();  // what was in `waves` is read
+        if ((tid & 63) == 63) waves[tid / 64] = upto;
         __syncthreads();
-        if ((tid & 63) == 0) waves[tid / 64] = (uint32_t)__builtin_popcountll(tk);
-        __syncthreads();
-        uint32_t at = done + before;
-        for (uint32_t j = 0; j < kThreads / 64; ++j) {
-            if (j < tid / 64) at += waves[j];
-            done += waves[j];
-        }
-        if (take && at < n_sel) out[at] = (int32_t)i;
-        __syncthreads();
+        for (uint32_t i = 0; i < tid / 64; ++i) upto += waves[i];
+        return upto - v;
+    };
+    const uint32_t run = (count + kThreads - 1) / kThreads, i0 = tid * run < count ? tid * run : count;
+    const uint32_t i1 = i0 + run < count ? i0 + run : count;
+    uint32_t equal = 0, above = 0;
+    for (uint32_t i = i0; i < i1; ++i) {
+        const uint64_t k = in_lds ? key_s[i] : keys[i];
+        equal += k == prefix;
+        above += k > prefix;
     }
+    const uint32_t ties = before(equal);
+    uint32_t left = ties < need ? need - ties : 0;  // ties that this thread may still take
+    uint32_t at = before(above + (equal < left ? equal : left));
+    for (uint32_t i = i0; i < i1; ++i) {
+        const uint64_t k = in_lds ? key_s[i] : keys[i];
+        const bool tie = k == prefix && left > 0;
+        if (tie) --left;
+        if ((k > prefix || tie) && at < n_sel) out[at++] = (int32_t)i;
+    }
+}
+
+template <int D>
+hipError_t launch_score(const KvbSelectParams& p, hipStream_t stream) {
+    return launch_kvb<KvbSelectTable>(reinterpret_cast<const void*>(&score_kernel<D, kKvbFew>),
+                                      reinterpret_cast<const void*>(&score_kernel<D, KVB_MAX_SEQ>), dim3(p.wgs), dim3(kThreads), p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_kvb_select(const KvbSelectParams& p, hipStream_t stream) {
     if (p.wgs == 0) return hipSuccess;
-    const void* fn = p.d == 64    ? reinterpret_cast<const void*>(&score_kernel<64>)
-                     : p.d == 128 ? reinterpret_cast<const void*>(&score_kernel<128>)
-                                  : reinterpret_cast<const void*>(&score_kernel<256>);
-    const hipError_t e = launch_kernel(fn, dim3(p.wgs), dim3(kThreads), p, stream);
+    const hipError_t e = p.d == 64 ? launch_score<64>(p, stream) : p.d == 128 ? launch_score<128>(p, stream) : launch_score<256>(p, stream);
     if (e != hipSuccess) return e;
-    return launch_kernel(reinterpret_cast<const void*>(&pick_kernel), dim3((uint32_t)(p.tokens * p.kv_heads)), dim3(kThreads), p,
-                         stream);
+    return launch_kvb<KvbSelectTable>(reinterpret_cast<const void*>(&pick_kernel<kKvbFew>), reinterpret_cast<const void*>(&pick_kernel<KVB_MAX_SEQ>),
+                                      dim3((uint32_t)(p.tokens * p.kv_heads)), dim3(kThreads), p, stream);
 }
 
 }  // namespace cap
