@@ -57,6 +57,13 @@ __device__ inline int scale_exponent(float amax) {
     return amax > 0.0f ? (e < -100 ? -100 : e > 119 ? 119 : e) : -100;
 }
 
+// Two codes with +0 for -0 (what a small negative value rounds to).
+__device__ inline uint16_t one_zero(uint32_t w) {
+    if ((w & 0xFFu) == 0x80u) w &= 0xFF00u;
+    if ((w & 0xFF00u) == 0x8000u) w &= 0xFFu;
+    return (uint16_t)w;
+}
+
 constexpr int kThreads = 256;
 
 template <int D, int N>
@@ -200,11 +207,11 @@ __global__ __launch_bounds__(kThreads, 4) void append_kernel(const KvbAppendTabl
             const uint32_t hi = __builtin_bit_cast(uint32_t, ordered(__builtin_bit_cast(uint32_t, z)));
             float y[4] = {bits_f32(lo << 16), bits_f32(lo & 0xFFFF0000u), bits_f32(hi << 16), bits_f32(hi & 0xFFFF0000u)};
             #pragma unroll
-            for (int c = 0; c < 4; ++c)  // the sum makes one zero of the two; a NaN in a channel is both of its bounds
-                y[c] = nan_s[2 * tid + (c & 1)] ? __builtin_nanf("") : saturate(y[c] * mul) + 0.0f;
+            for (int c = 0; c < 4; ++c)  // a NaN in a channel is both of its bounds
+                y[c] = nan_s[2 * tid + (c & 1)] ? __builtin_nanf("") : saturate(y[c] * mul);
             uint8_t* bounds = reinterpret_cast<uint8_t*>(s.bounds) + (b * 2 * p.kv_heads + h) * D + 2 * tid;
-            *reinterpret_cast<uint16_t*>(bounds) = (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-            *reinterpret_cast<uint16_t*>(bounds + rowb) = (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], 0, false);
+            *reinterpret_cast<uint16_t*>(bounds) = one_zero((uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false));
+            *reinterpret_cast<uint16_t*>(bounds + rowb) = one_zero((uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], 0, false));
         }
     }
     // The rows of the block that is open after the append.  The workgroup that

@@ -3,19 +3,23 @@
 //
 // A workgroup of four waves takes 128 query rows of a KV head, 32 to a wave, and
 // walks the blocks; K and V codes of a block go through LDS, two buffers, one
-// barrier a block.  Both products run on 32x32x64 FP8 tiles straight from the
-// codes, with the power-of-two scales as the instruction's scale operands:
-//  * S^T = K Q^T: a bf16 query row as hi + lo / 16 of E4M3 (kvb_attend.hip); the
-//    scales of K and of lo cost nothing.
-//  * O^T = V^T P^T: the weights of a block are taken against the block's own
-//    highest score, rounded up to an integer c in log2 units, w = 2^(x - c + 8) in
-//    (0, 256], and split like Q: w = hi + lo / 16 with a relative error of 2^-8 at
-//    most, that of bf16, or 2^-22 of the block's largest weight where that is more.
-//    2^(c - m) is the instruction's scale of a row, an exact power of two; m is the
-//    c of the row's first block, raised only where a later one is 2^64 above: O and
-//    l are floating, so their reference need not be the running maximum.
-// Against bf16 operands that is the same matrix time (FP8 runs at twice the rate),
-// half the LDS traffic and no conversion of K and V.
+// barrier a block.
+//  * S^T = K Q^T on 32x32x16 bf16 tiles: the codes times their power-of-two scale are
+//    exact in bf16, converted once for the four waves on their way into LDS.  (FP8
+//    instructions with Q split in two take the same matrix time, but their sums lose
+//    what is small against the largest product: scores off by 1.6e-3 where a head's
+//    channels differ in size.)
+//  * O^T = V^T P^T on 32x32x64 FP8 tiles straight from the codes, with the scales as the
+//    instruction's scale operands.  The weights of a block are taken against the block's
+//    own highest score, rounded up to an integer c in log2 units, w = 2^(x - c + 8) in
+//    (0, 256], and split into two E4M3 rows, w = hi + lo / 16 (relative 2^-8 at most, that
+//    of bf16, or 2^-21 of the block's largest weight where that is more); the
+//    instruction's sums lose 2^-12 of the sum of the products' magnitudes at most.
+//    2^(c - m) is the instruction's scale of a row, an exact power of two; m is the c of
+//    the row's first block, raised only where a later one is 2^64 above: O and l are
+//    floating, so their reference need not be the running maximum.
+//    Against bf16 operands that is the same matrix time (FP8 runs at twice the rate),
+//    half the LDS traffic and no conversion of V.
 //
 // One wave to a SIMD has registers for 32 rows of 256 channels, so the wave itself
 // keeps the matrix pipe busy: half of a block's softmax stands between the matrix
@@ -35,6 +39,7 @@
 namespace cap {
 namespace {
 
+using dev::bf16x8;
 using dev::rsrc_t;
 using dev::u32x4;
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -68,15 +73,24 @@ __device__ inline void split4(const float* y, int& hi, int& lo) {
     lo = __builtin_bit_cast(int, r);
 }
 
-__device__ inline f32x16 mma(const i32x8& a, const i32x8& b, const f32x16& c, int sa, int sb) {
+__device__ inline f32x16 mma8(const i32x8& a, const i32x8& b, const f32x16& c, int sa, int sb) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
 }
+__device__ inline f32x16 mma16(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// Eight codes times a power of two as bf16, exact.
+__device__ inline u32x4 decode8(uint32_t w0, uint32_t w1, float scale) {
+    return (u32x4){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true))};
+}
 
-// Where the 16-byte unit `u` of row `key` lies in its row: the reads of K take
-// one unit of eight neighbouring rows at a time, those of V of rows i and 8 + i
+// Where the 16-byte unit `u` of row `key` lies in its row (u ^ the value): the reads of K
+// take one unit of eight neighbouring rows at a time, those of V of rows i and 8 + i
 // (i = 0..3 or 4..7).
-template <int D>
-__device__ inline int swizzle_k(int key) { return D == 64 ? key >> 1 & 3 : key & 7; }
+__device__ inline int swizzle_k(int key) { return key & 7; }
 template <int D>
 __device__ inline int swizzle_v(int key) {
     return D == 64 ? (key >> 1 & 1) | (key >> 3 & 1) << 1 : (key & 3) | (key >> 3 & 1) << 2;
@@ -84,8 +98,8 @@ __device__ inline int swizzle_v(int key) {
 
 template <int D>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(const KvbAttendParams p) {
-    constexpr int NJ = D / 64, NT = D / 32, kUnits = D / 16, kRows = kThreads / kUnits, kLoads = kKvbBlock / kRows;
-    __shared__ __attribute__((aligned(1024))) uint8_t k_s[2][kKvbBlock * D];
+    constexpr int NJ = D / 32, NT = D / 32, kUnits = D / 16, kRows = kThreads / kUnits, kLoads = kKvbBlock / kRows;
+    __shared__ __attribute__((aligned(1024))) uint8_t k_s[2][kKvbBlock * D * 2];  // bf16
     __shared__ __attribute__((aligned(1024))) uint8_t v_s[3][kKvbBlock * D];
     __shared__ int nan_s[3];
 
@@ -106,45 +120,24 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     const int64_t wpos0 = before + (wrow0 < last ? wrow0 : last) / G;
     const int64_t tpos0 = before + row0 / G, tpos1 = before + (row0 + 127 < last ? row0 + 127 : last) / G;
 
-    i32x8 qh[NJ], ql[NJ];
-    float f;  // from the products to log2 units
+    // channels 16 s + 8 half .. + 7 of the lane's row; scores in log2 units are the products times f > 0
+    bf16x8 q[D / 16];
+    const float f = p.scale_log2 == 0.0f ? 1.0f : __builtin_fabsf(p.scale_log2);
     {
         const uint8_t* src = static_cast<const uint8_t*>(p.q) + (s.t0 + token) * p.q_stride + ((int64_t)h * G + row % G) * D * 2;
-        u32x4 x[NJ][4];
-        float amax = 0.0f;
         #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-            #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                x[j][c] = *reinterpret_cast<const u32x4*>(src + (64 * j + 32 * (c / 2) + 16 * half + 8 * (c % 2)) * 2);
+        for (int i = 0; i < D / 16; ++i) {
+            u32x4 x = *reinterpret_cast<const u32x4*>(src + (16 * i + 8 * half) * 2);
+            if (p.scale_log2 <= 0.0f) {  // a negative scale turns the row's signs, zero makes it zero (but not its NaN)
                 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    amax = __builtin_fmaxf(amax, __builtin_fmaxf(__builtin_fabsf(bits_f32(x[j][c][k] << 16)),
-                                                                 __builtin_fabsf(bits_f32(x[j][c][k] & 0xFFFF0000u))));
-            }
-        amax = pair_max(amax);
-        int e = (int)(f32_bits(amax) >> 23) - 127 - 7;  // amax 2^-e in [128, 256)
-        e = e < -100 ? -100 : e;
-        // an infinity stays one, and becomes NaN; f is positive
-        const float sign = p.scale_log2 < 0.0f ? -1.0f : p.scale_log2 > 0.0f ? 1.0f : 0.0f;
-        const float mul = bits_f32((uint32_t)(127 - e) << 23) * sign;
-        f = sign == 0.0f ? 1.0f : bits_f32((uint32_t)(127 + e) << 23) * __builtin_fabsf(p.scale_log2);
-        #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-            #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                float y[4];
-                #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t u = x[j][c / 2][2 * (c % 2) + k];
-                    y[2 * k] = bits_f32(u << 16) * mul;
-                    y[2 * k + 1] = bits_f32(u & 0xFFFF0000u) * mul;
+                for (int k = 0; k < 4; ++k) {
+                    const float a = bits_f32(x[k] << 16), b = bits_f32(x[k] & 0xFFFF0000u);
+                    const float by = p.scale_log2 < 0.0f ? -1.0f : 0.0f;
+                    x[k] = f32_bits(a * by) >> 16 | (f32_bits(b * by) & 0xFFFF0000u);
                 }
-                int a, b;
-                split4(y, a, b);
-                qh[j][c] = a;
-                ql[j][c] = b;
             }
+            q[i] = __builtin_bit_cast(bf16x8, x);
+        }
     }
 
     const int rowb = p.kv_heads * D;
@@ -163,11 +156,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
         #pragma unroll
         for (int i = 0; i < kLoads; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, svoff, i * kRows * rowb, 0);
     };
-    auto stage_k = [&](int buf) {
+    auto stage_k = [&](int buf, float scale) {
         #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int key = srow + i * kRows;
-            *reinterpret_cast<u32x4*>(&k_s[buf][key * D + 16 * (sunit ^ swizzle_k<D>(key))]) = ks[i];
+            uint8_t* dst = &k_s[buf][key * 2 * D];
+            *reinterpret_cast<u32x4*>(dst + 16 * ((2 * sunit) ^ swizzle_k(key))) = decode8(ks[i][0], ks[i][1], scale);
+            *reinterpret_cast<u32x4*>(dst + 16 * ((2 * sunit + 1) ^ swizzle_k(key))) = decode8(ks[i][2], ks[i][3], scale);
         }
     };
     auto stage_v = [&](int b, int buf) {
@@ -191,22 +186,23 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
             *reinterpret_cast<u32x4*>(&v_s[buf][key * D + 16 * (sunit ^ swizzle_v<D>(key))]) = vs[i];
         }
     };
-    // Exponents of the scales as the instruction takes them, of 64 blocks from e0 on: lane i has block e0 + i.
-    int e0 = begin, k_exps = 0, v_exps = 0;
-    auto load_exponents = [&]() {
+    // The scales of 64 blocks from e0 on: lane i has those of block e0 + i.
+    int e0 = begin;
+    uint32_t k_scales = 0, v_scales = 0;
+    auto load_scales = [&]() {
         const int64_t at = (int64_t)((e0 + lane < end ? e0 + lane : end - 1) * 2) * p.kv_heads + h;
-        k_exps = (int)(sc[at] >> 23);
-        v_exps = (int)(sc[at + p.kv_heads] >> 23);
+        k_scales = sc[at];
+        v_scales = sc[at + p.kv_heads];
     };
+    auto k_scale = [&](int b) { return bits_f32((uint32_t)__builtin_amdgcn_readlane((int)k_scales, b - e0)); };
+    auto v_exponent = [&](int b) { return __builtin_amdgcn_readlane((int)v_scales, b - e0) >> 23; };  // as the instruction takes it
 
     // addresses of a lane's reads; units and rows come in by xor and offset
-    const int kaddr = (lane & 31) * D + 16 * (half ^ swizzle_k<D>(lane & 31));
+    const int kaddr = (lane & 31) * 2 * D + 16 * (half ^ swizzle_k(lane & 31));
     const int vkey = 4 * half + ((lane & 15) >> 1 & 3) + 8 * ((lane & 15) >> 3);
     const int vaddr = vkey * D + 16 * ((lane >> 4 & 1) ^ swizzle_v<D>(vkey)) + 8 * (lane & 1);
-    auto read_k = [&](int buf, int t, int j) {  // keys 32 t .. + 31, channels 64 j .. + 63
-        const u32x4 a = *reinterpret_cast<const u32x4*>(&k_s[buf][(kaddr ^ (64 * j)) + t * 32 * D]);
-        const u32x4 b = *reinterpret_cast<const u32x4*>(&k_s[buf][(kaddr ^ (64 * j + 32)) + t * 32 * D]);
-        return (i32x8){(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+    auto read_k = [&](int buf, int t, int i) {  // keys 32 t .. + 31, channels 16 i .. + 15
+        return *reinterpret_cast<const bf16x8*>(&k_s[buf][(kaddr ^ (32 * i)) + t * 64 * D]);
     };
     auto read_v = [&](int buf, int i) {  // channels 32 i .. + 31
         i32x8 a;
@@ -263,31 +259,26 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     // Blocks past the end repeat the last one.
     if (tid < 3) nan_s[tid] = -1;
     auto clamp = [&](int b) { return b < end ? b : end - 1; };
-    int ke = 127, ve = 127;  // exponents of K of b + 1 and V of b
+    int ve = 127;  // exponent of V's scale of b
     if (begin < end) {
         fetch(kb, begin, ks);
         fetch(vb, begin, vs);
-        load_exponents();
+        load_scales();
         dev::lds_barrier();
-        stage_k(0);
+        stage_k(0, k_scale(begin));
         stage_v(begin, 0);
         fetch(kb, clamp(begin + 1), ks);
         fetch(vb, clamp(begin + 1), vs);
-        ke = __builtin_amdgcn_readlane(k_exps, 0);
-        ve = __builtin_amdgcn_readlane(v_exps, 0);
+        ve = v_exponent(begin);
         dev::lds_barrier();
+        x[0] = (f32x16){};
+        x[1] = (f32x16){};
         #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            x[t] = (f32x16){};
-            #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const i32x8 a = read_k(0, t, j);
-                x[t] = mma(a, qh[j], x[t], ke, 127);
-                x[t] = mma(a, ql[j], x[t], ke, 123);
-            }
+        for (int i = 0; i < D / 16; ++i) {
+            x[0] = mma16(read_k(0, 0, i), q[i], x[0]);
+            x[1] = mma16(read_k(0, 1, i), q[i], x[1]);
         }
-        ke = __builtin_amdgcn_readlane(k_exps, 1);
-        stage_k(1);
+        stage_k(1, k_scale(clamp(begin + 1)));
         stage_v(clamp(begin + 1), 1);
         fetch(kb, clamp(begin + 2), ks);
         fetch(vb, clamp(begin + 2), vs);
@@ -309,21 +300,22 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
             #pragma unroll
             for (int i = 0; i < NT; ++i) asm volatile("" : "+a"(acc[i]));
         }
-        const int next_ve = __builtin_amdgcn_readlane(v_exps, b + 1 - e0);
-        if (b + 2 - e0 >= 64) {
+        const int next_ve = v_exponent(clamp(b + 1));
+        if (b + 2 - e0 >= 64 && b + 2 < end) {
             e0 = b + 2;
-            load_exponents();
+            load_scales();
         }
-        const int next_ke = __builtin_amdgcn_readlane(k_exps, b + 2 - e0);
+        const float next_scale = k_scale(clamp(b + 2));
         i32x8 v0, v1;
         {
-            i32x8 k0 = read_k(kbuf ^ 1, 0, 0), k1 = read_k(kbuf ^ 1, 1, 0);
+            bf16x8 k[4], next[4];
+            #pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = read_k(kbuf ^ 1, i & 1, i >> 1);
             #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                i32x8 n0, n1;
                 if (j + 1 < NJ) {
-                    n0 = read_k(kbuf ^ 1, 0, j + 1);
-                    n1 = read_k(kbuf ^ 1, 1, j + 1);
+                    #pragma unroll
+                    for (int i = 0; i < 4; ++i) next[i] = read_k(kbuf ^ 1, i & 1, 2 * (j + 1) + (i >> 1));
                 } else {
                     v0 = read_v(vbuf, 0);
                     v1 = read_v(vbuf, 1);
@@ -332,20 +324,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
                 for (int i = 0; i < 4; ++i) {
                     const int step = 4 * j + i, steps = 4 * NJ;
                     if (step < 2) y[step] = (f32x16){};
-                    y[i & 1] = mma(i & 1 ? k1 : k0, i < 2 ? qh[j] : ql[j], y[i & 1], ke, i < 2 ? 127 : 123);
+                    y[i & 1] = mma16(k[i], q[2 * j + (i >> 1)], y[i & 1]);
                     #pragma unroll
-                    for (int q = 4 + step * 4 / steps; q < 4 + (step + 1) * 4 / steps; ++q) {
+                    for (int w = 4 + step * 4 / steps; w < 4 + (step + 1) * 4 / steps; ++w) {
                         int a, d;
-                        weights(q, x, a, d);
-                        ph[q] = a;
-                        pl[q] = d;
+                        weights(w, x, a, d);
+                        ph[w] = a;
+                        pl[w] = d;
                     }
-                    if (step == steps - 2) stage_k(kbuf);
+                    if (step == steps - 2) stage_k(kbuf, next_scale);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (j + 1 < NJ) {
-                    k0 = n0;
-                    k1 = n1;
+                    #pragma unroll
+                    for (int i = 0; i < 4; ++i) k[i] = next[i];
                 }
             }
         }
@@ -382,7 +374,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
             #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int step = 2 * i + k, steps = 2 * NT;
-                acc[i + (k & 1)] = mma(k & 1 ? v1 : v0, k < 2 ? ph : pl, acc[i + (k & 1)], ve, k < 2 ? se : sl);
+                acc[i + (k & 1)] = mma8(k & 1 ? v1 : v0, k < 2 ? ph : pl, acc[i + (k & 1)], ve, k < 2 ? se : sl);
                 if (step == (NT > 2 ? 1 : 0)) {  // ahead of its first use below
                     x[0] = y[0];
                     x[1] = y[1];
@@ -412,7 +404,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
         asm volatile("" : "+v"(sum), "+v"(nh), "+v"(nl));
         {
             const int64_t r0 = (int64_t)b * kKvbBlock;
-            if (r0 + kKvbBlock - 1 > wpos0 && nan_s[vbuf] == b) {
+            if (r0 + kKvbBlock - 1 > tpos0 && nan_s[vbuf] == b) {
                 for (int t = 0; t < kKvbBlock; ++t) {
                     if (r0 + t >= s.n) break;
                     #pragma unroll
@@ -432,7 +424,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
             ph[q] = nh[q];
             pl[q] = nl[q];
         }
-        ke = next_ke;
         ve = next_ve;
         vbuf = vbuf == 2 ? 0 : vbuf + 1;
     }

@@ -1,0 +1,562 @@
+"""The block-scaled FP8 KV cache on the GPU (through the C ABI) against its plain forms in 64 bits: append bit for bit,
+attention within bounds that follow from its roundings, selection exactly; sizes and masks where they can go wrong,
+streams, graphs, far offsets, and a whole session with a capsule."""
+import numpy as np
+import pytest
+import torch
+
+import kvb_plain as P
+import paper_2606_20537_amd as cap
+
+pytestmark = pytest.mark.gpu
+
+BLOCK = cap.KVB_BLOCK
+E4M3 = torch.float8_e4m3fn
+CANARY = 0x5A
+
+
+class Caches:
+    """Caches of several sequences; unwritten bytes hold a canary, or NaN codes."""
+
+    def __init__(self, rows, hkv, d, fill=CANARY, bounds=True, device="cuda"):
+        self.rows, self.hkv, self.d = rows, hkv, d
+        nb = [r // BLOCK for r in rows]
+        self.k, self.v = ([torch.full((r, hkv, d), fill, dtype=torch.uint8, device=device) for r in rows] for _ in range(2))
+        self.scales = [torch.full((b, 2, hkv), -3.0, device=device) for b in nb]
+        self.bounds = [torch.full((b, 2, hkv, d), fill, dtype=torch.uint8, device=device) for b in nb] if bounds else [None] * len(rows)
+        self.open = [torch.full((2, BLOCK, hkv, d), float("nan"), dtype=torch.bfloat16, device=device) for _ in rows]
+
+    def table(self, n, T):
+        return cap.kvb_seqs([(self.k[i], self.v[i], self.scales[i], self.bounds[i], self.open[i], self.rows[i], n[i], T[i])
+                             for i in range(len(n))])
+
+    def all(self):
+        return [x for part in (self.k, self.v, self.scales, self.bounds, self.open) for x in part if x is not None]
+
+
+def values(codes):
+    return codes.view(E4M3).double().cpu().numpy()
+
+
+def normal(seed, *shape, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * scale).bfloat16()
+
+
+def up(n):
+    return -(-n // BLOCK) * BLOCK
+
+
+def check_cache(c, i, k, v):
+    """Cache i holds exactly rows k, v [n, hkv, d] (on the host), and nothing else was written."""
+    n = k.shape[0]
+    for side, (codes, x) in enumerate(((c.k[i], k), (c.v[i], v))):
+        want, scales, bounds = P.cache(x.double().numpy())
+        got = values(codes[:n])
+        assert np.array_equal(got, want, equal_nan=True)
+        nb = scales.shape[0]
+        assert np.array_equal(c.scales[i][:nb, side].double().cpu().numpy(), scales)
+        assert (c.scales[i][nb:, side] == -3.0).all() and (codes[n:] == CANARY).all()
+        if side == 0 and c.bounds[i] is not None:
+            b = c.bounds[i][:nb]
+            assert np.array_equal(values(b), bounds, equal_nan=True)
+            assert not (b == 0x80).any()  # one zero only
+            assert (c.bounds[i][nb:] == CANARY).all()
+        tail = n % BLOCK
+        assert torch.equal(c.open[i][side, :tail].cpu().view(torch.int16), x[n - tail:].view(torch.int16))
+
+
+def append(c, n0, n1, ks, vs, **kw):
+    """Rows [n0, n1) of each sequence's ks, vs enter its cache, in one call."""
+    T = [b - a for a, b in zip(n0, n1)]
+    pack = lambda xs: torch.cat([x[a:b] for x, a, b in zip(xs, n0, n1)]).cuda()
+    cap.kvb_append(c.table(n1, T), pack(ks), pack(vs), **kw)
+
+
+# ----------------------------------------------------------------- append --
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("hkv", [1, 3])
+@pytest.mark.parametrize("cuts", [(1,), (64,), (65,), (1, 2, 63, 64, 65), (40, 70, 128, 129, 200), (63, 191, 192, 193, 319)])
+def test_append(d, hkv, cuts):
+    n = cuts[-1]
+    c = Caches([up(n) + BLOCK], hkv, d)
+    k, v = normal(d + n, n, hkv, d, scale=3.0), normal(d + n + 1, n, hkv, d, scale=1e-3)
+    k[::7] *= 100.0
+    for a, b in zip((0,) + cuts, cuts):
+        append(c, [a], [b], [k], [v])
+        check_cache(c, 0, k[:b], v[:b])
+
+
+def test_append_special_values():
+    """Zeros, a block of zeros, infinities, NaN, the smallest and largest numbers, values halfway between codes."""
+    n, hkv, d = 330, 2, 64
+    k, v = normal(1, n, hkv, d), normal(2, n, hkv, d)
+    k[0:64, 0] = 0.0
+    k[64:128, 0, 3] = -0.0
+    k[70, 0, 5], k[71, 0, 6], k[72, 0, 7], k[73, 0, 8] = float("inf"), -float("inf"), float("nan"), -float("nan")
+    k[74:76, 1, :] = float("inf")
+    k[130, 1, :] = 3.3e38
+    k[200:210] = 1e-39
+    v[0:64, 1] = float("nan")
+    v[128:192] *= 1e-38
+    v[192:256] = (torch.arange(64 * 2 * 64).view(64, 2, 64) % 256 - 128).bfloat16() / 2.0
+    v[320, 0, 0], v[325, 1, 9] = float("nan"), float("inf")
+    for cuts in ((330,), (100, 321, 330), (70, 72, 73, 74, 330)):
+        c = Caches([384], hkv, d)
+        for a, b in zip((0,) + cuts, cuts):
+            append(c, [a], [b], [k], [v])
+        check_cache(c, 0, k, v)
+
+
+def test_append_pieces_give_the_same_bytes():
+    n, hkv, d = 500, 4, 128
+    k, v = normal(5, n, hkv, d), normal(6, n, hkv, d)
+    k[::97] *= 50.0
+    whole = Caches([512], hkv, d)
+    append(whole, [0], [n], [k], [v])
+    rng = np.random.default_rng(0)
+    for _ in range(4):
+        cuts = sorted(set(rng.integers(1, n, 12).tolist())) + [n]
+        c = Caches([512], hkv, d)
+        for a, b in zip([0] + cuts, cuts):
+            append(c, [a], [b], [k], [v])
+        for x, y in zip(c.all()[:4], whole.all()[:4]):
+            assert torch.equal(x, y)
+
+
+def test_append_after_going_back():
+    """Rejected draft tokens leave no trace in the block's scale and bounds; the same call twice changes nothing."""
+    hkv, d = 2, 64
+    k, v = normal(7, 100, hkv, d), normal(8, 100, hkv, d)
+    c = Caches([128], hkv, d)
+    append(c, [0], [80], [k], [v])
+    append(c, [80], [84], [k * 1000], [v * 1000])
+    append(c, [80], [81], [k], [v])
+    c.k[0][81:], c.v[0][81:] = CANARY, CANARY  # rows of the rejected tokens
+    check_cache(c, 0, k[:81], v[:81])
+    append(c, [80], [81], [k], [v])
+    check_cache(c, 0, k[:81], v[:81])
+
+
+def test_append_ragged_strided_without_bounds():
+    """Views of a fused projection, sequences of their own lengths with none and one token among them, no bounds."""
+    hkv, d = 2, 128
+    n0, n1 = [0, 63, 70, 5, 128, 200], [130, 64, 70, 6, 193, 200]
+    ks, vs = [normal(20 + i, 200, hkv, d) for i in range(6)], [normal(40 + i, 200, hkv, d) for i in range(6)]
+    c = Caches([256, 64, 128, 64, 256, 256], hkv, d, bounds=False)
+    append(c, [0] * 6, n0, ks, vs)
+    fused = torch.cat([torch.cat([torch.full((b - a, 3, d), 9.0).bfloat16(), k[a:b], v[a:b]], 1) for a, b, k, v in zip(n0, n1, ks, vs)]).cuda()
+    cap.kvb_append(c.table(n1, [b - a for a, b in zip(n0, n1)]), fused[:, 3:5], fused[:, 5:7])
+    for i in range(6):
+        check_cache(c, i, ks[i][:n1[i]], vs[i][:n1[i]])
+
+
+def test_append_64_sequences():
+    hkv, d = 1, 64
+    n0, n1 = [i for i in range(64)], [2 * i + 1 for i in range(64)]
+    ks, vs = [normal(100 + i, 130, hkv, d) for i in range(64)], [normal(200 + i, 130, hkv, d) for i in range(64)]
+    c = Caches([up(b) for b in n1], hkv, d)
+    append(c, [0] * 64, n0, ks, vs)
+    append(c, n0, n1, ks, vs)
+    for i in range(64):
+        check_cache(c, i, ks[i][:n1[i]], vs[i][:n1[i]])
+
+
+# ----------------------------------------------------------------- attend --
+def filled(n, hkv, d, seed, fill=0x7F, spread=True):
+    """Caches with n[i] rows, the rest NaN codes; the rows as the codes hold them, on the host."""
+    c = Caches([up(m) + BLOCK for m in n], hkv, d, fill)
+    ks, vs = [], []
+    for i, m in enumerate(n):
+        k, v = normal(seed + i, m, hkv, d), normal(seed + 1000 + i, m, hkv, d)
+        if spread:
+            k, v = k * torch.exp(torch.randn(1, hkv, d, generator=torch.Generator().manual_seed(seed))).bfloat16(), v + 0.5
+        ks.append(k)
+        vs.append(v)
+    if sum(n):
+        append(c, [0] * len(n), n, ks, vs)
+    return c, *reread(c, n)
+
+
+def reread(c, n):
+    out = []
+    for codes, side in ((c.k, 0), (c.v, 1)):
+        out.append([values(x[:m]) * s[:, side].double().cpu().numpy().repeat(BLOCK, 0)[:m, :, None] for x, s, m in zip(codes, c.scales, n)])
+    return out
+
+
+def run_attend(c, n, T, q, scale, idx=None, lse=True, **kw):
+    o = torch.full(q.shape, 77.0, dtype=torch.bfloat16, device="cuda")
+    l = torch.full(q.shape[:2], 77.0, device="cuda") if lse else None
+    cap.kvb_attend(c.table(n, T), q, o, kv_heads=c.hkv, scale=scale, lse=l, idx=idx, **kw)
+    return o, l
+
+
+def check_attend(c, ks, vs, n, T, q, scale, o, lse, idx=None, rows=None):
+    """Every output row, or `rows` of them chosen at random, against the plain form."""
+    G = q.shape[1] // c.hkv
+    fp8 = idx is None and max(T) * G > 64
+    qh, oh, lh = q.double().cpu().numpy(), o.double().cpu().numpy(), lse.double().cpu().numpy()
+    at = [(i, t) for i in range(len(n)) for t in range(T[i])]
+    todo = [(x, h) for x in range(len(at)) for h in range(q.shape[1])]
+    if rows and len(todo) > rows:
+        rng = np.random.default_rng(1)
+        todo = [todo[j] for j in sorted(set(rng.integers(0, len(todo), rows).tolist()) | {0, len(todo) - 1})]
+    for x, h in todo:
+        i, t = at[x]
+        g = h // G
+        listed = None if idx is None else idx[x, g].cpu().tolist()
+        plain = P.attend(qh[x, h], ks[i][:, g], vs[i][:, g], scale, n[i] - T[i] + t, listed)
+        assert P.close(oh[x, h], lh[x, h], plain, c.d, fp8), (i, t, h, np.abs(oh[x, h] - plain[0]).max(), lh[x, h], plain[1])
+
+
+# lengths of one to a few blocks, one run and several, tiles of 16 rows (few queries) and of 128
+SHAPES = [([1], [1]), ([2], [2]), ([63], [1]), ([64], [1]), ([65], [3]), ([200], [1]), ([1000], [1]), ([3000], [2]),
+          ([70], [70]), ([129], [64]), ([300], [300]), ([1500], [40]), ([1, 64, 700, 65], [1, 2, 1, 3]), ([0, 5, 200], [0, 0, 1]),
+          ([400, 30, 130], [100, 1, 130])]
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("hkv, G", [(2, 1), (1, 8), (2, 5), (1, 17)])
+@pytest.mark.parametrize("n, T", SHAPES)
+def test_attend(d, hkv, G, n, T):
+    c, ks, vs = filled(n, hkv, d, seed=d + G)
+    q = normal(3, sum(T), hkv * G, d).cuda()
+    o, lse = run_attend(c, n, T, q, d ** -0.5)
+    check_attend(c, ks, vs, n, T, q, d ** -0.5, o, lse, rows=150)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+@pytest.mark.parametrize("T", [1, 60])
+def test_attend_scales(scale, T):
+    c, ks, vs = filled([200], 1, 64, seed=11, spread=False)
+    q = normal(4, T, 4, 64).cuda()
+    o, lse = run_attend(c, [200], [T], q, scale)
+    check_attend(c, ks, vs, [200], [T], q, scale, o, lse)
+
+
+@pytest.mark.parametrize("T", [1, 90])
+def test_attend_peaks_and_small_weights(T):
+    """One key far above the rest (a thousand equal weights of 2^-20 still count), and blocks that rise by more than 2^64."""
+    d, n = 64, 1100
+    k, v = torch.zeros(n, 1, d).bfloat16(), normal(5, n, 1, d)
+    k[3, 0, 0] = 14.0
+    c = Caches([up(n)], 1, d)
+    append(c, [0], [n], [k], [v])
+    q = torch.zeros(T, 1, d).bfloat16().cuda()
+    q[..., 0] = 1.0
+    ks, vs = reread(c, [n])
+    o, lse = run_attend(c, [n], [T], q, 1.0)
+    check_attend(c, ks, vs, [n], [T], q, 1.0, o, lse)
+    k[:, 0, 0] = (torch.arange(n) // 64 * 60).bfloat16()  # 87 in log2 units from block to block
+    for kk in (k, k.flip(0)):
+        append(c, [0], [n], [kk], [v])
+        ks, vs = reread(c, [n])
+        o, lse = run_attend(c, [n], [T], q, 1.0)
+        check_attend(c, ks, vs, [n], [T], q, 1.0, o, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n, T", [(130, 3), (200, 150), (700, 200), (64, 64), (5, 5)])
+def test_nan_and_infinities_stay_where_they_are_seen(d, n, T):
+    """A NaN in V or K reaches the tokens that see it and no earlier one; NaN queries their own row only."""
+    hkv, G = 1, 3
+    k, v = normal(31, n, hkv, d), normal(32, n, hkv, d)
+    first = n - T
+    bad_v, bad_k = [first + T // 2, n - 1], first + (T * 3) // 4
+    for r in bad_v:
+        v[r, 0, r % d] = float("nan")
+    k[bad_k, 0, 1] = float("nan")
+    v[n // 2, 0, 7] = float("inf")  # saturates
+    c = Caches([up(n)], hkv, d, 0xFF)
+    append(c, [0], [n], [k], [v])
+    ks, vs = reread(c, [n])
+    q = normal(33, T, G, d)
+    if T > 4:
+        q[1, 1, 0], q[2, 2, 5] = float("nan"), float("inf")
+    q = q.cuda()
+    o, lse = run_attend(c, [n], [T], q, d ** -0.5)
+    oh, lh = o.double().cpu().numpy(), lse.double().cpu().numpy()
+    for t in range(T):
+        for h in range(G):
+            row = q[t, h].double().cpu().numpy()
+            if not np.isfinite(row).all() or first + t >= bad_k:
+                assert np.isnan(oh[t, h]).all() and np.isnan(lh[t, h])
+                continue
+            plain = P.attend(row, ks[0][:, 0], np.nan_to_num(vs[0][:, 0]), d ** -0.5, first + t)
+            nan = np.isnan(vs[0][:first + t + 1, 0]).any(0)
+            assert np.array_equal(np.isnan(oh[t, h]), nan), (t, h)
+            assert P.close(np.where(nan, plain[0], oh[t, h]), lh[t, h], plain, d, T * G > 64)
+
+
+def test_attend_strided_queries_no_lse_and_64_sequences():
+    hkv, G, d = 1, 2, 64
+    n, T = [3 * i + 1 for i in range(64)], [1 + i % 3 if i else 1 for i in range(64)]
+    c, ks, vs = filled(n, hkv, d, seed=50)
+    fused = normal(51, sum(T), 5, d).cuda()
+    q = fused[:, 1:3]
+    o, lse = run_attend(c, n, T, q, 0.1)
+    check_attend(c, ks, vs, n, T, q, 0.1, o, lse)
+    o2, _ = run_attend(c, n, T, q.contiguous(), 0.1, lse=False)
+    assert torch.equal(o, o2)
+
+
+# long caches in several runs, whole prefills of uneven sizes
+@pytest.mark.parametrize("n, T, hkv, G, d", [([20000], [1], 2, 8, 256), ([9000, 333, 64], [1, 1, 1], 4, 2, 128), ([5000], [33], 1, 2, 64),
+                                             ([2111], [2111], 2, 4, 128), ([4500], [161], 2, 8, 256), ([1999], [1300], 1, 3, 64)])
+def test_attend_long(n, T, hkv, G, d):
+    c, ks, vs = filled(n, hkv, d, seed=60)
+    q = normal(61, sum(T), hkv * G, d).cuda()
+    o, lse = run_attend(c, n, T, q, d ** -0.5)
+    check_attend(c, ks, vs, n, T, q, d ** -0.5, o, lse, rows=100)
+    again, _ = run_attend(c, n, T, q, d ** -0.5)
+    assert torch.equal(o, again)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G", [1, 8, 20])
+def test_attend_lists(d, G):
+    """Block lists with holes, blocks behind the token, numbers out of range, repetitions, nothing at all."""
+    n, T, hkv, n_sel = [700, 64, 130], [3, 1, 2], 2, 7
+    c, ks, vs = filled(n, hkv, d, seed=70)
+    q = normal(71, sum(T), hkv * G, d).cuda()
+    rng = np.random.default_rng(2)
+    idx = rng.integers(-2, 12, (sum(T), hkv, n_sel)).astype(np.int32)
+    idx[0, 0] = -1
+    idx[1, 1] = [2, 2, 0, -1, 2, 0, 1]
+    idx[3, 0] = [1 << 30, -(1 << 31), 5, 1, 1, 2, (1 << 31) - 1]  # one block of its own, none of it listed
+    idx = torch.from_numpy(idx).cuda()
+    o, lse = run_attend(c, n, T, q, d ** -0.5, idx)
+    check_attend(c, ks, vs, n, T, q, d ** -0.5, o, lse, idx)
+    assert not o[0, :G].any() and (lse[0, :G] == -np.inf).all() and not o[3, :G].any()
+    full = torch.arange(12, dtype=torch.int32, device="cuda").expand(sum(T), hkv, 12).contiguous()
+    o, lse = run_attend(c, n, T, q, d ** -0.5, full)
+    check_attend(c, ks, vs, n, T, q, d ** -0.5, o, lse)
+
+
+def test_attend_long_list():
+    n, d = [64 * 150], 64
+    c, ks, vs = filled(n, 1, d, seed=75)
+    q = normal(76, 1, 2, d).cuda()
+    idx = torch.arange(149, -1, -1, dtype=torch.int32, device="cuda").view(1, 1, 150)
+    o, lse = run_attend(c, n, [1], q, 0.1, idx)
+    check_attend(c, ks, vs, n, [1], q, 0.1, o, lse, idx)
+
+
+# ----------------------------------------------------------------- select --
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("hkv, G", [(2, 1), (1, 8), (3, 18)])
+@pytest.mark.parametrize("n_sel, first, last", [(1, 0, 1), (4, 1, 3), (8, 1, 2), (12, 0, 1), (40, 2, 1)])
+def test_select(d, hkv, G, n_sel, first, last):
+    n, T = [1400, 64, 0, 500, 129], [3, 1, 0, 70, 2]
+    c, ks, _ = filled(n, hkv, d, seed=80)
+    q = normal(81, sum(T), hkv * G, d).cuda()
+    idx = torch.full((sum(T), hkv, n_sel), -7, dtype=torch.int32, device="cuda")
+    cap.kvb_select(c.table(n, T), q, idx, kv_heads=hkv, first=first, last=last)
+    at = [(i, t) for i in range(len(n)) for t in range(T[i])]
+    qh = q.double().cpu().numpy()
+    for x, (i, t) in list(enumerate(at))[::5] + [(len(at) - 1, at[-1])]:
+        for h in range(hkv):
+            want = P.select(qh[x, h * G:(h + 1) * G], values(c.bounds[i][:, :, h]), c.scales[i][:, 0, h].double().cpu().numpy(),
+                            n_sel, first, last, n[i] - T[i] + t)
+            assert idx[x, h].tolist() == want, (i, t, h)
+
+
+def test_selected_blocks_hold_the_highest_products():
+    """No key of a block scores above its bound: with one block selected beyond the own, the best key's block scores highest
+    among single-row blocks' bounds."""
+    hkv, d, n = 1, 64, 64 * 20
+    c, ks, _ = filled([n], hkv, d, seed=85)
+    q = normal(86, 1, 4, d).cuda()
+    b, s = values(c.bounds[0][:20, :, 0]), c.scales[0][:20, 0, 0].double().cpu().numpy()
+    for row in q[0].double().cpu().numpy():
+        bound = np.maximum(row * b[:, 0], row * b[:, 1]).sum(1) * s
+        assert ((ks[0][:, 0] @ row).reshape(20, 64).max(1) <= bound * (1 + 1e-12)).all()
+
+
+def test_select_ties_zeros_and_nan():
+    """Equal scores go to the lower block, also at the border; a NaN score counts as infinite; both zeros are one score."""
+    hkv, d, nb = 1, 64, 30
+    k = torch.ones(nb * 64, hkv, d).bfloat16()
+    k[64 * 20:64 * 22] = 2.0
+    k[64 * 11, 0, 5] = float("nan")
+    c = Caches([nb * 64], hkv, d)
+    append(c, [0], [nb * 64], [k], [k])
+    q = torch.ones(1, 1, d).bfloat16().cuda()
+    idx = torch.empty((1, 1, 6), dtype=torch.int32, device="cuda")
+    cap.kvb_select(c.table([nb * 64], [1]), q, idx, kv_heads=1, first=0, last=1)
+    assert idx[0, 0].tolist() == [0, 1, 11, 20, 21, 29]
+    cap.kvb_select(c.table([nb * 64], [1]), torch.zeros_like(q), idx, kv_heads=1, first=1, last=1)
+    assert idx[0, 0].tolist() == [0, 1, 2, 3, 11, 29]
+    cap.kvb_select(c.table([nb * 64], [1]), torch.full_like(q, float("nan")), idx, kv_heads=1, first=0, last=6)
+    assert idx[0, 0].tolist() == [24, 25, 26, 27, 28, 29]
+    k[:, 0, 1::2] = -1.0  # scores of zero: sums of +1 and -1
+    k[64 * 11, 0, 5] = 1.0
+    k[64 * 20:64 * 22] = -0.0
+    append(c, [0], [nb * 64], [k], [k])
+    cap.kvb_select(c.table([nb * 64], [1]), q, idx, kv_heads=1, first=0, last=1)
+    # channel 5 of row 64 * 11 is +1 where all others of its column are -1: that block's score is 2
+    assert idx[0, 0].tolist() == [0, 1, 2, 3, 11, 29]
+
+
+def test_select_many_blocks():
+    """More blocks than one workgroup's memory holds keys of (4096), made from bounds alone."""
+    hkv, d, G, nb, n_sel = 1, 64, 2, 9001, 333
+    g = torch.Generator().manual_seed(3)
+    lo = torch.randint(0, 0x78, (nb, 1, hkv, d), generator=g, dtype=torch.uint8)
+    bounds = torch.cat([lo | 0x80, torch.randint(0, 0x78, (nb, 1, hkv, d), generator=g, dtype=torch.uint8)], 1).cuda()
+    scales = torch.ones((nb, 2, hkv)).cuda()
+    q = normal(87, 1, G, d).cuda()
+    idx = torch.empty((1, hkv, n_sel), dtype=torch.int32, device="cuda")
+    cap.kvb_select(cap.kvb_seqs([(0, 0, scales, bounds, 0, nb * 64, nb * 64 - 5, 1)]), q, idx, kv_heads=hkv, first=2, last=3)
+    want = P.select(q[0].double().cpu().numpy(), values(bounds[:, :, 0]), np.ones(nb), n_sel, 2, 3, nb * 64 - 6)
+    assert idx[0, 0].tolist() == want
+
+
+# ------------------------------------------------- streams, graphs, sizes --
+def step(c, n, T, k, v, q, idx, o, lse, ws, **kw):
+    """One decode step, the calls as they follow each other."""
+    t = c.table(n, T)
+    cap.kvb_append(t, k, v, **kw)
+    cap.kvb_select(t, q, idx, kv_heads=c.hkv, workspace=ws, **kw)
+    cap.kvb_attend(t, q, o[0], kv_heads=c.hkv, scale=0.1, lse=lse[0], workspace=ws, **kw)
+    cap.kvb_attend(t, q, o[1], kv_heads=c.hkv, scale=0.1, lse=lse[1], idx=idx, workspace=ws, **kw)
+
+
+def step_buffers(T, hkv, G, d, n_sel=4):
+    return (torch.empty((T, hkv, n_sel), dtype=torch.int32, device="cuda"), torch.empty((2, T, hkv * G, d), dtype=torch.bfloat16, device="cuda"),
+            torch.empty((2, T, hkv * G), device="cuda"), torch.empty(64 << 20, dtype=torch.uint8, device="cuda"))
+
+
+def test_other_stream():
+    hkv, G, d, n, T = 2, 4, 128, [2000, 300], [1, 1]
+    results = []
+    for s in (None, torch.cuda.Stream()):
+        c, _, _ = filled([m - 1 for m in n], hkv, d, seed=90)
+        k, v, q = normal(91, 2, hkv, d).cuda(), normal(92, 2, hkv, d).cuda(), normal(93, 2, hkv * G, d).cuda()
+        idx, o, lse, ws = step_buffers(2, hkv, G, d)
+        torch.cuda.synchronize()
+        step(c, n, T, k, v, q, idx, o, lse, ws, stream=s)
+        torch.cuda.synchronize()
+        results.append([idx.clone(), o.clone(), lse.clone()] + [x.clone() for x in c.all()[:8]])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_two_graphs_share_a_workspace():
+    """Two recorded steps with one workspace, replayed in turn with eager work between, give what eager calls give."""
+    hkv, G, d = 2, 8, 256
+    made = []
+    idx_, o_, lse_, ws = step_buffers(1, hkv, G, d)
+    for i, m in enumerate((3000, 777)):
+        c, _, _ = filled([m - 1], hkv, d, seed=100 + i)
+        k, v, q = normal(110 + i, 1, hkv, d).cuda(), normal(112 + i, 1, hkv, d).cuda(), normal(114 + i, 1, hkv * G, d).cuda()
+        idx, o, lse, _ = step_buffers(1, hkv, G, d)
+        step(c, [m], [1], k, v, q, idx, o, lse, ws)
+        torch.cuda.synchronize()
+        want = [idx.clone(), o.clone(), lse.clone()]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(c, [m], [1], k, v, q, idx, o, lse, ws)
+        made.append((graph, (idx, o, lse), want, (c, k, v, q)))
+    for _ in range(4):
+        for graph, out, want, _keep in made:
+            for x in out:
+                x.zero_()
+            graph.replay()
+            (torch.randn(512, 512, device="cuda") @ torch.randn(512, 512, device="cuda")).sum().item()
+            torch.cuda.synchronize()
+            for x, y in zip(out, want):
+                assert torch.equal(x, y)
+        ws.fill_(0xFF)
+
+
+def test_offsets_past_32_bits():
+    """Rows whose codes lie beyond 4 GiB of K and of V: append, decode over them, selection of them."""
+    hkv, d, G = 8, 256, 2
+    rows = (1 << 21) + 4096  # 4.3 GB each of K and V
+    c = Caches([rows], hkv, d, fill=0)
+    c.scales[0].fill_(1.0)
+    n0, n1 = rows - 700, rows - 3
+    k, v, q = normal(120, n1 - n0, hkv, d), normal(121, n1 - n0, hkv, d), normal(122, 1, hkv * G, d).cuda()
+    n0 -= n0 % BLOCK
+    n1 = n0 + k.shape[0]
+    cap.kvb_append(c.table([n1], [n1 - n0]), k.cuda(), v.cuda())
+    want, scales, _ = P.cache(k.double().numpy())
+    assert np.array_equal(values(c.k[0][n0:n1]), want)
+    idx = torch.empty((1, hkv, 12), dtype=torch.int32, device="cuda")
+    cap.kvb_select(c.table([n1], [1]), q, idx, kv_heads=hkv, first=1, last=2)
+    ids = idx.cpu().numpy()
+    assert (ids[:, :, 0] == 0).all() and (ids[:, :, 1:] >= n0 // BLOCK).all()  # all others are blocks of zeros
+    o, lse = run_attend(c, [n1], [1], q, 0.1, idx)
+    full, full_lse = run_attend(c, [n1], [1], q, 0.1)
+    kh = np.concatenate([np.zeros((BLOCK, hkv, d)), want * scales.repeat(BLOCK, 0)[:n1 - n0, :, None]])
+    wv, sv, _ = P.cache(v.double().numpy())
+    vh = np.concatenate([np.zeros((BLOCK, hkv, d)), wv * sv.repeat(BLOCK, 0)[:n1 - n0, :, None]])
+    qh, oh, lh, fh, flh = (x.double().cpu().numpy() for x in (q, o, lse, full, full_lse))
+    for h in (0, 7, 15):
+        local = [0] + [b - n0 // BLOCK + 1 for b in ids[0, h // G, 1:]]  # block 0, then the blocks from n0 on
+        plain = P.attend(qh[0, h], kh[:, h // G], vh[:, h // G], 0.1, kh.shape[0] - 1, local)
+        assert P.close(oh[0, h], lh[0, h], plain, d, False)
+        # the whole: n0 keys with a score and a value of zero before the rows appended
+        x = 0.1 * (kh[BLOCK:, h // G] @ qh[0, h])
+        z = np.exp(x).sum() + n0
+        assert abs(flh[0, h] - np.log(z)) < 1e-4
+        assert np.abs(fh[0, h] - np.exp(x) @ vh[BLOCK:, h // G] / z).max() <= 2.0 ** -7 * (np.exp(x) @ np.abs(vh[BLOCK:, h // G])).max() / z
+
+
+def test_device_of_the_tensors_and_no_device_writes_on_refusal():
+    c, _, _ = filled([100], 1, 64, seed=130)
+    before = [x.clone() for x in c.all()]
+    k = normal(131, 1, 1, 64).cuda()
+    with pytest.raises(cap.CapsuleError):
+        cap.kvb_append(c.table([c.rows[0] + 1], [1]), k, k)
+    with pytest.raises(cap.CapsuleError):
+        cap.kvb_attend(c.table([100], [1]), k, k.clone(), kv_heads=1, scale=float("nan"))
+    torch.cuda.synchronize()
+    for x, y in zip(c.all(), before):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+# ------------------------------------------------------- a whole session --
+def test_session_with_a_capsule():
+    """Prefill, decode, a capsule at the aligned boundary, restore into another session's buffers, the same continuation:
+    the same bytes and bits as the session that went on."""
+    hkv, G, d, P0, steps = 4, 2, 128, 320, 30
+    k, v, q = (normal(140 + i, P0 + steps, h, d).cuda() for i, h in enumerate((hkv, hkv, hkv * G)))
+
+    def session():
+        rows = 512
+        c = Caches([rows], hkv, d, fill=0)
+        live = cap.cap_set_create([("k", c.k[0], hkv * d, rows, cap.CAP_KIND_POSITIONAL), ("v", c.v[0], hkv * d, rows, cap.CAP_KIND_POSITIONAL),
+                                   ("scales", c.scales[0], rows // 64 * 2 * hkv * 4, 1, cap.CAP_KIND_FIXED),
+                                   ("bounds", c.bounds[0], hkv * d // 32, rows, cap.CAP_KIND_POSITIONAL)], 64, 9)
+        return c, live
+
+    def decode(c):
+        out = []
+        for t in range(P0, P0 + steps):
+            idx, o, lse, ws = step_buffers(1, hkv, G, d)
+            step(c, [t + 1], [1], k[t:t + 1], v[t:t + 1], q[t:t + 1], idx, o, lse, ws)
+            out += [idx, o, lse]
+        return out
+
+    a, live_a = session()
+    cap.kvb_append(a.table([P0], [P0]), k[:P0], v[:P0])
+    o, lse = run_attend(a, [P0], [P0], q[:P0], 0.1)
+    ks, vs = reread(a, [P0])
+    check_attend(a, ks, vs, [P0], [P0], q[:P0], 0.1, o, lse, rows=60)
+    cap.cap_set_set_position(live_a, P0)
+    arena = torch.empty(cap.capsule_bytes(live_a, P0), dtype=torch.uint8, device="cuda")
+    capsule = cap.capsule_snapshot(live_a, P0, 3, arena)
+    cold = decode(a)
+    b, live_b = session()
+    assert cap.capsule_restore(capsule, live_b, 3) == P0
+    warm = decode(b)
+    for x, y in zip(cold, warm):
+        assert torch.equal(x, y)
+    n = P0 + steps
+    for x, y in ((a.k[0][:n], b.k[0][:n]), (a.v[0][:n], b.v[0][:n]), (a.scales[0][:n // 64 + 1], b.scales[0][:n // 64 + 1])):
+        assert torch.equal(x, y)
+    ks, vs = reread(a, [n])
+    check_attend(a, ks, vs, [n], [1], q[n - 1:n], 0.1, cold[-2][0], cold[-1][0])
