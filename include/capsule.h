@@ -589,7 +589,7 @@ CAP_API int kvb_append(const kvb_append_args* args, void* stream);
  * see have no part in its result, NaN codes included.  The softmax is held in
  * fp32; scores take the query rows in full, weights enter the second product as
  * bf16.  One launch, or two where a sequence is cut along its rows (the parts
- * lie in the workspace).  Results are reproducible for the same arguments. */
+ * lie in the workspace), apart for sequences of few and of many query rows.  Results are reproducible for the same arguments. */
 typedef struct kvb_attend_args {
     const kvb_seq* seqs;       /* HOST array of n_seq (bounds, open: not read) */
     const void*    q;

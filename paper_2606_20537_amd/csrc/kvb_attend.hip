@@ -382,10 +382,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendTable<N> 
             if (p.seq[mid].t0 <= (int64_t)tok) seq = mid; else hi = mid - 1;
         }
     }
+    seq = seq < 0 ? 0 : seq;
     const KvbAttendSeq& s = p.seq[seq];
-    const int n = s.nsplit;  // 1: written by its workgroup, nothing to do
     const int G = p.heads / p.kv_heads, h = head / G;
     const int64_t t = (int64_t)tok - s.t0;
+    const int n = t >= 0 && t < s.T ? s.nsplit : 1;  // 1: written by its workgroup (or by another launch), nothing to do
     int64_t item;
     int rr;
     if (p.idx) {

@@ -102,79 +102,95 @@ int64_t run_of_16(int64_t total) {
     return std::max<int64_t>(2, one <= 16 ? one : (total + 511) / 512);
 }
 
-int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams* p) {
-    const int64_t tokens = a->tokens;
-    const int rc = check_sizes(a->seqs, a->n_seq, a->heads, a->kv_heads, a->d, a->in_dtype, tokens);
+// The same for tiles of 128 rows: the length whose estimate is lowest.  `rows` of all
+// tiles, `tiles` of them, the longest's blocks, the blocks of all.  A block takes a
+// workgroup `alone` us by itself on a CU; where two fit, they take `both` us for a block
+// each.  Writing, reading and joining the runs' parts takes 4 us and 2.5 TB/s.  Measured
+// (us; cut into 1, 2, 4, 5, 6, 8): 161 tokens behind 16384, 32 heads on 4 of 256 channels
+// 574, 300, 160, 137, 217 (a second round), 171; 16 heads on 4 of 128 368, 188, 105, 91, 104,
+// 85; a whole prefill of 2048 tokens, 128 channels 55, 62, 72; of 1024 30, 30, 34.
+int64_t run_of_128(int32_t d, int64_t rows, int64_t tiles, int64_t longest, int64_t total) {
+    const double alone = d == 256 ? 2.2 : d == 128 ? 1.42 : 1.15, both = d == 128 ? 2.27 : 1.97;
+    int64_t per = longest;
+    double best = 1e30;
+    for (int64_t cut = 1; cut <= 32 && cut <= longest && (cut == 1 || tiles * cut <= 1024); ++cut) {
+        const int64_t run = (longest + cut - 1) / cut, wgs = tiles * cut;
+        const double mean = (double)total / (double)wgs;
+        double us = alone * (double)run;
+        if (wgs > 256) us = std::max(us, d == 256 ? alone * mean * (double)((wgs + 255) / 256) : both * mean * (double)((wgs + 511) / 512));
+        if (cut > 1) us += 4.0 + (double)(rows * cut * d) * 8.0 / 2.5e6;
+        if (us < best) {
+            best = us;
+            per = run;
+        }
+    }
+    return per;
+}
+
+// Query rows of a sequence and KV head from which it takes tiles of 128 (with a block list
+// never).  Measured (us, tiles of 16 / of 128): 8 heads on each of 4 KV heads of 256, 16385
+// rows, 64 query rows 26.8 / 36.3, 128 37.2 / 41.5, 256 59.1 / 49.3; 128 channels, 131072 rows,
+// 64 query rows 59.9 / 110, 96 110 / 108; 300 rows, 256 query rows 13.6 / 16.2.
+constexpr int64_t kRowsFor128 = 129;
+
+// p[0]: the sequences in tiles of 16 rows, p[1]: those in tiles of 128, a launch each.
+int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams (&p)[2]) {
+    const int rc = check_sizes(a->seqs, a->n_seq, a->heads, a->kv_heads, a->d, a->in_dtype, a->tokens);
     if (rc != CAP_OK) return rc;
     if (a->idx ? a->n_sel < 1 : a->n_sel != 0) return CAP_E_INVAL;
     const int64_t G = a->heads / a->kv_heads;
-    p->heads = a->heads;
-    p->kv_heads = a->kv_heads;
-    p->d = a->d;
-    p->n_sel = a->n_sel;
-    p->tokens = tokens;
-    int64_t most = 0, longest = 0;  // query rows of a KV head, blocks
+    struct { int64_t longest, total, rows, items, per; } sum[2] = {};
+    auto kind = [&](const kvb_seq& s) { return !a->idx && s.T * G >= kRowsFor128 ? 1 : 0; };
     auto blocks = [&](const kvb_seq& s) { return a->idx ? (int64_t)a->n_sel : (s.n + kKvbBlock - 1) / kKvbBlock; };
-    for (int32_t i = 0; i < a->n_seq; ++i) {
-        if (a->seqs[i].T == 0) continue;
-        most = std::max(most, a->seqs[i].T * G);
-        longest = std::max(longest, blocks(a->seqs[i]));
-    }
-    p->tile = !a->idx && most > 64 ? 128 : 16;
-    auto tiles = [&](const kvb_seq& s) { return a->idx ? s.T * ((G + 15) / 16) : (s.T * G + p->tile - 1) / p->tile; };
-    int64_t total = 0, rows = 0;
-    for (int32_t i = 0; i < a->n_seq; ++i) {
-        const kvb_seq& s = a->seqs[i];
-        int64_t seen = tiles(s) * blocks(s);
-        if (p->tile == 128) seen -= tiles(s) * (s.T / kKvbBlock) / 2;  // the tiles of a prefill see half of its blocks
-        total += seen * a->kv_heads;
-        rows += s.T * a->heads;
-    }
-    int64_t per = longest;
-    if (p->tile == 16) {
-        per = run_of_16(total);
-        if (a->idx) per = std::min<int64_t>(per, cap::kKvbListRun);
-    } else {
-        // The time in blocks: that of the longest workgroup or of all of them in turn, and that of
-        // writing, reading and joining the parts (3 TB/s and a launch).
-        const int64_t at_once = a->d == 256 ? 256 : 512;
-        const double block_us = a->d == 256 ? 2.0 : a->d == 128 ? 1.3 : 0.9;
-        double best = 1e30;
-        for (int64_t cut = 1; cut <= 32 && cut <= longest; ++cut) {
-            const int64_t run = (longest + cut - 1) / cut;
-            double us = block_us * (double)std::max(run, (total + at_once - 1) / at_once);
-            if (cut > 1) us += 5.0 + (double)(rows * cut * a->d) * 8.0 / 3e6;
-            if (us < best) {
-                best = us;
-                per = run;
-            }
-        }
-    }
-    int64_t wgs = 0, slots = 0, t0 = 0;
-    int32_t n = 0;
+    auto tiles = [&](const kvb_seq& s) {  // of all KV heads
+        const int64_t tile = kind(s) ? 128 : 16;
+        return (a->idx ? s.T * ((G + 15) / 16) : (s.T * G + tile - 1) / tile) * a->kv_heads;
+    };
     for (int32_t i = 0; i < a->n_seq; ++i) {
         const kvb_seq& s = a->seqs[i];
         if (s.T == 0) continue;
-        cap::KvbAttendSeq& x = p->seq[n++];
+        auto& x = sum[kind(s)];
+        x.longest = std::max(x.longest, blocks(s));
+        x.total += tiles(s) * (blocks(s) - (kind(s) ? s.T / kKvbBlock / 2 : 0));  // the tiles of a prefill see half of its blocks
+        x.rows += s.T * a->heads;
+        x.items += tiles(s);
+    }
+    for (int k = 0; k < 2; ++k) {
+        p[k].tokens = a->tokens;
+        p[k].heads = a->heads;
+        p[k].kv_heads = a->kv_heads;
+        p[k].d = a->d;
+        p[k].n_sel = a->n_sel;
+        p[k].tile = k ? 128 : 16;
+        sum[k].per = k ? run_of_128(a->d, sum[k].rows, sum[k].items, sum[k].longest, sum[k].total) : run_of_16(sum[k].total);
+        if (a->idx) sum[k].per = std::min<int64_t>(sum[k].per, cap::kKvbListRun);
+    }
+    int64_t wgs[2] = {}, slots[2] = {}, t0 = 0;
+    for (int32_t i = 0; i < a->n_seq; ++i) {
+        const kvb_seq& s = a->seqs[i];
+        if (s.T == 0) continue;
+        const int k = kind(s);
+        cap::KvbAttendSeq& x = p[k].seq[p[k].n_seq++];
         x.k = addr(s.k);
         x.v = addr(s.v);
         x.scales = addr(s.scales);
         x.n = s.n;
         x.t0 = t0;
         x.T = (int32_t)s.T;
-        const int64_t nb = blocks(s), items = tiles(s) * a->kv_heads;
-        x.nsplit = (int32_t)((nb + per - 1) / per);
+        const int64_t nb = blocks(s);
+        x.nsplit = (int32_t)((nb + sum[k].per - 1) / sum[k].per);
         x.per = (int32_t)((nb + x.nsplit - 1) / x.nsplit);  // of even lengths
-        x.first_wg = (uint32_t)wgs;
-        x.first_slot = (uint32_t)slots;
-        wgs += items * x.nsplit;
-        if (x.nsplit > 1) slots += items * x.nsplit;
-        if (wgs > 0x7fffffff) return CAP_E_UNSUPPORTED;
+        x.first_wg = (uint32_t)wgs[k];
+        x.first_slot = (uint32_t)slots[k];
+        wgs[k] += tiles(s) * x.nsplit;
+        if (x.nsplit > 1) slots[k] += tiles(s) * x.nsplit;
+        if (wgs[k] > 0x7fffffff) return CAP_E_UNSUPPORTED;
         t0 += s.T;
     }
-    p->n_seq = n;
-    p->wgs = (uint32_t)wgs;
-    p->slots = (uint32_t)slots;
+    for (int k = 0; k < 2; ++k) {
+        p[k].wgs = (uint32_t)wgs[k];
+        p[k].slots = (uint32_t)slots[k];
+    }
     return CAP_OK;
 }
 
@@ -276,20 +292,21 @@ int kvb_append(const kvb_append_args* a, void* stream) {
 }
 
 uint64_t kvb_attend_workspace_bytes(const kvb_attend_args* a) {
-    cap::KvbAttendParams p{};
-    return a && plan_attend(a, &p) == CAP_OK ? attend_workspace(p) : 0;
+    cap::KvbAttendParams p[2]{};
+    return a && plan_attend(a, p) == CAP_OK ? attend_workspace(p[0]) + attend_workspace(p[1]) : 0;
 }
 
 int kvb_attend(const kvb_attend_args* a, void* stream) {
     if (!a || a->reserved != 0 || !std::isfinite(a->scale)) return CAP_E_INVAL;
-    cap::KvbAttendParams p{};
-    int rc = plan_attend(a, &p);
+    cap::KvbAttendParams p[2]{};
+    int rc = plan_attend(a, p);
     if (rc != CAP_OK) return rc;
     const int64_t width = (int64_t)a->heads * a->d;
-    if ((rc = check_stride(a->q_stride, width, &p.q_stride)) != CAP_OK) return rc;
-    if (p.tokens == 0) return CAP_OK;
+    int64_t q_stride = 0;
+    if ((rc = check_stride(a->q_stride, width, &q_stride)) != CAP_OK) return rc;
+    if (a->tokens == 0) return CAP_OK;
     if (!a->q || !a->o) return CAP_E_INVAL;
-    const uint64_t need = attend_workspace(p);
+    const uint64_t need = attend_workspace(p[0]) + attend_workspace(p[1]);
     if (need && !a->workspace) return CAP_E_INVAL;
     if (a->workspace_bytes < need) return CAP_E_SIZE;
     for (int32_t i = 0; i < a->n_seq; ++i) {
@@ -298,8 +315,8 @@ int kvb_attend(const kvb_attend_args* a, void* stream) {
         if ((rc = check_align(a->seqs[i])) != CAP_OK) return rc;
     }
     if (((addr(a->q) | addr(a->o) | (need ? addr(a->workspace) : 0)) & 15) || ((addr(a->lse) | addr(a->idx)) & 3)) return CAP_E_ALIGN;
-    const uint64_t tokens = (uint64_t)p.tokens;
-    const Range in[2] = {range(a->q, span(p.tokens, p.q_stride, width)),
+    const uint64_t tokens = (uint64_t)a->tokens;
+    const Range in[2] = {range(a->q, span(a->tokens, q_stride, width)),
                          range(a->idx, tokens * (uint64_t)a->kv_heads * (uint64_t)a->n_sel * 4)};
     const Range out[3] = {range(a->o, tokens * (uint64_t)width * 2), range(a->lse, tokens * (uint64_t)a->heads * 4),
                           range(need ? a->workspace : nullptr, need)};
@@ -310,14 +327,20 @@ int kvb_attend(const kvb_attend_args* a, void* stream) {
         for (int32_t j = 0; j < a->n_seq; ++j)
             if (a->seqs[j].T && meets_cache(out[i], a->seqs[j], bit(K) | bit(V) | bit(SCALES), a->kv_heads, a->d)) return CAP_E_INVAL;
     }
-    p.q = a->q;
-    p.o = a->o;
-    p.lse = a->lse;
-    p.idx = a->idx;
-    p.part_o = static_cast<float*>(a->workspace);
-    p.part_ml = p.part_o + (uint64_t)p.slots * (uint64_t)p.tile * (uint64_t)p.d;
-    p.scale_log2 = a->scale * 1.4426950408889634f;
-    return launch_status(cap::launch_kvb_attend(p, static_cast<hipStream_t>(stream)));
+    float* part = static_cast<float*>(a->workspace);
+    for (cap::KvbAttendParams& x : p) {
+        x.q = a->q;
+        x.o = a->o;
+        x.lse = a->lse;
+        x.idx = a->idx;
+        x.q_stride = q_stride;
+        x.part_o = part;
+        x.part_ml = part + (uint64_t)x.slots * (uint64_t)x.tile * (uint64_t)x.d;
+        part = x.part_ml + (uint64_t)x.slots * (uint64_t)x.tile * 2;
+        x.scale_log2 = a->scale * 1.4426950408889634f;
+        if ((rc = launch_status(cap::launch_kvb_attend(x, static_cast<hipStream_t>(stream)))) != CAP_OK) return rc;
+    }
+    return CAP_OK;
 }
 
 uint64_t kvb_select_workspace_bytes(const kvb_select_args* a) {

@@ -87,13 +87,15 @@ __device__ inline u32x4 decode8(uint32_t w0, uint32_t w1, float scale) {
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true))};
 }
 
-// Where the 16-byte unit `u` of row `key` lies in its row (u ^ the value): the reads of K
-// take one unit of eight neighbouring rows at a time, those of V of rows i and 8 + i
-// (i = 0..3 or 4..7).
-__device__ inline int swizzle_k(int key) { return key & 7; }
+// Where the 16-byte unit `u` of row `key` lies in its row: u ^ the value.  LDS serves 256
+// bytes at a time: of K one unit of 16 neighbouring rows (bf16, 2 D bytes), of V two
+// neighbouring units of rows i and 8 + i, i = 0..3 or 4..7 (D bytes).
+template <int D>
+__device__ inline int swizzle_k(int key) { return D == 64 ? key >> 1 & 7 : key & 15; }
 template <int D>
 __device__ inline int swizzle_v(int key) {
-    return D == 64 ? (key >> 1 & 1) | (key >> 3 & 1) << 1 : (key & 3) | (key >> 3 & 1) << 2;
+    const int i = D == 256 ? (key & 3) | (key >> 3 & 1) << 2 : D == 128 ? (key >> 1 & 1) | (key >> 3 & 1) << 1 : key >> 3 & 1;
+    return 2 * i;
 }
 
 template <int D>
@@ -156,14 +158,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
         #pragma unroll
         for (int i = 0; i < kLoads; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, svoff, i * kRows * rowb, 0);
     };
-    auto stage_k = [&](int buf, float scale) {
-        #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int key = srow + i * kRows;
-            uint8_t* dst = &k_s[buf][key * 2 * D];
-            *reinterpret_cast<u32x4*>(dst + 16 * ((2 * sunit) ^ swizzle_k(key))) = decode8(ks[i][0], ks[i][1], scale);
-            *reinterpret_cast<u32x4*>(dst + 16 * ((2 * sunit + 1) ^ swizzle_k(key))) = decode8(ks[i][2], ks[i][3], scale);
-        }
+    auto stage_k = [&](int buf, int i, float scale) {  // load i
+        const int key = srow + i * kRows;
+        uint8_t* dst = &k_s[buf][key * 2 * D];
+        *reinterpret_cast<u32x4*>(dst + 16 * ((2 * sunit) ^ swizzle_k<D>(key))) = decode8(ks[i][0], ks[i][1], scale);
+        *reinterpret_cast<u32x4*>(dst + 16 * ((2 * sunit + 1) ^ swizzle_k<D>(key))) = decode8(ks[i][2], ks[i][3], scale);
     };
     auto stage_v = [&](int b, int buf) {
         // Where some row does not see every key, NaN codes of V go (a weight of zero
@@ -198,7 +197,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     auto v_exponent = [&](int b) { return __builtin_amdgcn_readlane((int)v_scales, b - e0) >> 23; };  // as the instruction takes it
 
     // addresses of a lane's reads; units and rows come in by xor and offset
-    const int kaddr = (lane & 31) * 2 * D + 16 * (half ^ swizzle_k(lane & 31));
+    const int kaddr = (lane & 31) * 2 * D + 16 * (half ^ swizzle_k<D>(lane & 31));
     const int vkey = 4 * half + ((lane & 15) >> 1 & 3) + 8 * ((lane & 15) >> 3);
     const int vaddr = vkey * D + 16 * ((lane >> 4 & 1) ^ swizzle_v<D>(vkey)) + 8 * (lane & 1);
     auto read_k = [&](int buf, int t, int i) {  // keys 32 t .. + 31, channels 16 i .. + 15
@@ -265,7 +264,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
         fetch(vb, begin, vs);
         load_scales();
         dev::lds_barrier();
-        stage_k(0, k_scale(begin));
+        #pragma unroll
+        for (int i = 0; i < kLoads; ++i) stage_k(0, i, k_scale(begin));
         stage_v(begin, 0);
         fetch(kb, clamp(begin + 1), ks);
         fetch(vb, clamp(begin + 1), vs);
@@ -278,7 +278,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
             x[0] = mma16(read_k(0, 0, i), q[i], x[0]);
             x[1] = mma16(read_k(0, 1, i), q[i], x[1]);
         }
-        stage_k(1, k_scale(clamp(begin + 1)));
+        #pragma unroll
+        for (int i = 0; i < kLoads; ++i) stage_k(1, i, k_scale(clamp(begin + 1)));
         stage_v(clamp(begin + 1), 1);
         fetch(kb, clamp(begin + 2), ks);
         fetch(vb, clamp(begin + 2), vs);
@@ -332,7 +333,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
                         ph[w] = a;
                         pl[w] = d;
                     }
-                    if (step == steps - 2) stage_k(kbuf, next_scale);
+                    #pragma unroll
+                    for (int u = 0; u < kLoads; ++u)
+                        if (step == (2 * u + 1) * steps / (2 * kLoads)) stage_k(kbuf, u, next_scale);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (j + 1 < NJ) {
