@@ -544,7 +544,8 @@ CAP_API int kv_fp8_dequantize(const kv_fp8_seg* segs, uint32_t n_seg, void* stre
  * small), CAP_E_UNSUPPORTED (shape or dtype outside the list, n_seq >
  * KVB_MAX_SEQ), CAP_E_ALIGN.  A call reads the sequence table before it returns,
  * and its kernel arguments carry every address, length and position: it can be
- * recorded in a stream capture and replayed for the same n. */
+ * recorded in a stream capture and replayed for the same n.  A workspace holds
+ * nothing between calls; calls that may overlap need workspaces of their own. */
 #define KVB_BLOCK   64
 #define KVB_MAX_SEQ 64
 

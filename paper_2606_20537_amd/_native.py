@@ -546,7 +546,23 @@ def _kvb_table(fn, seqs):
     if seqs.ndim != 2 or seqs.shape[1] != 8 or seqs.dtype.str != "<i8" or not seqs.flags.c_contiguous:
         raise ValueError("%s: the sequence table is a contiguous int64 array [n_seq, 8]" % fn)
     n = seqs.shape[0]
+    if not seqs.flags.writeable:
+        return seqs.ctypes.data, n
     return (ct.addressof(ct.c_char.from_buffer(seqs)) if n else 0), n
+
+
+def _kvb_device(fn, first, *rest):
+    """The tensors are on the current device, where the call launches."""
+    index = first.get_device()
+    ok = index >= 0
+    for x in rest:
+        if x is not None and x.get_device() != index:
+            ok = False
+    if ok:
+        raw = _raw if _raw is not None else _raw_lookups(_kvb_torch()[0])
+        ok = index == (raw[1]() if raw else _kvb_torch()[0].cuda.current_device())
+    if not ok:
+        raise ValueError("%s: every tensor is on the current GPU" % fn)
 
 
 def _kvb_tokens(fn, name, x):
@@ -588,6 +604,7 @@ def kvb_append(seqs, k, v, *, stream=None):
     vs, dv, other = _kvb_tokens("kvb_append", "v", v)
     if other != shape or dv != dt:
         raise ValueError("kvb_append: k and v have the same shape and dtype")
+    _kvb_device("kvb_append", k, v)
     a = kvb_append_args(at, k.data_ptr(), v.data_ptr(), ks, vs, shape[0], n_seq, shape[1], shape[2], dt)
     return _check("kvb_append", load().kvb_append(ct.byref(a), _stream(stream)))
 
@@ -605,6 +622,7 @@ def kvb_attend(seqs, q, o, *, kv_heads, scale, lse=None, idx=None, workspace=Non
     if idx is not None:
         n_sel = idx.shape[-1]
         _kvb_out("kvb_attend", "idx", idx, (tokens, kv_heads, n_sel), i32)
+    _kvb_device("kvb_attend", q, o, lse, idx, workspace)
     a = kvb_attend_args(at, q.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else 0,
                         idx.data_ptr() if idx is not None else 0, 0, 0, qs, tokens, n_seq, heads, kv_heads, d, n_sel, dt,
                         scale, 0)
@@ -619,6 +637,7 @@ def kvb_select(seqs, q, idx, *, kv_heads, first=1, last=2, workspace=None, strea
     qs, dt, (tokens, heads, d) = _kvb_tokens("kvb_select", "q", q)
     n_sel = idx.shape[-1]
     _kvb_out("kvb_select", "idx", idx, (tokens, kv_heads, n_sel), _kvb_torch()[3])
+    _kvb_device("kvb_select", q, idx, workspace)
     a = kvb_select_args(at, q.data_ptr(), idx.data_ptr(), 0, 0, qs, tokens, n_seq, heads, kv_heads, d, n_sel, first, last, dt)
     lib = load()
     workspace = _kvb_workspace(a, workspace, lib.kvb_select_workspace_bytes, q)

@@ -20,6 +20,13 @@
 // V's rows in that order.  A lane reads d / 16 contiguous bytes of eight rows and
 // transposes them in registers.  K and V go from memory to registers; LDS only
 // joins the four waves, which take 32 rows of the cache in turn.
+//
+// What bounds it, 8 query heads on each KV head of 256 channels, one token: 131072 +
+// 18561 rows, 307 MB, 57.8 us (5.3 TB/s, the rate of a copy); 16385 rows, 33.8 MB, 11.3 us
+// and 4.5 of the join, of which the data take 6.5 and the launches 2.2 each.  A wave
+// takes about 1 us for 32 rows by itself (128 byte permutes and conversions, 32 matrix
+// instructions, little of it side by side), so runs stay a few blocks long.  Registers for
+// V of a second unit pay up to 128 channels; at 256 they spill.
 #include <hip/hip_runtime.h>
 
 #include "device_util.h"
@@ -116,7 +123,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
     constexpr bool kAhead = D < 256;  // registers for V of two units
     constexpr int kPitch = D + 4;
     __shared__ float o_s[4][16][kPitch];
-    __shared__ float ml_s[4][16][2];
+    __shared__ float ml_s[4][16][2], all_s[16][2];
 
     const KvbAttendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
     const uint32_t w = blockIdx.x - s.first_wg;
@@ -152,7 +159,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
     const int kvoff = li * rowb + h * D + 16 * g, vvoff = 4 * g * rowb + h * D + li * VB;
     const int32_t* list = SPARSE ? p.idx + ((s.t0 + token) * p.kv_heads + h) * p.n_sel : nullptr;
 
-    const int nblk = SPARSE ? p.n_sel : (int)(pos1 / kKvbBlock + 1);
+    const int nblk = SPARSE ? p.n_sel : tile_blocks(s, r0, 16, total, G), runs = tile_runs(s, nblk);
+    if (split >= runs) return;
     const int begin = split * s.per, end = begin + s.per < nblk ? begin + s.per : nblk;
     const int units = 2 * (end - begin);
 
@@ -321,11 +329,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
             *reinterpret_cast<f32x4*>(&o_s[wave][li][(4 * g + j) * VB + c]) =
                 (f32x4){acc[c][j] * fade, acc[c + 1][j] * fade, acc[c + 2][j] * fade, acc[c + 3][j] * fade};
     if (tid < 16) {  // wave 0: lane = row
-        ml_s[0][li][0] = top;
-        ml_s[0][li][1] = sum;
+        all_s[li][0] = top;
+        all_s[li][1] = sum;
     }
     __syncthreads();
-    const bool whole = s.nsplit == 1;
+    const bool whole = runs == 1;
     const uint32_t slot = s.first_slot + w;
     constexpr int kPer = D / 4;  // threads of a row
     #pragma unroll
@@ -339,7 +347,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
             *reinterpret_cast<f32x4*>(p.part_o + ((int64_t)slot * 16 + rr) * D + c) = o;
             continue;
         }
-        const float z = ml_s[0][rr][1], inv = z > 0.0f || z != z ? 1.0f / z : 0.0f;
+        const float z = all_s[rr][1], inv = z > 0.0f || z != z ? 1.0f / z : 0.0f;
         const int64_t tok = s.t0 + (SPARSE ? token : (r0 + rr) / G);
         const int64_t at = (tok * p.heads + (int64_t)h * G + (r0 + rr) % G) * D + c;
         const bf16x2 a = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
@@ -348,7 +356,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
             (u32x2){__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
     }
     if (tid < rows) {
-        const float mm = ml_s[0][tid][0], z = ml_s[0][tid][1];
+        const float mm = all_s[tid][0], z = all_s[tid][1];
         if (!whole) {
             *reinterpret_cast<f32x2*>(p.part_ml + ((int64_t)slot * 16 + tid) * 2) = (f32x2){mm, z};
         } else if (p.lse) {
@@ -386,18 +394,19 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendTable<N> 
     const KvbAttendSeq& s = p.seq[seq];
     const int G = p.heads / p.kv_heads, h = head / G;
     const int64_t t = (int64_t)tok - s.t0;
-    const int n = t >= 0 && t < s.T ? s.nsplit : 1;  // 1: written by its workgroup (or by another launch), nothing to do
     int64_t item;
-    int rr;
+    int rr, n = 1;  // one run: written by its workgroup (or by another launch), nothing to do
     if (p.idx) {
         item = (t * ((G + 15) / 16) + head % G / 16) * p.kv_heads + h;
         rr = head % G % 16;
+        n = s.nsplit;
     } else {
         const int64_t row = t * G + head % G;
         item = row / p.tile * p.kv_heads + h;
         rr = (int)(row % p.tile);
+        if (t >= 0 && t < s.T) n = tile_runs(s, tile_blocks(s, row - rr, p.tile, (int64_t)s.T * G, G));
     }
-    const int64_t slot = s.first_slot + item * n;
+    const int64_t slot = s.first_slot + item * s.nsplit;
     const global_ptr<f32x2> ml = (global_ptr<f32x2>)(p.part_ml + (slot * p.tile + rr) * 2);
     const global_ptr<f32x4> po = (global_ptr<f32x4>)(p.part_o + (slot * p.tile + rr) * D + c);
     const int ml_step = p.tile, po_step = p.tile * D / 4;

@@ -90,6 +90,10 @@ bool meets_cache(const Range& out, const kvb_seq& s, unsigned used, int32_t kv_h
 constexpr unsigned bit(int i) { return 1u << i; }
 
 // ---- attend: the launch plan ----
+// Sequences of few blocks stay whole: 256 channels, runs of 2 blocks and their join 8.8 + 4.9
+// us, 8 blocks whole 11.5; a pass at 200 rows of 64 channels 10.8 us cut, 6.8 whole.
+constexpr int64_t kWholeBlocks = 8;
+
 // Blocks that a run of a cut sequence takes, for tiles of 16 rows; `total`: the
 // blocks of all tiles.  A workgroup to a CU while runs stay short, two where they
 // are long enough for one's loads to cover the other's arithmetic.  Measured (us,
@@ -97,7 +101,8 @@ constexpr unsigned bit(int i) { return 1u << i; }
 // 2: 19.3, 4: 16.4, 6: 15.6, 8: 16.7, 16: 20.8; 131072 + 18561 rows x 4 heads
 // 8: 66, 12: 67, 16: 63, 24: 72; 32 sequences of 816 rows x 1 head 2: 13.2, 4: 14.4,
 // 8: 16.0, whole (13, no second launch) 15.6.
-int64_t run_of_16(int64_t total) {
+int64_t run_of_16(int64_t total, int64_t longest) {
+    if (longest <= kWholeBlocks) return longest;
     const int64_t one = (total + 255) / 256;
     return std::max<int64_t>(2, one <= 16 ? one : (total + 511) / 512);
 }
@@ -114,11 +119,16 @@ int64_t run_of_128(int32_t d, int64_t rows, int64_t tiles, int64_t longest, int6
     int64_t per = longest;
     double best = 1e30;
     for (int64_t cut = 1; cut <= 32 && cut <= longest && (cut == 1 || tiles * cut <= 1024); ++cut) {
-        const int64_t run = (longest + cut - 1) / cut, wgs = tiles * cut;
+        const int64_t run = (longest + cut - 1) / cut;
+        // the tiles' blocks are taken as spread evenly about their mean, up to the longest: how many
+        // runs they have, and the share of rows with more than one
+        const double mid = (double)total / (double)tiles, low = std::max(1.0, 2.0 * mid - (double)longest);
+        const double share = run >= longest ? 0.0 : (double)run <= low ? 1.0 : (double)(longest - run) / ((double)longest - low);
+        const int64_t wgs = cut == 1 ? tiles : (int64_t)std::ceil((double)tiles * (mid / (double)run + 0.5 * share));
         const double mean = (double)total / (double)wgs;
         double us = alone * (double)run;
         if (wgs > 256) us = std::max(us, d == 256 ? alone * mean * (double)((wgs + 255) / 256) : both * mean * (double)((wgs + 511) / 512));
-        if (cut > 1) us += 4.0 + (double)(rows * cut * d) * 8.0 / 2.5e6;
+        if (cut > 1) us += 4.0 + share * (double)(rows * cut * d) * 8.0 / 2.5e6;
         if (us < best) {
             best = us;
             per = run;
@@ -162,7 +172,7 @@ int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams (&p)[2]) {
         p[k].d = a->d;
         p[k].n_sel = a->n_sel;
         p[k].tile = k ? 128 : 16;
-        sum[k].per = k ? run_of_128(a->d, sum[k].rows, sum[k].items, sum[k].longest, sum[k].total) : run_of_16(sum[k].total);
+        sum[k].per = k ? run_of_128(a->d, sum[k].rows, sum[k].items, sum[k].longest, sum[k].total) : run_of_16(sum[k].total, sum[k].longest);
         if (a->idx) sum[k].per = std::min<int64_t>(sum[k].per, cap::kKvbListRun);
     }
     int64_t wgs[2] = {}, slots[2] = {}, t0 = 0;

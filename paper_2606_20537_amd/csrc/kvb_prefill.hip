@@ -27,6 +27,13 @@
 // between those of V^T P^T of the block before it, in slices that the scheduler
 // must not move.
 //
+// 16384 tokens, 32 heads on 4 KV heads of 256 channels: 4.7 to 4.9 ms, 900 to 940 TFLOP/s (the
+// library's bf16 product of 8192 reaches 1243).  Of the 5200 cycles of a block's step the
+// matrix pipe is busy 2050 and the vector unit 2400, little of it side by side (a wave's
+// vector instructions add most of their time to its own matrix instructions), and 1000 are
+// waits for LDS and the barrier.  The plain order of a step took 6.0 ms with FP8 scores, the
+// slices 4.0 to 4.2.
+//
 // A lane has one query row in both products and S^T's accumulators are P^T's
 // operand: byte 4 j + i of lane half h is key 8 j + 4 h + i.  V's operand has its
 // keys in the same order, read with the transposing 8-byte LDS read.  Rows in LDS
@@ -115,12 +122,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     const int64_t tile = tiles - 1 - item / (uint32_t)p.kv_heads;  // the longest first
     const int tid = (int)threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int nblk = tile_blocks(s, tile * 128, 128, total, G), runs = tile_runs(s, nblk);
+    if (split >= runs) return;
     const int64_t row0 = tile * 128, wrow0 = row0 + wave * 32, last = total - 1;
     const int64_t row = wrow0 + (lane & 31) < last ? wrow0 + (lane & 31) : last;  // rows past the last repeat it
     const int64_t before = s.n - s.T, token = row / G, pos = before + token;     // the last key that the row sees
-    // the wave's first position, the tile's first and last
+    // the wave's first position, the tile's
     const int64_t wpos0 = before + (wrow0 < last ? wrow0 : last) / G;
-    const int64_t tpos0 = before + row0 / G, tpos1 = before + (row0 + 127 < last ? row0 + 127 : last) / G;
+    const int64_t tpos0 = before + row0 / G;
 
     // channels 16 s + 8 half .. + 7 of the lane's row; scores in log2 units are the products times f > 0
     bf16x8 q[D / 16];
@@ -147,7 +156,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     const uint8_t* vb = reinterpret_cast<const uint8_t*>(s.v);
     const global_ptr<uint32_t> sc = (global_ptr<uint32_t>)s.scales;
     const int begin = split * s.per;
-    const int nblk = (int)(tpos1 / kKvbBlock) + 1, end = begin + s.per < nblk ? begin + s.per : nblk;
+    const int end = begin + s.per < nblk ? begin + s.per : nblk;
 
     // Staging: thread tid moves unit tid % kUnits of rows tid / kUnits + i kRows.
     const int srow = tid / kUnits, sunit = tid % kUnits;
@@ -433,7 +442,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
 
     l += __shfl_xor(l, 32);
     if (wrow0 + (lane & 31) > last) return;
-    if (s.nsplit > 1) {
+    if (runs > 1) {
         const uint32_t slot = s.first_slot + (uint32_t)((tile * p.kv_heads + h) * s.nsplit + split);
         const int64_t at = (int64_t)slot * 128 + wave * 32 + (lane & 31);
         #pragma unroll

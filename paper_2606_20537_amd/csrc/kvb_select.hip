@@ -138,14 +138,22 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const KvbSelectTable<N> 
     // the highest and lowest key of those that the token need not have, and how many it has to
     uint64_t low = ~0ull, high = 0;
     uint32_t must = 0;
-    for (uint32_t i = tid; i < count; i += kThreads) {
-        const uint64_t k = keys[i];
-        if (in_lds) key_s[i] = k;
-        if (k == kMust) {
-            ++must;
-        } else {
-            low = k < low ? k : low;
-            high = k > high ? k : high;
+    constexpr int kBatch = 8;  // loads in flight
+    for (uint32_t i0 = tid; i0 < count; i0 += kBatch * kThreads) {
+        uint64_t k[kBatch];
+        #pragma unroll
+        for (int j = 0; j < kBatch; ++j) k[j] = keys[i0 + j * kThreads < count ? i0 + j * kThreads : i0];
+        #pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const uint32_t i = i0 + j * kThreads;
+            if (i >= count) continue;
+            if (in_lds) key_s[i] = k[j];
+            if (k[j] == kMust) {
+                ++must;
+            } else {
+                low = k[j] < low ? k[j] : low;
+                high = k[j] > high ? k[j] : high;
+            }
         }
     }
     #pragma unroll

@@ -513,9 +513,19 @@ def test_device_of_the_tensors_and_no_device_writes_on_refusal():
         cap.kvb_append(c.table([c.rows[0] + 1], [1]), k, k)
     with pytest.raises(cap.CapsuleError):
         cap.kvb_attend(c.table([100], [1]), k, k.clone(), kv_heads=1, scale=float("nan"))
+    with pytest.raises(cap.CapsuleError) as e:  # fp32 reaches the library's own check
+        cap.kvb_append(c.table([100], [1]), k.float(), k.float())
+    assert e.value.status == cap.CAP_E_UNSUPPORTED
+    with pytest.raises(ValueError):
+        cap.kvb_attend(c.table([100], [1]), k, k.cpu(), kv_heads=1, scale=1.0)
     torch.cuda.synchronize()
     for x, y in zip(c.all(), before):
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    table = c.table([100], [1])
+    table.setflags(write=False)
+    o = torch.empty_like(k)
+    cap.kvb_attend(table, k, o, kv_heads=1, scale=0.1)
+    assert torch.equal(o, run_attend(c, [100], [1], k, 0.1)[0])
 
 
 # ------------------------------------------------------- a whole session --

@@ -190,9 +190,11 @@ def test_binding_refusals():
     for bad in (idx.long(), idx[:2], torch.zeros((2, 3, 4), dtype=torch.int32).transpose(0, 1)):
         with pytest.raises(ValueError):
             cap.kvb_select(t, q, bad, kv_heads=2, stream=0)
-    with pytest.raises(cap.CapsuleError) as e:  # fp32 reaches the library's own check
-        cap.kvb_append(t, k.float(), k.float(), stream=0)
-    assert e.value.status == cap.CAP_E_UNSUPPORTED
+    for call_ in (lambda: cap.kvb_append(t, k, k, stream=0), lambda: cap.kvb_attend(t, q, o, kv_heads=2, scale=1.0, stream=0),
+                  lambda: cap.kvb_select(t, q, idx, kv_heads=2, stream=0)):
+        with pytest.raises(ValueError, match="GPU"):  # host tensors
+            call_()
+    assert cap.kvb_seqs([]).shape == (0, 8)
 
 
 def test_plain_forms():
