@@ -39,8 +39,9 @@
  *     runtime refused; in a multi-launch call (a fork into many sets, a
  *     gather of more than 64 environments, an append to more than 128
  *     buffers, a linear-attention prefill of many chunks, a delta-rule
- *     prefill) the launches before it stay enqueued, and what they wrote of
- *     the outputs is not a result.
+ *     prefill, attention over an FP8 cache with long or many-rowed
+ *     sequences, a block selection) the launches before it stay enqueued,
+ *     and what they wrote of the outputs is not a result.
  *   - The library reads launch status from the launch calls themselves and
  *     never clears an error the caller left pending (the runtime's "last
  *     error"); it clears only the error its own pointer-attribute query

@@ -10,7 +10,7 @@ namespace cap {
 constexpr int kKvbBlock = KVB_BLOCK;
 
 // Parameters carry a table of sequences by value, of KVB_MAX_SEQ or of kKvbFew: a launch
-// copies its arguments, and 4 KB of them cost the host about as much as the launch.
+// copies its arguments (4 KB of them 0.4 us of the host's 3.1).
 // The table comes last, so that the short form is the beginning of the long one.
 constexpr int kKvbFew = 4;
 

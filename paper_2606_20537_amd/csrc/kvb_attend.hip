@@ -131,26 +131,27 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
     const uint32_t item = w / (uint32_t)s.nsplit;  // (tile, kv head)
     const int split = (int)(w - item * (uint32_t)s.nsplit);
     const int h = (int)(item % (uint32_t)p.kv_heads);
-    const int64_t tile = item / (uint32_t)p.kv_heads;
+    int64_t tile = item / (uint32_t)p.kv_heads;
     // the tile's rows: `rows` of them from row r0 of the sequence, or of token `token` (sparse)
     int64_t r0, total;
     int64_t token = 0;
     if (SPARSE) {
         const int per = (G + 15) / 16;
-        token = tile / per;
+        token = row_div(tile, per);
         r0 = (tile - token * per) * 16;
         total = G;
     } else {
-        r0 = tile * 16;
         total = (int64_t)s.T * G;
+        tile = (total + 15) / 16 - 1 - tile;  // the longest first
+        r0 = tile * 16;
     }
     const int rows = (int)(total - r0 < 16 ? total - r0 : 16);
     const int tid = (int)threadIdx.x, lane = tid & 63, li = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = r0 + (li < rows ? li : rows - 1);  // rows past the last repeat it
-    const int64_t my_token = SPARSE ? token : row / G;
+    const int64_t my_token = SPARSE ? token : row_div(row, G);
     const int64_t pos = s.n - s.T + my_token;              // the last key that the row sees
-    const int64_t pos0 = s.n - s.T + (SPARSE ? token : r0 / G), pos1 = s.n - s.T + (SPARSE ? token : (r0 + rows - 1) / G);
+    const int64_t pos0 = s.n - s.T + (SPARSE ? token : row_div(r0, G)), pos1 = s.n - s.T + (SPARSE ? token : row_div(r0 + rows - 1, G));
 
     const int rowb = p.kv_heads * D;
     const uint8_t* kb = reinterpret_cast<const uint8_t*>(s.k);
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
     // the query rows, while the first keys are on their way
     bf16x8 q[D / 32];
     {
-        const uint8_t* src = static_cast<const uint8_t*>(p.q) + (s.t0 + my_token) * p.q_stride + ((int64_t)h * G + row % G) * D * 2;
+        const uint8_t* src = static_cast<const uint8_t*>(p.q) + (s.t0 + my_token) * p.q_stride + ((int64_t)h * G + row_mod(row, G)) * D * 2;
         #pragma unroll
         for (int j = 0; j < D / 32; ++j) q[j] = *reinterpret_cast<const bf16x8*>(src + (64 * (j / 2) + 16 * g + 8 * (j % 2)) * 2);
     }
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
     }
     __syncthreads();
     const bool whole = runs == 1;
-    const uint32_t slot = s.first_slot + w;
+    const uint32_t slot = s.first_slot + (uint32_t)((tile * p.kv_heads + h) * s.nsplit + split);
     constexpr int kPer = D / 4;  // threads of a row
     #pragma unroll
     for (int i = 0; i < 16 * kPer / kThreads; ++i) {
@@ -348,8 +349,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
             continue;
         }
         const float z = all_s[rr][1], inv = z > 0.0f || z != z ? 1.0f / z : 0.0f;
-        const int64_t tok = s.t0 + (SPARSE ? token : (r0 + rr) / G);
-        const int64_t at = (tok * p.heads + (int64_t)h * G + (r0 + rr) % G) * D + c;
+        const int64_t tok = s.t0 + (SPARSE ? token : row_div(r0 + rr, G));
+        const int64_t at = (tok * p.heads + (int64_t)h * G + row_mod(r0 + rr, G)) * D + c;
         const bf16x2 a = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
         const bf16x2 b = __builtin_convertvector((f32x2){o[2] * inv, o[3] * inv}, bf16x2);
         *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + at) =
@@ -360,8 +361,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
         if (!whole) {
             *reinterpret_cast<f32x2*>(p.part_ml + ((int64_t)slot * 16 + tid) * 2) = (f32x2){mm, z};
         } else if (p.lse) {
-            const int64_t tok = s.t0 + (SPARSE ? token : (r0 + tid) / G);
-            p.lse[tok * p.heads + (int64_t)h * G + (r0 + tid) % G] = (mm + __builtin_amdgcn_logf(z)) * kLn2;
+            const int64_t tok = s.t0 + (SPARSE ? token : row_div(r0 + tid, G));
+            p.lse[tok * p.heads + (int64_t)h * G + row_mod(r0 + tid, G)] = (mm + __builtin_amdgcn_logf(z)) * kLn2;
         }
     }
 }
@@ -402,8 +403,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendTable<N> 
         n = s.nsplit;
     } else {
         const int64_t row = t * G + head % G;
-        item = row / p.tile * p.kv_heads + h;
-        rr = (int)(row % p.tile);
+        item = (int64_t)row_div(row, p.tile) * p.kv_heads + h;
+        rr = (int)row_mod(row, p.tile);
         if (t >= 0 && t < s.T) n = tile_runs(s, tile_blocks(s, row - rr, p.tile, (int64_t)s.T * G, G));
     }
     const int64_t slot = s.first_slot + item * s.nsplit;

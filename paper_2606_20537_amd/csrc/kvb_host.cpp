@@ -95,7 +95,8 @@ constexpr unsigned bit(int i) { return 1u << i; }
 constexpr int64_t kWholeBlocks = 8;
 
 // Blocks that a run of a cut sequence takes, for tiles of 16 rows; `total`: the
-// blocks of all tiles.  A workgroup to a CU while runs stay short, two where they
+// blocks of all tiles, each with its sequence's (512 tokens of 1024, 256 channels, 512 tiles
+// that see 12 of 16 blocks in the mean: 27 us whole, 42 as two runs).  A workgroup to a CU while runs stay short, two where they
 // are long enough for one's loads to cover the other's arithmetic.  Measured (us,
 // both launches, 8 query heads on each KV head of 256; runs of): 16385 rows x 4 heads
 // 2: 19.3, 4: 16.4, 6: 15.6, 8: 16.7, 16: 20.8; 131072 + 18561 rows x 4 heads
@@ -107,41 +108,57 @@ int64_t run_of_16(int64_t total, int64_t longest) {
     return std::max<int64_t>(2, one <= 16 ? one : (total + 511) / 512);
 }
 
-// The same for tiles of 128 rows: the length whose estimate is lowest.  `rows` of all
-// tiles, `tiles` of them, the longest's blocks, the blocks of all.  A block takes a
-// workgroup `alone` us by itself on a CU; where two fit, they take `both` us for a block
-// each.  Writing, reading and joining the runs' parts takes 4 us and 2.5 TB/s.  Measured
-// (us; cut into 1, 2, 4, 5, 6, 8): 161 tokens behind 16384, 32 heads on 4 of 256 channels
-// 574, 300, 160, 137, 217 (a second round), 171; 16 heads on 4 of 128 368, 188, 105, 91, 104,
-// 85; a whole prefill of 2048 tokens, 128 channels 55, 62, 72; of 1024 30, 30, 34.
-int64_t run_of_128(int32_t d, int64_t rows, int64_t tiles, int64_t longest, int64_t total) {
-    const double alone = d == 256 ? 2.2 : d == 128 ? 1.42 : 1.15, both = d == 128 ? 2.27 : 1.97;
-    int64_t per = longest;
-    double best = 1e30;
-    for (int64_t cut = 1; cut <= 32 && cut <= longest && (cut == 1 || tiles * cut <= 1024); ++cut) {
-        const int64_t run = (longest + cut - 1) / cut;
-        // the tiles' blocks are taken as spread evenly about their mean, up to the longest: how many
-        // runs they have, and the share of rows with more than one
-        const double mid = (double)total / (double)tiles, low = std::max(1.0, 2.0 * mid - (double)longest);
-        const double share = run >= longest ? 0.0 : (double)run <= low ? 1.0 : (double)(longest - run) / ((double)longest - low);
-        const int64_t wgs = cut == 1 ? tiles : (int64_t)std::ceil((double)tiles * (mid / (double)run + 0.5 * share));
-        const double mean = (double)total / (double)wgs;
-        double us = alone * (double)run;
-        if (wgs > 256) us = std::max(us, d == 256 ? alone * mean * (double)((wgs + 255) / 256) : both * mean * (double)((wgs + 511) / 512));
-        if (cut > 1) us += 4.0 + share * (double)(rows * cut * d) * 8.0 / 2.5e6;
-        if (us < best) {
-            best = us;
-            per = run;
-        }
+// What the sequences of a launch have: blocks of the longest, blocks of all tiles, those
+// that they see, rows, tiles.
+struct Work { int64_t longest, total, seen, rows, tiles; };
+
+// The same for tiles of 128 rows: the length whose estimate is lowest.  A workgroup takes 5 us
+// to begin and end and `alone` us a block by itself on a CU; where two fit, they take `both` us
+// for a block each.  Joining takes 3 us, the runs' parts 3 TB/s.  Measured (us, both
+// launches; cut into 1, 2, 3, 4, 5, 6, 8): 161 tokens behind 16384, 32 heads on 4 of 256
+// channels 459, 247, 174, 138, 120, 186 (a second round), 155; of 128 355, 189, 133, 104, 87,
+// 104, 86; a whole prefill of 2048 tokens, 16 heads on 4 of 128 channels 55, 59, 50, 68, 58,
+// 61, 87; of 1024 30, 29, 32, 32, 32, 29, 44; of 8192 372, 468, 376.
+struct Plan128 { int64_t run; double us; };
+Plan128 plan_128(int32_t d, const Work& x) {
+    const double alone = d == 256 ? 1.75 : d == 128 ? 1.37 : 1.15, both = d == 128 ? 2.5 : 1.85, ends = 5.0;
+    const double tiles = (double)x.tiles, mid = (double)x.seen / tiles;
+    Plan128 best{x.longest, 1e30};
+    for (int64_t cut = 1; cut <= 32 && cut <= x.longest; ++cut) {
+        if (cut > 1 && (x.longest <= kWholeBlocks || x.tiles * cut > 1024)) break;
+        const int64_t run = (x.longest + cut - 1) / cut;
+        // the tiles' blocks are taken as spread evenly about their mean, up to the longest: the
+        // share of tiles with more than one run, and how many runs there are
+        const double low = std::max(1.0, 2.0 * mid - (double)x.longest);
+        const double share = run >= x.longest ? 0.0 : (double)run <= low ? 1.0 : (double)(x.longest - run) / ((double)x.longest - low);
+        const double wgs = cut == 1 ? tiles : std::ceil(tiles * (mid / (double)run + 0.5 * share));
+        const double mean = (double)x.seen / wgs;
+        double us = alone * (double)run + ends;
+        if (wgs > 256) us = std::max(us, std::ceil(wgs / (d == 256 ? 256 : 512)) * ((d == 256 ? alone : both) * mean + ends));
+        if (cut > 1) us += 3.0 + (wgs - tiles * (1.0 - share)) * (double)x.rows / tiles * (double)d * 8.0 / 3e6;
+        if (us < best.us) best = {run, us};
     }
-    return per;
+    return best;
 }
 
-// Query rows of a sequence and KV head from which it takes tiles of 128 (with a block list
-// never).  Measured (us, tiles of 16 / of 128): 8 heads on each of 4 KV heads of 256, 16385
-// rows, 64 query rows 26.8 / 36.3, 128 37.2 / 41.5, 256 59.1 / 49.3; 128 channels, 131072 rows,
-// 64 query rows 59.9 / 110, 96 110 / 108; 300 rows, 256 query rows 13.6 / 16.2.
+// Query rows of a sequence and KV head from which it may take tiles of 128 (with a block list
+// never), and what tiles of 16 take instead: a time for each block and tile, more of it where
+// less than a workgroup to a CU leaves them in runs, and a join.  Both launches' estimates are
+// without their 4 us from call to call.  Measured (us, tiles of 16 / of 128; tokens, rows held,
+// query heads on KV heads of d channels):
+//     512 of 512, 16 on 4 of 256        17 / 25      16 such sequences     174 / 95
+//     2048 of 2048, 16 on 4 of 256     112 / 77      of 128  66 / 50       of 64  36 / 39
+//     161 behind 16384, 4 on 4 of 256   57 / 40      of 128  36 / 30       of 64  23 / 23
+//     64 of 300, 16 on 4 of 256         13 / 19      32 such sequences      53 / 27
+//     8192 of 8192, 16 on 4 of 256    1230 / 590     of 128 751 / 353      of 64 374 / 246
+// Over 135 such calls the estimates' choice is 1.5% behind the better one, tiles of 128
+// throughout 15%.  A tile of 128 for 64 rows takes 110 where tiles of 16 take 60 (131072 rows).
 constexpr int64_t kRowsFor128 = 129;
+double us_of_16(int32_t d, const Work& x) {
+    const double block = d == 256 ? 2.3e-3 : d == 128 ? 1.4e-3 : 0.72e-3, tile = d == 256 ? 10e-3 : d == 128 ? 4.2e-3 : 2.6e-3;
+    return 4.0 + block * (double)x.seen * (x.tiles < 256 ? 1.6 : 1.0) + tile * (double)x.tiles +
+           (run_of_16(x.total, x.longest) < x.longest ? 4.0 : 0.0);
+}
 
 // p[0]: the sequences in tiles of 16 rows, p[1]: those in tiles of 128, a launch each.
 int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams (&p)[2]) {
@@ -149,22 +166,27 @@ int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams (&p)[2]) {
     if (rc != CAP_OK) return rc;
     if (a->idx ? a->n_sel < 1 : a->n_sel != 0) return CAP_E_INVAL;
     const int64_t G = a->heads / a->kv_heads;
-    struct { int64_t longest, total, rows, items, per; } sum[2] = {};
-    auto kind = [&](const kvb_seq& s) { return !a->idx && s.T * G >= kRowsFor128 ? 1 : 0; };
     auto blocks = [&](const kvb_seq& s) { return a->idx ? (int64_t)a->n_sel : (s.n + kKvbBlock - 1) / kKvbBlock; };
-    auto tiles = [&](const kvb_seq& s) {  // of all KV heads
-        const int64_t tile = kind(s) ? 128 : 16;
+    auto tiles = [&](const kvb_seq& s, int k) {  // of all KV heads
+        const int64_t tile = k ? 128 : 16;
         return (a->idx ? s.T * ((G + 15) / 16) : (s.T * G + tile - 1) / tile) * a->kv_heads;
     };
-    for (int32_t i = 0; i < a->n_seq; ++i) {
-        const kvb_seq& s = a->seqs[i];
-        if (s.T == 0) continue;
-        auto& x = sum[kind(s)];
+    auto add = [&](Work& x, const kvb_seq& s, int k) {
         x.longest = std::max(x.longest, blocks(s));
-        x.total += tiles(s) * (blocks(s) - (kind(s) ? s.T / kKvbBlock / 2 : 0));  // the tiles of a prefill see half of its blocks
+        x.total += tiles(s, k) * blocks(s);
+        x.seen += tiles(s, k) * (blocks(s) - (a->idx ? 0 : s.T / kKvbBlock / 2));  // a prefill's tiles see half of its own
         x.rows += s.T * a->heads;
-        x.items += tiles(s);
-    }
+        x.tiles += tiles(s, k);
+    };
+    auto many = [&](const kvb_seq& s) { return !a->idx && s.T * G >= kRowsFor128; };
+    Work as[2] = {}, work[2] = {};  // the sequences of many rows, were they in tiles of 16 or 128; each launch
+    for (int32_t i = 0; i < a->n_seq; ++i)
+        for (int k = 0; k < 2 && many(a->seqs[i]); ++k) add(as[k], a->seqs[i], k);
+    const bool wide = as[1].tiles > 0 && plan_128(a->d, as[1]).us < us_of_16(a->d, as[0]);
+    auto kind = [&](const kvb_seq& s) { return wide && many(s) ? 1 : 0; };
+    for (int32_t i = 0; i < a->n_seq; ++i)
+        if (a->seqs[i].T > 0) add(work[kind(a->seqs[i])], a->seqs[i], kind(a->seqs[i]));
+    int64_t per[2];
     for (int k = 0; k < 2; ++k) {
         p[k].tokens = a->tokens;
         p[k].heads = a->heads;
@@ -172,8 +194,8 @@ int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams (&p)[2]) {
         p[k].d = a->d;
         p[k].n_sel = a->n_sel;
         p[k].tile = k ? 128 : 16;
-        sum[k].per = k ? run_of_128(a->d, sum[k].rows, sum[k].items, sum[k].longest, sum[k].total) : run_of_16(sum[k].total, sum[k].longest);
-        if (a->idx) sum[k].per = std::min<int64_t>(sum[k].per, cap::kKvbListRun);
+        per[k] = k == 0 ? run_of_16(work[k].total, work[k].longest) : work[k].tiles > 0 ? plan_128(a->d, work[k]).run : 1;
+        if (a->idx) per[k] = std::min<int64_t>(per[k], cap::kKvbListRun);
     }
     int64_t wgs[2] = {}, slots[2] = {}, t0 = 0;
     for (int32_t i = 0; i < a->n_seq; ++i) {
@@ -188,12 +210,12 @@ int plan_attend(const kvb_attend_args* a, cap::KvbAttendParams (&p)[2]) {
         x.t0 = t0;
         x.T = (int32_t)s.T;
         const int64_t nb = blocks(s);
-        x.nsplit = (int32_t)((nb + sum[k].per - 1) / sum[k].per);
+        x.nsplit = (int32_t)((nb + per[k] - 1) / per[k]);
         x.per = (int32_t)((nb + x.nsplit - 1) / x.nsplit);  // of even lengths
         x.first_wg = (uint32_t)wgs[k];
         x.first_slot = (uint32_t)slots[k];
-        wgs[k] += tiles(s) * x.nsplit;
-        if (x.nsplit > 1) slots[k] += tiles(s) * x.nsplit;
+        wgs[k] += tiles(s, k) * x.nsplit;
+        if (x.nsplit > 1) slots[k] += tiles(s, k) * x.nsplit;
         if (wgs[k] > 0x7fffffff) return CAP_E_UNSUPPORTED;
         t0 += s.T;
     }

@@ -1,19 +1,23 @@
 // Causal attention of many query rows over a block-scaled FP8 KV cache on gfx950
 // (the formulas and the sharing of K and V by a group's heads: kvb_attend.hip).
 //
-// A workgroup of four waves takes 128 query rows of a KV head, 32 to a wave, and
-// walks the blocks; K and V codes of a block go through LDS, two buffers, one
-// barrier a block.
+// A workgroup takes 128 query rows of a KV head and walks the blocks; K and V of a block go
+// through LDS, one barrier a block.  A wave has 32 of the rows; of 256 channels, where a
+// row's outputs leave registers for one wave on a SIMD, two waves share the 32: each forms
+// the scores and weights of half of the block's 64 keys, leaves the weights in LDS for the
+// other, and multiplies all 64 with half of the channels of V, so that every SIMD has two.
+// (161 tokens behind 16384, 32 heads on 4 of 256 channels, uncut: 575 us alone, 459 shared;
+// of 128 channels, where two workgroups fit a CU, a prefill of 8192 takes 372 alone, 448 shared.)
 //  * S^T = K Q^T on 32x32x16 bf16 tiles: the codes times their power-of-two scale are
-//    exact in bf16, converted once for the four waves on their way into LDS.  (FP8
+//    exact in bf16, converted once for all waves on their way into LDS.  (FP8
 //    instructions with Q split in two take the same matrix time, but their sums lose
 //    what is small against the largest product: scores off by 1.6e-3 where a head's
 //    channels differ in size.)
 //  * O^T = V^T P^T on 32x32x64 FP8 tiles straight from the codes, with the scales as the
-//    instruction's scale operands.  The weights of a block are taken against the block's
+//    instruction's scale operands.  The weights of 32 rows are taken against their
 //    own highest score, rounded up to an integer c in log2 units, w = 2^(x - c + 8) in
 //    (0, 256], and split into two E4M3 rows, w = hi + lo / 16 (relative 2^-8 at most, that
-//    of bf16, or 2^-21 of the block's largest weight where that is more); the
+//    of bf16, or 2^-21 of the 32's largest weight where that is more); the
 //    instruction's sums lose 2^-12 of the sum of the products' magnitudes at most.
 //    2^(c - m) is the instruction's scale of a row, an exact power of two; m is the c of
 //    the row's first block, raised only where a later one is 2^64 above: O and l are
@@ -21,18 +25,16 @@
 //    Against bf16 operands that is the same matrix time (FP8 runs at twice the rate),
 //    half the LDS traffic and no conversion of V.
 //
-// One wave to a SIMD has registers for 32 rows of 256 channels, so the wave itself
-// keeps the matrix pipe busy: half of a block's softmax stands between the matrix
-// instructions of K Q^T of the block after it, the other half (the maximum first)
-// between those of V^T P^T of the block before it, in slices that the scheduler
-// must not move.
+// Half of a block's softmax stands between the matrix instructions of K Q^T of the block
+// after it, the other half (the maximum first) between those of V^T P^T of the block before
+// it, in slices that the scheduler must not move: a wave's vector instructions run beside
+// its matrix instructions only where they are issued between them.
 //
-// 16384 tokens, 32 heads on 4 KV heads of 256 channels: 4.7 to 4.9 ms, 900 to 940 TFLOP/s (the
-// library's bf16 product of 8192 reaches 1243).  Of the 5200 cycles of a block's step the
-// matrix pipe is busy 2050 and the vector unit 2400, little of it side by side (a wave's
-// vector instructions add most of their time to its own matrix instructions), and 1000 are
-// waits for LDS and the barrier.  The plain order of a step took 6.0 ms with FP8 scores, the
-// slices 4.0 to 4.2.
+// 16384 tokens, 32 heads on 4 KV heads of 256 channels: 4.2 to 4.3 ms, 1030 to 1050 TFLOP/s
+// (the library's bf16 product of 8192 reaches 1243).  Of the 4700 cycles of a block's step
+// the matrix pipe is busy 2050; the rest are vector instructions beyond what stands beside
+// them, reads of LDS and the barrier, at clocks that fall under matrix load.  A workgroup
+// begins and ends in 5 us, which short prefills feel (512 tokens, 16 heads on 4 of 256: 25 us).
 //
 // A lane has one query row in both products and S^T's accumulators are P^T's
 // operand: byte 4 j + i of lane half h is key 8 j + 4 h + i.  V's operand has its
@@ -58,7 +60,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kThreads = 256;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -105,11 +106,22 @@ __device__ inline int swizzle_v(int key) {
     return 2 * i;
 }
 
+// Waves that share 32 query rows, and threads of a workgroup.
 template <int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(const KvbAttendParams p) {
-    constexpr int NJ = D / 32, NT = D / 32, kUnits = D / 16, kRows = kThreads / kUnits, kLoads = kKvbBlock / kRows;
+constexpr int kShare = D == 256 ? 2 : 1;
+template <int D>
+constexpr int kThreads = 256 * kShare<D>;
+
+template <int D>
+__global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttendParams p) {
+    constexpr int W = kShare<D>, S = 2 / W, NT = D / 32 / W;  // a wave's score tiles of 32 keys, its tiles of 32 channels of V
+    constexpr int NJ = D / 32;
+    constexpr int kUnits = D / 16, kRows = kThreads<D> / kUnits, kLoads = kKvbBlock / kRows;
     __shared__ __attribute__((aligned(1024))) uint8_t k_s[2][kKvbBlock * D * 2];  // bf16
     __shared__ __attribute__((aligned(1024))) uint8_t v_s[3][kKvbBlock * D];
+    // of two waves that share their rows:
+    __shared__ u32x4 p_s[2][4][2][2][64];  // weights: parity of the block, rows, half of the keys, hi or lo
+    __shared__ float c_s[2][4][2][32];     // their references
     __shared__ int nan_s[3];
 
     const KvbAttendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
@@ -121,35 +133,15 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     const int64_t total = (int64_t)s.T * G, tiles = (total + 127) / 128;
     const int64_t tile = tiles - 1 - item / (uint32_t)p.kv_heads;  // the longest first
     const int tid = (int)threadIdx.x, lane = tid & 63, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = wave / W, part = wave % W;
     const int nblk = tile_blocks(s, tile * 128, 128, total, G), runs = tile_runs(s, nblk);
     if (split >= runs) return;
-    const int64_t row0 = tile * 128, wrow0 = row0 + wave * 32, last = total - 1;
+    const int64_t row0 = tile * 128, wrow0 = row0 + group * 32, last = total - 1;
     const int64_t row = wrow0 + (lane & 31) < last ? wrow0 + (lane & 31) : last;  // rows past the last repeat it
-    const int64_t before = s.n - s.T, token = row / G, pos = before + token;     // the last key that the row sees
+    const int64_t before = s.n - s.T, token = row_div(row, G), pos = before + token;     // the last key that the row sees
     // the wave's first position, the tile's
-    const int64_t wpos0 = before + (wrow0 < last ? wrow0 : last) / G;
-    const int64_t tpos0 = before + row0 / G;
-
-    // channels 16 s + 8 half .. + 7 of the lane's row; scores in log2 units are the products times f > 0
-    bf16x8 q[D / 16];
-    const float f = p.scale_log2 == 0.0f ? 1.0f : __builtin_fabsf(p.scale_log2);
-    {
-        const uint8_t* src = static_cast<const uint8_t*>(p.q) + (s.t0 + token) * p.q_stride + ((int64_t)h * G + row % G) * D * 2;
-        #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            u32x4 x = *reinterpret_cast<const u32x4*>(src + (16 * i + 8 * half) * 2);
-            if (p.scale_log2 <= 0.0f) {  // a negative scale turns the row's signs, zero makes it zero (but not its NaN)
-                #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float a = bits_f32(x[k] << 16), b = bits_f32(x[k] & 0xFFFF0000u);
-                    const float by = p.scale_log2 < 0.0f ? -1.0f : 0.0f;
-                    x[k] = f32_bits(a * by) >> 16 | (f32_bits(b * by) & 0xFFFF0000u);
-                }
-            }
-            q[i] = __builtin_bit_cast(bf16x8, x);
-        }
-    }
+    const int64_t wpos0 = before + row_div(wrow0 < last ? wrow0 : last, G);
+    const int64_t tpos0 = before + row_div(row0, G);
 
     const int rowb = p.kv_heads * D;
     const uint8_t* kb = reinterpret_cast<const uint8_t*>(s.k);
@@ -209,70 +201,120 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
     const int kaddr = (lane & 31) * 2 * D + 16 * (half ^ swizzle_k<D>(lane & 31));
     const int vkey = 4 * half + ((lane & 15) >> 1 & 3) + 8 * ((lane & 15) >> 3);
     const int vaddr = vkey * D + 16 * ((lane >> 4 & 1) ^ swizzle_v<D>(vkey)) + 8 * (lane & 1);
-    auto read_k = [&](int buf, int t, int i) {  // keys 32 t .. + 31, channels 16 i .. + 15
-        return *reinterpret_cast<const bf16x8*>(&k_s[buf][(kaddr ^ (32 * i)) + t * 64 * D]);
+    // Rows of q and o are 2 D bytes, as those of K, and pass through its buffers, 16 bytes of a
+    // row to a thread: straight from a lane's row an instruction takes a cycle a lane (the 16
+    // loads of 8 waves 8600 cycles).
+    constexpr int kRowUnits = D / 8, kRowPass = kThreads<D> / kRowUnits, kPasses = 128 / kRowPass;
+    const int qrow = tid / kRowUnits, qunit = tid % kRowUnits;
+    auto row_bytes = [&](int r) { return &k_s[0][0] + r * 2 * D + 16 * (qunit ^ swizzle_k<D>(r)); };
+    auto token_of = [&](int64_t r) { return s.t0 + row_div(r, G); };
+    auto head_of = [&](int64_t r) { return h * G + (int)row_mod(r, G); };
+
+    // channels 16 s + 8 half .. + 7 of the lane's row; scores in log2 units are the products times f > 0
+    bf16x8 q[D / 16];
+    const float f = p.scale_log2 == 0.0f ? 1.0f : __builtin_fabsf(p.scale_log2);
+    {
+        u32x4 x[kPasses];
+        #pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int64_t at = row0 + qrow + i * kRowPass, r = at < last ? at : last;
+            x[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.q) + token_of(r) * p.q_stride + (int64_t)head_of(r) * D * 2 + 16 * qunit);
+        }
+        if (p.scale_log2 <= 0.0f) {  // a negative scale turns the rows' signs, zero makes them zero (but not their NaN)
+            const float by = p.scale_log2 < 0.0f ? -1.0f : 0.0f;
+            #pragma unroll
+            for (int i = 0; i < kPasses; ++i)
+                #pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float a = bits_f32(x[i][k] << 16), b = bits_f32(x[i][k] & 0xFFFF0000u);
+                    x[i][k] = f32_bits(a * by) >> 16 | (f32_bits(b * by) & 0xFFFF0000u);
+                }
+        }
+        #pragma unroll
+        for (int i = 0; i < kPasses; ++i) *reinterpret_cast<u32x4*>(row_bytes(qrow + i * kRowPass)) = x[i];
+    }
+    if (tid < 3) nan_s[tid] = -1;
+    fetch(kb, begin, ks);
+    fetch(vb, begin, vs);
+    load_scales();
+    dev::lds_barrier();
+    #pragma unroll
+    for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const bf16x8*>(&k_s[0][0] + (kaddr ^ (32 * i)) + group * 64 * D);
+
+    auto read_k = [&](int buf, int t, int i) {  // keys 32 (part + t) .. + 31, channels 16 i .. + 15
+        return *reinterpret_cast<const bf16x8*>(&k_s[buf][(kaddr ^ (32 * i)) + (part + t) * 64 * D]);
     };
-    auto read_v = [&](int buf, int i) {  // channels 32 i .. + 31
+    auto read_v = [&](int buf, int i) {  // channels 32 (part NT + i) .. + 31
         i32x8 a;
         #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                (__attribute__((address_space(3))) i32x2*)&v_s[buf][(vaddr ^ (32 * i)) + 16 * k * D]);
+                (__attribute__((address_space(3))) i32x2*)&v_s[buf][(vaddr ^ (32 * (part * NT + i))) + 16 * k * D]);
             a[2 * k] = v[0];
             a[2 * k + 1] = v[1];
         }
         return a;
     };
 
-    f32x16 acc[NT], x[2], y[2];  // O^T; scores of block b and of block b + 1
+    f32x16 acc[NT], x[S], y[S];  // O^T; scores of block b and of block b + 1
     #pragma unroll
     for (int i = 0; i < NT; ++i) acc[i] = (f32x16){};
     float m = kNegInf, l = 0.0f;
     float c = 0.0f, base = 0.0f, sum = 0.0f;  // of block b's softmax, whose first half is done when its step begins
-    i32x8 ph, pl;
+    int ph[4 * S], pl[4 * S];                 // its weights, of the wave's keys
 
-    auto mask = [&](int b, f32x16 (&z)[2]) {
+    auto mask = [&](int b, f32x16 (&z)[S]) {
         const int64_t r0 = (int64_t)b * kKvbBlock;
         if (r0 + kKvbBlock - 1 <= wpos0) return;  // every row sees every key
-        int sees = (int)(pos - r0 < kKvbBlock ? pos - r0 : kKvbBlock) - 4 * half;  // keys up to here
+        int sees = (int)(pos - r0 < kKvbBlock ? pos - r0 : kKvbBlock) - 4 * half - 32 * part;  // keys up to here
         asm volatile("" : "+v"(sees));  // rare: not to be computed ahead of the branch
         #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < S; ++t)
             #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (32 * t + 8 * (r / 4) + r % 4 > sees) z[t][r] = kNegInf;
     };
-    auto weights = [&](int q, const f32x16 (&z)[2], int& hi4, int& lo4) {  // of keys 8 q + 4 half .. + 3
+    auto weights = [&](int i) {  // of the wave's keys 8 i + 4 half .. + 3
         float e[4];
         #pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[q / 4][4 * (q % 4) + i], f, -base));
+        for (int k = 0; k < 4; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i / 4][4 * (i % 4) + k], f, -base));
         sum += (e[0] + e[1]) + (e[2] + e[3]);
-        split4(e, hi4, lo4);
+        split4(e, ph[i], pl[i]);
     };
-    auto highest = [&](const f32x16 (&z)[2], int part) {  // of a quarter of a lane's scores
-        const int t = part / 2, r = 8 * (part % 2);
-        const float u = __builtin_fmaxf(__builtin_fmaxf(z[t][r], z[t][r + 1]), z[t][r + 2]);
-        const float v = __builtin_fmaxf(__builtin_fmaxf(z[t][r + 3], z[t][r + 4]), z[t][r + 5]);
-        return __builtin_fmaxf(__builtin_fmaxf(u, v), __builtin_fmaxf(z[t][r + 6], z[t][r + 7]));
+    auto highest = [&](int i) {  // of 8 of a lane's scores
+        const int t = i / 2, r = 8 * (i % 2);
+        const float u = __builtin_fmaxf(__builtin_fmaxf(x[t][r], x[t][r + 1]), x[t][r + 2]);
+        const float v = __builtin_fmaxf(__builtin_fmaxf(x[t][r + 3], x[t][r + 4]), x[t][r + 5]);
+        return __builtin_fmaxf(__builtin_fmaxf(u, v), __builtin_fmaxf(x[t][r + 6], x[t][r + 7]));
     };
     auto reference = [&](float top) {
         c = __builtin_ceilf(pair_max(top) * f);
         base = c == kNegInf ? 0.0f : c - 8.0f;
         sum = 0.0f;
     };
+    // The first half of block b's softmax in slices 0..7, from its scores in y.
+    float top = kNegInf;
+    auto slice = [&](int u, int b) {
+        if (u == 1) {
+            #pragma unroll
+            for (int t = 0; t < S; ++t) x[t] = y[t];
+            mask(b, x);
+            #pragma unroll
+            for (int t = 0; t < S; ++t) asm volatile("" : "+v"(x[t]));
+            top = S == 2 ? __builtin_fmaxf(highest(0), highest(1)) : highest(0);
+        }
+        if (u == 2) reference(__builtin_fmaxf(top, S == 2 ? __builtin_fmaxf(highest(2), highest(3)) : highest(1)));
+        if (u >= 3 && u < 7 && (S == 2 || u % 2 == 0)) weights((u - 3) * S / 2);
+    };
 
     // Block b's K lies in buffer (b - begin) & 1, its V in (b - begin) % 3.  The step
     // of block b reads K of b + 1, then V of b; in its first half K of b + 2 is
     // written, in its second V of b + 2, each where the block before the last was read.
     // Blocks past the end repeat the last one.
-    if (tid < 3) nan_s[tid] = -1;
     auto clamp = [&](int b) { return b < end ? b : end - 1; };
     int ve = 127;  // exponent of V's scale of b
-    if (begin < end) {
-        fetch(kb, begin, ks);
-        fetch(vb, begin, vs);
-        load_scales();
-        dev::lds_barrier();
+    {
+        dev::lds_barrier();  // q has been read
         #pragma unroll
         for (int i = 0; i < kLoads; ++i) stage_k(0, i, k_scale(begin));
         stage_v(begin, 0);
@@ -280,140 +322,126 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
         fetch(vb, clamp(begin + 1), vs);
         ve = v_exponent(begin);
         dev::lds_barrier();
-        x[0] = (f32x16){};
-        x[1] = (f32x16){};
         #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            x[0] = mma16(read_k(0, 0, i), q[i], x[0]);
-            x[1] = mma16(read_k(0, 1, i), q[i], x[1]);
+        for (int t = 0; t < S; ++t) {
+            y[t] = (f32x16){};
+            #pragma unroll
+            for (int i = 0; i < D / 16; ++i) y[t] = mma16(read_k(0, t, i), q[i], y[t]);
         }
         #pragma unroll
         for (int i = 0; i < kLoads; ++i) stage_k(1, i, k_scale(clamp(begin + 1)));
         stage_v(clamp(begin + 1), 1);
         fetch(kb, clamp(begin + 2), ks);
         fetch(vb, clamp(begin + 2), vs);
-        mask(begin, x);
-        reference(__builtin_fmaxf(__builtin_fmaxf(highest(x, 0), highest(x, 1)), __builtin_fmaxf(highest(x, 2), highest(x, 3))));
         #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            int a, d;
-            weights(q, x, a, d);
-            ph[q] = a;
-            pl[q] = d;
-        }
+        for (int u = 0; u < 8; ++u) slice(u, begin);
         dev::lds_barrier();
     }
     int vbuf = 0;
     for (int b = begin; b < end; ++b) {
         const int kbuf = (b - begin) & 1;
-        if constexpr (D == 256) {  // O stays in accumulation registers
-            #pragma unroll
-            for (int i = 0; i < NT; ++i) asm volatile("" : "+a"(acc[i]));
-        }
         const int next_ve = v_exponent(clamp(b + 1));
         if (b + 2 - e0 >= 64 && b + 2 < end) {
             e0 = b + 2;
             load_scales();
         }
         const float next_scale = k_scale(clamp(b + 2));
-        i32x8 v0, v1;
+        i32x8 v[S];
         {
-            bf16x8 k[4], next[4];
+            bf16x8 k[2 * S], next[2 * S];
             #pragma unroll
-            for (int i = 0; i < 4; ++i) k[i] = read_k(kbuf ^ 1, i & 1, i >> 1);
+            for (int i = 0; i < 2 * S; ++i) k[i] = read_k(kbuf ^ 1, i % S, i / S);
             #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 if (j + 1 < NJ) {
                     #pragma unroll
-                    for (int i = 0; i < 4; ++i) next[i] = read_k(kbuf ^ 1, i & 1, 2 * (j + 1) + (i >> 1));
+                    for (int i = 0; i < 2 * S; ++i) next[i] = read_k(kbuf ^ 1, i % S, 2 * (j + 1) + i / S);
                 } else {
-                    v0 = read_v(vbuf, 0);
-                    v1 = read_v(vbuf, 1);
+                    #pragma unroll
+                    for (int i = 0; i < S; ++i) v[i] = read_v(vbuf, i);
                 }
                 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int step = 4 * j + i, steps = 4 * NJ;
-                    if (step < 2) y[step] = (f32x16){};
-                    y[i & 1] = mma16(k[i], q[2 * j + (i >> 1)], y[i & 1]);
+                for (int i = 0; i < 2 * S; ++i) {
+                    const int step = 2 * S * j + i, steps = 2 * S * NJ;
+                    if (j == 0 && i < S) y[i] = (f32x16){};
+                    y[i % S] = mma16(k[i], q[2 * j + i / S], y[i % S]);
                     #pragma unroll
-                    for (int w = 4 + step * 4 / steps; w < 4 + (step + 1) * 4 / steps; ++w) {
-                        int a, d;
-                        weights(w, x, a, d);
-                        ph[w] = a;
-                        pl[w] = d;
-                    }
+                    for (int u = 0; u < 2 * S; ++u)
+                        if (step == u * steps / (2 * S)) weights(2 * S + u);
                     #pragma unroll
                     for (int u = 0; u < kLoads; ++u)
                         if (step == (2 * u + 1) * steps / (2 * kLoads)) stage_k(kbuf, u, next_scale);
+                    if (W == 2 && step == steps * 3 / 4) {
+                        p_s[kbuf][group][part][0][lane] = (u32x4){(uint32_t)ph[0], (uint32_t)ph[1], (uint32_t)ph[2], (uint32_t)ph[3]};
+                        p_s[kbuf][group][part][1][lane] = (u32x4){(uint32_t)pl[0], (uint32_t)pl[1], (uint32_t)pl[2], (uint32_t)pl[3]};
+                        if (half == 0) c_s[kbuf][group][part][lane] = c;
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (j + 1 < NJ) {
                     #pragma unroll
-                    for (int i = 0; i < 4; ++i) k[i] = next[i];
+                    for (int i = 0; i < 2 * S; ++i) k[i] = next[i];
                 }
             }
         }
         // (what is needed late is not to be moved there)
-        asm volatile("" : "+v"(sum), "+v"(ph), "+v"(pl));
-        if constexpr (D == 256) asm volatile("" : "+a"(y[0]), "+a"(y[1]));
-        else asm volatile("" : "+v"(y[0]), "+v"(y[1]));
+        asm volatile("" : "+v"(sum));
+        #pragma unroll
+        for (int t = 0; t < S; ++t) asm volatile("" : "+v"(y[t]));
+        i32x8 wh, wl;       // weights of the block's 64 rows
+        float c0 = c, c1 = c;  // references of its two halves
+        if constexpr (W == 1) {
+            wh = (i32x8){ph[0], ph[1], ph[2], ph[3], ph[4], ph[5], ph[6], ph[7]};
+            wl = (i32x8){pl[0], pl[1], pl[2], pl[3], pl[4], pl[5], pl[6], pl[7]};
+            asm volatile("" : "+v"(wh), "+v"(wl));
+        }
         dev::lds_barrier();
         fetch(kb, clamp(b + 3), ks);
-        if (m == kNegInf) m = c;  // O and l are zero so far
-        float shift = c - m;
-        if (__any(shift > 64.0f)) {
-            float up = shift > 64.0f ? c : m;
+        if constexpr (W == 2) {
+            const u32x4 h0 = p_s[kbuf][group][0][0][lane], h1 = p_s[kbuf][group][1][0][lane];
+            const u32x4 l0 = p_s[kbuf][group][0][1][lane], l1 = p_s[kbuf][group][1][1][lane];
+            wh = (i32x8){(int)h0[0], (int)h0[1], (int)h0[2], (int)h0[3], (int)h1[0], (int)h1[1], (int)h1[2], (int)h1[3]};
+            wl = (i32x8){(int)l0[0], (int)l0[1], (int)l0[2], (int)l0[3], (int)l1[0], (int)l1[1], (int)l1[2], (int)l1[3]};
+            c0 = c_s[kbuf][group][0][lane & 31];
+            c1 = c_s[kbuf][group][1][lane & 31];
+        }
+        const float cm = __builtin_fmaxf(c0, c1);
+        if (m == kNegInf) m = cm;  // O and l are zero so far
+        if (__any(cm - m > 64.0f)) {
+            float up = cm - m > 64.0f ? cm : m;
             asm volatile("" : "+v"(up));  // rare: not to be computed ahead of the branch
             const float fade = __builtin_amdgcn_exp2f(m - up);
             #pragma unroll
             for (int i = 0; i < NT; ++i) acc[i] *= fade;
             l *= fade;
             m = up;
-            shift = c - m;
         }
-        shift = __builtin_fmaxf(shift, -127.0f);  // no score: -127, with weights of zero
-        l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(shift), l);
-        const int se = 127 + (int)shift, sl = se < 4 ? 0 : se - 4;
-        i32x4 nh, nl;
-        float top = kNegInf;
+        // no score: -127, with weights of zero
+        l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(__builtin_fmaxf((part ? c1 : c0) - m, -127.0f)), l);
+        // the instruction takes the scale of rows 0..31 from lanes 0..31, that of rows 32..63 from the others
+        const int se = 127 + (int)__builtin_fmaxf((half ? c1 : c0) - m, -127.0f), sl = se < 4 ? 0 : se - 4;
         #pragma unroll
-        for (int i = 0; i < NT; i += 2) {
-            i32x8 n0, n1;
-            if (i + 2 < NT) {
-                n0 = read_v(vbuf, i + 2);
-                n1 = read_v(vbuf, i + 3);
+        for (int i = 0; i < NT; i += S) {
+            i32x8 next[S];
+            if (i + S < NT) {
+                #pragma unroll
+                for (int t = 0; t < S; ++t) next[t] = read_v(vbuf, i + S + t);
             }
             #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 2 * S; ++k) {
                 const int step = 2 * i + k, steps = 2 * NT;
-                acc[i + (k & 1)] = mma8(k & 1 ? v1 : v0, k < 2 ? ph : pl, acc[i + (k & 1)], ve, k < 2 ? se : sl);
-                if (step == (NT > 2 ? 1 : 0)) {  // ahead of its first use below
-                    x[0] = y[0];
-                    x[1] = y[1];
-                    mask(b + 1, x);
-                    asm volatile("" : "+v"(x[0]), "+v"(x[1]));
-                }
-                // the first half of block b + 1's softmax: the maximum in the first quarter of the steps
+                acc[i + k % S] = mma8(v[k % S], k < S ? wh : wl, acc[i + k % S], ve, k < S ? se : sl);
                 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    if (u * steps / 8 != step) continue;
-                    if (u == 1) top = __builtin_fmaxf(highest(x, 0), highest(x, 1));
-                    if (u == 2) reference(__builtin_fmaxf(top, __builtin_fmaxf(highest(x, 2), highest(x, 3))));
-                    if (u >= 3 && u < 7) {
-                        int a, d;
-                        weights(u - 3, x, a, d);
-                        nh[u - 3] = a;
-                        nl[u - 3] = d;
-                    }
-                }
+                for (int u = 0; u < 8; ++u)
+                    if (u * steps / 8 == step) slice(u, b + 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (i + 2 < NT) {
-                v0 = n0;
-                v1 = n1;
+            if (i + S < NT) {
+                #pragma unroll
+                for (int t = 0; t < S; ++t) v[t] = next[t];
             }
         }
-        asm volatile("" : "+v"(sum), "+v"(nh), "+v"(nl));
+        asm volatile("" : "+v"(sum));
         {
             const int64_t r0 = (int64_t)b * kKvbBlock;
             if (r0 + kKvbBlock - 1 > tpos0 && nan_s[vbuf] == b) {
@@ -423,7 +451,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
                     for (int i = 0; i < NT; ++i)
                         #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            const uint8_t code = vb[(r0 + t) * rowb + h * D + 32 * i + 8 * (r / 4) + 4 * half + r % 4];
+                            const uint8_t code = vb[(r0 + t) * rowb + h * D + 32 * (part * NT + i) + 8 * (r / 4) + 4 * half + r % 4];
                             if ((code & 0x7F) == 0x7F && r0 + t <= pos) acc[i][r] = __builtin_nanf("");
                         }
                 }
@@ -431,41 +459,56 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void prefill_kernel(con
         }
         stage_v(clamp(b + 2), vbuf == 0 ? 2 : vbuf - 1);
         fetch(vb, clamp(b + 3), vs);
-        #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            ph[q] = nh[q];
-            pl[q] = nl[q];
-        }
         ve = next_ve;
         vbuf = vbuf == 2 ? 0 : vbuf + 1;
     }
 
     l += __shfl_xor(l, 32);
-    if (wrow0 + (lane & 31) > last) return;
+    if constexpr (W == 2) {
+        __syncthreads();  // the references have been read
+        if (half == 0) c_s[0][group][part][lane] = l;
+        __syncthreads();
+        l = c_s[0][group][0][lane & 31] + c_s[0][group][1][lane & 31];
+    }
+    int orow = qrow, orow0 = lane & 31;
+    asm volatile("" : "+v"(orow), "+v"(orow0));  // where rows lie: again, rather than held through the loop
+    const int channel = 32 * NT * part + 4 * half;  // the lane's first
     if (runs > 1) {
+        if (wrow0 + orow0 > last) return;
         const uint32_t slot = s.first_slot + (uint32_t)((tile * p.kv_heads + h) * s.nsplit + split);
-        const int64_t at = (int64_t)slot * 128 + wave * 32 + (lane & 31);
+        const int64_t at = (int64_t)slot * 128 + group * 32 + orow0;
         #pragma unroll
         for (int i = 0; i < NT; ++i)
             #pragma unroll
             for (int r = 0; r < 16; r += 4)
-                *reinterpret_cast<f32x4*>(p.part_o + at * D + 32 * i + 8 * (r / 4) + 4 * half) =
+                *reinterpret_cast<f32x4*>(p.part_o + at * D + channel + 32 * i + 8 * (r / 4)) =
                     (f32x4){acc[i][r], acc[i][r + 1], acc[i][r + 2], acc[i][r + 3]};
-        if (half == 0) *reinterpret_cast<f32x2*>(p.part_ml + at * 2) = (f32x2){m - 8.0f, l};
+        if (lane < 32 && part == 0) *reinterpret_cast<f32x2*>(p.part_ml + at * 2) = (f32x2){m - 8.0f, l};
         return;
     }
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    const int64_t out = (s.t0 + token) * p.heads + (int64_t)h * G + row % G;
+    const int out_addr = (kaddr ^ (16 * half)) + 8 * half + group * 64 * D;  // unit 0 of the lane's row, its half
     #pragma unroll
     for (int i = 0; i < NT; ++i)
         #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const bf16x2 a = __builtin_convertvector((f32x2){acc[i][r] * inv, acc[i][r + 1] * inv}, bf16x2);
             const bf16x2 b = __builtin_convertvector((f32x2){acc[i][r + 2] * inv, acc[i][r + 3] * inv}, bf16x2);
-            *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + out * D + 32 * i + 8 * (r / 4) + 4 * half) =
+            *reinterpret_cast<u32x2*>(&k_s[0][0] + (out_addr ^ (16 * (4 * (part * NT + i) + r / 4)))) =
                 (u32x2){__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
         }
-    if (half == 0 && p.lse) p.lse[out] = (m - 8.0f + __builtin_amdgcn_logf(l)) * kLn2;
+    if (lane < 32 && part == 0 && p.lse && wrow0 + orow0 <= last) {
+        const int64_t r = wrow0 + orow0;
+        p.lse[token_of(r) * p.heads + head_of(r)] = (m - 8.0f + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+    dev::lds_barrier();
+    #pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int64_t r = row0 + orow + i * kRowPass;
+        if (r <= last)
+            *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(p.o) + (token_of(r) * p.heads + head_of(r)) * D * 2 + 16 * qunit) =
+                *reinterpret_cast<const u32x4*>(row_bytes(orow + i * kRowPass));
+    }
 }
 
 }  // namespace
@@ -474,7 +517,7 @@ hipError_t launch_kvb_prefill(const KvbAttendParams& p, hipStream_t stream) {
     const void* fn = p.d == 64    ? reinterpret_cast<const void*>(&prefill_kernel<64>)
                      : p.d == 128 ? reinterpret_cast<const void*>(&prefill_kernel<128>)
                                   : reinterpret_cast<const void*>(&prefill_kernel<256>);
-    return launch_kernel(fn, dim3(p.wgs), dim3(kThreads), p, stream);
+    return launch_kernel(fn, dim3(p.wgs), dim3(p.d == 256 ? kThreads<256> : kThreads<128>), p, stream);
 }
 
 }  // namespace cap

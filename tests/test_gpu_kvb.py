@@ -27,8 +27,9 @@ class Caches:
         self.open = [torch.full((2, BLOCK, hkv, d), float("nan"), dtype=torch.bfloat16, device=device) for _ in rows]
 
     def table(self, n, T):
-        return cap.kvb_seqs([(self.k[i], self.v[i], self.scales[i], self.bounds[i], self.open[i], self.rows[i], n[i], T[i])
-                             for i in range(len(n))])
+        m = len(self.rows)  # a sequence may stand in the table more than once
+        return cap.kvb_seqs([(self.k[i % m], self.v[i % m], self.scales[i % m], self.bounds[i % m], self.open[i % m], self.rows[i % m],
+                              n[i], T[i]) for i in range(len(n))])
 
     def all(self):
         return [x for part in (self.k, self.v, self.scales, self.bounds, self.open) for x in part if x is not None]
@@ -185,10 +186,17 @@ def reread(c, n):
     return out
 
 
-def run_attend(c, n, T, q, scale, idx=None, lse=True, **kw):
+def run_attend(c, n, T, q, scale, idx=None, lse=True, copies=1, **kw):
+    """`copies`: the same sequences and queries so many times in one call, which must all come out alike."""
+    shape, q = q.shape, q.repeat(copies, 1, 1) if copies > 1 else q
     o = torch.full(q.shape, 77.0, dtype=torch.bfloat16, device="cuda")
     l = torch.full(q.shape[:2], 77.0, device="cuda") if lse else None
-    cap.kvb_attend(c.table(n, T), q, o, kv_heads=c.hkv, scale=scale, lse=l, idx=idx, **kw)
+    cap.kvb_attend(c.table(list(n) * copies, list(T) * copies), q, o, kv_heads=c.hkv, scale=scale, lse=l, idx=idx, **kw)
+    if copies > 1:
+        for x in (o.view(torch.int16), l.view(torch.int32)):
+            x = x.view(copies, shape[0], -1)
+            assert (x == x[:1]).all()
+        o, l = o[:shape[0]], l[:shape[0]]
     return o, l
 
 
@@ -226,6 +234,30 @@ def test_attend(d, hkv, G, n, T):
     check_attend(c, ks, vs, n, T, q, d ** -0.5, o, lse, rows=150)
 
 
+# The same sequences many times: enough work for tiles of 128 rows at every length (a rule of
+# the call's total work), with rows past the last, one block, tiles of several tokens and of one
+# token's heads, blocks that some waves see whole and others in part, and one run or several.
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n, T, hkv, G, copies", [([300], [300], 2, 5, 48), ([129], [129], 1, 17, 64), ([64], [64], 2, 3, 64), ([33], [33], 2, 8, 64),
+                                                  ([700], [60], 2, 5, 64), ([400, 30, 130], [100, 1, 130], 2, 5, 21), ([70], [8], 3, 20, 64),
+                                                  ([1999], [250], 1, 4, 16), ([129], [1], 4, 130, 64), ([3500], [120], 2, 4, 12),
+                                                  ([4500], [161], 2, 8, 1)])
+def test_attend_many_rows(d, n, T, hkv, G, copies):
+    c, ks, vs = filled(n, hkv, d, seed=d + G)
+    q = normal(3, sum(T), hkv * G, d).cuda()
+    o, lse = run_attend(c, n, T, q, d ** -0.5, copies=copies)
+    check_attend(c, ks, vs, n, T, q, d ** -0.5, o, lse, rows=250)
+
+
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+def test_attend_scales_many_rows(scale, d):
+    c, ks, vs = filled([200], 2, d, seed=11, spread=False)
+    q = normal(4, 60, 8, d).cuda()
+    o, lse = run_attend(c, [200], [60], q, scale, copies=64)
+    check_attend(c, ks, vs, [200], [60], q, scale, o, lse, rows=300)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
 @pytest.mark.parametrize("T", [1, 60])
 def test_attend_scales(scale, T):
@@ -235,30 +267,31 @@ def test_attend_scales(scale, T):
     check_attend(c, ks, vs, [200], [T], q, scale, o, lse)
 
 
-@pytest.mark.parametrize("T", [1, 90])
-def test_attend_peaks_and_small_weights(T):
+@pytest.mark.parametrize("d, T, G, copies", [(64, 1, 1, 1), (64, 90, 1, 1), (64, 90, 8, 32), (256, 90, 8, 32)])
+def test_attend_peaks_and_small_weights(d, T, G, copies):
     """One key far above the rest (a thousand equal weights of 2^-20 still count), and blocks that rise by more than 2^64."""
-    d, n = 64, 1100
+    n = 1100
     k, v = torch.zeros(n, 1, d).bfloat16(), normal(5, n, 1, d)
     k[3, 0, 0] = 14.0
     c = Caches([up(n)], 1, d)
     append(c, [0], [n], [k], [v])
-    q = torch.zeros(T, 1, d).bfloat16().cuda()
+    q = torch.zeros(T, G, d).bfloat16().cuda()
     q[..., 0] = 1.0
     ks, vs = reread(c, [n])
-    o, lse = run_attend(c, [n], [T], q, 1.0)
+    o, lse = run_attend(c, [n], [T], q, 1.0, copies=copies)
     check_attend(c, ks, vs, [n], [T], q, 1.0, o, lse)
     k[:, 0, 0] = (torch.arange(n) // 64 * 60).bfloat16()  # 87 in log2 units from block to block
     for kk in (k, k.flip(0)):
         append(c, [0], [n], [kk], [v])
         ks, vs = reread(c, [n])
-        o, lse = run_attend(c, [n], [T], q, 1.0)
+        o, lse = run_attend(c, [n], [T], q, 1.0, copies=copies)
         check_attend(c, ks, vs, [n], [T], q, 1.0, o, lse)
 
 
 @pytest.mark.parametrize("d", [64, 128, 256])
-@pytest.mark.parametrize("n, T", [(130, 3), (200, 150), (700, 200), (64, 64), (5, 5)])
-def test_nan_and_infinities_stay_where_they_are_seen(d, n, T):
+@pytest.mark.parametrize("n, T, copies", [(130, 3, 1), (200, 150, 1), (700, 200, 1), (64, 64, 1), (5, 5, 1), (200, 150, 64), (700, 200, 40),
+                                          (64, 64, 64)])
+def test_nan_and_infinities_stay_where_they_are_seen(d, n, T, copies):
     """A NaN in V or K reaches the tokens that see it and no earlier one; NaN queries their own row only."""
     hkv, G = 1, 3
     k, v = normal(31, n, hkv, d), normal(32, n, hkv, d)
@@ -275,7 +308,7 @@ def test_nan_and_infinities_stay_where_they_are_seen(d, n, T):
     if T > 4:
         q[1, 1, 0], q[2, 2, 5] = float("nan"), float("inf")
     q = q.cuda()
-    o, lse = run_attend(c, [n], [T], q, d ** -0.5)
+    o, lse = run_attend(c, [n], [T], q, d ** -0.5, copies=copies)
     oh, lh = o.double().cpu().numpy(), lse.double().cpu().numpy()
     for t in range(T):
         for h in range(G):
