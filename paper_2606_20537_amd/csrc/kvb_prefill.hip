@@ -313,30 +313,28 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
     // Blocks past the end repeat the last one.
     auto clamp = [&](int b) { return b < end ? b : end - 1; };
     int ve = 127;  // exponent of V's scale of b
-    {
-        dev::lds_barrier();  // q has been read
+    dev::lds_barrier();  // q has been read
+    #pragma unroll
+    for (int i = 0; i < kLoads; ++i) stage_k(0, i, k_scale(begin));
+    stage_v(begin, 0);
+    fetch(kb, clamp(begin + 1), ks);
+    fetch(vb, clamp(begin + 1), vs);
+    ve = v_exponent(begin);
+    dev::lds_barrier();
+    #pragma unroll
+    for (int t = 0; t < S; ++t) {
+        y[t] = (f32x16){};
         #pragma unroll
-        for (int i = 0; i < kLoads; ++i) stage_k(0, i, k_scale(begin));
-        stage_v(begin, 0);
-        fetch(kb, clamp(begin + 1), ks);
-        fetch(vb, clamp(begin + 1), vs);
-        ve = v_exponent(begin);
-        dev::lds_barrier();
-        #pragma unroll
-        for (int t = 0; t < S; ++t) {
-            y[t] = (f32x16){};
-            #pragma unroll
-            for (int i = 0; i < D / 16; ++i) y[t] = mma16(read_k(0, t, i), q[i], y[t]);
-        }
-        #pragma unroll
-        for (int i = 0; i < kLoads; ++i) stage_k(1, i, k_scale(clamp(begin + 1)));
-        stage_v(clamp(begin + 1), 1);
-        fetch(kb, clamp(begin + 2), ks);
-        fetch(vb, clamp(begin + 2), vs);
-        #pragma unroll
-        for (int u = 0; u < 8; ++u) slice(u, begin);
-        dev::lds_barrier();
+        for (int i = 0; i < D / 16; ++i) y[t] = mma16(read_k(0, t, i), q[i], y[t]);
     }
+    #pragma unroll
+    for (int i = 0; i < kLoads; ++i) stage_k(1, i, k_scale(clamp(begin + 1)));
+    stage_v(clamp(begin + 1), 1);
+    fetch(kb, clamp(begin + 2), ks);
+    fetch(vb, clamp(begin + 2), vs);
+    #pragma unroll
+    for (int u = 0; u < 8; ++u) slice(u, begin);
+    dev::lds_barrier();
     int vbuf = 0;
     for (int b = begin; b < end; ++b) {
         const int kbuf = (b - begin) & 1;
