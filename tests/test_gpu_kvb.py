@@ -236,12 +236,13 @@ def test_attend(d, hkv, G, n, T):
 
 # The same sequences many times: enough work for tiles of 128 rows at every length (a rule of
 # the call's total work), with rows past the last, one block, tiles of several tokens and of one
-# token's heads, blocks that some waves see whole and others in part, and one run or several.
+# token's heads, blocks that some waves see whole and others in part, and one run or several
+# (at the last, beside sequences in tiles of 16 that are cut too).
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("n, T, hkv, G, copies", [([300], [300], 2, 5, 48), ([129], [129], 1, 17, 64), ([64], [64], 2, 3, 64), ([33], [33], 2, 8, 64),
                                                   ([700], [60], 2, 5, 64), ([400, 30, 130], [100, 1, 130], 2, 5, 21), ([70], [8], 3, 20, 64),
                                                   ([1999], [250], 1, 4, 16), ([129], [1], 4, 130, 64), ([3500], [120], 2, 4, 12),
-                                                  ([4500], [161], 2, 8, 1)])
+                                                  ([4500], [161], 2, 8, 1), ([9000, 4500, 70], [1, 161, 1], 2, 8, 1)])
 def test_attend_many_rows(d, n, T, hkv, G, copies):
     c, ks, vs = filled(n, hkv, d, seed=d + G)
     q = normal(3, sum(T), hkv * G, d).cuda()
