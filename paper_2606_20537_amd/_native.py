@@ -576,6 +576,9 @@ def _kvb_tokens(fn, name, x):
         if x.stride(2) != 1 or x.stride(1) != shape[2]:
             raise ValueError("%s: the heads of a token of %s are contiguous" % (fn, name))
         stride = x.stride(0) if shape[0] > 1 else 0
+        # a stride of zero means contiguous to the library, which would read past a broadcast row
+        if shape[0] > 1 and stride < shape[1] * shape[2]:
+            raise ValueError("%s: the tokens of %s overlap in memory (a broadcast tensor? call .contiguous())" % (fn, name))
     return stride, CAP_DTYPE_BF16 if dtype == bf16 else CAP_DTYPE_F32, shape
 
 

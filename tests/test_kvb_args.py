@@ -209,3 +209,24 @@ def test_plain_forms():
     for amax in (0.0, 1e-40, 448.0, 448.001, 3e38, 7.5, 896.0):
         e = P.exponent(amax)
         assert e in (-100, 119) or 448.0 * 2.0 ** (e - 1) < amax <= 448.0 * 2.0 ** e
+
+
+def test_binding_refuses_tokens_that_overlap():
+    """One row broadcast over the tokens has a stride of zero, which the library takes for contiguous; rows that share
+    elements have one below a row."""
+    t = cap.kvb_seqs([[0, 0, 0, 0, 0, 64, 3, 3]])
+    k, q = torch.zeros((3, 2, 64), dtype=torch.bfloat16), torch.zeros((3, 4, 64), dtype=torch.bfloat16)
+    idx = torch.zeros((3, 2, 4), dtype=torch.int32)
+    flat = torch.zeros(1024, dtype=torch.bfloat16)
+    for bad in (k[:1].expand(3, 2, 64), flat.as_strided((3, 2, 64), (64, 64, 1))):
+        for args in ((bad, k), (k, bad)):
+            with pytest.raises(ValueError, match="overlap"):
+                cap.kvb_append(t, *args, stream=0)
+    for bad in (q[:1].expand(3, 4, 64), flat.as_strided((3, 4, 64), (8, 64, 1))):
+        with pytest.raises(ValueError, match="overlap"):
+            cap.kvb_attend(t, bad, torch.empty_like(q), kv_heads=2, scale=1.0, stream=0)
+        with pytest.raises(ValueError, match="overlap"):
+            cap.kvb_select(t, bad, idx, kv_heads=2, stream=0)
+    # a single token broadcast over one is one token
+    assert N._kvb_tokens("kvb_append", "k", k[:1].expand(1, 2, 64))[0] == 0
+    assert N._kvb_tokens("kvb_append", "k", torch.zeros((3, 5, 64), dtype=torch.bfloat16)[:, 1:3])[0] == 320
