@@ -203,6 +203,21 @@ def _stream(s):
     return s.cuda_stream
 
 
+def _scratch(need, device, handle):
+    """`need` device bytes for one call on the stream `handle`, dropped when the call returns.
+
+    They come from the pool of that stream: torch hands them on to work behind the
+    call's kernels only, and what they held before is done with.  Of another
+    stream's pool they could be written by both at once."""
+    import torch
+    if handle == _stream(None):
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    # (ExternalStream takes 0 for "any stream"; 1 is HIP's name for the default stream)
+    s = torch.cuda.ExternalStream(handle, device=device) if handle > 1 else torch.cuda.default_stream(device)
+    with torch.cuda.stream(s):
+        return torch.empty(need, dtype=torch.uint8, device=device)
+
+
 class CapSet:
     """Handle of a live set (owns the C handle; destroy() or GC frees it).
     The set only points at its buffers, so the handle keeps the buffer
@@ -588,12 +603,12 @@ def _kvb_out(fn, name, x, shape, dtype):
         raise ValueError("%s: %s is a contiguous %s tensor of shape %s" % (fn, name, dtype, list(shape)))
 
 
-def _kvb_workspace(a, workspace, size_of, like):
-    """Enter the caller's workspace, or one allocated for this call, into the arguments."""
+def _kvb_workspace(a, workspace, size_of, like, handle):
+    """Enter the caller's workspace, or one allocated for this call on the stream `handle`, into the arguments."""
     if workspace is None:
         need = size_of(ct.byref(a))
         if need:
-            workspace = _kvb_torch()[0].empty(need, dtype=_kvb_torch()[0].uint8, device=like.device)
+            workspace = _scratch(need, like.device, handle)
             a.workspace, a.workspace_bytes = workspace.data_ptr(), need
     else:
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -615,7 +630,7 @@ def kvb_append(seqs, k, v, *, stream=None):
 def kvb_attend(seqs, q, o, *, kv_heads, scale, lse=None, idx=None, workspace=None, stream=None):
     """Causal attention of the step's tokens q [sum of T, heads, d] over the caches, whole or (idx
     [sum of T, kv_heads, n_sel]) the listed blocks.  With no workspace given, one is allocated as a
-    torch tensor for the duration of the call."""
+    torch tensor of the call's stream for the duration of the call."""
     _, bf16, f32, i32 = _kvb_torch()
     at, n_seq = _kvb_table("kvb_attend", seqs)
     qs, dt, (tokens, heads, d) = _kvb_tokens("kvb_attend", "q", q)
@@ -629,19 +644,19 @@ def kvb_attend(seqs, q, o, *, kv_heads, scale, lse=None, idx=None, workspace=Non
     a = kvb_attend_args(at, q.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else 0,
                         idx.data_ptr() if idx is not None else 0, 0, 0, qs, tokens, n_seq, heads, kv_heads, d, n_sel, dt,
                         scale, 0)
-    lib = load()
-    workspace = _kvb_workspace(a, workspace, lib.kvb_attend_workspace_bytes, q)
-    return _check("kvb_attend", lib.kvb_attend(ct.byref(a), _stream(stream)))
+    lib, handle = load(), _stream(stream)
+    workspace = _kvb_workspace(a, workspace, lib.kvb_attend_workspace_bytes, q, handle)
+    return _check("kvb_attend", lib.kvb_attend(ct.byref(a), handle))
 
 
 def kvb_select(seqs, q, idx, *, kv_heads, first=1, last=2, workspace=None, stream=None):
-    """For each token and KV head the idx.shape[-1] blocks that kvb_attend is to read."""
+    """For each token and KV head the idx.shape[-1] blocks that kvb_attend is to read (workspace: as for kvb_attend)."""
     at, n_seq = _kvb_table("kvb_select", seqs)
     qs, dt, (tokens, heads, d) = _kvb_tokens("kvb_select", "q", q)
     n_sel = idx.shape[-1]
     _kvb_out("kvb_select", "idx", idx, (tokens, kv_heads, n_sel), _kvb_torch()[3])
     _kvb_device("kvb_select", q, idx, workspace)
     a = kvb_select_args(at, q.data_ptr(), idx.data_ptr(), 0, 0, qs, tokens, n_seq, heads, kv_heads, d, n_sel, first, last, dt)
-    lib = load()
-    workspace = _kvb_workspace(a, workspace, lib.kvb_select_workspace_bytes, q)
-    return _check("kvb_select", lib.kvb_select(ct.byref(a), _stream(stream)))
+    lib, handle = load(), _stream(stream)
+    workspace = _kvb_workspace(a, workspace, lib.kvb_select_workspace_bytes, q, handle)
+    return _check("kvb_select", lib.kvb_select(ct.byref(a), handle))

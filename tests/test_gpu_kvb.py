@@ -604,3 +604,35 @@ def test_session_with_a_capsule():
         assert torch.equal(x, y)
     ks, vs = reread(a, [n])
     check_attend(a, ks, vs, [n], [1], q[n - 1:n], 0.1, cold[-2][0], cold[-1][0])
+
+
+# ------------------------------------ a workspace allocated for the call --
+def test_no_workspace_on_another_stream():
+    """Calls that allocate their own workspace, held up on a stream of their own while the current stream allocates as much
+    again and fills it: the same bits as on the current stream."""
+    hkv, G, d, n = 2, 8, 128, [9000, 4000]
+    c, _, _ = filled(n, hkv, d, seed=150)
+    q = normal(151, 2, hkv * G, d).cuda()
+    idx = torch.empty((2, hkv, 8), dtype=torch.int32, device="cuda")
+    table = c.table(n, [1, 1])
+
+    def call(**kw):
+        out = (torch.empty_like(idx), torch.empty_like(q), torch.empty_like(q), torch.empty(q.shape[:2], device="cuda"))
+        torch.cuda.synchronize()
+        if kw:
+            with torch.cuda.stream(kw["stream"]):
+                torch.cuda._sleep(20_000_000)
+        cap.kvb_select(table, q, out[0], kv_heads=hkv, **kw)
+        cap.kvb_attend(table, q, out[1], kv_heads=hkv, scale=0.1, idx=out[0], **kw)
+        cap.kvb_attend(table, q, out[2], kv_heads=hkv, scale=0.1, lse=out[3], **kw)
+        if kw:
+            for m in range(10, 25):  # what the current stream would be handed, had it the workspaces back
+                torch.full((1 << m,), 0xFF, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        return out
+
+    want = call()
+    for s in (torch.cuda.Stream(), torch.cuda.default_stream()):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for x, y in zip(call(stream=s), want):
+                assert torch.equal(x, y)
