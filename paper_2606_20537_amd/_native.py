@@ -465,21 +465,21 @@ def gdn_chunked_prefill(q, k, v, g, beta, o, *, state_in=None, chunk_states=None
     """Marshal tensors (or addresses with explicit sizes) into gdn_args.
 
     With no workspace given, one is allocated as a torch uint8 tensor on q's
-    device for the duration of the call (stream-ordered by torch's caching
-    allocator)."""
+    device for the duration of the call (of the call's stream, in whose order
+    torch's caching allocator hands it on)."""
     if T is None:
         T, H, dk = q.shape
         dv = v.shape[2]
     need = gdn_workspace_bytes(T, H, chunk) if chunk > 0 and H > 0 else 0
+    handle = _stream(stream)
     if workspace is None and need > 0:
-        import torch
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _scratch(need, q.device, handle)
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size() if hasattr(workspace, "numel") else need
     a = gdn_args(_addr(q), _addr(k), _addr(v), _addr(g), _addr(beta), _addr(state_in), _addr(o),
                  _addr(chunk_states), _addr(final_state), _addr(workspace), int(workspace_bytes), int(T), int(H),
                  int(dk), int(dv), int(chunk), int(in_dtype), float(scale))
-    return _check("gdn_chunked_prefill", load().gdn_chunked_prefill(ct.byref(a), _stream(stream)))
+    return _check("gdn_chunked_prefill", load().gdn_chunked_prefill(ct.byref(a), handle))
 
 
 GDN_NOALLOC_SCRATCH_BYTES = 32 << 20

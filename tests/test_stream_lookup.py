@@ -85,3 +85,25 @@ def test_calls_take_their_scratch_on_their_stream(monkeypatch, name):
     else:
         N.kvb_select(t, q, torch.zeros((3, 2, 4), dtype=torch.int32), kv_heads=2, stream=5)
     assert asked == [(640, 5)] and called == [(scratch.data_ptr(), 640, 5)]
+
+
+def test_delta_rule_prefill_takes_its_scratch_on_its_stream(monkeypatch):
+    """The delta-rule prefill likewise."""
+    import ctypes as ct
+
+    class Lib:
+        def gdn_workspace_bytes(self, T, H, chunk):
+            return 640
+
+        def gdn_chunked_prefill(self, a, handle):
+            args = ct.cast(a, ct.POINTER(N.gdn_args)).contents
+            called.append((args.workspace, args.workspace_bytes, handle))
+            return 0
+
+    called, asked = [], []
+    scratch = torch.zeros(640, dtype=torch.uint8)
+    monkeypatch.setattr(N, "load", lambda: Lib())
+    monkeypatch.setattr(N, "_scratch", lambda need, device, handle: asked.append((need, handle)) or scratch)
+    q, g = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((3, 4))
+    N.gdn_chunked_prefill(q, q, q, g, g, torch.zeros((3, 4, 64)), stream=5)
+    assert asked == [(640, 5)] and called == [(scratch.data_ptr(), 640, 5)]
