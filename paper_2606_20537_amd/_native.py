@@ -603,7 +603,7 @@ def _kvb_out(fn, name, x, shape, dtype):
         raise ValueError("%s: %s is a contiguous %s tensor of shape %s" % (fn, name, dtype, list(shape)))
 
 
-def _kvb_workspace(a, workspace, size_of, like, handle):
+def _kvb_workspace(fn, a, workspace, size_of, like, handle):
     """Enter the caller's workspace, or one allocated for this call on the stream `handle`, into the arguments."""
     if workspace is None:
         need = size_of(ct.byref(a))
@@ -611,6 +611,8 @@ def _kvb_workspace(a, workspace, size_of, like, handle):
             workspace = _scratch(need, like.device, handle)
             a.workspace, a.workspace_bytes = workspace.data_ptr(), need
     else:
+        if not workspace.is_contiguous():  # its elements are not the bytes behind its address
+            raise ValueError("%s: the workspace is a contiguous tensor" % fn)
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     return workspace
 
@@ -645,7 +647,7 @@ def kvb_attend(seqs, q, o, *, kv_heads, scale, lse=None, idx=None, workspace=Non
                         idx.data_ptr() if idx is not None else 0, 0, 0, qs, tokens, n_seq, heads, kv_heads, d, n_sel, dt,
                         scale, 0)
     lib, handle = load(), _stream(stream)
-    workspace = _kvb_workspace(a, workspace, lib.kvb_attend_workspace_bytes, q, handle)
+    workspace = _kvb_workspace("kvb_attend", a, workspace, lib.kvb_attend_workspace_bytes, q, handle)
     return _check("kvb_attend", lib.kvb_attend(ct.byref(a), handle))
 
 
@@ -658,5 +660,5 @@ def kvb_select(seqs, q, idx, *, kv_heads, first=1, last=2, workspace=None, strea
     _kvb_device("kvb_select", q, idx, workspace)
     a = kvb_select_args(at, q.data_ptr(), idx.data_ptr(), 0, 0, qs, tokens, n_seq, heads, kv_heads, d, n_sel, first, last, dt)
     lib, handle = load(), _stream(stream)
-    workspace = _kvb_workspace(a, workspace, lib.kvb_select_workspace_bytes, q, handle)
+    workspace = _kvb_workspace("kvb_select", a, workspace, lib.kvb_select_workspace_bytes, q, handle)
     return _check("kvb_select", lib.kvb_select(ct.byref(a), handle))

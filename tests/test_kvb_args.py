@@ -230,3 +230,16 @@ def test_binding_refuses_tokens_that_overlap():
     # a single token broadcast over one is one token
     assert N._kvb_tokens("kvb_append", "k", k[:1].expand(1, 2, 64))[0] == 0
     assert N._kvb_tokens("kvb_append", "k", torch.zeros((3, 5, 64), dtype=torch.bfloat16)[:, 1:3])[0] == 320
+
+
+def test_binding_refuses_a_workspace_that_is_not_contiguous(monkeypatch):
+    """A view's elements are not the bytes behind its address: 64 elements of one broadcast byte, every other byte."""
+    monkeypatch.setattr(N, "_kvb_device", lambda *a: None)
+    t = cap.kvb_seqs([[0, 0, 0, 0, 0, 64, 3, 3]])  # (no addresses: the library refuses the call behind the check)
+    q, idx = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((3, 2, 4), dtype=torch.int32)
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    for bad in (ws[:1].expand(4096), ws[::2], ws.view(64, 64).t()):
+        with pytest.raises(ValueError, match="contiguous"):
+            cap.kvb_attend(t, q, torch.empty_like(q), kv_heads=2, scale=1.0, workspace=bad, stream=0)
+        with pytest.raises(ValueError, match="contiguous"):
+            cap.kvb_select(t, q, idx, kv_heads=2, workspace=bad, stream=0)
