@@ -537,9 +537,14 @@ def kvb_seqs(caches):
     """The sequence table of a step: an int64 array [n_seq, 8], one kvb_seq a row.
 
     caches: iterable of (k, v, scales, bounds, open, rows, n, T); the first five
-    are tensors, addresses or None.  A program may keep the table and advance the
+    are contiguous tensors, addresses or None.  A program may keep the table and advance the
     last two columns (n, T) itself; it does not keep the tensors alive."""
     import numpy as np
+    caches = [tuple(c) for c in caches]
+    for c in caches:
+        for x in c[:5]:
+            if hasattr(x, "is_contiguous") and not x.is_contiguous():  # a row would not follow the one before it
+                raise ValueError("kvb_seqs: the buffers of a cache are contiguous")
     return np.array([[_addr(x) for x in c[:5]] + [int(x) for x in c[5:]] for c in caches],
                     dtype=np.int64).reshape(-1, 8)
 

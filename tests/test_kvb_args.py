@@ -243,3 +243,16 @@ def test_binding_refuses_a_workspace_that_is_not_contiguous(monkeypatch):
             cap.kvb_attend(t, q, torch.empty_like(q), kv_heads=2, scale=1.0, workspace=bad, stream=0)
         with pytest.raises(ValueError, match="contiguous"):
             cap.kvb_select(t, q, idx, kv_heads=2, workspace=bad, stream=0)
+
+
+def test_sequence_table_refuses_buffers_that_are_not_contiguous():
+    """One layer's rows out of a buffer of several layers: the library would read the other layers' as the next rows."""
+    k = torch.zeros((128, 2, 64), dtype=torch.uint8)
+    scales, bounds = torch.zeros((2, 2, 2)), torch.zeros((2, 2, 2, 64), dtype=torch.uint8)
+    open_ = torch.zeros((2, 64, 2, 64), dtype=torch.bfloat16)
+    good = [k, k.clone(), scales, bounds, open_]
+    assert cap.kvb_seqs([(*good, 128, 3, 3)])[0].tolist() == [x.data_ptr() for x in good] + [128, 3, 3]
+    for i, x in enumerate(good):
+        layers = torch.zeros((x.shape[0], 4, *x.shape[1:]), dtype=x.dtype)
+        with pytest.raises(ValueError, match="contiguous"):
+            cap.kvb_seqs([(*good, 128, 3, 3), (*good[:i], layers[:, 1], *good[i + 1:], 128, 3, 3)])
