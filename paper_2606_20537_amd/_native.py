@@ -593,7 +593,7 @@ def _kvb_tokens(fn, name, x):
         raise ValueError("%s: %s is a bfloat16 tensor [tokens, heads, d], not %s %s" % (fn, name, dtype, list(shape)))
     stride = 0
     if not x.is_contiguous():
-        if x.stride(2) != 1 or x.stride(1) != shape[2]:
+        if x.stride(2) != 1 or (shape[1] > 1 and x.stride(1) != shape[2]):
             raise ValueError("%s: the heads of a token of %s are contiguous" % (fn, name))
         stride = x.stride(0) if shape[0] > 1 else 0
         # a stride of zero means contiguous to the library, which would read past a broadcast row

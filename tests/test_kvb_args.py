@@ -256,3 +256,10 @@ def test_sequence_table_refuses_buffers_that_are_not_contiguous():
         layers = torch.zeros((x.shape[0], 4, *x.shape[1:]), dtype=x.dtype)
         with pytest.raises(ValueError, match="contiguous"):
             cap.kvb_seqs([(*good, 128, 3, 3), (*good[:i], layers[:, 1], *good[i + 1:], 128, 3, 3)])
+
+
+def test_binding_takes_a_single_head_of_any_stride():
+    """One head of a token has no neighbour: every fifth of five, or the last, with the stride of the tokens alone."""
+    x = torch.zeros((3, 5, 64), dtype=torch.bfloat16)
+    for one in (x[:, ::5], x.transpose(0, 1).contiguous().transpose(0, 1)[:, 4:], x.as_strided((3, 1, 64), (320, 7, 1))):
+        assert N._kvb_tokens("kvb_append", "k", one)[0] == (one.stride(0) if not one.is_contiguous() else 0)
