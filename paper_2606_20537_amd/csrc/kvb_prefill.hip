@@ -21,7 +21,8 @@
 //    instruction's sums lose 2^-12 of the sum of the products' magnitudes at most.
 //    2^(c - m) is the instruction's scale of a row, an exact power of two; m is the c of
 //    the row's first block, raised only where a later one is 2^64 above: O and l are
-//    floating, so their reference need not be the running maximum.
+//    floating, so their reference need not be the running maximum.  Beside values of V above 2^24
+//    it is raised earlier, or above c, so that O stays below 2^127 for any rows of V.
 //    Against bf16 operands that is the same matrix time (FP8 runs at twice the rate),
 //    half the LDS traffic and no conversion of V.
 //
@@ -404,11 +405,13 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
             c1 = c_s[kbuf][group][1][lane & 31];
         }
         const float cm = __builtin_fmaxf(c0, c1);
+        // 2^31 products of weights up to 2^8 and values below 2^9 2^(ve - 127) stay below 2^127
+        const float rise = (float)(206 - ve < 64 ? 206 - ve : 64);
         if (m == kNegInf) m = cm;  // O and l are zero so far
-        if (__any(cm - m > 64.0f)) {
-            float up = cm - m > 64.0f ? cm : m;
+        if (__any(cm - m > rise)) {
+            float up = cm - m > rise ? cm + __builtin_fmaxf(-rise, 0.0f) : m;
             asm volatile("" : "+v"(up));  // rare: not to be computed ahead of the branch
-            const float fade = __builtin_amdgcn_exp2f(m - up);
+            const float fade = up == m ? 1.0f : __builtin_amdgcn_exp2f(m - up);  // (a row that sees nothing yet: both -inf)
             #pragma unroll
             for (int i = 0; i < NT; ++i) acc[i] *= fade;
             l *= fade;
