@@ -46,6 +46,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int kThreads = 256;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLargeV = 0x1p87f;  // a scale: codes are below 2^9
 
 __device__ inline float bits_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ inline uint32_t f32_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
@@ -257,7 +258,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
         }
         float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3])),
                                     __builtin_fmaxf(__builtin_fmaxf(x[4], x[5]), __builtin_fmaxf(x[6], x[7])));
-        top = __builtin_fmaxf(m, group_max(top));
+        // Sums of 2^31 values of 2^96 would overflow: beside such blocks the reference stands 2^32
+        // above the highest score, with weights of 2^-32 (any reference will do, as long as O and l share it).
+        top = __builtin_fmaxf(m, group_max(top) + (v_scale > kLargeV ? 32.0f : 0.0f));
         const float base = top == kNegInf ? 0.0f : top;
         const float fade = __builtin_amdgcn_exp2f(m - base);
         m = top;
