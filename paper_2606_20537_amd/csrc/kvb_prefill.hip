@@ -107,6 +107,9 @@ __device__ inline int swizzle_v(int key) {
     return 2 * i;
 }
 
+// Exponent of V's scale and the rise of a block above the reference together (below).
+constexpr int kRiseEnd = 206;
+
 // Waves that share 32 query rows, and threads of a workgroup.
 template <int D>
 constexpr int kShare = D == 256 ? 2 : 1;
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
         }
         const float cm = __builtin_fmaxf(c0, c1);
         // 2^31 products of weights up to 2^8 and values below 2^9 2^(ve - 127) stay below 2^127
-        const float rise = (float)(206 - ve < 64 ? 206 - ve : 64);
+        const float rise = (float)(kRiseEnd - ve < 64 ? kRiseEnd - ve : 64);
         if (m == kNegInf) m = cm;  // O and l are zero so far
         if (__any(cm - m > rise)) {
             float up = cm - m > rise ? cm + __builtin_fmaxf(-rise, 0.0f) : m;
@@ -416,6 +419,18 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
             for (int i = 0; i < NT; ++i) acc[i] *= fade;
             l *= fade;
             m = up;
+        }
+        // The instruction's scales end at 2^-127, those of lo at 2^-123 of hi's: what is further below
+        // weighs 2^-126 of the largest at most, but of large values that would show, and counts as none.
+        if (__builtin_expect(ve > kRiseEnd - 64, 0)) {
+            float d0 = c0 - m, d1 = c1 - m;
+            asm volatile("" : "+v"(d0), "+v"(d1));  // (as above)
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool none = (W == 2 && i >= 4 ? d1 : d0) < -123.0f;
+                wh[i] = none ? 0 : wh[i];
+                wl[i] = none ? 0 : wl[i];
+            }
         }
         // no score: -127, with weights of zero
         l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(__builtin_fmaxf((part ? c1 : c0) - m, -127.0f)), l);

@@ -59,3 +59,37 @@ def test_large_values_of_listed_blocks(d, size):
     o, lse = run_attend(c, [n], [T], q, 1.0, idx)
     assert torch.isfinite(o).all() and not o[1].any()
     check_attend(c, ks, vs, [n], [T], q, 1.0, o, lse, idx)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n, T, G, copies", NARROW + WIDE)
+@pytest.mark.parametrize("by", [-80.0, -84.0, -87.0, -120.0, -1000.0])
+@pytest.mark.parametrize("parts", [(0, 64), (32, 96), (0, 32)])
+def test_large_values_of_keys_far_below(d, n, T, G, copies, by, parts):
+    """The largest values at keys whose scores are so far below the others' that nothing of them is left (or, 2^115 below,
+    a tenth of the others), whether they fill a block, halves of two blocks, or half of one."""
+    k, v = torch.zeros(n, 1, d), normal(6, n, 1, d).float()
+    for b in range(0, n, 3 * BLOCK):
+        k[b + parts[0]:b + parts[1], 0, 0] = by
+        v[b + parts[0]:b + parts[1]] = 2.0 ** 115
+    c, ks, vs = made(n, d, k.bfloat16(), v.bfloat16())
+    q = torch.zeros(T, G, d).bfloat16().cuda()
+    q[..., 0] = 1.0
+    o, lse = run_attend(c, [n], [T], q, 1.0, copies=copies)
+    for t, h in [(t, h) for t in (0, T // 2, T - 1) for h in (0, G - 1)]:
+        row, pos = q[t, h].double().cpu().numpy(), n - T + t
+        want, want_lse, mass, top, size = P.attend(row, ks[0][:, 0], vs[0][:, 0], 1.0, pos)
+        # as kvb_plain.close has it, and weights below 2^-80 of the largest may count as none
+        x = ks[0][:pos + 1, 0] @ row
+        weight = np.exp(x - want_lse)
+        none = (weight * (weight < weight.max() * 2.0 ** -80)) @ np.abs(vs[0][:pos + 1, 0])
+        far = mass * (2.0 ** -8 + 2 * (d * 2.0 ** -24 * size + 2.0 ** -22 * (abs(want_lse) + size))) + 1e-37 + none
+        if T * G > 128:
+            # lo's step is 2^-21 of the block's largest weight at most: a weight below half of it is lost, no more
+            block = np.arange(pos + 1) // BLOCK
+            largest = np.array([weight[block == b].max() for b in range(block[-1] + 1)])[block]
+            far = far + mass * 2.0 ** -12 + np.minimum(weight, 2.0 ** -21 * largest) @ np.abs(vs[0][:pos + 1, 0])
+        far = far + 2.0 ** -8 * (np.abs(want) + far)
+        got = o[t, h].double().cpu().numpy()
+        assert (np.abs(got - want) <= far).all(), (t, h, np.abs(got - want).max(), far.min(), np.abs(want).max())
+        assert abs(lse[t, h].item() - want_lse) <= 2.0 ** -20 * (1 + abs(want_lse))
