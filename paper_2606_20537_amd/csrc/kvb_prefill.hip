@@ -15,10 +15,11 @@
 //    channels differ in size.)
 //  * O^T = V^T P^T on 32x32x64 FP8 tiles straight from the codes, with the scales as the
 //    instruction's scale operands.  The weights of 32 rows are taken against their
-//    own highest score, rounded up to an integer c in log2 units, w = 2^(x - c + 8) in
-//    (0, 256], and split into two E4M3 rows, w = hi + lo / 16 (relative 2^-8 at most, that
-//    of bf16, or 2^-21 of the 32's largest weight where that is more); the
-//    instruction's sums lose 2^-12 of the sum of the products' magnitudes at most.
+//    own highest score, rounded up to an integer c in log2 units, w = 2^(x - c + 8) up to
+//    2^8 (2^8.25 where scores near 2^23 are rounded), and split into two E4M3 rows,
+//    w = hi + lo / 16 (relative 2^-8 at most, that of bf16, or 2^-21 of the 32's largest
+//    weight where that is more); the instruction's sums lose 2^-12 of the sum of the
+//    products' magnitudes at most.
 //    2^(c - m) is the instruction's scale of a row, an exact power of two; m is the c of
 //    the row's first block, raised only where a later one is 2^64 above: O and l are
 //    floating, so their reference need not be the running maximum.  Beside values of V above 2^24
@@ -56,6 +57,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -70,6 +72,16 @@ __device__ inline uint32_t f32_bits(float f) { return __builtin_bit_cast(uint32_
 __device__ inline float pair_max(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(x), f32_bits(x), false, false);
     return __builtin_fmaxf(bits_f32(r[0]), bits_f32(r[1]));
+}
+// The highest of a wave's lanes, in lane 63.
+template <int CTRL, int ROWS>
+__device__ inline uint32_t dpp_max(uint32_t x) {
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+    return x > y ? x : y;
+}
+__device__ inline uint32_t wave_max(uint32_t x) {
+    x = dpp_max<0x118, 0xf>(dpp_max<0x114, 0xf>(dpp_max<0x112, 0xf>(dpp_max<0x111, 0xf>(x))));  // row_shr 1, 2, 4, 8
+    return dpp_max<0x143, 0xc>(dpp_max<0x142, 0xa>(x));  // row_bcast 15 and 31
 }
 // Four values to four E4M3 codes, and their remainders times 16 to four more.
 __device__ inline void split4(const float* y, int& hi, int& lo) {
@@ -127,6 +139,7 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
     __shared__ u32x4 p_s[2][4][2][2][64];  // weights: parity of the block, rows, half of the keys, hi or lo
     __shared__ float c_s[2][4][2][32];     // their references
     __shared__ int nan_s[3];
+    __shared__ uint32_t top_s[kThreads<D> / 64];  // largest magnitude of q, of a wave's threads
 
     const KvbAttendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
     const uint32_t w = blockIdx.x - s.first_wg;
@@ -224,6 +237,13 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
             const int64_t at = row0 + qrow + i * kRowPass, r = at < last ? at : last;
             x[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.q) + token_of(r) * p.q_stride + (int64_t)head_of(r) * D * 2 + 16 * qunit);
         }
+        u16x2 top2 = {0, 0};
+        #pragma unroll
+        for (int i = 0; i < kPasses; ++i)
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) top2 = __builtin_elementwise_max(top2, __builtin_bit_cast(u16x2, x[i][k] & 0x7FFF7FFFu));
+        const uint32_t top = wave_max(top2[0] > top2[1] ? top2[0] : top2[1]);
+        if (lane == 63) top_s[wave] = top;
         if (p.scale_log2 <= 0.0f) {  // a negative scale turns the rows' signs, zero makes them zero (but not their NaN)
             const float by = p.scale_log2 < 0.0f ? -1.0f : 0.0f;
             #pragma unroll
@@ -244,6 +264,18 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
     dev::lds_barrier();
     #pragma unroll
     for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const bf16x8*>(&k_s[0][0] + (kaddr ^ (32 * i)) + group * 64 * D);
+    // Whether a score of the blocks so far may reach 2^23 in log2 units: D products below 2^(exponent of q + 1),
+    // 2^9 2^(exponent of the scale) and 2^(exponent of f + 1); exponents as they are stored, 127 too high.
+    int far_from = 0;  // exponent of K's scale from which it may
+    {
+        uint32_t top = 0;
+        #pragma unroll
+        for (int i = 0; i < kThreads<D> / 64; ++i) top = top_s[i] > top ? top_s[i] : top;
+        const int log2d = D == 64 ? 6 : D == 128 ? 7 : 8;
+        far_from = __builtin_amdgcn_readfirstlane(23 + 3 * 127 - log2d - 1 - 9 - 1 - (int)(top >> 7) - (int)(f32_bits(f) >> 23));
+    }
+    int64_t whole = wpos0;  // keys up to here need nothing done to their scores; -1: all do
+    auto check_scales = [&]() { whole = __any((int)(k_scales >> 23) >= far_from) ? -1 : whole; };
 
     auto read_k = [&](int buf, int t, int i) {  // keys 32 (part + t) .. + 31, channels 16 i .. + 15
         return *reinterpret_cast<const bf16x8*>(&k_s[buf][(kaddr ^ (32 * i)) + (part + t) * 64 * D]);
@@ -267,9 +299,10 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
     float c = 0.0f, base = 0.0f, sum = 0.0f;  // of block b's softmax, whose first half is done when its step begins
     int ph[4 * S], pl[4 * S];                 // its weights, of the wave's keys
 
+    float off = 0.0f;  // what block b's scores have been lowered by, in log2 units
     auto mask = [&](int b, f32x16 (&z)[S]) {
         const int64_t r0 = (int64_t)b * kKvbBlock;
-        if (r0 + kKvbBlock - 1 <= wpos0) return;  // every row sees every key
+        if (r0 + kKvbBlock - 1 <= whole) return;  // every row sees every key
         int sees = (int)(pos - r0 < kKvbBlock ? pos - r0 : kKvbBlock) - 4 * half - 32 * part;  // keys up to here
         asm volatile("" : "+v"(sees));  // rare: not to be computed ahead of the branch
         #pragma unroll
@@ -277,6 +310,22 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
             #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (32 * t + 8 * (r / 4) + r % 4 > sees) z[t][r] = kNegInf;
+        if (whole >= 0) return;
+        // x f - base is rounded once, c from the rounded product: from 2^24 on that differs by 1 and more, and a
+        // weight above 2^8.8 has no code.  Scores as high as that are taken from their highest before the product.
+        float high = z[0][0];
+        #pragma unroll
+        for (int t = 0; t < S; ++t)
+            #pragma unroll
+            for (int r = 0; r < 16; ++r) high = __builtin_fmaxf(high, z[t][r]);
+        high = pair_max(high);
+        off = __builtin_ceilf(high * f);
+        if (__builtin_fabsf(off) < 0x1p23f || off == kNegInf) off = high = 0.0f;
+        if (off == -kNegInf) high = __builtin_nanf("");  // beyond fp32
+        #pragma unroll
+        for (int t = 0; t < S; ++t)
+            #pragma unroll
+            for (int r = 0; r < 16; ++r) z[t][r] -= high;
     };
     auto weights = [&](int i) {  // of the wave's keys 8 i + 4 half .. + 3
         float e[4];
@@ -294,6 +343,7 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
     auto reference = [&](float top) {
         c = __builtin_ceilf(pair_max(top) * f);
         base = c == kNegInf ? 0.0f : c - 8.0f;
+        c += off;
         sum = 0.0f;
     };
     // The first half of block b's softmax in slices 0..7, from its scores in y.
@@ -317,6 +367,7 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
     // Blocks past the end repeat the last one.
     auto clamp = [&](int b) { return b < end ? b : end - 1; };
     int ve = 127;  // exponent of V's scale of b
+    check_scales();
     dev::lds_barrier();  // q has been read
     #pragma unroll
     for (int i = 0; i < kLoads; ++i) stage_k(0, i, k_scale(begin));
@@ -346,6 +397,7 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
         if (b + 2 - e0 >= 64 && b + 2 < end) {
             e0 = b + 2;
             load_scales();
+            check_scales();
         }
         const float next_scale = k_scale(clamp(b + 2));
         i32x8 v[S];

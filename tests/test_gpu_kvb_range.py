@@ -93,3 +93,32 @@ def test_large_values_of_keys_far_below(d, n, T, G, copies, by, parts):
         got = o[t, h].double().cpu().numpy()
         assert (np.abs(got - want) <= far).all(), (t, h, np.abs(got - want).max(), far.min(), np.abs(want).max())
         assert abs(lse[t, h].item() - want_lse) <= 2.0 ** -20 * (1 + abs(want_lse))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n, T, G, copies", NARROW + WIDE)
+@pytest.mark.parametrize("scale", [3e4, -3e4, 1e6, -1e6, 1e20, -1e20])
+def test_large_scores(d, n, T, G, copies, scale):
+    """Scores far above 2^24, whose roundings are larger than one: the mean of the keys with the highest score, from the
+    first blocks to the last, whichever score that is.  Products of q and k are integers, so that equal scores are equal in
+    any arithmetic and others lie `scale` apart at least."""
+    g = torch.Generator().manual_seed(8)
+    k, q = (torch.randint(-3, 4, shape, generator=g).float() for shape in ((n, 1, d), (T, G, d)))
+    k, q = k * 8, q * 8  # (products of 64 and more: scores above 2^24 from a scale of 3e4 on)
+    c, ks, vs = made(n, d, k.bfloat16(), normal(9, n, 1, d))
+    o, lse = run_attend(c, [n], [T], q.bfloat16().cuda(), scale, copies=copies)
+    scale = float(np.float32(scale))
+    for t, h in {(t, h) for t in range(0, T, max(1, T // 40)) for h in (0, G // 2, G - 1)}:
+        pos = n - T + t
+        x = (ks[0][:pos + 1, 0] @ q[t, h].double().numpy()) * np.sign(scale)
+        best = vs[0][:pos + 1, 0][x == x.max()]
+        want, mass, want_lse = best.mean(0), np.abs(best).mean(0), abs(scale) * x.max() + np.log(len(best))
+        # equal weights are rounded alike, the sum of 64 products by 2^-12 of their magnitudes, the output by 2^-8; the
+        # other weights are no higher than 2^-126 of the sum: up to 2^8 times the instruction's smallest scale 2^-127 (and
+        # their low halves, up to 2^3, times the same), against 2^7 and more
+        far = mass * 2.0 ** -12 + 2.0 ** -125 * np.abs(vs[0][:pos + 1, 0]).sum(0)
+        far = far + 2.0 ** -8 * (np.abs(want) + far)
+        got = o[t, h].double().cpu().numpy()
+        assert (np.abs(got - want) <= far).all(), (t, h, len(best), np.abs(got - want).max())
+        # scale log2(e), its product with the score and the way back are each rounded
+        assert abs(lse[t, h].item() - want_lse) <= 2.0 ** -21 * abs(want_lse)
