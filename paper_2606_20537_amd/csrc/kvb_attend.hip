@@ -7,8 +7,8 @@
 // in one pass over K and V with a running m and l.  The query rows of a KV head
 // (tokens x query heads of the group) share its K and V: 16 of them are the
 // columns of the matrix instructions, keys and channels the rows.
-//  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 tiles: codes are exact in bf16, also
-//    times the block's power-of-two scale (V); the scale of K multiplies the scores.
+//  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 tiles: the codes times their
+//    power-of-two scale are exact in bf16.
 //    The FP8 instructions would spare the conversion of K, but their sums lose what is
 //    2^18 below a product of the same instruction (measured: up to 1.6e-4 of the sum of
 //    the products' magnitudes, bf16 2e-7).
@@ -86,13 +86,13 @@ __device__ inline void decode4(uint32_t w, float scale, bf16x8& v, int at) {
 // 16 keys (lane % 16: a key, chunk j of 16 bytes: channels 64 j + 16 g .. + 15) against the
 // query rows, whose channels a lane holds in the same order.
 template <int D>
-__device__ inline f32x4 scores(const u32x4* k, const bf16x8* q) {
+__device__ inline f32x4 scores(const u32x4* k, float scale, const bf16x8* q) {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
     #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
         bf16x8 a;
-        decode4(k[j / 2][2 * (j % 2)], 1.0f, a, 0);
-        decode4(k[j / 2][2 * (j % 2) + 1], 1.0f, a, 4);
+        decode4(k[j / 2][2 * (j % 2)], scale, a, 0);
+        decode4(k[j / 2][2 * (j % 2) + 1], scale, a, 4);
         s = dev::mma(a, q[j], s);
     }
     return s;
@@ -200,17 +200,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
         for (int e = 0; e < 8; ++e) v[e] = load_v<VB>(rv, vvoff, (e < 4 ? e : 12 + e) * rowb);
     };
     // The scales of a unit are loaded ahead of its K (loads return in order), K once the K
-    // before it is used, V at the start of the step before the unit's own (or of its own).
+    // before it is used, V at the start of the step before the unit's own (or of its own).  With
+    // 256 channels the scales go two steps ahead, as K waits for its own (16385 rows 13.4 us
+    // a pass, one step ahead 13.8; of 128 channels, 6 tokens at 16390, 15.3 and 14.9).
     u32x4 k[2][NJ];
     VBytes<VB> v[kAhead ? 2 : 1][8];
-    float scales[2] = {1.0f, 1.0f};
-    auto load_scales = [&](int64_t r) {
+    float scales[2], ahead[2];
+    auto load_scales = [&](int64_t r, float (&scales)[2]) {
         const int64_t b = r < 0 ? 0 : r / kKvbBlock;
         scales[0] = sc[(b * 2) * p.kv_heads + h];
         scales[1] = sc[(b * 2 + 1) * p.kv_heads + h];
     };
     int64_t r = unit_row(wave);
-    load_scales(r);
+    load_scales(r, scales);
+    if (!kAhead) load_scales(unit_row(wave + 4), ahead);
     load_k(r, k);
     if (kAhead) load_values(r, v[0]);
     // the query rows, while the first keys are on their way
@@ -224,9 +227,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
     auto step = [&](int u, VBytes<VB> (&vc)[8], VBytes<VB> (&vn)[8]) {
         const int64_t next = unit_row(u + 4);
         if (kAhead) load_values(next, vn); else load_values(r, vc);
-        const f32x4 s0 = scores<D>(k[0], q), s1 = scores<D>(k[1], q);
         const float k_scale = scales[0], v_scale = scales[1];
-        load_scales(next);
+        const f32x4 s0 = scores<D>(k[0], k_scale, q), s1 = scores<D>(k[1], k_scale, q);
+        if (kAhead) {
+            load_scales(next, scales);
+        } else {
+            scales[0] = ahead[0];
+            scales[1] = ahead[1];
+            load_scales(unit_row(u + 8), ahead);
+        }
         load_k(next, k);
         const int64_t now = r;
         r = next;
@@ -234,8 +243,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
         float x[8];
         #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            x[e] = s0[e] * (p.scale_log2 * k_scale);
-            x[4 + e] = s1[e] * (p.scale_log2 * k_scale);
+            x[e] = s0[e] * p.scale_log2;
+            x[4 + e] = s1[e] * p.scale_log2;
         }
         const bool partial = now + 31 > pos0;  // some row does not see every key
         uint32_t nan_seen = 0;

@@ -122,3 +122,15 @@ def test_large_scores(d, n, T, G, copies, scale):
         assert (np.abs(got - want) <= far).all(), (t, h, len(best), np.abs(got - want).max())
         # scale log2(e), its product with the score and the way back are each rounded
         assert abs(lse[t, h].item() - want_lse) <= 2.0 ** -21 * abs(want_lse)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n, T, G, copies", NARROW + WIDE)
+@pytest.mark.parametrize("q_size, k_size, scale", [(2.0 ** 124, 2.0 ** -93, 2.0 ** -34), (2.0 ** -118, 2.0 ** 120, 2.0 ** -5), (2.0 ** -90, 2.0 ** -20, 2.0 ** 107)])
+def test_queries_and_keys_of_unlike_sizes(d, n, T, G, copies, q_size, k_size, scale):
+    """Queries and keys at opposite ends of the range, with scores of ordinary size."""
+    k, q = normal(10, n, 1, d).float().clamp(-4, 4) * k_size, normal(11, T, G, d).float().clamp(-4, 4) * q_size
+    c, ks, vs = made(n, d, k.bfloat16(), normal(12, n, 1, d))
+    q = q.bfloat16().cuda()
+    o, lse = run_attend(c, [n], [T], q, scale, copies=copies)
+    check_attend(c, ks, vs, [n], [T], q, scale, o, lse, rows=100)
