@@ -608,7 +608,7 @@ typedef struct kvb_attend_args {
     int32_t        d;
     int32_t        n_sel;      /* entries of a list; 0 when idx is NULL */
     int32_t        in_dtype;   /* CAP_DTYPE_BF16 */
-    float          scale;      /* finite */
+    float          scale;      /* finite, and below 2.3e38 in magnitude (CAP_E_INVAL) */
     int32_t        reserved;   /* 0 */
 } kvb_attend_args;
 

@@ -329,7 +329,9 @@ uint64_t kvb_attend_workspace_bytes(const kvb_attend_args* a) {
 }
 
 int kvb_attend(const kvb_attend_args* a, void* stream) {
-    if (!a || a->reserved != 0 || !std::isfinite(a->scale)) return CAP_E_INVAL;
+    if (!a || a->reserved != 0) return CAP_E_INVAL;
+    const float scale_log2 = a->scale * 1.4426950408889634f;
+    if (!std::isfinite(scale_log2)) return CAP_E_INVAL;
     cap::KvbAttendParams p[2]{};
     int rc = plan_attend(a, p);
     if (rc != CAP_OK) return rc;
@@ -369,7 +371,7 @@ int kvb_attend(const kvb_attend_args* a, void* stream) {
         x.part_o = part;
         x.part_ml = part + (uint64_t)x.slots * (uint64_t)x.tile * (uint64_t)x.d;
         part = x.part_ml + (uint64_t)x.slots * (uint64_t)x.tile * 2;
-        x.scale_log2 = a->scale * 1.4426950408889634f;
+        x.scale_log2 = scale_log2;
         if ((rc = launch_status(cap::launch_kvb_attend(x, static_cast<hipStream_t>(stream)))) != CAP_OK) return rc;
     }
     return CAP_OK;

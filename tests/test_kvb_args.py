@@ -263,3 +263,9 @@ def test_binding_takes_a_single_head_of_any_stride():
     x = torch.zeros((3, 5, 64), dtype=torch.bfloat16)
     for one in (x[:, ::5], x.transpose(0, 1).contiguous().transpose(0, 1)[:, 4:], x.as_strided((3, 1, 64), (320, 7, 1))):
         assert N._kvb_tokens("kvb_append", "k", one)[0] == (one.stride(0) if not one.is_contiguous() else 0)
+
+
+def test_attend_refuses_a_scale_whose_multiple_of_log2_e_is_not_finite():
+    """Scores are held in units of log 2: 3e38 log2(e) would be infinite, and times a score of zero NaN."""
+    for scale in (3e38, -3e38, 2.4e38):
+        assert call("kvb_attend", scale=scale) == cap.CAP_E_INVAL
