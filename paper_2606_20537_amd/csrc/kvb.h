@@ -14,6 +14,10 @@ constexpr int kKvbBlock = KVB_BLOCK;
 // The table comes last, so that the short form is the beginning of the long one.
 constexpr int kKvbFew = 4;
 
+// A grid of workgroups of 256 (kvb_device.h: kvb_block): a launch counts its threads along x in
+// 32 bits, which the scores of 46000 tokens on 8 KV heads pass.
+inline dim3 kvb_grid(uint32_t wgs) { return dim3(fp8_grid_x(wgs), fp8_grid_y(wgs)); }
+
 // ---- append ----
 // Workgroup w works on sequence s with first_wg <= w < the next one's, on its
 // block, KV head and side (K or V) number w - first_wg.

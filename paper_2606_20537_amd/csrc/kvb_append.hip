@@ -80,8 +80,10 @@ __global__ __launch_bounds__(kThreads, 4) void append_kernel(const KvbAppendTabl
     __shared__ i16x2 lo_s[kRows][D / 2 + 4], hi_s[kRows][D / 2 + 4];
     __shared__ uint8_t nan_s[D];
 
-    const KvbAppendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
-    const uint32_t w = blockIdx.x - s.first_wg;
+    const uint32_t block = kvb_block();
+    if (block >= p.wgs) return;
+    const KvbAppendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, block)];
+    const uint32_t w = block - s.first_wg;
     const int side = (int)(w & 1), h = (int)((w >> 1) % (uint32_t)p.kv_heads);
     const int64_t held = s.n - s.T;              // rows before the append
     const int64_t b0 = held / kKvbBlock, b = b0 + (w >> 1) / (uint32_t)p.kv_heads;
@@ -235,7 +237,7 @@ __global__ __launch_bounds__(kThreads, 4) void append_kernel(const KvbAppendTabl
 template <int D>
 hipError_t launch(const KvbAppendParams& p, hipStream_t stream) {
     return launch_kvb<KvbAppendTable>(reinterpret_cast<const void*>(&append_kernel<D, kKvbFew>),
-                                      reinterpret_cast<const void*>(&append_kernel<D, KVB_MAX_SEQ>), dim3(p.wgs), dim3(kThreads), p, stream);
+                                      reinterpret_cast<const void*>(&append_kernel<D, KVB_MAX_SEQ>), kvb_grid(p.wgs), dim3(kThreads), p, stream);
 }
 
 }  // namespace

@@ -126,8 +126,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvbAttendTabl
     __shared__ float o_s[4][16][kPitch];
     __shared__ float ml_s[4][16][2], all_s[16][2];
 
-    const KvbAttendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
-    const uint32_t w = blockIdx.x - s.first_wg;
+    const uint32_t block = kvb_block();
+    if (block >= p.wgs) return;
+    const KvbAttendSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, block)];
+    const uint32_t w = block - s.first_wg;
     const int G = p.heads / p.kv_heads;
     const uint32_t item = w / (uint32_t)s.nsplit;  // (tile, kv head)
     const int split = (int)(w - item * (uint32_t)s.nsplit);
@@ -388,8 +390,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvbAttendTable<N> 
     constexpr int kAhead = 4;  // runs whose loads are in flight
     static_assert(kPer * kParts == D / 4 && kRows * kPer * WAYS == kThreads, "threads of a row");
     const int tid = (int)threadIdx.x, way = tid / kPer % WAYS, mine = tid / (kPer * WAYS);
-    const int c = (int)(blockIdx.x % kParts) * 4 * kPer + tid % kPer * 4;
-    const uint32_t all = (uint32_t)(p.tokens * p.heads), out = blockIdx.x / kParts * kRows + (uint32_t)mine;
+    const uint32_t block = kvb_block();
+    const int c = (int)(block % kParts) * 4 * kPer + tid % kPer * 4;
+    const uint32_t all = (uint32_t)(p.tokens * p.heads), out = block / kParts * kRows + (uint32_t)mine;
     const uint32_t at = out < all ? out : all - 1;  // threads past the last row repeat it
     const uint32_t tok = at / (uint32_t)p.heads;
     const int head = (int)(at - tok * (uint32_t)p.heads);
@@ -481,8 +484,8 @@ template <int D>
 hipError_t launch(const KvbAttendParams& p, hipStream_t stream) {
     const dim3 block(kThreads);
     const hipError_t e = p.tile == 128 ? launch_kvb_prefill(p, stream)
-                         : p.idx ? launch_kvb<KvbAttendTable>(KVB_FORMS(attend_kernel, D, true), dim3(p.wgs), block, p, stream)
-                                 : launch_kvb<KvbAttendTable>(KVB_FORMS(attend_kernel, D, false), dim3(p.wgs), block, p, stream);
+                         : p.idx ? launch_kvb<KvbAttendTable>(KVB_FORMS(attend_kernel, D, true), kvb_grid(p.wgs), block, p, stream)
+                                 : launch_kvb<KvbAttendTable>(KVB_FORMS(attend_kernel, D, false), kvb_grid(p.wgs), block, p, stream);
     if (e != hipSuccess || p.slots == 0) return e;
     // Threads side by side on the runs of a row where there are few rows for the chip: 161 tokens x
     // 32 heads x 256 channels of 8 runs took 30 us with them, 32 heads of one token and 43 runs 10 us without.
@@ -490,8 +493,8 @@ hipError_t launch(const KvbAttendParams& p, hipStream_t stream) {
     int runs = 0;
     for (int i = 0; i < p.n_seq; ++i) runs = p.seq[i].nsplit > runs ? p.seq[i].nsplit : runs;
     return runs > 4 && rows * (D / 64) <= 4096
-               ? launch_kvb<KvbAttendTable>(KVB_FORMS(join_kernel, D, 16), dim3(rows * (D / 64)), block, p, stream)
-               : launch_kvb<KvbAttendTable>(KVB_FORMS(join_kernel, D, 1), dim3((rows + per - 1) / per), block, p, stream);
+               ? launch_kvb<KvbAttendTable>(KVB_FORMS(join_kernel, D, 16), kvb_grid(rows * (D / 64)), block, p, stream)
+               : launch_kvb<KvbAttendTable>(KVB_FORMS(join_kernel, D, 1), kvb_grid((rows + per - 1) / per), block, p, stream);
 }
 
 }  // namespace

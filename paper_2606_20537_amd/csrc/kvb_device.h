@@ -11,6 +11,9 @@ namespace cap {
 template <typename T>
 using global_ptr = const T __attribute__((address_space(1)))*;
 
+// A workgroup's number in a kvb_grid; those from the launch's count on have nothing to do.
+__device__ inline uint32_t kvb_block() { return blockIdx.y * kFp8GridX + blockIdx.x; }
+
 // The last sequence whose `field` (ascending) is at most x: lane i looks at
 // sequence i, so that the table is read once, not once for each step of a search.
 static_assert(KVB_MAX_SEQ <= 64, "a lane for each sequence");

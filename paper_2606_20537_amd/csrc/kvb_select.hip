@@ -46,10 +46,12 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const KvbSelectTable<N>
     constexpr int kSteps = D / 16;  // channels of a lane: D / 4 to a wave, a quarter of them to a lane group
     __shared__ double part_s[4][4][64];
     __shared__ double best_s[4][16];
-    const KvbSelectSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, blockIdx.x)];
+    const uint32_t block = kvb_block();
+    if (block >= p.wgs) return;
+    const KvbSelectSeq& s = p.seq[KVB_SEQ_OF(p, first_wg, block)];
     const uint32_t nb = (uint32_t)((s.n + kKvbBlock - 1) / kKvbBlock);
     const uint32_t parts = (nb + kKvbScoreBlocks - 1) / kKvbScoreBlocks;
-    const uint32_t w = blockIdx.x - s.first_wg, pair = w / parts;
+    const uint32_t w = block - s.first_wg, pair = w / parts;
     const int h = (int)(pair % (uint32_t)p.kv_heads);
     const int64_t t = pair / (uint32_t)p.kv_heads;
     const uint32_t mine = (uint32_t)((s.n - s.T + t) / kKvbBlock);  // the token's own block
@@ -128,14 +130,16 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const KvbSelectTable<N> 
     __shared__ uint64_t sums_s[kThreads / 64];
     __shared__ __attribute__((aligned(16))) uint32_t bins[8][256];  // a histogram for each digit
     static_assert(kThreads == 256, "a bin for each thread");
-    const int64_t tok = blockIdx.x / (uint32_t)p.kv_heads;
-    const int h = (int)(blockIdx.x - tok * p.kv_heads);
+    const uint32_t block = kvb_block();
+    if (block >= (uint32_t)(p.tokens * p.kv_heads)) return;
+    const int64_t tok = block / (uint32_t)p.kv_heads;
+    const int h = (int)(block - tok * p.kv_heads);
     const KvbSelectSeq& s = p.seq[KVB_SEQ_OF(p, t0, tok)];
     const int64_t t = tok - s.t0;
     const uint32_t nb = (uint32_t)((s.n + kKvbBlock - 1) / kKvbBlock);
     const uint32_t count = (uint32_t)((s.n - s.T + t) / kKvbBlock) + 1;  // blocks that the token sees some of
     const uint64_t* keys = p.keys + s.keys + (t * p.kv_heads + h) * (uint64_t)nb;
-    int32_t* out = p.idx + (int64_t)blockIdx.x * p.n_sel;
+    int32_t* out = p.idx + (int64_t)block * p.n_sel;
     const uint32_t n_sel = (uint32_t)p.n_sel, tid = threadIdx.x;
     if (count <= n_sel) {
         for (uint32_t i = tid; i < n_sel; i += kThreads) out[i] = i < count ? (int32_t)i : -1;
@@ -263,7 +267,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const KvbSelectTable<N> 
 template <int D>
 hipError_t launch_score(const KvbSelectParams& p, hipStream_t stream) {
     return launch_kvb<KvbSelectTable>(reinterpret_cast<const void*>(&score_kernel<D, kKvbFew>),
-                                      reinterpret_cast<const void*>(&score_kernel<D, KVB_MAX_SEQ>), dim3(p.wgs), dim3(kThreads), p, stream);
+                                      reinterpret_cast<const void*>(&score_kernel<D, KVB_MAX_SEQ>), kvb_grid(p.wgs), dim3(kThreads), p, stream);
 }
 
 }  // namespace
@@ -273,7 +277,7 @@ hipError_t launch_kvb_select(const KvbSelectParams& p, hipStream_t stream) {
     const hipError_t e = p.d == 64 ? launch_score<64>(p, stream) : p.d == 128 ? launch_score<128>(p, stream) : launch_score<256>(p, stream);
     if (e != hipSuccess) return e;
     return launch_kvb<KvbSelectTable>(reinterpret_cast<const void*>(&pick_kernel<kKvbFew>), reinterpret_cast<const void*>(&pick_kernel<KVB_MAX_SEQ>),
-                                      dim3((uint32_t)(p.tokens * p.kv_heads)), dim3(kThreads), p, stream);
+                                      kvb_grid((uint32_t)(p.tokens * p.kv_heads)), dim3(kThreads), p, stream);
 }
 
 }  // namespace cap
