@@ -542,7 +542,7 @@ CAP_API int kv_fp8_dequantize(const kv_fp8_seg* segs, uint32_t n_seg, void* stre
  * Errors: CAP_E_INVAL (null required pointer, counts below their range, T > n,
  * tokens not the sum of T, rows not a multiple of 64, heads not a multiple of kv_heads, an output that
  * overlaps an input or another output), CAP_E_SIZE (n > rows, workspace too
- * small), CAP_E_UNSUPPORTED (shape or dtype outside the list, n_seq >
+ * small, a buffer that ends past the last address), CAP_E_UNSUPPORTED (shape or dtype outside the list, n_seq >
  * KVB_MAX_SEQ), CAP_E_ALIGN.  A call reads the sequence table before it returns,
  * and its kernel arguments carry every address, length and position: it can be
  * recorded in a stream capture and replayed for the same n.  A workspace holds

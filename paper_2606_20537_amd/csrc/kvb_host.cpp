@@ -15,6 +15,7 @@ struct Range { uint64_t a, b; };
 uint64_t addr(const void* p) { return (uint64_t)(uintptr_t)p; }
 Range range(const void* p, uint64_t bytes) { return {addr(p), addr(p) + (p ? bytes : 0)}; }
 bool meet(const Range& x, const Range& y) { return x.a < y.b && y.a < x.b; }
+bool wraps(const Range& x) { return x.b < x.a; }  // past the last address
 uint64_t up(uint64_t x, uint64_t m) { return (x + m - 1) / m * m; }
 
 // The sizes that every call shares.
@@ -78,6 +79,13 @@ int check_parts(const kvb_seq& s, unsigned need) {
 }
 int check_align(const kvb_seq& s) {
     return ((addr(s.k) | addr(s.v) | addr(s.bounds) | addr(s.open)) & 15) || (addr(s.scales) & 3) ? CAP_E_ALIGN : CAP_OK;
+}
+
+// Whether every part that a call uses ends below the last address.
+int check_ends(const kvb_seq& s, unsigned used, int32_t kv_heads, int32_t d) {
+    for (int i = 0; i < PARTS; ++i)
+        if ((used >> i & 1) && wraps(part(s, i, kv_heads, d))) return CAP_E_SIZE;
+    return CAP_OK;
 }
 
 // Whether an output meets one of the parts `used` of a sequence.
@@ -287,6 +295,7 @@ int kvb_append(const kvb_append_args* a, void* stream) {
     if (tokens == 0) return CAP_OK;
     if (!a->k || !a->v) return CAP_E_INVAL;
     const Range in[2] = {range(a->k, span(tokens, p.k_stride, row)), range(a->v, span(tokens, p.v_stride, row))};
+    if (wraps(in[0]) || wraps(in[1])) return CAP_E_SIZE;
     Range out[KVB_MAX_SEQ * PARTS];
     int n_out = 0, n = 0;
     int64_t wgs = 0, t0 = 0;
@@ -295,6 +304,7 @@ int kvb_append(const kvb_append_args* a, void* stream) {
         if (s.T == 0) continue;
         if ((rc = check_parts(s, bit(K) | bit(V) | bit(SCALES) | bit(OPEN))) != CAP_OK) return rc;
         if ((rc = check_align(s)) != CAP_OK) return rc;
+        if ((rc = check_ends(s, ~0u, a->kv_heads, a->d)) != CAP_OK) return rc;
         cap::KvbAppendSeq& x = p.seq[n++];
         x = {addr(s.k), addr(s.v), addr(s.scales), addr(s.bounds), addr(s.open), s.n, t0, (int32_t)s.T, (uint32_t)wgs};
         const int64_t begun = (s.n + kKvbBlock - 1) / kKvbBlock - (s.n - s.T) / kKvbBlock;
@@ -347,6 +357,7 @@ int kvb_attend(const kvb_attend_args* a, void* stream) {
         if (a->seqs[i].T == 0) continue;
         if ((rc = check_parts(a->seqs[i], bit(K) | bit(V) | bit(SCALES))) != CAP_OK) return rc;
         if ((rc = check_align(a->seqs[i])) != CAP_OK) return rc;
+        if ((rc = check_ends(a->seqs[i], bit(K) | bit(V) | bit(SCALES), a->kv_heads, a->d)) != CAP_OK) return rc;
     }
     if (((addr(a->q) | addr(a->o) | (need ? addr(a->workspace) : 0)) & 15) || ((addr(a->lse) | addr(a->idx)) & 3)) return CAP_E_ALIGN;
     const uint64_t tokens = (uint64_t)a->tokens;
@@ -354,6 +365,10 @@ int kvb_attend(const kvb_attend_args* a, void* stream) {
                          range(a->idx, tokens * (uint64_t)a->kv_heads * (uint64_t)a->n_sel * 4)};
     const Range out[3] = {range(a->o, tokens * (uint64_t)width * 2), range(a->lse, tokens * (uint64_t)a->heads * 4),
                           range(need ? a->workspace : nullptr, need)};
+    for (const Range& x : in)
+        if (wraps(x)) return CAP_E_SIZE;
+    for (const Range& x : out)
+        if (wraps(x)) return CAP_E_SIZE;
     for (int i = 0; i < 3; ++i) {
         for (int j = 0; j < i; ++j)
             if (meet(out[i], out[j])) return CAP_E_INVAL;
@@ -398,10 +413,12 @@ int kvb_select(const kvb_select_args* a, void* stream) {
         if (a->seqs[i].T == 0) continue;
         if ((rc = check_parts(a->seqs[i], bit(SCALES) | bit(BOUNDS))) != CAP_OK) return rc;
         if ((rc = check_align(a->seqs[i])) != CAP_OK) return rc;
+        if ((rc = check_ends(a->seqs[i], bit(SCALES) | bit(BOUNDS), a->kv_heads, a->d)) != CAP_OK) return rc;
     }
     if (((addr(a->q) | addr(a->workspace)) & 15) || (addr(a->idx) & 3)) return CAP_E_ALIGN;
     const Range q = range(a->q, span(p.tokens, p.q_stride, width));
     const Range out[2] = {range(a->idx, (uint64_t)p.tokens * (uint64_t)a->kv_heads * (uint64_t)a->n_sel * 4), range(a->workspace, need)};
+    if (wraps(q) || wraps(out[0]) || wraps(out[1])) return CAP_E_SIZE;
     if (meet(out[0], out[1]) || meet(out[0], q) || meet(out[1], q)) return CAP_E_INVAL;
     for (int i = 0; i < 2; ++i)
         for (int32_t j = 0; j < a->n_seq; ++j)

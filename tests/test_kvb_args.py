@@ -269,3 +269,23 @@ def test_attend_refuses_a_scale_whose_multiple_of_log2_e_is_not_finite():
     """Scores are held in units of log 2: 3e38 log2(e) would be infinite, and times a score of zero NaN."""
     for scale in (3e38, -3e38, 2.4e38):
         assert call("kvb_attend", scale=scale) == cap.CAP_E_INVAL
+
+
+def test_buffers_that_end_past_the_last_address():
+    """An end that wraps round to a small address would overlap nothing."""
+    end = (1 << 64) - 256
+    for part in ("k", "v", "scales", "bounds", "open"):
+        assert call("kvb_append", [seq(**{part: end})]) == cap.CAP_E_SIZE
+    for part in ("k", "v", "scales"):
+        assert call("kvb_attend", [seq(**{part: end})]) == cap.CAP_E_SIZE
+    for part in ("scales", "bounds"):
+        assert call("kvb_select", [seq(**{part: end})]) == cap.CAP_E_SIZE
+    wide = dict(k_stride=1 << 20, v_stride=1 << 20)
+    for x in ("k", "v"):
+        assert call("kvb_append", **{x: end, **wide}) == cap.CAP_E_SIZE
+    big = [seq(rows=1 << 16, n=1 << 16)]
+    for x in ("q", "o", "lse", "workspace"):
+        assert call("kvb_attend", big, **{x: end if x != "lse" else (1 << 64) - 16, "q_stride": 1 << 20}) == cap.CAP_E_SIZE
+    assert call("kvb_attend", idx=(1 << 64) - 16, n_sel=4) == cap.CAP_E_SIZE
+    for x in ("q", "idx", "workspace"):
+        assert call("kvb_select", big, **{x: end if x == "q" else (1 << 64) - 16, "q_stride": 1 << 20}) == cap.CAP_E_SIZE
