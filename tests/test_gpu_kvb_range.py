@@ -14,6 +14,7 @@ pytestmark = pytest.mark.gpu
 # whole and in runs
 NARROW = [(500, 5, 3, 1), (3000, 1, 8, 1)]
 WIDE = [(1100, 90, 8, 32), (4500, 161, 16, 1)]
+LONG = (8400, 70, 32, 48)  # tiles of 128, more than 128 blocks in a run
 
 
 def made(n, d, k, v, fill=0x7F):
@@ -134,3 +135,40 @@ def test_queries_and_keys_of_unlike_sizes(d, n, T, G, copies, q_size, k_size, sc
     q = q.bfloat16().cuda()
     o, lse = run_attend(c, [n], [T], q, scale, copies=copies)
     check_attend(c, ks, vs, [n], [T], q, scale, o, lse, rows=100)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_long_runs(d):
+    """Runs of more than 128 blocks, whose scales are loaded 64 blocks at a time: sizes of K and V that differ from block
+    to block."""
+    n, T, G, copies = LONG
+    by = 2.0 ** torch.randint(-6, 7, (up(n) // BLOCK, 2), generator=torch.Generator().manual_seed(13)).float().repeat_interleave(BLOCK, 0)[:n]
+    c, ks, vs = made(n, d, (normal(14, n, 1, d).float() * by[:, :1, None]).bfloat16(), (normal(15, n, 1, d).float() * by[:, 1:, None]).bfloat16())
+    q = normal(16, T, G, d).cuda()
+    o, lse = run_attend(c, [n], [T], q, 0.02, copies=copies)
+    check_attend(c, ks, vs, [n], [T], q, 0.02, o, lse, rows=60)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("block", [0, 63, 64, 66, 127, 130])
+def test_large_scores_of_one_block(d, block):
+    """Scores above 2^24 in one block of a long run alone: the mean of that block's best keys, and of the others' rows
+    that do not see it what they see."""
+    n, T, G, copies = LONG
+    g = torch.Generator().manual_seed(17)
+    k, q = torch.zeros(n, 1, d), torch.full((T, G, d), 8.0)
+    rows = k[block * BLOCK:(block + 1) * BLOCK]
+    rows[:] = 8.0 * torch.randint(0, 3, rows.shape, generator=g)
+    c, ks, vs = made(n, d, k.bfloat16(), normal(18, n, 1, d))
+    o, lse = run_attend(c, [n], [T], q.bfloat16().cuda(), 1e6, copies=copies)
+    for t in (0, T - 1):
+        pos = n - T + t
+        x = ks[0][:pos + 1, 0] @ q[t, 0].double().numpy()
+        best = vs[0][:pos + 1, 0][x == x.max()]
+        want, mass = best.mean(0), np.abs(best).mean(0)
+        far = mass * 2.0 ** -12 + 2.0 ** -125 * np.abs(vs[0][:pos + 1, 0]).sum(0)  # as in test_large_scores
+        far = far + 2.0 ** -8 * (np.abs(want) + far)
+        for h in (0, G - 1):
+            got = o[t, h].double().cpu().numpy()
+            assert (np.abs(got - want) <= far).all(), (t, h, len(best), np.abs(got - want).max())
+            assert abs(lse[t, h].item() - (1e6 * x.max() + np.log(len(best)))) <= 2.0 ** -21 * 1e6 * x.max() + 2.0 ** -20
