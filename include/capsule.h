@@ -532,7 +532,12 @@ CAP_API int kv_fp8_dequantize(const kv_fp8_seg* segs, uint32_t n_seg, void* stre
  * One step covers n_seq sequences (at most KVB_MAX_SEQ), each with T new tokens
  * at positions [n - T, n): n counts the rows held with the new ones, for every
  * call of the step alike (append first, then select and attend).  Going back to
- * an earlier n needs the open rows of that n; at a multiple of 64 there are none.
+ * an earlier n (rejected draft tokens) needs the open rows of that n; at a multiple
+ * of 64 there are none.  An append leaves those before it as they are unless it ends
+ * in a later block: one that may be taken back across a block's beginning needs a copy
+ * of `open` from before it, put back first.  The library cannot tell: without it the
+ * block would be encoded from the later block's rows.  Until the next append the block
+ * keeps the scale and bounds that the rejected rows gave it.
  * Tokens are packed: sequence 0's T tokens, then sequence 1's, and so on;
  * strides are in elements between tokens (0: contiguous), multiples of 8.
  * Sequences with T = 0 are passed over.

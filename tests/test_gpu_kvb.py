@@ -139,6 +139,28 @@ def test_append_after_going_back():
     check_cache(c, 0, k[:81], v[:81])
 
 
+@pytest.mark.parametrize("n0, n1, n2", [(62, 68, 63), (62, 64, 63), (100, 200, 101), (5, 128, 5), (63, 65, 64)])
+def test_append_after_going_back_to_an_earlier_block(n0, n1, n2):
+    """Draft tokens that began a new block, rejected: with `open` kept from before them and put back, no trace of them."""
+    hkv, d = 2, 64
+    k, v = normal(9, 256, hkv, d), normal(10, 256, hkv, d)
+    c = Caches([256], hkv, d)
+    append(c, [0], [n0], [k], [v])
+    kept = c.open[0].clone()
+    append(c, [n0], [n1], [k * 1000], [v * 1000])
+    c.open[0].copy_(kept)
+    for x in (c.k[0][n2:], c.v[0][n2:]):  # rows and blocks of the rejected tokens
+        x.fill_(CANARY)
+    nb = up(n2) // BLOCK
+    c.scales[0][nb:] = -3.0
+    c.bounds[0][nb:] = CANARY
+    if n2 > n0:
+        append(c, [n0], [n2], [k], [v])
+    else:  # back to n0 itself: its block was encoded with the drafts' rows
+        append(c, [n0 - 1], [n0], [k], [v])
+    check_cache(c, 0, k[:n2], v[:n2])
+
+
 def test_append_ragged_strided_without_bounds():
     """Views of a fused projection, sequences of their own lengths with none and one token among them, no bounds."""
     hkv, d = 2, 128
