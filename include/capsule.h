@@ -593,10 +593,22 @@ CAP_API int kvb_append(const kvb_append_args* args, void* stream);
  *         entry below 0 or of a block beyond t's is passed over; a block that is
  *         listed twice counts twice.
  * A row that sees nothing has o = 0 and lse = -inf.  Rows that a token does not
- * see have no part in its result, NaN codes included.  The softmax is held in
- * fp32; scores take the query rows in full, weights enter the second product as
- * bf16.  One launch, or two where a sequence is cut along its rows (the parts
- * lie in the workspace), apart for sequences of few and of many query rows.  Results are reproducible for the same arguments. */
+ * see have no part in its result, NaN codes included.
+ * Precision: scores take the query rows in full; scores, the softmax and the sums
+ * are fp32 (a score beyond fp32 gives NaN).  Weights are rounded to 8 bits before
+ * the second product.  In tiles of 16 query rows they are bf16.  In tiles of 128,
+ * which sequences of many query rows may take, they are two E4M3 codes, hi + lo / 16:
+ * relative 2^-8 as well, or 2^-21 of the largest weight in the block of 64 rows
+ * where that is more, and the products' sums lose 2^-12 of the sum of their magnitudes.
+ * Weights below 2^-80 of a row's largest may count as none, or, of values below 2^24,
+ * as 2^-126.  Means of finite values are finite.
+ * One launch, or two where a sequence is cut along its rows (the parts
+ * lie in the workspace), apart for sequences of few and of many query rows.
+ * Results are reproducible for the same arguments.  Between other calls they are
+ * not bit for bit: tiles begin at n - T, and tiles and runs are chosen by estimates
+ * over the whole call, so a row's last bits depend on how its prompt was divided
+ * into calls and on the other sequences.  (kvb_append and kvb_select do not: a
+ * block's bytes and a token's list are the same whatever calls brought them.) */
 typedef struct kvb_attend_args {
     const kvb_seq* seqs;       /* HOST array of n_seq (bounds, open: not read) */
     const void*    q;

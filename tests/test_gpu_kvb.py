@@ -418,6 +418,22 @@ def test_select(d, hkv, G, n_sel, first, last):
             assert idx[x, h].tolist() == want, (i, t, h)
 
 
+def test_select_of_a_step_and_of_its_tokens_alone():
+    """A token's list does not depend on how the tokens were divided into calls, rows appended since then or not."""
+    hkv, G, d, n, T, n_sel = 2, 3, 128, 1500, 90, 9
+    k, q = normal(82, n, hkv, d), normal(83, T, hkv * G, d).cuda()
+    c, piece = Caches([up(n)], hkv, d), Caches([up(n)], hkv, d)
+    append(c, [0], [n], [k], [k])
+    whole, alone = (torch.empty((T, hkv, n_sel), dtype=torch.int32, device="cuda") for _ in range(2))
+    cap.kvb_select(c.table([n], [T]), q, whole, kv_heads=hkv, first=1, last=2)
+    append(piece, [0], [n - T], [k], [k])
+    for t in range(T):
+        m = n - T + t + 1
+        append(piece, [m - 1], [m], [k], [k])
+        cap.kvb_select(piece.table([m], [1]), q[t:t + 1], alone[t:t + 1], kv_heads=hkv, first=1, last=2)
+    assert torch.equal(whole, alone)
+
+
 def test_selected_blocks_hold_the_highest_products():
     """No key of a block scores above its bound: with one block selected beyond the own, the best key's block scores highest
     among single-row blocks' bounds."""
