@@ -289,3 +289,22 @@ def test_buffers_that_end_past_the_last_address():
     assert call("kvb_attend", idx=(1 << 64) - 16, n_sel=4) == cap.CAP_E_SIZE
     for x in ("q", "idx", "workspace"):
         assert call("kvb_select", big, **{x: end if x == "q" else (1 << 64) - 16, "q_stride": 1 << 20}) == cap.CAP_E_SIZE
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_attend_workspace_is_bounded(d):
+    """Whatever the batch: 1024 parts of 128 rows, and as many of 16 (runs of a 512th of their blocks and more, of which a
+    cut sequence's last may be short)."""
+    most = (1024 * 128 + 1024 * 16) * (d + 2) * 4
+    rng = np.random.default_rng(4)
+    for _ in range(300):
+        seqs = []
+        for i in range(rng.integers(1, 9)):
+            T = int(2 ** rng.uniform(0, 12)) if rng.random() < 0.6 else 1
+            n = T + int(2 ** rng.uniform(0, 17))
+            seqs.append(seq(i, n=n, T=T, rows=-(-n // 64) * 64))
+        arr = table(*seqs)
+        hkv = int(rng.choice([1, 2, 4, 8]))
+        a = N.kvb_attend_args(seqs=ct.addressof(arr), tokens=sum(s["T"] for s in seqs), n_seq=len(seqs), heads=hkv * int(rng.choice([1, 4, 8])),
+                              kv_heads=hkv, d=d, in_dtype=cap.CAP_DTYPE_BF16)
+        assert cap.load().kvb_attend_workspace_bytes(ct.byref(a)) <= most
