@@ -3,9 +3,10 @@
 // A block's score for a token and KV head is the highest value that the product
 // of a key within the block's bounds with any query of the head's group can have,
 //   max_g sum_c max(q_gc lo_c, q_gc hi_c) * scale_k .
-// Products of bf16 and E4M3 values have 12 bits, so in 64 bits their sums are
-// exact in any order (as long as a row's values span less than 2^30), and the
-// choice does not depend on how a kernel adds.  A score that is NaN counts as
+// With 2^a and 2^b the powers of two of a row's smallest (but zero) and largest values,
+// the products with codes are multiples of 2^(a - 16) and 256 of them sum to less than
+// 2^(b + 18): while the row spans less than 2^19 their sums are exact in 64 bits, in any
+// order, and the choice does not depend on how a kernel adds.  A score that is NaN counts as
 // infinite, as attention over the block gives NaN.
 //
 // Two launches.  Scores: q+ . hi + q- . lo (q+ and q- the positive and the negative part
