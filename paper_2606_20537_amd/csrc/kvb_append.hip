@@ -15,7 +15,7 @@
 // its codes, scale and bounds are a function of its rows alone, whatever calls
 // brought them, also after a session went back to an earlier row.
 //
-// Bound by memory: 16384 rows x 4 heads x 256 channels, 101 MB, 17.0 us (5.9 TB/s read and
+// Bound by memory: 16384 rows x 4 heads x 256 channels, 101 MB, 17.5 us (5.8 TB/s read and
 // written; a copy of 1 GiB 5.2).  With the maximum, the bounds and the conversion in 32
 // bits an element took some 12 instructions and the call 26 us; now maximum and bounds are
 // 16-bit integers, two at a time, and the conversion one instruction for two values.

@@ -22,7 +22,7 @@
 // joins the four waves, which take 32 rows of the cache in turn.
 //
 // What bounds it, 8 query heads on each KV head of 256 channels, one token: 131072 +
-// 18561 rows, 307 MB, 57.8 us (5.3 TB/s, the rate of a copy); 16385 rows, 33.8 MB, 11.3 us
+// 18561 rows, 307 MB, 58.2 us (5.3 TB/s, the rate of a copy); 16385 rows, 33.8 MB, 10.8 us
 // and 4.5 of the join, of which the data take 6.5 and the launches 2.2 each.  A wave
 // takes about 1 us for 32 rows by itself (128 byte permutes and conversions, 32 matrix
 // instructions, little of it side by side), so runs stay a few blocks long.  Registers for

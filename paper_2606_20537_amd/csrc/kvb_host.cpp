@@ -157,13 +157,13 @@ Plan128 plan_128(int32_t d, const Work& x) {
 // less than a workgroup to a CU leaves them in runs, and a join.  Both launches' estimates are
 // without their 4 us from call to call.  Measured (us, tiles of 16 / of 128; tokens, rows held,
 // query heads on KV heads of d channels):
-//     512 of 512, 16 on 4 of 256        17 / 25      16 such sequences     174 / 95
-//     2048 of 2048, 16 on 4 of 256     112 / 77      of 128  66 / 50       of 64  36 / 39
-//     161 behind 16384, 4 on 4 of 256   57 / 40      of 128  36 / 30       of 64  23 / 23
-//     64 of 300, 16 on 4 of 256         13 / 19      32 such sequences      53 / 27
-//     8192 of 8192, 16 on 4 of 256    1230 / 590     of 128 751 / 353      of 64 374 / 246
-// Over 135 such calls the estimates' choice is 1.5% behind the better one, tiles of 128
-// throughout 15%.  A tile of 128 for 64 rows takes 110 where tiles of 16 take 60 (131072 rows).
+//     512 of 512, 16 on 4 of 256        16 / 25      16 such sequences     169 / 92
+//     2048 of 2048, 16 on 4 of 256      90 / 70      of 128  55 / 46       of 64  29 / 37
+//     161 behind 16384, 4 on 4 of 256   54 / 38      of 128  35 / 27       of 64  21 / 22
+//     64 of 300, 16 on 4 of 256         10 / 19      32 such sequences      47 / 26
+//     8192 of 8192, 16 on 4 of 256    1181 / 573     of 128 701 / 321      of 64 334 / 239
+// Over 135 such calls the estimates' choice is 0.3 % behind the better one (30 % at 2048 of 2048
+// of 64 channels, the worst), tiles of 128 throughout 34 %.  A tile of 128 for 64 rows takes 110 where tiles of 16 take 60 (131072 rows).
 constexpr int64_t kRowsFor128 = 129;
 double us_of_16(int32_t d, const Work& x) {
     const double block = d == 256 ? 2.3e-3 : d == 128 ? 1.4e-3 : 0.72e-3, tile = d == 256 ? 10e-3 : d == 128 ? 4.2e-3 : 2.6e-3;

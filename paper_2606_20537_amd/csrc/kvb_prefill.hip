@@ -32,9 +32,9 @@
 // it, in slices that the scheduler must not move: a wave's vector instructions run beside
 // its matrix instructions only where they are issued between them.
 //
-// 16384 tokens, 32 heads on 4 KV heads of 256 channels: 4.2 to 4.3 ms, 1030 to 1050 TFLOP/s
-// (the library's bf16 product of 8192 reaches 1243).  Of the 4700 cycles of a block's step
-// the matrix pipe is busy 2050; the rest are vector instructions beyond what stands beside
+// 16384 tokens, 32 heads on 4 KV heads of 256 channels: 4.1 to 4.4 ms, 1000 to 1070 TFLOP/s
+// (the library's bf16 product of 8192 reaches 1243).  Of the 4550 cycles of a block's step
+// (counters) the matrix pipe is busy 2050; the rest are vector instructions beyond what stands beside
 // them, reads of LDS and the barrier, at clocks that fall under matrix load.  A workgroup
 // begins and ends in 5 us, which short prefills feel (512 tokens, 16 heads on 4 of 256: 25 us).
 //

@@ -16,8 +16,8 @@
 // eight bits, from the highest bit in which the keys differ (above it every key would
 // count into one bin), and writes the blocks in ascending order.  Blocks that a token
 // has to have carry the highest key, those behind it the lowest.
-// Both are bound by latency (16385 rows, 4 KV heads of 256 channels, one token: 4.9 us and 5.5;
-// up to 131072 rows, 13 tokens: 9.8 and 9.8; with each digit found by the workgroup together
+// Both are bound by latency (16385 rows, 4 KV heads of 256 channels, one token: 5.0 us and 5.5;
+// up to 131072 rows, 13 tokens: 10.6 and 9.7; with each digit found by the workgroup together
 // instead of by every wave for itself, four barriers more to a digit, the choice took 6.2 and 10.9).
 #include <hip/hip_runtime.h>
 
