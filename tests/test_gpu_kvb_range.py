@@ -172,3 +172,17 @@ def test_large_scores_of_one_block(d, block):
             got = o[t, h].double().cpu().numpy()
             assert (np.abs(got - want) <= far).all(), (t, h, len(best), np.abs(got - want).max())
             assert abs(lse[t, h].item() - (1e6 * x.max() + np.log(len(best)))) <= 2.0 ** -21 * 1e6 * x.max() + 2.0 ** -20
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n_sel", [3, 8, 31, 90])
+def test_sizes_that_differ_by_block_in_lists(d, n_sel):
+    """Each listed block with scales of its own, in lists of one run and of several, with holes, blocks behind the token and
+    repetitions: a block's codes never meet another's scale."""
+    n, T, G = 2500, 4, 8
+    by = 2.0 ** torch.randint(-8, 3, (up(n) // BLOCK, 2), generator=torch.Generator().manual_seed(19)).float().repeat_interleave(BLOCK, 0)[:n]
+    c, ks, vs = made(n, d, (normal(20, n, 1, d).float() * by[:, :1, None]).bfloat16(), (normal(21, n, 1, d).float() * by[:, 1:, None]).bfloat16())
+    q = normal(22, T, G, d).cuda()
+    idx = torch.randint(-1, 42, (T, 1, n_sel), generator=torch.Generator().manual_seed(n_sel), dtype=torch.int32).cuda()
+    o, lse = run_attend(c, [n], [T], q, 0.05, idx)
+    check_attend(c, ks, vs, [n], [T], q, 0.05, o, lse, idx)
