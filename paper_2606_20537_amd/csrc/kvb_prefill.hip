@@ -237,6 +237,9 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
             const int64_t at = row0 + qrow + i * kRowPass, r = at < last ? at : last;
             x[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.q) + token_of(r) * p.q_stride + (int64_t)head_of(r) * D * 2 + 16 * qunit);
         }
+        fetch(kb, begin, ks);
+        fetch(vb, begin, vs);
+        load_scales();
         u16x2 top2 = {0, 0};
         #pragma unroll
         for (int i = 0; i < kPasses; ++i)
@@ -258,9 +261,6 @@ __global__ __launch_bounds__(kThreads<D>, 2) void prefill_kernel(const KvbAttend
         for (int i = 0; i < kPasses; ++i) *reinterpret_cast<u32x4*>(row_bytes(qrow + i * kRowPass)) = x[i];
     }
     if (tid < 3) nan_s[tid] = -1;
-    fetch(kb, begin, ks);
-    fetch(vb, begin, vs);
-    load_scales();
     dev::lds_barrier();
     #pragma unroll
     for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const bf16x8*>(&k_s[0][0] + (kaddr ^ (32 * i)) + group * 64 * D);
