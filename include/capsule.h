@@ -667,6 +667,170 @@ typedef struct kvb_select_args {
 CAP_API uint64_t kvb_select_workspace_bytes(const kvb_select_args* args);
 CAP_API int kvb_select(const kvb_select_args* args, void* stream);
 
+/* --------------------------- norm and rotation of queries and keys (qk) ---- */
+/* What a full-attention layer does to a token's queries and keys before they meet,
+ * for each head's d channels y:
+ *   norm     y = x (mean x^2 + eps)^-1/2 (w_add + w)
+ *   rotation pair i < rot / 2 turns by a_i = sum over axes of pos_axis freqs[axis][i]:
+ *            (y_a, y_b) -> (y_a cos a_i - y_b sin a_i, y_b cos a_i + y_a sin a_i),
+ *            (a, b) = (i, i + rot / 2), or (2 i, 2 i + 1) with QK_PAIRS;
+ *            channels from rot on stay
+ * Angles are taken in 64 bits (within 2^-20 at any position), the rest in fp32, and
+ * the result is rounded once.  Text has one axis; images and video give a patch a time, a
+ * height and a width, each with a row of freqs that is zero for the pairs it does not turn. */
+#define QK_NORM  1u
+#define QK_PAIRS 2u
+
+typedef struct qk_rule {
+    const double* freqs;    /* device [axes, rot / 2], radians per position; NULL where rot is 0 */
+    const void*   wq;       /* device [d] of w_dtype, or NULL: a factor of 1; read with QK_NORM only */
+    const void*   wk;
+    int32_t       rot;      /* rotated channels: a multiple of 16, at most d and 512 */
+    int32_t       axes;     /* 1 to 8 (0 or more where rot is 0) */
+    float         eps;      /* with QK_NORM: finite, at least 1e-20 */
+    float         w_add;    /* 0, or 1 for weights held as their distance from 1; finite */
+    int32_t       w_dtype;  /* CAP_DTYPE_* */
+    uint32_t      flags;    /* QK_* */
+} qk_rule;
+
+/* Frequencies of a rule, host: pair i turns by base^(-2 i / rot) a position on one of the
+ * axes.  sections[a]: pairs of axis a, their sum rot / 2; NULL: one axis has them all
+ * (axes = 1).  The pairs of an axis follow each other, or (interleave != 0) pairs are dealt out in
+ * turn: pair i to axis i mod axes while that axis has pairs left, else to the first that has.
+ * out: HOST [axes, rot / 2], to be copied to the device.  base > 0 and finite, rot even and > 0. */
+CAP_API int qk_fill_freqs(double base, int32_t rot, int32_t axes, const int32_t* sections,
+                          int32_t interleave, double* out);
+
+/* A packed tensor [tokens, heads, d] of a larger one: strides in elements, multiples of 8;
+ * 0: the heads of a token follow each other, and so do tokens.  Heads and tokens do not overlap. */
+typedef struct qk_rows {
+    void*   p;
+    int64_t token_stride;
+    int64_t head_stride;
+} qk_rows;
+
+/* Norm and rotation of q [tokens, heads, d] and k [tokens, kv_heads, d] to q_out and k_out, one
+ * launch.  An output may be its input (same address and strides), and overlaps nothing else.  heads or
+ * kv_heads may be 0 (then q or k is not looked at), d is a multiple of 16 up to 512, tokens *
+ * (heads + kv_heads) < 2^31.
+ * Errors: CAP_E_INVAL (null required pointer, counts or constants outside their range, overlaps),
+ * CAP_E_UNSUPPORTED (d, rot or axes outside the list, strides above 2^30), CAP_E_ALIGN (tensors
+ * and weights 16 bytes, strides 8 elements, freqs 8 bytes, pos 4), CAP_E_SIZE (past the last
+ * address). */
+typedef struct qk_norm_rope_args {
+    const qk_rule* rule;     /* HOST */
+    qk_rows        q;
+    qk_rows        k;
+    qk_rows        q_out;
+    qk_rows        k_out;
+    const int32_t* pos;      /* device [tokens, axes]; NULL where rot is 0 */
+    int64_t        tokens;
+    int32_t        heads;
+    int32_t        kv_heads;
+    int32_t        d;
+    int32_t        dtype;    /* CAP_DTYPE_* of q, k and the outputs */
+} qk_norm_rope_args;
+
+CAP_API int qk_norm_rope(const qk_norm_rope_args* args, void* stream);
+
+/* -------------------------------------------- paged bf16 KV cache (kvp) ---- */
+/* K and V of many sequences in pools of pages, and a table on the device that names the pages of
+ * each sequence in order: row r of sequence s is row r % page of page table[s][r / page].  A positional
+ * K or V buffer of a live set ([rows, kv_heads, d], rows a multiple of page) is a pool of
+ * rows / page pages; sequences may share pages that no one appends to (a fork at a page's
+ * boundary copies nothing).
+ *   An entry outside [0, pages) names no page: rows there are not written and not seen, and
+ * neither are rows from columns * page on.  So a table's unused entries may hold -1, and those of pages
+ * that a window has passed.
+ * Lengths are on the device as well:
+ *   lens [n_seq]      rows held, those of the step included (append first, then attend);
+ *                     below 0 counts as 0
+ *   tok0 [n_seq + 1]  sequence s has the packed tokens [tok0[s], tok0[s + 1]), T of them, at rows
+ *                     [lens[s] - T, lens[s]); ascending, within [0, tokens].  NULL: one token for each
+ *                     sequence (tokens = n_seq)
+ * They are read by the kernels, so a call that a stream capture has recorded goes on with the
+ * sequences when the program advances lens, tok0 and the table in place.  Tokens of no sequence
+ * (behind the last one) stay as they are in every output.  Nothing read from the device is trusted with an
+ * address: a table or lengths that break these rules give wrong results, not accesses out of bounds.
+ *
+ * Supported: d in {64, 128, 256}, heads a multiple of kv_heads, bf16, page a multiple
+ * of 16, n_seq <= KVP_MAX_SEQ, columns * page <= 2^24, 16 * kv_heads * d * 2 < 2^31.
+ * Errors: as for qk_norm_rope. */
+#define KVP_MAX_SEQ 1024
+
+typedef struct kvp_cache {
+    void*          k;             /* device [pages, page, kv_heads, d] bf16 */
+    void*          v;
+    const int32_t* table;         /* device [n_seq, columns] */
+    int64_t        page_stride;   /* elements between pages of k, and of v; 0: contiguous */
+    int64_t        table_stride;  /* entries between sequences; 0: contiguous */
+    int64_t        pages;
+    int32_t        page;          /* rows of a page */
+    int32_t        columns;
+    int32_t        n_seq;
+    int32_t        kv_heads;
+    int32_t        d;
+    int32_t        reserved;      /* 0 */
+} kvp_cache;
+
+/* Append: the tokens' rows of k and v [tokens, kv_heads, d] to their pages, one launch.  With a
+ * rule, k is normed and rotated on the way, and so is q to q_out (both p NULL: there is no q);
+ * positions are pos, or where that is NULL the row's own number on every axis.
+ * No row of a page may be given to two tokens. */
+typedef struct kvp_append_args {
+    const kvp_cache* cache;   /* HOST */
+    const int32_t*   lens;
+    const int32_t*   tok0;    /* or NULL */
+    const qk_rule*   rule;    /* HOST, or NULL */
+    qk_rows          k;
+    qk_rows          v;
+    qk_rows          q;       /* [tokens, heads, d] */
+    qk_rows          q_out;
+    const int32_t*   pos;     /* device [tokens, axes], or NULL */
+    int64_t          tokens;
+    int32_t          heads;   /* 0 where there is no q */
+    int32_t          reserved;
+} kvp_append_args;
+
+CAP_API int kvp_append(const kvp_append_args* args, void* stream);
+
+/* Causal attention of the step's tokens: the token at row t sees rows
+ * [max(0, t - window + 1), t] (window 0: [0, t]) that lie on a page; query head i belongs to
+ * KV head i / (heads / kv_heads).
+ *   o   : [tokens, heads, d] bf16, contiguous = softmax(scale * q K^T) V
+ *   lse : [tokens, heads] fp32 or NULL: log of the sum of exp(scale * q . k)
+ * A token that sees nothing has o = 0 and lse = -inf.  Rows that a token does not see have no part in
+ * its result, infinities and NaN included; a row with such values that it sees makes those channels
+ * infinite or NaN.
+ * Precision: products and sums are fp32, weights enter the second product with 16 bits (two bf16),
+ * o is rounded once.  Weights below 2^-100 of the largest may count as none.  Means of finite
+ * values are finite.  A score beyond fp32 gives NaN.
+ * Made for one token or a few drafts of each sequence: 16 query rows (tokens x heads / kv_heads)
+ * read the cache once, so long runs of tokens are right but read it often.
+ * Two launches; one where columns * page is 512 at most.  Results are reproducible for the same arguments and
+ * device data; a row's last bits depend on the other sequences of the call, over which work is
+ * dealt out evenly. */
+typedef struct kvp_attend_args {
+    const kvp_cache* cache;      /* HOST */
+    const int32_t*   lens;
+    const int32_t*   tok0;       /* or NULL */
+    qk_rows          q;
+    void*            o;
+    float*           lse;
+    void*            workspace;  /* kvp_attend_workspace_bytes(args), 16-byte aligned */
+    uint64_t         workspace_bytes;
+    int64_t          tokens;
+    int32_t          heads;
+    int32_t          window;     /* 0: none */
+    float            scale;      /* finite, and below 2.3e38 in magnitude (CAP_E_INVAL) */
+    int32_t          reserved;   /* 0 */
+} kvp_attend_args;
+
+/* Workspace of a call with these sizes (the cache's, tokens and heads); 0 where the call needs none
+ * or is refused.  It holds nothing between calls; calls that may overlap need their own. */
+CAP_API uint64_t kvp_attend_workspace_bytes(const kvp_attend_args* args);
+CAP_API int kvp_attend(const kvp_attend_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,7 +15,8 @@ from ._native import (  # noqa: F401
     capsule_move, capsule_release, capsule_restore, capsule_snapshot, capsule_tier, gdn_chunked_prefill,
     gdn_chunked_prefill_noalloc, GDN_NOALLOC_SCRATCH_BYTES,
     KVB_BLOCK, KVB_MAX_SEQ, kvb_append, kvb_append_args, kvb_attend, kvb_attend_args, kvb_select, kvb_select_args,
-    kvb_seqs,
+    kvb_seqs, KVP_MAX_SEQ, KvpCache, kvp_append, kvp_append_args, kvp_attend, kvp_attend_args, kvp_attend_workspace_bytes,
+    kvp_cache, kvp_cache_args, QK_NORM, QK_PAIRS, QkRule, qk_freqs, qk_norm_rope, qk_norm_rope_args, qk_rows, qk_rule, qk_rule_args,
     gdn_decode_step, gdn_workspace_bytes, kv_fp8_dequantize, kv_fp8_quantize, linattn_chunked_prefill,
     linattn_decode_step, load,
 )

@@ -98,6 +98,43 @@ class kvb_select_args(ct.Structure):
                 ("first", ct.c_int32), ("last", ct.c_int32), ("in_dtype", ct.c_int32)]
 
 
+QK_NORM = 1
+QK_PAIRS = 2
+KVP_MAX_SEQ = 1024
+
+
+class qk_rows(ct.Structure):
+    _fields_ = [("p", ct.c_void_p), ("token_stride", ct.c_int64), ("head_stride", ct.c_int64)]
+
+
+class qk_rule_args(ct.Structure):
+    _fields_ = [("freqs", ct.c_void_p), ("wq", ct.c_void_p), ("wk", ct.c_void_p), ("rot", ct.c_int32), ("axes", ct.c_int32),
+                ("eps", ct.c_float), ("w_add", ct.c_float), ("w_dtype", ct.c_int32), ("flags", ct.c_uint32)]
+
+
+class qk_norm_rope_args(ct.Structure):
+    _fields_ = [("rule", ct.c_void_p), ("q", qk_rows), ("k", qk_rows), ("q_out", qk_rows), ("k_out", qk_rows), ("pos", ct.c_void_p),
+                ("tokens", ct.c_int64), ("heads", ct.c_int32), ("kv_heads", ct.c_int32), ("d", ct.c_int32), ("dtype", ct.c_int32)]
+
+
+class kvp_cache_args(ct.Structure):
+    _fields_ = [("k", ct.c_void_p), ("v", ct.c_void_p), ("table", ct.c_void_p), ("page_stride", ct.c_int64),
+                ("table_stride", ct.c_int64), ("pages", ct.c_int64), ("page", ct.c_int32), ("columns", ct.c_int32),
+                ("n_seq", ct.c_int32), ("kv_heads", ct.c_int32), ("d", ct.c_int32), ("reserved", ct.c_int32)]
+
+
+class kvp_append_args(ct.Structure):
+    _fields_ = [("cache", ct.c_void_p), ("lens", ct.c_void_p), ("tok0", ct.c_void_p), ("rule", ct.c_void_p), ("k", qk_rows),
+                ("v", qk_rows), ("q", qk_rows), ("q_out", qk_rows), ("pos", ct.c_void_p), ("tokens", ct.c_int64),
+                ("heads", ct.c_int32), ("reserved", ct.c_int32)]
+
+
+class kvp_attend_args(ct.Structure):
+    _fields_ = [("cache", ct.c_void_p), ("lens", ct.c_void_p), ("tok0", ct.c_void_p), ("q", qk_rows), ("o", ct.c_void_p),
+                ("lse", ct.c_void_p), ("workspace", ct.c_void_p), ("workspace_bytes", ct.c_uint64), ("tokens", ct.c_int64),
+                ("heads", ct.c_int32), ("window", ct.c_int32), ("scale", ct.c_float), ("reserved", ct.c_int32)]
+
+
 # (name, restype, argtypes) of every exported entry point
 _vp, _u64, _u32, _i32 = ct.c_void_p, ct.c_uint64, ct.c_uint32, ct.c_int32
 SIGNATURES = [
@@ -138,6 +175,11 @@ SIGNATURES = [
     ("kvb_attend", ct.c_int, [ct.POINTER(kvb_attend_args), _vp]),
     ("kvb_select_workspace_bytes", _u64, [ct.POINTER(kvb_select_args)]),
     ("kvb_select", ct.c_int, [ct.POINTER(kvb_select_args), _vp]),
+    ("qk_fill_freqs", ct.c_int, [ct.c_double, _i32, _i32, ct.POINTER(_i32), _i32, ct.POINTER(ct.c_double)]),
+    ("qk_norm_rope", ct.c_int, [ct.POINTER(qk_norm_rope_args), _vp]),
+    ("kvp_append", ct.c_int, [ct.POINTER(kvp_append_args), _vp]),
+    ("kvp_attend_workspace_bytes", _u64, [ct.POINTER(kvp_attend_args)]),
+    ("kvp_attend", ct.c_int, [ct.POINTER(kvp_attend_args), _vp]),
 ]
 
 _lib = None
@@ -667,3 +709,212 @@ def kvb_select(seqs, q, idx, *, kv_heads, first=1, last=2, workspace=None, strea
     lib, handle = load(), _stream(stream)
     workspace = _kvb_workspace("kvb_select", a, workspace, lib.kvb_select_workspace_bytes, q, handle)
     return _check("kvb_select", lib.kvb_select(ct.byref(a), handle))
+
+
+# ------------------------------------- norm and rotation of q and k ----
+def qk_freqs(base, rot, sections=None, interleave=False):
+    """Frequencies of a rule (qk_fill_freqs): a float64 tensor [axes, rot / 2] on the host, for .cuda().
+
+    sections: how many pairs each axis turns; None: one axis turns them all."""
+    import torch
+    axes = 1 if sections is None else len(sections)
+    out = torch.empty((axes, rot // 2), dtype=torch.float64)
+    sec = None if sections is None else (_i32 * max(1, axes))(*sections)
+    _check("qk_fill_freqs", load().qk_fill_freqs(base, rot, axes, sec, int(interleave), ct.cast(out.data_ptr(), ct.POINTER(ct.c_double))))
+    return out
+
+
+class QkRule:
+    """A rule's C struct; keeps its tensors alive."""
+
+    def __init__(self, args, tensors, d, device):
+        self.args = args
+        self.address = ct.addressof(args)
+        self.tensors = tensors
+        self.d = d  # of the weights; None: there are none
+        self.device = device
+        self.axes = args.axes
+        self.rot = args.rot
+
+
+def qk_rule(freqs=None, *, wq=None, wk=None, eps=None, w_add=0.0, pairs=False):
+    """How q and k are normed and rotated, made once for a layer.
+
+    freqs: float64 [axes, rot / 2] on the GPU (qk_freqs), or None for no rotation.  eps: None for no norm.
+    wq, wk: weights [d] of the norm, bfloat16 or float32, or None."""
+    torch, bf16, f32, _ = _kvb_torch()
+    tensors = [x for x in (freqs, wq, wk) if x is not None]
+    if eps is None and (wq is not None or wk is not None):
+        raise ValueError("qk_rule: weights without a norm (eps)")
+    device = None
+    for x in tensors:
+        if device is None:
+            device = x.get_device()
+        if x.get_device() < 0 or x.get_device() != device or not x.is_contiguous():
+            raise ValueError("qk_rule: freqs and weights are contiguous and on one GPU")
+    if freqs is not None and (freqs.dtype != torch.float64 or freqs.ndim != 2):
+        raise ValueError("qk_rule: freqs is a float64 tensor [axes, rot / 2]")
+    weights = [x for x in (wq, wk) if x is not None]
+    for x in weights:
+        if x.ndim != 1 or x.dtype not in (bf16, f32) or x.dtype != weights[0].dtype or x.shape != weights[0].shape:
+            raise ValueError("qk_rule: wq and wk are bfloat16 or float32 tensors [d] of one kind")
+    axes, rot = (0, 0) if freqs is None else (freqs.shape[0], 2 * freqs.shape[1])
+    a = qk_rule_args(_addr(freqs) if rot else 0, _addr(wq), _addr(wk), rot, axes if rot else 0, 0.0 if eps is None else eps, w_add,
+                     CAP_DTYPE_F32 if weights and weights[0].dtype == f32 else CAP_DTYPE_BF16,
+                     (QK_NORM if eps is not None else 0) | (QK_PAIRS if pairs else 0))
+    return QkRule(a, tensors, weights[0].shape[0] if weights else None, device)
+
+
+def _qk_rows(fn, name, x, shape, dtype):
+    """qk_rows of a tensor [tokens, heads, d]."""
+    if x.dtype != dtype or x.shape != shape:
+        raise ValueError("%s: %s is a %s tensor of shape %s, not %s %s" % (fn, name, dtype, list(shape), x.dtype, list(x.shape)))
+    if x.is_contiguous():
+        return qk_rows(x.data_ptr(), 0, 0)
+    tokens, heads, d = shape
+    st, sh, sd = x.stride()
+    head = sh if heads > 1 else d
+    # (strides of zero mean contiguous to the library, which would read past a broadcast row)
+    if sd != 1 or head < d or (tokens > 1 and st < (heads - 1) * head + d):
+        raise ValueError("%s: the channels of a head of %s follow each other, and heads and tokens do not overlap" % (fn, name))
+    return qk_rows(x.data_ptr(), st if tokens > 1 else 0, head)
+
+
+def _qk_shape(fn, name, x):
+    if x.ndim != 3:
+        raise ValueError("%s: %s is a tensor [tokens, heads, d]" % (fn, name))
+    return x.shape
+
+
+def _qk_ints(fn, name, x, shape):
+    """Address of a contiguous int32 tensor of the GPU (None: 0)."""
+    if x is None:
+        return 0
+    if x.dtype != _kvb_torch()[3] or x.shape != shape or not x.is_contiguous():
+        raise ValueError("%s: %s is a contiguous int32 tensor of shape %s" % (fn, name, list(shape)))
+    return x.data_ptr()
+
+
+def _qk_pos(fn, rule, pos, tokens):
+    if pos is not None and pos.ndim == 1 and rule.axes == 1:
+        return _qk_ints(fn, "pos", pos, (tokens,))
+    return _qk_ints(fn, "pos", pos, (tokens, rule.axes))
+
+
+def _qk_rule(fn, rule, d, device):
+    if rule.d is not None and rule.d != d:
+        raise ValueError("%s: the rule's weights are of %d channels, the heads of %d" % (fn, rule.d, d))
+    if rule.device is not None and rule.device != device:
+        raise ValueError("%s: the rule is on another GPU" % fn)
+
+
+def qk_norm_rope(rule, q, k, q_out=None, k_out=None, *, pos=None, stream=None):
+    """Norm and rotation of q [tokens, heads, d] and k [tokens, kv_heads, d] (either may be None), to q_out and
+    k_out (None: in place).  pos: int32 [tokens, axes]."""
+    fn = "qk_norm_rope"
+    _, bf16, f32, _ = _kvb_torch()
+    like = q if q is not None else k
+    if like is None:
+        raise ValueError("qk_norm_rope: neither q nor k")
+    tokens, _, d = _qk_shape(fn, "q" if q is not None else "k", like)
+    dtype = like.dtype
+    if dtype != bf16 and dtype != f32:
+        raise ValueError("qk_norm_rope: bfloat16 or float32 tensors, not %s" % dtype)
+    a = qk_norm_rope_args(rule=rule.address, tokens=tokens, d=d, dtype=CAP_DTYPE_F32 if dtype == f32 else CAP_DTYPE_BF16)
+    if q is not None:
+        shape, q_out = q.shape, q if q_out is None else q_out
+        a.heads, a.q, a.q_out = shape[1], _qk_rows(fn, "q", q, shape, dtype), _qk_rows(fn, "q_out", q_out, shape, dtype)
+    elif q_out is not None:
+        raise ValueError("qk_norm_rope: q_out without q")
+    if k is not None:
+        shape, k_out = (tokens, _qk_shape(fn, "k", k)[1], d), k if k_out is None else k_out
+        a.kv_heads, a.k, a.k_out = shape[1], _qk_rows(fn, "k", k, shape, dtype), _qk_rows(fn, "k_out", k_out, shape, dtype)
+    elif k_out is not None:
+        raise ValueError("qk_norm_rope: k_out without k")
+    a.pos = _qk_pos(fn, rule, pos, tokens)
+    _kvb_device(fn, like, q_out, k, k_out, pos)
+    _qk_rule(fn, rule, d, like.get_device())
+    return _check(fn, load().qk_norm_rope(ct.byref(a), _stream(stream)))
+
+
+# ------------------------------------------------ paged bf16 KV cache ----
+class KvpCache:
+    """A paged cache's C struct; keeps its tensors alive."""
+
+    def __init__(self, args, tensors, like):
+        self.args = args
+        self.address = ct.addressof(args)
+        self.tensors = tensors
+        self.like = like  # a tensor on the cache's GPU
+        self.n_seq, self.kv_heads, self.d = args.n_seq, args.kv_heads, args.d
+
+
+def kvp_cache(k_pages, v_pages, table):
+    """A paged cache: pools k_pages and v_pages [pages, page, kv_heads, d] bfloat16 (pages may be apart, e.g. the
+    halves of one tensor [pages, 2, page, kv_heads, d]) and table [n_seq, columns] int32, all on one GPU.  The
+    program goes on writing the table in place; the handle is made once."""
+    _, bf16, _, i32 = _kvb_torch()
+    for x in (k_pages, v_pages):
+        if x.ndim != 4 or x.dtype != bf16 or x.shape != k_pages.shape or x.stride()[1:] != (x.shape[2] * x.shape[3], x.shape[3], 1) \
+                or x.stride(0) != k_pages.stride(0) or (x.shape[0] > 1 and x.stride(0) < x.shape[1] * x.shape[2] * x.shape[3]):
+            raise ValueError("kvp_cache: k_pages and v_pages are bfloat16 tensors [pages, page, kv_heads, d] whose pages are contiguous")
+    if table.ndim != 2 or table.dtype != i32 or (table.shape[1] > 1 and table.stride(1) != 1) or (table.shape[0] > 1 and table.stride(0) < table.shape[1]):
+        raise ValueError("kvp_cache: table is an int32 tensor [n_seq, columns] whose rows are contiguous")
+    if not k_pages.get_device() == v_pages.get_device() == table.get_device() >= 0:
+        raise ValueError("kvp_cache: the pools and the table are on one GPU")
+    pages, page, kv_heads, d = k_pages.shape
+    n_seq, columns = table.shape
+    a = kvp_cache_args(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), k_pages.stride(0) if pages > 1 else 0,
+                       table.stride(0) if n_seq > 1 else 0, pages, page, columns, n_seq, kv_heads, d, 0)
+    return KvpCache(a, (k_pages, v_pages, table), k_pages)
+
+
+def kvp_append(cache, lens, k, v, *, tok0=None, rule=None, q=None, q_out=None, pos=None, stream=None):
+    """Append rows k, v [tokens, kv_heads, d] of the step's tokens to their pages; with a rule, k is normed and rotated on
+    the way, and q [tokens, heads, d] to q_out (None: in place).  lens [n_seq], tok0 [n_seq + 1] and pos [tokens, axes]
+    are int32 tensors on the GPU."""
+    fn = "kvp_append"
+    bf16 = _kvb_torch()[1]
+    shape = (_qk_shape(fn, "k", k)[0], cache.kv_heads, cache.d)
+    tokens = shape[0]
+    a = kvp_append_args(cache=cache.address, lens=_qk_ints(fn, "lens", lens, (cache.n_seq,)),
+                        tok0=_qk_ints(fn, "tok0", tok0, (cache.n_seq + 1,)), k=_qk_rows(fn, "k", k, shape, bf16),
+                        v=_qk_rows(fn, "v", v, shape, bf16), tokens=tokens)
+    if rule is None:
+        if q is not None or q_out is not None or pos is not None:
+            raise ValueError("kvp_append: q, q_out and pos go with a rule")
+    else:
+        _qk_rule(fn, rule, cache.d, cache.like.get_device())
+        a.rule, a.pos = rule.address, _qk_pos(fn, rule, pos, tokens)
+        if q is not None:
+            of_q, q_out = (tokens, _qk_shape(fn, "q", q)[1], cache.d), q if q_out is None else q_out
+            a.heads, a.q, a.q_out = of_q[1], _qk_rows(fn, "q", q, of_q, bf16), _qk_rows(fn, "q_out", q_out, of_q, bf16)
+        elif q_out is not None:
+            raise ValueError("kvp_append: q_out without q")
+    _kvb_device(fn, cache.like, lens, k, v, tok0, q, q_out, pos)
+    return _check(fn, load().kvp_append(ct.byref(a), _stream(stream)))
+
+
+def kvp_attend_workspace_bytes(cache, tokens, heads):
+    """Bytes of workspace kvp_attend needs for this many packed tokens and query heads."""
+    a = kvp_attend_args(cache=cache.address, tokens=tokens, heads=heads)
+    return int(load().kvp_attend_workspace_bytes(ct.byref(a)))
+
+
+def kvp_attend(cache, lens, q, o, *, scale, tok0=None, window=0, lse=None, workspace=None, stream=None):
+    """Causal attention of the step's tokens q [tokens, heads, d] over the pages, to o (bfloat16, contiguous) and lse
+    [tokens, heads] (float32).  lens [n_seq] and tok0 [n_seq + 1] are int32 tensors on the GPU.  With no workspace
+    given, one is allocated as a torch tensor of the call's stream for the duration of the call."""
+    fn = "kvp_attend"
+    _, bf16, f32, _ = _kvb_torch()
+    tokens, heads, _ = _qk_shape(fn, "q", q)
+    shape = (tokens, heads, cache.d)
+    _kvb_out(fn, "o", o, shape, bf16)
+    _kvb_out(fn, "lse", lse, (tokens, heads), f32)
+    _kvb_device(fn, cache.like, lens, q, o, tok0, lse, workspace)
+    a = kvp_attend_args(cache=cache.address, lens=_qk_ints(fn, "lens", lens, (cache.n_seq,)),
+                        tok0=_qk_ints(fn, "tok0", tok0, (cache.n_seq + 1,)), q=_qk_rows(fn, "q", q, shape, bf16), o=o.data_ptr(),
+                        lse=lse.data_ptr() if lse is not None else 0, tokens=tokens, heads=heads, window=window, scale=scale)
+    lib, handle = load(), _stream(stream)
+    workspace = _kvb_workspace(fn, a, workspace, lib.kvp_attend_workspace_bytes, q, handle)
+    return _check(fn, lib.kvp_attend(ct.byref(a), handle))

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB_PATH = os.path.join(PKG, "_build", "libcapsule.so")
 SOURCES = ["capsule_host.cpp", "capsule_copy.hip", "linattn_scan.hip", "linattn_seg.hip", "linattn_step.hip", "gdn_scan.hip", "gdn_step.hip", "gdn_noalloc.hip", "kv_fp8.hip", "append.hip",
-           "kvb_host.cpp", "kvb_append.hip", "kvb_attend.hip", "kvb_prefill.hip", "kvb_select.hip"]
+           "kvb_host.cpp", "kvb_append.hip", "kvb_attend.hip", "kvb_prefill.hip", "kvb_select.hip",
+           "kvp_host.cpp", "qk_rotate.hip", "kvp_attend.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # gfx950 only.  Packed-fp32 instructions are disabled for all device code.

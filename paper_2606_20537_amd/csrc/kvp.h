@@ -1,0 +1,75 @@
+// Internal interface of the paged bf16 KV cache and of the norm and rotation of
+// queries and keys: the host checks (kvp_host.cpp) and the kernels
+// (qk_rotate.hip, kvp_attend.hip).  Not part of the public ABI.
+#pragma once
+
+#include "internal.h"
+
+namespace cap {
+
+// A grid of n workgroups of 256 (a launch counts its threads along x in 32 bits).  Those
+// from n on have nothing to do.
+inline dim3 wide_grid(uint64_t n) { return dim3(fp8_grid_x((uint32_t)n), fp8_grid_y((uint32_t)n)); }
+
+// A packed tensor [tokens, heads, d]; strides in bytes.
+struct QkRows {
+    uint64_t p;
+    int64_t  token, head;
+};
+
+// The pools and the table of a cache, and the step's lengths.
+struct KvpPages {
+    uint64_t       k, v;
+    const int32_t* table;
+    const int32_t* lens;
+    const int32_t* tok0;          // null: sequence s has token s
+    int64_t        table_stride;  // entries
+    int64_t        page_stride;   // bytes
+    int32_t        pages, page, columns, n_seq, kv_heads;
+    int32_t        capacity;      // columns * page
+};
+
+// ---- norm and rotation, with or without an append ----
+// The rows of a token: `heads` of q, kv_heads of k and, with an append, as many of v.
+struct QkParams {
+    QkRows         q, k, v, q_out, k_out;  // (an append: k_out is the pages)
+    const double*  freqs;
+    const void*    wq;
+    const void*    wk;
+    const int32_t* pos;                    // null: the row number on every axis (append)
+    int64_t        tokens;
+    int32_t        heads, kv_heads, d, rot, axes;
+    int32_t        tokens_wg;              // tokens of a workgroup, kQkTokens at most
+    float          eps, w_add;
+    bool           norm, pairs, w_f32;
+    KvpPages       pages;
+};
+constexpr int kQkTokens = 8;
+hipError_t launch_qk(const QkParams& p, bool f32, bool append, hipStream_t stream);
+
+// ---- attend ----
+// A segment is a KV head and 16 query rows of a sequence (row r: token r / G, query head
+// h G + r % G).  Its rows of the cache are cut into units of 32.  Units of all segments in a row, each
+// segment with kKvpBegin more before it for what a segment costs, are dealt out
+// to the workgroups in equal runs; a workgroup has at most two segments that it shares with others,
+// whose parts lie in its two slots of the workspace.
+constexpr int kKvpUnit = 32;
+constexpr int kKvpBegin = 4;
+struct KvpAttendParams {
+    QkRows   q;
+    void*    o;
+    float*   lse;      // may be null
+    float*   part_o;   // [2 wgs][16][d], not divided by l
+    float*   part_ml;  // [2 wgs][16][2]: highest score (log2 units), sum
+    uint64_t* meta;    // [tokens, heads]: first workgroup, parts, row of the segment
+    int64_t  tokens;
+    int32_t  heads, d, window;
+    uint32_t wgs;
+    uint32_t least;    // units of a run at least
+    int32_t  whole;    // segments are not cut, and there is no second launch
+    float    scale_log2;
+    KvpPages pages;
+};
+hipError_t launch_kvp_attend(const KvpAttendParams& p, hipStream_t stream);
+
+}  // namespace cap

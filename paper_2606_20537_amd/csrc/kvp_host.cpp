@@ -1,0 +1,322 @@
+// Host side of the norm and rotation of queries and keys and of the paged bf16 KV
+// cache: argument checks and launches of qk_norm_rope, kvp_append and kvp_attend.
+#include <cmath>
+#include <cstdint>
+
+#include "kvp.h"
+
+namespace {
+
+constexpr int64_t kMostStride = (int64_t)1 << 30;
+
+uint64_t addr(const void* p) { return (uint64_t)(uintptr_t)p; }
+
+// `count` pieces of `width` bytes, `step` bytes apart, from `a` on: the tokens of a packed tensor, the pages of a
+// pool, or (count 1) a plain array.
+struct Span {
+    uint64_t a = 0, width = 0, step = 0, count = 0;
+    bool empty() const { return a == 0 || width == 0 || count == 0; }
+    uint64_t bytes() const { return empty() ? 0 : (count - 1) * step + width; }
+    bool wraps() const { return a + bytes() < a; }
+    bool same(const Span& x) const { return a == x.a && width == x.width && (step == x.step || count == 1) && count == x.count; }
+};
+Span plain(const void* p, uint64_t bytes) { return {addr(p), bytes, 0, 1}; }
+
+bool meet(const Span& x, const Span& y) {
+    if (x.empty() || y.empty() || x.a >= y.a + y.bytes() || y.a >= x.a + x.bytes()) return false;
+    if (x.count == 1 || y.count == 1 || x.step != y.step) return true;
+    // pieces of one step: slices of one larger tensor, beside each other in each of its tokens
+    const uint64_t d = y.a >= x.a ? (y.a - x.a) % x.step : (x.step - (x.a - y.a) % x.step) % x.step;
+    return d < x.width || d + y.width > x.step;
+}
+
+// A tensor [tokens, heads, d] of `size`-byte elements: strides in bytes, and what it covers.
+int check_rows(const qk_rows& r, int64_t tokens, int32_t heads, int32_t d, int size, cap::QkRows* out, Span* span) {
+    int64_t head = r.head_stride, token = r.token_stride;
+    if (head == 0) head = d;
+    if (head < d) return CAP_E_INVAL;
+    if (head > kMostStride) return CAP_E_UNSUPPORTED;
+    const int64_t width = (int64_t)(heads - 1) * head + d;
+    if (token == 0) token = (int64_t)heads * head;
+    if (token < width) return CAP_E_INVAL;
+    if (token > kMostStride) return CAP_E_UNSUPPORTED;
+    if ((head | token) % 8 != 0) return CAP_E_ALIGN;
+    *out = {addr(r.p), token * size, head * size};
+    *span = {addr(r.p), (uint64_t)width * size, (uint64_t)token * size, (uint64_t)tokens};
+    return CAP_OK;
+}
+
+int check_rule(const qk_rule* r, int32_t d) {
+    if (r->flags & ~(QK_NORM | QK_PAIRS)) return CAP_E_INVAL;
+    if (r->rot < 0 || r->axes < 0 || (r->rot > 0 && (r->axes < 1 || !r->freqs))) return CAP_E_INVAL;
+    if (r->rot % 16 != 0 || r->rot > d || r->axes > 8) return CAP_E_UNSUPPORTED;
+    if (r->w_dtype != CAP_DTYPE_BF16 && r->w_dtype != CAP_DTYPE_F32) return CAP_E_INVAL;
+    if ((r->flags & QK_NORM) && !(std::isfinite(r->eps) && r->eps >= 1e-20f && std::isfinite(r->w_add))) return CAP_E_INVAL;
+    if ((addr(r->freqs) & 7) || ((addr(r->wq) | addr(r->wk)) & 15)) return CAP_E_ALIGN;
+    return CAP_OK;
+}
+
+void enter_rule(const qk_rule* r, cap::QkParams* p) {
+    p->norm = r->flags & QK_NORM;
+    p->pairs = r->flags & QK_PAIRS;
+    p->w_f32 = r->w_dtype == CAP_DTYPE_F32;
+    p->freqs = r->freqs;
+    p->wq = r->wq;
+    p->wk = r->wk;
+    p->rot = r->rot;
+    p->axes = r->rot ? r->axes : 0;
+    p->eps = r->eps;
+    p->w_add = r->w_add;
+}
+
+// What a rule's call reads besides the tokens.
+constexpr int kRuleSpans = 4;
+void rule_spans(const qk_rule* r, const int32_t* pos, int64_t tokens, int32_t d, Span* out) {
+    const uint64_t w = (r->flags & QK_NORM) ? (uint64_t)d * (r->w_dtype == CAP_DTYPE_F32 ? 4 : 2) : 0;
+    out[0] = plain(r->freqs, (uint64_t)r->axes * (uint64_t)r->rot * 4);
+    out[1] = plain(r->wq, w);
+    out[2] = plain(r->wk, w);
+    out[3] = plain(pos, r->rot ? (uint64_t)tokens * (uint64_t)r->axes * 4 : 0);
+}
+
+// Tokens of a workgroup: heads of a token are 256 lanes or less where there are few, and one workgroup's
+// sines serve all of them; no more than leaves two workgroups for each CU.
+int32_t tokens_of_wg(int64_t tokens, int64_t rows, int32_t d) {
+    int64_t n = 1;
+    while (n < cap::kQkTokens && (n * 2) * 512 <= tokens && n * rows * (d / 16) < 2048) n *= 2;
+    return (int32_t)n;
+}
+
+int check_cache(const kvp_cache* c, cap::KvpPages* g, Span (&span)[3]) {
+    if (!c || c->reserved != 0) return CAP_E_INVAL;
+    if (c->pages < 0 || c->page < 1 || c->columns < 1 || c->n_seq < 0 || c->kv_heads < 1 || c->d < 1) return CAP_E_INVAL;
+    if (c->d != 64 && c->d != 128 && c->d != 256) return CAP_E_UNSUPPORTED;
+    if (c->page % 16 != 0 || c->n_seq > KVP_MAX_SEQ || c->pages > 0x7fffffff) return CAP_E_UNSUPPORTED;
+    const int64_t row = (int64_t)c->kv_heads * c->d, capacity = (int64_t)c->columns * c->page;
+    if (row > 0x7fffffff / 32 || capacity > (int64_t)1 << 24) return CAP_E_UNSUPPORTED;
+    const int64_t width = row * c->page, stride = c->page_stride ? c->page_stride : width;
+    const int64_t columns = c->table_stride ? c->table_stride : c->columns;
+    if (stride < width || columns < c->columns) return CAP_E_INVAL;
+    if (stride > (int64_t)1 << 40 || columns > kMostStride) return CAP_E_UNSUPPORTED;
+    if (c->n_seq > 0 && !c->table) return CAP_E_INVAL;
+    if (c->pages > 0 && (!c->k || !c->v)) return CAP_E_INVAL;
+    if (stride % 8 != 0 || ((addr(c->k) | addr(c->v)) & 15) || (addr(c->table) & 3)) return CAP_E_ALIGN;
+    if (c->pages > 0 && (uint64_t)stride * 2 > UINT64_MAX / (uint64_t)c->pages) return CAP_E_SIZE;
+    *g = {addr(c->k), addr(c->v), c->table, nullptr, nullptr, columns, stride * 2, (int32_t)c->pages, c->page, c->columns, c->n_seq,
+          c->kv_heads, (int32_t)capacity};
+    span[0] = {addr(c->k), (uint64_t)width * 2, (uint64_t)stride * 2, (uint64_t)c->pages};
+    span[1] = {addr(c->v), (uint64_t)width * 2, (uint64_t)stride * 2, (uint64_t)c->pages};
+    span[2] = {addr(c->table), (uint64_t)c->columns * 4, (uint64_t)columns * 4, (uint64_t)c->n_seq};
+    for (const Span& x : span)
+        if (x.wraps()) return CAP_E_SIZE;
+    return CAP_OK;
+}
+
+int check_step(const int32_t* lens, const int32_t* tok0, int64_t tokens, int32_t heads, cap::KvpPages* g, Span (&span)[2]) {
+    if (tokens < 0 || heads < 0) return CAP_E_INVAL;
+    if (tokens > 0x7fffffff / (heads > g->kv_heads ? heads : g->kv_heads) / 3) return CAP_E_UNSUPPORTED;
+    if (!tok0 && tokens != g->n_seq) return CAP_E_INVAL;
+    if (g->n_seq > 0 && tokens > 0 && !lens) return CAP_E_INVAL;
+    if ((addr(lens) | addr(tok0)) & 3) return CAP_E_ALIGN;
+    g->lens = lens;
+    g->tok0 = tok0;
+    span[0] = plain(lens, (uint64_t)g->n_seq * 4);
+    span[1] = plain(tok0, (uint64_t)(g->n_seq + 1) * 4);
+    return span[0].wraps() || span[1].wraps() ? CAP_E_SIZE : CAP_OK;
+}
+
+// Each output apart from the others and from what is read, except from the input that it may be (own[i], or null).
+int check_apart(const Span* out, const Span* const* own, int n_out, const Span* in, int n_in) {
+    for (int i = 0; i < n_out; ++i)
+        if (out[i].wraps()) return CAP_E_SIZE;
+    for (int i = 0; i < n_in; ++i)
+        if (in[i].wraps()) return CAP_E_SIZE;
+    for (int i = 0; i < n_out; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j])) return CAP_E_INVAL;
+        for (int j = 0; j < n_in; ++j)
+            if (&in[j] == own[i] && out[i].same(in[j])) continue;
+            else if (meet(out[i], in[j])) return CAP_E_INVAL;
+    }
+    return CAP_OK;
+}
+
+// ---- attend: the launch ----
+// A run of units in whole mode is never cut; short capacities gain nothing from a second launch.
+constexpr int64_t kWholeRows = 512;
+constexpr int64_t kWgs = 512;   // two to a CU
+constexpr int64_t kLeast = 12;  // units of a run at least, its beginning among them
+
+int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)[3], Span (&step)[2]) {
+    int rc = check_cache(a->cache, &p->pages, cache);
+    if (rc != CAP_OK) return rc;
+    if ((rc = check_step(a->lens, a->tok0, a->tokens, a->heads, &p->pages, step)) != CAP_OK) return rc;
+    const kvp_cache& c = *a->cache;
+    if (a->heads < 1 || a->heads % c.kv_heads != 0 || a->window < 0) return CAP_E_INVAL;
+    const int64_t capacity = (int64_t)c.columns * c.page, rows = a->tokens * (a->heads / c.kv_heads);
+    // segments at most, and units of all of them, which the kernel counts in 32 bits
+    const int64_t segments = (rows / 16 + c.n_seq) * c.kv_heads, units = (capacity + cap::kKvpUnit - 1) / cap::kKvpUnit + cap::kKvpBegin;
+    if (segments > 0x7fffffff / units) return CAP_E_UNSUPPORTED;
+    p->tokens = a->tokens;
+    p->heads = a->heads;
+    p->d = c.d;
+    p->window = a->window;
+    p->whole = capacity <= kWholeRows;
+    p->least = p->whole ? 1 : (uint32_t)kLeast;
+    const int64_t most = p->whole ? segments : (segments * units + kLeast - 1) / kLeast;
+    p->wgs = (uint32_t)(most < kWgs ? most : kWgs);
+    return CAP_OK;
+}
+
+uint64_t attend_parts(const cap::KvpAttendParams& p) { return p.whole ? 0 : (uint64_t)p.wgs * 2 * 16; }
+uint64_t attend_workspace(const cap::KvpAttendParams& p) {
+    return p.whole || p.tokens == 0 ? 0 : attend_parts(p) * ((uint64_t)p.d + 2) * 4 + (uint64_t)p.tokens * (uint64_t)p.heads * 8;
+}
+
+int launch_status(hipError_t e) { return e == hipSuccess ? CAP_OK : CAP_E_HIP; }
+
+}  // namespace
+
+extern "C" {
+
+int qk_fill_freqs(double base, int32_t rot, int32_t axes, const int32_t* sections, int32_t interleave, double* out) {
+    if (!(base > 0.0) || !std::isfinite(base) || rot < 2 || rot % 2 != 0 || axes < 1 || !out || (!sections && axes != 1)) return CAP_E_INVAL;
+    if (axes > 8) return CAP_E_UNSUPPORTED;
+    const int32_t pairs = rot / 2;
+    int32_t left[8];
+    int64_t sum = 0;
+    for (int32_t a = 0; a < axes; ++a) {
+        left[a] = sections ? sections[a] : pairs;
+        if (left[a] < 0) return CAP_E_INVAL;
+        sum += left[a];
+    }
+    if (sum != pairs) return CAP_E_INVAL;
+    for (int32_t i = 0; i < pairs; ++i) {
+        int32_t axis = interleave ? i % axes : 0;
+        if (left[axis] == 0)
+            for (axis = 0; left[axis] == 0;) ++axis;
+        --left[axis];
+        for (int32_t a = 0; a < axes; ++a) out[(int64_t)a * pairs + i] = a == axis ? std::pow(base, -2.0 * i / rot) : 0.0;
+    }
+    return CAP_OK;
+}
+
+int qk_norm_rope(const qk_norm_rope_args* a, void* stream) {
+    if (!a || !a->rule || a->tokens < 0 || a->heads < 0 || a->kv_heads < 0 || a->d < 1) return CAP_E_INVAL;
+    if (a->dtype != CAP_DTYPE_BF16 && a->dtype != CAP_DTYPE_F32) return CAP_E_INVAL;
+    if (a->d % 16 != 0 || a->d > 512) return CAP_E_UNSUPPORTED;
+    const int64_t rows = (int64_t)a->heads + a->kv_heads;
+    int rc = check_rule(a->rule, a->d);
+    if (rc != CAP_OK) return rc;
+    if (rows > 0 && a->tokens > 0x7fffffff / rows) return CAP_E_UNSUPPORTED;
+    if (a->tokens == 0 || rows == 0) return CAP_OK;
+    const int size = a->dtype == CAP_DTYPE_F32 ? 4 : 2;
+    cap::QkParams p{};
+    Span out[2], in[2 + kRuleSpans];
+    if (a->heads > 0) {
+        if (!a->q.p || !a->q_out.p) return CAP_E_INVAL;
+        if ((rc = check_rows(a->q, a->tokens, a->heads, a->d, size, &p.q, &in[0])) != CAP_OK) return rc;
+        if ((rc = check_rows(a->q_out, a->tokens, a->heads, a->d, size, &p.q_out, &out[0])) != CAP_OK) return rc;
+    }
+    if (a->kv_heads > 0) {
+        if (!a->k.p || !a->k_out.p) return CAP_E_INVAL;
+        if ((rc = check_rows(a->k, a->tokens, a->kv_heads, a->d, size, &p.k, &in[1])) != CAP_OK) return rc;
+        if ((rc = check_rows(a->k_out, a->tokens, a->kv_heads, a->d, size, &p.k_out, &out[1])) != CAP_OK) return rc;
+    }
+    if (a->rule->rot > 0 && !a->pos) return CAP_E_INVAL;
+    if (((p.q.p | p.k.p | p.q_out.p | p.k_out.p) & 15) || (addr(a->pos) & 3)) return CAP_E_ALIGN;
+    rule_spans(a->rule, a->pos, a->tokens, a->d, in + 2);
+    const Span* const own[2] = {&in[0], &in[1]};
+    if (a->heads > 0 && p.q_out.p == p.q.p && p.q_out.head != p.q.head) return CAP_E_INVAL;
+    if (a->kv_heads > 0 && p.k_out.p == p.k.p && p.k_out.head != p.k.head) return CAP_E_INVAL;
+    if ((rc = check_apart(out, own, 2, in, 2 + kRuleSpans)) != CAP_OK) return rc;
+    enter_rule(a->rule, &p);
+    p.pos = a->pos;
+    p.tokens = a->tokens;
+    p.heads = a->heads;
+    p.kv_heads = a->kv_heads;
+    p.d = a->d;
+    p.tokens_wg = tokens_of_wg(a->tokens, rows, a->d);
+    return launch_status(cap::launch_qk(p, a->dtype == CAP_DTYPE_F32, false, static_cast<hipStream_t>(stream)));
+}
+
+int kvp_append(const kvp_append_args* a, void* stream) {
+    if (!a || a->reserved != 0) return CAP_E_INVAL;
+    cap::QkParams p{};
+    Span cache[3], step[2];
+    int rc = check_cache(a->cache, &p.pages, cache);
+    if (rc != CAP_OK) return rc;
+    if ((rc = check_step(a->lens, a->tok0, a->tokens, a->heads, &p.pages, step)) != CAP_OK) return rc;
+    const kvp_cache& c = *a->cache;
+    if (a->heads > 0 && !a->rule) return CAP_E_INVAL;
+    if (a->rule && (rc = check_rule(a->rule, c.d)) != CAP_OK) return rc;
+    if (a->tokens == 0 || c.n_seq == 0) return CAP_OK;
+    if (!a->k.p || !a->v.p) return CAP_E_INVAL;
+    Span out[3], in[6 + kRuleSpans];
+    if ((rc = check_rows(a->k, a->tokens, c.kv_heads, c.d, 2, &p.k, &in[0])) != CAP_OK) return rc;
+    if ((rc = check_rows(a->v, a->tokens, c.kv_heads, c.d, 2, &p.v, &in[1])) != CAP_OK) return rc;
+    if (a->heads > 0) {
+        if (!a->q.p || !a->q_out.p) return CAP_E_INVAL;
+        if ((rc = check_rows(a->q, a->tokens, a->heads, c.d, 2, &p.q, &in[2])) != CAP_OK) return rc;
+        if ((rc = check_rows(a->q_out, a->tokens, a->heads, c.d, 2, &p.q_out, &out[2])) != CAP_OK) return rc;
+        if (p.q_out.p == p.q.p && p.q_out.head != p.q.head) return CAP_E_INVAL;
+    }
+    if (((p.q.p | p.k.p | p.v.p | p.q_out.p) & 15) || (addr(a->pos) & 3)) return CAP_E_ALIGN;
+    out[0] = cache[0];
+    out[1] = cache[1];
+    in[3] = cache[2];
+    in[4] = step[0];
+    in[5] = step[1];
+    if (a->rule) rule_spans(a->rule, a->pos, a->tokens, c.d, in + 6);
+    const Span* const own[3] = {nullptr, nullptr, &in[2]};
+    if ((rc = check_apart(out, own, 3, in, 6 + kRuleSpans)) != CAP_OK) return rc;
+    if (a->rule) enter_rule(a->rule, &p);
+    p.pos = a->pos;
+    p.tokens = a->tokens;
+    p.heads = a->heads;
+    p.kv_heads = c.kv_heads;
+    p.d = c.d;
+    p.tokens_wg = tokens_of_wg(a->tokens, (int64_t)a->heads + 2 * c.kv_heads, c.d);
+    return launch_status(cap::launch_qk(p, false, true, static_cast<hipStream_t>(stream)));
+}
+
+uint64_t kvp_attend_workspace_bytes(const kvp_attend_args* a) {
+    cap::KvpAttendParams p{};
+    Span cache[3], step[2];
+    if (!a) return 0;
+    kvp_attend_args sizes = *a;  // (lens and tok0 do not matter)
+    static const int32_t none = 0;
+    sizes.lens = sizes.tok0 = &none;
+    return plan_attend(&sizes, &p, cache, step) == CAP_OK ? attend_workspace(p) : 0;
+}
+
+int kvp_attend(const kvp_attend_args* a, void* stream) {
+    if (!a || a->reserved != 0) return CAP_E_INVAL;
+    cap::KvpAttendParams p{};
+    p.scale_log2 = a->scale * 1.4426950408889634f;
+    if (!std::isfinite(p.scale_log2)) return CAP_E_INVAL;
+    Span cache[3], step[2];
+    int rc = plan_attend(a, &p, cache, step);
+    if (rc != CAP_OK) return rc;
+    if (a->tokens == 0 || a->cache->n_seq == 0) return CAP_OK;
+    if (!a->q.p || !a->o) return CAP_E_INVAL;
+    Span out[3], in[6] = {{}, cache[0], cache[1], cache[2], step[0], step[1]};
+    if ((rc = check_rows(a->q, a->tokens, a->heads, p.d, 2, &p.q, &in[0])) != CAP_OK) return rc;
+    const uint64_t need = attend_workspace(p), rows = (uint64_t)a->tokens * (uint64_t)a->heads;
+    if (need && !a->workspace) return CAP_E_INVAL;
+    if (a->workspace_bytes < need) return CAP_E_SIZE;
+    if (((p.q.p | addr(a->o) | (need ? addr(a->workspace) : 0)) & 15) || (addr(a->lse) & 3)) return CAP_E_ALIGN;
+    out[0] = plain(a->o, rows * (uint64_t)p.d * 2);
+    out[1] = plain(a->lse, rows * 4);
+    out[2] = plain(need ? a->workspace : nullptr, need);
+    const Span* const own[3] = {};
+    if ((rc = check_apart(out, own, 3, in, 6)) != CAP_OK) return rc;
+    p.o = a->o;
+    p.lse = a->lse;
+    p.part_o = static_cast<float*>(a->workspace);
+    p.part_ml = p.part_o + attend_parts(p) * (uint64_t)p.d;
+    p.meta = reinterpret_cast<uint64_t*>(p.part_ml + attend_parts(p) * 2);
+    return launch_status(cap::launch_kvp_attend(p, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

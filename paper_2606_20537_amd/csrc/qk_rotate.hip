@@ -1,0 +1,288 @@
+// Norm of each head of q and k, rotation by position, and the append of the
+// result to a paged bf16 cache, on gfx950.
+//
+//   y = x (mean x^2 + eps)^-1/2 (w_add + w)              over a head's d channels
+//   a_i = sum over the axes of pos_axis freqs[axis][i]    i < rot / 2, in 64 bits
+//   (y_a, y_b) -> (y_a cos a - y_b sin a, y_b cos a + y_a sin a)
+//
+// One pass: a row (one head of one token) lies in the registers of d / 16 lanes, each
+// with two vectors of 8 channels that hold both channels of its pairs, so the only
+// values that cross lanes are the sums of squares.  Sines and cosines are those
+// of the token: a workgroup takes all heads of its tokens, computes each once and
+// hands it round in LDS.  Everything between load and store is fp32, rounded once.
+// The angle is taken in 64 bits and in turns, of which the whole ones go before it is
+// rounded: at position 2^20 the products alone would be off by 2^-4 in 32 bits.
+//
+// An append has the rows of v besides (copied), and k and v go to the row of the page
+// that the table names.
+#include <hip/hip_runtime.h>
+
+#include "kvp.h"
+
+namespace cap {
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256;
+constexpr int kMostPairs = 256;  // rot <= 512
+
+__device__ inline float bits_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
+
+// Eight channels as they lie in memory.
+template <bool F32>
+struct Vec { u32x4 w[F32 ? 2 : 1]; };
+
+template <bool F32>
+__device__ inline Vec<F32> load8(const char* at) {
+    Vec<F32> x;
+    x.w[0] = *reinterpret_cast<const u32x4*>(at);
+    if constexpr (F32) x.w[1] = *reinterpret_cast<const u32x4*>(at + 16);
+    return x;
+}
+template <bool F32>
+__device__ inline void store8(char* at, const Vec<F32>& x) {
+    *reinterpret_cast<u32x4*>(at) = x.w[0];
+    if constexpr (F32) *reinterpret_cast<u32x4*>(at + 16) = x.w[1];
+}
+template <bool F32>
+__device__ inline void widen(const Vec<F32>& x, float* f) {
+    #pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if constexpr (F32) f[e] = bits_f32(x.w[e / 4][e % 4]);
+        else f[e] = bits_f32(e & 1 ? x.w[0][e / 2] & 0xFFFF0000u : x.w[0][e / 2] << 16);
+}
+template <bool F32>
+__device__ inline Vec<F32> narrow(const float* f) {
+    Vec<F32> x;
+    #pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        if constexpr (F32) {
+            x.w[e / 4][e % 4] = __builtin_bit_cast(uint32_t, f[e]);
+            x.w[e / 4][e % 4 + 1] = __builtin_bit_cast(uint32_t, f[e + 1]);
+        } else {
+            x.w[0][e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){f[e], f[e + 1]}, bf16x2));
+        }
+    }
+    return x;
+}
+
+// Sum over `lanes` (a power of two) neighbouring lanes, in all of them.
+__device__ inline float sum_lanes(float x, int lanes) {
+    for (int i = 1; i < lanes; i *= 2) x += __shfl_xor(x, i);
+    return x;
+}
+
+// The factors of channels c .. c + 7.
+__device__ inline void weights8(const void* w, int c, const QkParams& p, float* f) {
+    #pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = 1.0f;
+    if (!p.norm || !w) return;
+    if (p.w_f32) widen<true>(load8<true>(static_cast<const char*>(w) + c * 4), f);
+    else widen<false>(load8<false>(static_cast<const char*>(w) + c * 2), f);
+    #pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] += p.w_add;
+}
+
+// The sequence of packed token t: the last one that begins at or before it (-1: none).
+// A wave looks at 64 of them at once.
+__device__ inline int seq_of(const KvpPages& g, int t) {
+    const int lane = (int)(threadIdx.x & 63);
+    const int step = (g.n_seq + 63) / 64;  // 16 at most
+    int s = -1;
+    if (step > 1) {
+        const int i = lane * step;
+        const int n = __builtin_popcountll(__ballot(i < g.n_seq && g.tok0[i < g.n_seq ? i : 0] <= t));
+        if (n == 0) return -1;
+        s = (n - 1) * step;
+    } else {
+        s = 0;
+    }
+    const int i = s + lane;
+    const bool here = lane < (step > 1 ? step : 64) && i < g.n_seq;
+    return s + __builtin_popcountll(__ballot(here && g.tok0[here ? i : 0] <= t)) - 1;
+}
+
+template <bool F32, bool APPEND>
+__global__ __launch_bounds__(kThreads) void rotate_kernel(const QkParams p) {
+    constexpr int kSize = F32 ? 4 : 2;
+    __shared__ __attribute__((aligned(16))) float cs_s[kQkTokens * kMostPairs * 2];  // cosine, sine
+    __shared__ int64_t off_s[kQkTokens];  // bytes from a pool's begin to the token's row, -1: nowhere
+    __shared__ int row_s[kQkTokens];      // its number
+    const int tid = (int)threadIdx.x;
+    const int64_t t0 = ((int64_t)blockIdx.y * kFp8GridX + blockIdx.x) * p.tokens_wg;
+    if (t0 >= p.tokens) return;
+    const int here = (int)(p.tokens - t0 < p.tokens_wg ? p.tokens - t0 : p.tokens_wg);
+    const int half = p.rot / 2;
+
+    if constexpr (APPEND) {
+        const KvpPages& g = p.pages;
+        for (int i = tid >> 6; i < here; i += kThreads / 64) {
+            const int t = (int)(t0 + i);
+            int64_t off = -1;
+            int row = 0;
+            if (g.tok0) {
+                const int s = __builtin_amdgcn_readfirstlane(seq_of(g, t));
+                if (s >= 0) {
+                    const int end = g.tok0[s + 1];
+                    row = (int)((int64_t)g.lens[s] - end + t);
+                    off = t < end && row >= 0 ? s : -1;
+                }
+            } else if (t < g.n_seq) {
+                row = g.lens[t] - 1;
+                off = row >= 0 ? t : -1;
+            }
+            const bool known = off >= 0;
+            if (known && row < g.capacity) {
+                const int column = (int)((uint32_t)row / (uint32_t)g.page);
+                const int page = g.table[off * g.table_stride + column];
+                off = (uint32_t)page < (uint32_t)g.pages
+                          ? (int64_t)page * g.page_stride + (int64_t)(row - column * g.page) * (g.kv_heads * p.d * 2) : -1;
+            } else {
+                off = -1;
+            }
+            if ((tid & 63) == 0) {
+                off_s[i] = off >= 0 ? off : known ? -1 : -2;  // -2: no sequence has the token
+                row_s[i] = row;
+            }
+        }
+        __syncthreads();
+    }
+
+    // sines and cosines of the workgroup's tokens
+    for (int i = tid; i < here * half; i += kThreads) {
+        const int t = (int)((uint32_t)i / (uint32_t)half), pair = i - t * half;
+        double turns = 0.0;
+        for (int a = 0; a < p.axes; ++a) {
+            const int at = APPEND && !p.pos ? row_s[t] : p.pos[(t0 + t) * p.axes + a];
+            turns += (double)at * p.freqs[(int64_t)a * half + pair];
+        }
+        turns *= 0.15915494309189533577;  // 1 / (2 pi)
+        turns -= __builtin_rint(turns);
+        float sine, cosine;
+        sincospif(2.0f * (float)turns, &sine, &cosine);
+        *reinterpret_cast<f32x2*>(&cs_s[2 * i]) = (f32x2){cosine, sine};
+    }
+
+    // a lane's channels: 8 from `a` and 8 from `b`
+    const int slots = p.d / 16;
+    int lanes = 1;
+    while (lanes < slots) lanes *= 2;
+    const int slot = tid & (lanes - 1);
+    const bool in = slot < slots;
+    int a, b, first = -1;  // first: a's first pair; -1: not rotated (halves)
+    if (p.pairs) {
+        a = 8 * slot;
+        b = p.d / 2 + 8 * slot;
+    } else if (8 * slot < half) {
+        a = first = 8 * slot;
+        b = half + 8 * slot;
+    } else {
+        a = p.rot + 8 * slot - half;
+        b = a + (p.d - p.rot) / 2;
+    }
+    float wq[16], wk[16];
+    weights8(p.wq, in ? a : 0, p, wq);
+    weights8(p.wq, in ? b : 0, p, wq + 8);
+    weights8(p.wk, in ? a : 0, p, wk);
+    weights8(p.wk, in ? b : 0, p, wk + 8);
+    __syncthreads();
+
+    const int of_q = p.heads, of_qk = p.heads + p.kv_heads, all = APPEND ? of_qk + p.kv_heads : of_qk;
+    const int per = kThreads / lanes;
+    for (int r = tid / lanes; r < here * all; r += per) {
+        const int t = (int)((uint32_t)r / (uint32_t)all), head = r - t * all;
+        const QkRows& src = head < of_q ? p.q : head < of_qk ? p.k : p.v;
+        const int h = head < of_q ? head : head < of_qk ? head - of_q : head - of_qk;
+        const char* from = reinterpret_cast<const char*>(src.p) + (t0 + t) * src.token + (int64_t)h * src.head;
+        char* to;
+        bool write = in;
+        if (APPEND && head >= of_q) {
+            to = reinterpret_cast<char*>(head < of_qk ? p.pages.k : p.pages.v) + off_s[t] + (int64_t)h * p.d * 2;
+            write = in && off_s[t] >= 0;
+        } else {
+            const QkRows& dst = head < of_q ? p.q_out : p.k_out;
+            to = reinterpret_cast<char*>(dst.p) + (t0 + t) * dst.token + (int64_t)h * dst.head;
+            if (APPEND) write = in && off_s[t] != -2;
+        }
+        Vec<F32> va, vb;
+        if (in) {
+            va = load8<F32>(from + a * kSize);
+            vb = load8<F32>(from + b * kSize);
+        }
+        if (head < of_qk) {  // (uniform over a row's lanes)
+            float x[16];
+            #pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+            if (in) {
+                widen<F32>(va, x);
+                widen<F32>(vb, x + 8);
+            }
+            if (p.norm) {
+                float sum = 0.0f;
+                #pragma unroll
+                for (int e = 0; e < 16; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
+                sum = sum_lanes(sum, lanes);
+                float eps = p.eps;
+                if (!(sum < __builtin_inff())) {  // squares that overflow: the row in units of 2^70
+                    sum = 0.0f;
+                    #pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        x[e] *= 0x1p-70f;
+                        sum = __builtin_fmaf(x[e], x[e], sum);
+                    }
+                    sum = sum_lanes(sum, lanes);
+                    eps = 0.0f;
+                }
+                const float f = 1.0f / __builtin_sqrtf(sum / (float)p.d + eps);
+                const bool q = head < of_q;
+                #pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = x[e] * f * (q ? wq[e] : wk[e]);
+            }
+            if (p.pairs) {
+                #pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const int pair = ((e < 8 ? a + e : b + e - 8)) / 2;
+                    if (in && pair < half) {
+                        const f32x2 cs = *reinterpret_cast<const f32x2*>(&cs_s[2 * (t * half + pair)]);
+                        const float y0 = x[e], y1 = x[e + 1];
+                        x[e] = y0 * cs[0] - y1 * cs[1];
+                        x[e + 1] = y1 * cs[0] + y0 * cs[1];
+                    }
+                }
+            } else if (in && first >= 0) {
+                #pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const f32x4 cs = *reinterpret_cast<const f32x4*>(&cs_s[2 * (t * half + first + e)]);
+                    #pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float y0 = x[e + i], y1 = x[8 + e + i];
+                        x[e + i] = y0 * cs[2 * i] - y1 * cs[2 * i + 1];
+                        x[8 + e + i] = y1 * cs[2 * i] + y0 * cs[2 * i + 1];
+                    }
+                }
+            }
+            va = narrow<F32>(x);
+            vb = narrow<F32>(x + 8);
+        }
+        if (write) {
+            store8<F32>(to + a * kSize, va);
+            store8<F32>(to + b * kSize, vb);
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_qk(const QkParams& p, bool f32, bool append, hipStream_t stream) {
+    const void* kernel = append ? reinterpret_cast<const void*>(&rotate_kernel<false, true>)
+                         : f32  ? reinterpret_cast<const void*>(&rotate_kernel<true, false>)
+                                : reinterpret_cast<const void*>(&rotate_kernel<false, false>);
+    void* args[] = {const_cast<QkParams*>(&p)};
+    return hipLaunchKernel(kernel, wide_grid((uint64_t)((p.tokens + p.tokens_wg - 1) / p.tokens_wg)), dim3(kThreads), args, 0, stream);
+}
+
+}  // namespace cap
