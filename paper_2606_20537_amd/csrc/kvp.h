@@ -54,7 +54,10 @@ hipError_t launch_qk(const QkParams& p, bool f32, bool append, hipStream_t strea
 // to the workgroups in equal runs; a workgroup has at most two segments that it shares with others,
 // whose parts lie in its two slots of the workspace.
 constexpr int kKvpUnit = 32;
-constexpr int kKvpBegin = 4;
+#ifndef KBEGIN
+#define KBEGIN 4
+#endif
+constexpr int kKvpBegin = KBEGIN;
 struct KvpAttendParams {
     QkRows   q;
     void*    o;

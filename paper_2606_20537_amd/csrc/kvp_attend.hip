@@ -25,6 +25,8 @@
 // several workgroups share are joined by a second launch.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "device_util.h"
 #include "kvp.h"
 
@@ -46,7 +48,79 @@ constexpr float kLn2 = 0.6931471805599453f;
 // sequence has, cannot overflow and means of finite values stay finite.
 constexpr float kAbove = 24.0f;
 
+typedef const char __attribute__((address_space(1)))* global_bytes;
+typedef __attribute__((address_space(3))) char* lds_bytes;
+typedef const void __attribute__((address_space(1)))* lds_source;
+typedef __attribute__((address_space(3))) void* lds_target;
+// Reads of what load_lds has brought, which wait for their answers themselves.  (Before its own reads of LDS the compiler
+// would wait for every load on its way.)
+// 16 bytes at `at` and `more` behind it, for four addresses.
+template <int MORE>
+__device__ inline void read_k4(const uint32_t (&at)[4], u32x4 (&x)[8]) {
+    asm volatile(
+        "ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:%12\n\t"
+        "ds_read_b128 %2, %9\n\tds_read_b128 %3, %9 offset:%12\n\t"
+        "ds_read_b128 %4, %10\n\tds_read_b128 %5, %10 offset:%12\n\t"
+        "ds_read_b128 %6, %11\n\tds_read_b128 %7, %11 offset:%12\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "i"(MORE)
+        : "memory");
+}
+template <int MORE>
+__device__ inline void read_k2(const uint32_t (&at)[2], u32x4 (&x)[4]) {
+    asm volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:%6\n\t"
+        "ds_read_b128 %2, %5\n\tds_read_b128 %3, %5 offset:%6\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+        : "v"(at[0]), "v"(at[1]), "i"(MORE)
+        : "memory");
+}
+// Transposing reads of bf16 rows: lane n of 16 gets four rows of channel n, at `at` and `more` behind it.
+template <int MORE>
+__device__ inline void read_v4(const uint32_t (&at)[4], u32x2 (&x)[8]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "i"(MORE)
+        : "memory");
+}
+// 1 KiB into LDS, 16 bytes from each lane's address.
+__device__ inline void load_lds(global_bytes from, lds_bytes to) {
+    __builtin_amdgcn_global_load_lds((lds_source)from, (lds_target)to, 16, 0, 2);  // (2: streamed)
+}
+// What a row's number changes in the places of its pieces: rows that lie over the same banks differ.
+template <int D>
+__device__ constexpr int fold_k(int row) { return D == 64 ? row >> 1 & 7 : row & 15; }
+template <int D>
+__device__ constexpr int fold_v(int row) { return D == 256 ? row & 15 : D == 128 ? row & 7 : row >> 1 & 3; }
+// The same value, of which the compiler does not know that it stays the same: what is derived from it is not
+// kept in registers over a loop.
+template <class T>
+__device__ inline T hidden(T x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+// Until at most N loads of this wave are on their way (they come in order).
+template <int N>
+__device__ inline void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// Until this wave's reads of LDS have been answered.
+__device__ inline void wait_lds() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 __device__ inline float bits_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
+__device__ inline uint32_t f32_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
 
 // Maximum / sum over the four lanes that share lane % 16.
 __device__ inline float group_max(float x) {
@@ -115,27 +189,27 @@ __device__ inline Seq load_seq(const KvpAttendParams& p, int s) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvpAttendParams p) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void attend_kernel(const KvpAttendParams p) {
     constexpr int NJ = D / 32;                        // K: fragments of 32 channels
-    constexpr int NV = D >= 128 ? D / 128 : 1;        // V: vectors of a lane
-    constexpr int VC = D >= 128 ? 8 : 4;              // and their channels
-    constexpr bool kAhead = D < 256;                  // registers for the next K beside V
+    constexpr int NC = D / 16;                        // V: blocks of 16 channels
     constexpr int kPitch = D + 4;
-    __shared__ __attribute__((aligned(16))) float o_s[4][16][kPitch];
+    constexpr int kSlot = kKvpUnit * D * 2;           // a unit of K, or of V
+    __shared__ __attribute__((aligned(1024))) char lds[8 * kSlot];
+    static_assert(8 * kSlot >= 4 * 16 * kPitch * 4, "o_s");
     __shared__ float ml_s[4][16][2], all_s[16][2];
+    float (*o_s)[16][kPitch] = reinterpret_cast<float (*)[16][kPitch]>(lds);  // once the waves are through with K and V
 
     const KvpPages& g = p.pages;
-    const int tid = (int)threadIdx.x, lane = tid & 63, li = lane & 15, grp = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const uint32_t w = blockIdx.x;
     const int G = p.heads / g.kv_heads;
 
     // the run [begin, end) of this workgroup
     const int chunks = (g.n_seq + 63) / 64;
-    Seq q = load_seq(p, lane);
+    Seq q = load_seq(p, (int)(threadIdx.x & 63));
     uint32_t scan = scan_lanes(q.weight), before = 0;
     uint32_t total = lane_u32(scan, 63);
-    for (int c = 1; c < chunks; ++c) total += lane_u32(scan_lanes(load_seq(p, 64 * c + lane).weight), 63);
+    for (int c = 1; c < chunks; ++c) total += lane_u32(scan_lanes(load_seq(p, 64 * c + (int)(threadIdx.x & 63)).weight), 63);
     uint32_t per = (total + p.wgs - 1) / p.wgs;
     if (per < p.least) per = p.least;
     const uint32_t begin = w * per;
@@ -145,8 +219,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvpAttendPara
     const int rowb = g.kv_heads * D * 2;
     uint32_t at = begin;  // where in the run we are
     int chunk = 0;
-    bool again = false;   // LDS is in use
     while (at < end) {
+        const int tid = hidden((int)threadIdx.x), lane = tid & 63, li = lane & 15, grp = lane >> 4;
         // the sequence that `at` is in (tok0 that does not ascend may make this fail: the run ends)
         while (at - before >= lane_u32(scan, 63)) {
             before += lane_u32(scan, 63);
@@ -174,6 +248,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvpAttendPara
             at = next;
             if (u1 <= 0) continue;
         }
+        if (g.pages == 0) u1 = u0;  // there is nothing to read
         const int tile = segment / g.kv_heads, h = segment - tile * g.kv_heads;
         const int first_unit = lane_int(q.first, s);
         const int seq = 64 * chunk + s;
@@ -189,25 +264,31 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvpAttendPara
         const int low = p.window > 0 ? (pos < 0 ? -1 : pos - window) : -1;
         const int low0 = p.window > 0 ? (pos0 < 0 ? -1 : pos0 - window) : -1, low1 = p.window > 0 ? (pos1 < 0 ? -1 : pos1 - window) : -1;
 
-        // where 64 groups of 16 rows begin in the pools, a lane each; -1: on no page
-        int64_t groups = -1;
-        int group0 = 2 * (first_unit + u0);
+        // Where a wave's next 64 units have their two groups of 16 rows in the pools, a lane each (unit u0 + wave
+        // + 4 (step0 + lane)); -1: on no page.
+        int64_t off[2] = {-1, -1};
+        int step0 = 0;
+        bool whole_unit = false;  // on pages, and every row of the tile sees all of it
         const int32_t* table = g.table + (int64_t)seq * g.table_stride;
-        auto load_groups = [&]() {
-            const uint32_t r = 16u * (uint32_t)(group0 + lane);
-            groups = -1;
-            if (r < (uint32_t)g.capacity && (int)r <= pos1) {
-                const uint32_t column = r / (uint32_t)g.page;
-                const int page = table[column];
-                if ((uint32_t)page < (uint32_t)g.pages)
-                    groups = (int64_t)page * g.page_stride + (int64_t)(r - column * (uint32_t)g.page) * rowb;
+        auto look_up = [&]() {
+            const int u = u0 + wave + 4 * (step0 + lane);
+            #pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t r = (uint32_t)(first_unit + u) * kKvpUnit + 16 * t;
+                off[t] = -1;
+                if (u < u1 && r < (uint32_t)g.capacity && (int)r <= pos1) {
+                    const uint32_t column = r / (uint32_t)g.page;
+                    const int page = table[column];
+                    if ((uint32_t)page < (uint32_t)g.pages)
+                        off[t] = (int64_t)page * g.page_stride + (int64_t)(r - column * (uint32_t)g.page) * rowb;
+                }
             }
+            const int r = (first_unit + u) * kKvpUnit;
+            whole_unit = off[0] >= 0 && off[1] >= 0 && r + kKvpUnit - 1 <= pos0 && r > low1;
         };
-        auto group_at = [&](int i) -> int64_t {
-            const uint32_t lo = (uint32_t)lane_int((int)(uint32_t)groups, i), hi = (uint32_t)lane_int((int)(groups >> 32), i);
-            return (int64_t)((uint64_t)hi << 32 | lo);
+        auto lane_i64 = [&](int64_t x, int i) -> int64_t {
+            return (int64_t)((uint64_t)lane_u32((uint32_t)(x >> 32), i) << 32 | lane_u32((uint32_t)x, i));
         };
-        load_groups();
 
         // the query rows, while the table is on its way
         bf16x8 qf[NJ];
@@ -218,163 +299,227 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvpAttendPara
             for (int j = 0; j < NJ; ++j) qf[j] = *reinterpret_cast<const bf16x8*>(src + 64 * j);
         }
 
-        f32x4 acc[NV * VC];
+        f32x4 acc[NC];  // channels 16 c + 4 grp ..
         #pragma unroll
-        for (int c = 0; c < NV * VC; ++c) acc[c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+        for (int c = 0; c < NC; ++c) acc[c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
         float m = kNegInf, l = 0.0f;
 
-        u32x4 k[2][NJ];
-        uint32_t v[8][NV * VC / 2];
-        const int kvoff = li * rowb + h * D * 2 + 16 * grp, vvoff = 4 * grp * rowb + h * D * 2 + li * VC * 2;
-        const char* kb = reinterpret_cast<const char*>(g.k);
-        const char* vb = reinterpret_cast<const char*>(g.v);
-        // (an absent group: nothing is read)
+        // Units in LDS, a slot for K and one for V to each wave: rows of D channels, in which 16 bytes (K: those of channels
+        // 8 c .. at the place of c ^ fold_k(row)) or 32 (V: 16 c .., c ^ fold_v(row)) change places, so that reads of 16 rows
+        // meet all banks.  An instruction brings 1 KiB: kRows rows, a lane 16 bytes.
+        constexpr int kRows = 512 / D, kLoads = kKvpUnit / kRows;
+        const int my_row = lane / (D / 8), chunk = lane % (D / 8);
+        const uint32_t lane_at = (uint32_t)(my_row * rowb + h * D * 2);
+        const uint32_t kvoff = lane_at + ((chunk ^ fold_k<D>(my_row)) << 4);
+        const uint32_t vvoff = lane_at + (((chunk >> 1) ^ fold_v<D>(my_row)) << 5) + ((chunk & 1) << 4);
+        lds_bytes k_slot = (lds_bytes)lds + wave * (2 * kSlot), v_slot = k_slot + kSlot;
+        const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_bytes)lds;  // (a multiple of the slots, which exchanges leave alone)
+        const uint32_t kread = lds_at + (uint32_t)(wave * (2 * kSlot) + li * D * 2 + ((grp ^ fold_k<D>(li)) << 4));
+        const int vrow = 4 * grp + (li >> 2);
+        const uint32_t vread = lds_at + (uint32_t)(wave * (2 * kSlot) + kSlot + vrow * D * 2 + (fold_v<D>(vrow) << 5) + 8 * (li & 3));
+        const global_bytes kb = (global_bytes)g.k, vb = (global_bytes)g.v;
+        // (folds are linear: that of my_row + row is fold(my_row) ^ fold(row))
         auto load_k = [&](const int64_t (&a)[2]) {
+            const uint32_t from = hidden(kvoff);
             #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const rsrc_t r = dev::make_rsrc_u32(kb + (a[t] < 0 ? 0 : a[t]), a[t] < 0 ? 0 : 16u * (uint32_t)rowb);
-                #pragma unroll
-                for (int j = 0; j < NJ; ++j) k[t][j] = __builtin_amdgcn_raw_buffer_load_b128(r, kvoff + 64 * j, 0, 0);
+            for (int i = 0; i < kLoads; ++i) {
+                const int row = i * kRows % 16;
+                load_lds(kb + a[i * kRows / 16] + row * rowb + (from ^ (uint32_t)(fold_k<D>(row) << 4)), k_slot + i * 1024);
             }
         };
         auto load_v = [&](const int64_t (&a)[2]) {
+            const uint32_t from = hidden(vvoff);
             #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const rsrc_t r = dev::make_rsrc_u32(vb + (a[t] < 0 ? 0 : a[t]), a[t] < 0 ? 0 : 16u * (uint32_t)rowb);
+            for (int i = 0; i < kLoads; ++i) {
+                const int row = i * kRows % 16;
+                load_lds(vb + a[i * kRows / 16] + row * rowb + (from ^ (uint32_t)(fold_v<D>(row) << 5)), v_slot + i * 1024);
+            }
+        };
+        float x[8];
+        auto scores = [&]() {
+            const uint32_t from = hidden(kread);
+            f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
+            constexpr int kAtOnce = NJ < 4 ? 2 : 4;
+            #pragma unroll
+            for (int j0 = 0; j0 < NJ; j0 += kAtOnce) {
+                uint32_t at[kAtOnce];
+                u32x4 k[2 * kAtOnce];
                 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    #pragma unroll
-                    for (int x = 0; x < NV; ++x) {
-                        if constexpr (VC == 8) {
-                            const u32x4 d = __builtin_amdgcn_raw_buffer_load_b128(r, vvoff + 256 * x, e * rowb, 0);
-                            #pragma unroll
-                            for (int i = 0; i < 4; ++i) v[4 * t + e][4 * x + i] = d[i];
-                        } else {
-                            const u32x2 d = __builtin_amdgcn_raw_buffer_load_b64(r, vvoff, e * rowb, 0);
-                            v[4 * t + e][0] = d[0];
-                            v[4 * t + e][1] = d[1];
-                        }
-                    }
+                for (int j = 0; j < kAtOnce; ++j) at[j] = from ^ (uint32_t)((j0 + j) << 6);
+                if constexpr (kAtOnce == 2) read_k2<16 * D * 2>(at, k);
+                else read_k4<16 * D * 2>(at, k);
+                #pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    s0 = dev::mma(__builtin_bit_cast(bf16x8, k[2 * j]), qf[j0 + j], s0);
+                    s1 = dev::mma(__builtin_bit_cast(bf16x8, k[2 * j + 1]), qf[j0 + j], s1);
+                }
             }
-        };
-
-        // Groups of unit u (of the segment), those that the tile does not see as absent; waves move together
-        // through the 64 groups that lanes hold.
-        auto unit_groups = [&](int u, int64_t (&a)[2]) {
-            const int r = (first_unit + u) * kKvpUnit;
-            const bool seen = u < u1 && r <= pos1 && r + kKvpUnit - 1 > low0;
-            #pragma unroll
-            for (int t = 0; t < 2; ++t) a[t] = seen ? group_at(2 * (first_unit + u) + t - group0) : -1;
-        };
-
-        int64_t a[2];
-        int u = u0 + wave;
-        unit_groups(u, a);
-        load_k(a);
-        load_v(a);
-        for (; u < u1; u += 4) {
-            const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-            f32x4 s0 = zero, s1 = zero;
-            #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                s0 = dev::mma(__builtin_bit_cast(bf16x8, k[0][j]), qf[j], s0);
-                s1 = dev::mma(__builtin_bit_cast(bf16x8, k[1][j]), qf[j], s1);
-            }
-            const int64_t now[2] = {a[0], a[1]};
-            if (2 * (first_unit + u + 4) + 1 - group0 > 63) {
-                group0 = 2 * (first_unit + u + 4);
-                load_groups();
-            }
-            unit_groups(u + 4, a);
-            if (kAhead) load_k(a);
-
-            const int r = (first_unit + u) * kKvpUnit;
-            float x[8];
             #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 x[e] = s0[e] * p.scale_log2;
                 x[4 + e] = s1[e] * p.scale_log2;
             }
-            const bool partial = r + kKvpUnit - 1 > pos0 || r <= low1 || now[0] < 0 || now[1] < 0;  // some row does not see every key
-            bool bad = false;
-            if (partial) {
-                #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int key = r + 4 * grp + (e < 4 ? e : 12 + e);
-                    const bool there = now[e / 4] >= 0;
-                    x[e] = there && key <= pos && key > low ? x[e] : kNegInf;
-                    // a key that no row sees has no part in the product, whatever its V holds
-                    const bool some = there && key <= pos1 && key > low0;
-                    #pragma unroll
-                    for (int i = 0; i < NV * VC / 2; ++i) {
-                        uint32_t d = some ? v[e][i] : 0u;
-                        // neither have infinities and NaN that some rows see and others do not: put back below
-                        const uint32_t out = ((d & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((d & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-                        bad |= out != 0;
-                        v[e][i] = d & ~out;
-                    }
-                }
-            }
+        };
+        // x becomes the weights.  hi is cut off, not rounded, and lo above zero, so that an infinity in V, times both, is
+        // one (lo: 2^-16 of the weight; 2^-20 at least).
+        auto weigh = [&](bf16x8& hi, bf16x8& lo) {
             float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3])),
                                         __builtin_fmaxf(__builtin_fmaxf(x[4], x[5]), __builtin_fmaxf(x[6], x[7])));
             top = __builtin_fmaxf(m, group_max(top));
             const float from = reference(top);
             const float fade = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(reference(m) - from);
             m = top;
-            float sum = 0.0f, pf[8];
-            bf16x8 hi, lo;
+            float sum = 0.0f;
             #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                pf[e] = __builtin_amdgcn_exp2f(x[e] - from);
-                sum += pf[e];
+                x[e] = __builtin_amdgcn_exp2f(x[e] - from);
+                sum += x[e];
             }
-            dev::split_n<8>(pf, hi, lo);
+            u32x4 h, low_part;
+            #pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                h[e / 2] = __builtin_amdgcn_perm(f32_bits(x[e + 1]), f32_bits(x[e]), 0x07060302u);
+                const float h0 = bits_f32(h[e / 2] << 16), h1 = bits_f32(h[e / 2] & 0xFFFF0000u);
+                low_part[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                    (f32x2){__builtin_fmaxf(x[e] - h0, h0 * 0x1p-20f), __builtin_fmaxf(x[e + 1] - h1, h1 * 0x1p-20f)}, bf16x2));
+            }
+            hi = __builtin_bit_cast(bf16x8, h);
+            lo = __builtin_bit_cast(bf16x8, low_part);
             l = l * fade + sum;
             if (__any(fade != 1.0f)) {
                 #pragma unroll
-                for (int c = 0; c < NV * VC; ++c) acc[c] *= fade;
+                for (int c = 0; c < NC; ++c) acc[c] *= fade;
             }
+        };
+        // f(c, the eight keys of a lane in channel 16 c + li), for all blocks of 16 channels.
+        auto each_block = [&](auto&& f) {
+            const uint32_t from = hidden(vread);
             #pragma unroll
-            for (int i = 0; i < NV * VC / 2; ++i) {
-                u32x4 even, odd;  // channels 2i and 2i + 1 of the eight keys
+            for (int c0 = 0; c0 < NC; c0 += 4) {
+                uint32_t at[4];
+                u32x2 v[8];
                 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    even[e] = __builtin_amdgcn_perm(v[2 * e + 1][i], v[2 * e][i], 0x05040100u);
-                    odd[e] = __builtin_amdgcn_perm(v[2 * e + 1][i], v[2 * e][i], 0x07060302u);
-                }
-                acc[2 * i] = dev::mma(__builtin_bit_cast(bf16x8, even), hi, acc[2 * i]);
-                acc[2 * i + 1] = dev::mma(__builtin_bit_cast(bf16x8, odd), hi, acc[2 * i + 1]);
-                acc[2 * i] = dev::mma(__builtin_bit_cast(bf16x8, even), lo, acc[2 * i]);
-                acc[2 * i + 1] = dev::mma(__builtin_bit_cast(bf16x8, odd), lo, acc[2 * i + 1]);
+                for (int c = 0; c < 4; ++c) at[c] = from ^ (uint32_t)((c0 + c) << 5);
+                read_v4<16 * D * 2>(at, v);
+                #pragma unroll
+                for (int c = 0; c < 4; ++c) f(c0 + c, (u32x4){v[2 * c][0], v[2 * c][1], v[2 * c + 1][0], v[2 * c + 1][1]});
             }
-            if (partial && __any(bad)) {
-                for (int t = 0; t < kKvpUnit; ++t) {
-                    const int key = r + t;
-                    const int64_t off = now[t / 16];
-                    if (off < 0 || key > pos1 || key <= low0) continue;  // (uniform)
-                    const int e = (t & 3) + (t >= 16 ? 4 : 0);
-                    const float mine = e == 0 ? pf[0] : e == 1 ? pf[1] : e == 2 ? pf[2] : e == 3 ? pf[3] : e == 4 ? pf[4] : e == 5 ? pf[5] : e == 6 ? pf[6] : pf[7];
-                    const float pk = __shfl(mine, li + 16 * (t % 16 / 4));
-                    const uint16_t* src = reinterpret_cast<const uint16_t*>(vb + off + (int64_t)(t % 16) * rowb) + h * D;
-                    #pragma unroll
-                    for (int x = 0; x < NV; ++x)
+        };
+        auto add_values = [&](const bf16x8& hi, const bf16x8& lo) {
+            each_block([&](int c, const u32x4& v) {
+                acc[c] = dev::mma(__builtin_bit_cast(bf16x8, v), hi, acc[c]);
+                acc[c] = dev::mma(__builtin_bit_cast(bf16x8, v), lo, acc[c]);
+            });
+        };
+
+        // A unit that some row does not see in full, or that lies on no page in part.  A key that a row does not see has
+        // to leave the product, as its V may hold an infinity or NaN, of which no weight makes zero: keys that no row
+        // sees are cleared; where one that some rows see and others do not holds such a value, the
+        // rows of each position are taken by themselves.
+        auto edge_unit = [&](int r, const int64_t (&a)[2]) {
+            const int64_t there[2] = {a[0] < 0 ? 0 : a[0], a[1] < 0 ? 0 : a[1]};  // (rows of the first page, which count for nothing)
+            wait_lds();  // the last reads of both slots
+            load_k(there);
+            load_v(there);
+            wait_loads<0>();
+            scores();
+            auto seen = [&](int e, int first, int last) {  // key e lies on a page and in (first, last]
+                const int key = r + 4 * grp + (e < 4 ? e : 12 + e);
+                return a[e / 4] >= 0 && key <= last && key > first;
+            };
+            #pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = seen(e, low, pos) ? x[e] : kNegInf;
+            bf16x8 hi, lo;
+            weigh(hi, lo);
+            int first = low0, last = pos1, at = pos1;
+            bool each = false;
+            for (bool look = pos0 != pos1; at <= pos1;) {
+                uint32_t keep[4];  // bits of keys 2i and 2i + 1
+                #pragma unroll
+                for (int i = 0; i < 4; ++i) keep[i] = (seen(2 * i, first, last) ? 0xFFFFu : 0u) | (seen(2 * i + 1, first, last) ? 0xFFFF0000u : 0u);
+                if (look) {
+                    bool found = false;
+                    each_block([&](int, const u32x4& v) {
                         #pragma unroll
-                        for (int i = 0; i < VC; ++i)
-                            #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const uint32_t b = src[128 * x + VC * (4 * grp + j) + i];
-                                if ((b & 0x7F80u) == 0x7F80u && key <= pos && key > low) acc[VC * x + i][j] += pk * bits_f32(b << 16);
-                            }
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t d = v[i] & keep[i] & 0x7F807F80u;
+                            found |= (d & 0xFFFFu) == 0x7F80u || (d >> 16) == 0x7F80u;
+                        }
+                    });
+                    look = false;
+                    each = __any(found);
+                    if (!each) continue;
+                    at = pos0;
+                } else {
+                    each_block([&](int c, u32x4 v) {
+                        #pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] &= keep[i];
+                        f32x4 sum = dev::mma(__builtin_bit_cast(bf16x8, v), hi, acc[c]);
+                        sum = dev::mma(__builtin_bit_cast(bf16x8, v), lo, sum);
+                        #pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[c][j] = !each || pos == at ? sum[j] : acc[c][j];
+                    });
+                    ++at;
                 }
+                first = p.window > 0 ? (at < 0 ? -1 : at - window) : -1;
+                last = at;
             }
-            if (!kAhead) load_k(a);
-            load_v(a);
+        };
+
+        const int steps = u1 - u0 > wave ? (u1 - u0 - wave + 3) / 4 : 0;
+        look_up();
+        for (int i = 0; i < steps;) {
+            if (i - step0 >= 64) {
+                step0 = i;
+                look_up();
+            }
+            // whole units from step i on, of those that lanes hold
+            const int at0 = i - step0;
+            const uint64_t gaps = ~__ballot(whole_unit) >> at0;
+            int count = gaps ? __builtin_ctzll(gaps) : 64;
+            if (count > 64 - at0) count = 64 - at0;
+            if (count == 0) {
+                const int r = (first_unit + u0 + wave + 4 * i) * kKvpUnit;
+                const int64_t a[2] = {lane_i64(off[0], at0), lane_i64(off[1], at0)};
+                if (r <= pos1 && r + kKvpUnit - 1 > low0 && (a[0] >= 0 || a[1] >= 0)) edge_unit(r, a);
+                ++i;
+                continue;
+            }
+            // The next K is on its way once its slot has been read, the next V likewise: loads come in
+            // order, so the ones behind those that are waited for tell how many may be outstanding.
+            auto step = [&](int j, auto more) {
+                bf16x8 hi, lo;
+                int64_t a[2];
+                wait_loads<kLoads>();  // K: V's are behind it
+                scores();
+                if constexpr (decltype(more)::value) {
+                    a[0] = lane_i64(off[0], at0 + j + 1);
+                    a[1] = lane_i64(off[1], at0 + j + 1);
+                    wait_lds();
+                    load_k(a);
+                }
+                weigh(hi, lo);
+                wait_loads<decltype(more)::value ? kLoads : 0>();  // V: the next K's are behind it
+                add_values(hi, lo);
+                if constexpr (decltype(more)::value) {
+                    wait_lds();
+                    load_v(a);
+                }
+            };
+            {
+                const int64_t a[2] = {lane_i64(off[0], at0), lane_i64(off[1], at0)};
+                wait_lds();  // the last reads of both slots
+                load_k(a);
+                load_v(a);
+            }
+            for (int j = 0; j + 1 < count; ++j) step(j, std::true_type{});
+            step(count - 1, std::false_type{});
+            i += count;
         }
 
         // join the waves
         l = group_sum(l);
-        if (again) __syncthreads();
-        again = true;
+        __syncthreads();  // V, and the last segment's values, are done with
         if (grp == 0) {
             ml_s[wave][li][0] = m;
             ml_s[wave][li][1] = l;
@@ -390,13 +535,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvpAttendPara
         const float fade = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m) - from);
         // (m is -inf where the wave saw nothing: zeros; or only NaN, which stays)
         #pragma unroll
-        for (int x = 0; x < NV; ++x)
-            #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                #pragma unroll
-                for (int i = 0; i < VC; i += 4)
-                    *reinterpret_cast<f32x4*>(&o_s[wave][li][128 * x + VC * (4 * grp + j) + i]) =
-                        (f32x4){acc[VC * x + i][j] * fade, acc[VC * x + i + 1][j] * fade, acc[VC * x + i + 2][j] * fade, acc[VC * x + i + 3][j] * fade};
+        for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4*>(&o_s[wave][li][16 * c + 4 * grp]) = acc[c] * fade;
         if (tid < 16) {  // wave 0: lane = row
             all_s[li][0] = top;
             all_s[li][1] = sum;
@@ -409,7 +548,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const KvpAttendPara
         constexpr int kPer = D / 4;  // threads of a row
         #pragma unroll
         for (int i = 0; i < 16 * kPer / kThreads; ++i) {
-            const int rr = (i * kThreads + tid) / kPer, c = (tid % kPer) * 4;
+            const int rr = (i * kThreads + hidden(tid)) / kPer, c = (tid % kPer) * 4;
             if (rr >= rows) continue;
             f32x4 o = *reinterpret_cast<const f32x4*>(&o_s[0][rr][c]);
             #pragma unroll

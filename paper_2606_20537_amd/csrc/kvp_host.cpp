@@ -1,5 +1,6 @@
 // Host side of the norm and rotation of queries and keys and of the paged bf16 KV
 // cache: argument checks and launches of qk_norm_rope, kvp_append and kvp_attend.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -144,8 +145,12 @@ int check_apart(const Span* out, const Span* const* own, int n_out, const Span* 
 // ---- attend: the launch ----
 // A run of units in whole mode is never cut; short capacities gain nothing from a second launch.
 constexpr int64_t kWholeRows = 512;
-constexpr int64_t kWgs = 512;   // two to a CU
-constexpr int64_t kLeast = 12;  // units of a run at least, its beginning among them
+#ifndef KLEAST
+#define KLEAST 12
+#endif
+// Workgroups: as many as fit the chip at once (LDS of two units to a wave).
+int64_t wgs_of(int32_t d) { return d == 256 ? 256 : d == 128 ? 512 : 1024; }
+constexpr int64_t kLeast = KLEAST;  // units of a run at least, its beginning among them
 
 int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)[3], Span (&step)[2]) {
     int rc = check_cache(a->cache, &p->pages, cache);
@@ -164,7 +169,7 @@ int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)
     p->whole = capacity <= kWholeRows;
     p->least = p->whole ? 1 : (uint32_t)kLeast;
     const int64_t most = p->whole ? segments : (segments * units + kLeast - 1) / kLeast;
-    p->wgs = (uint32_t)(most < kWgs ? most : kWgs);
+    p->wgs = (uint32_t)std::min(most, wgs_of(c.d));
     return CAP_OK;
 }
 
