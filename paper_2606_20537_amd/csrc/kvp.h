@@ -11,6 +11,20 @@ namespace cap {
 // from n on have nothing to do.
 inline dim3 wide_grid(uint64_t n) { return dim3(fp8_grid_x((uint32_t)n), fp8_grid_y((uint32_t)n)); }
 
+// Division of numbers below 2^31 by a number that the host knows: n m / 2^shift with m = ceil(2^shift / d),
+// shift = 31 + log2 d rounded up, is exact (m d exceeds 2^shift by less than d <= 2^(shift - 31)).
+struct Divisor {
+    uint32_t m, shift;
+};
+inline Divisor divisor(uint32_t d) {
+    uint32_t shift = 31;
+    while (((uint64_t)1 << (shift - 31)) < d) ++shift;
+    return {(uint32_t)((((uint64_t)1 << shift) + d - 1) / d), shift};
+}
+#if defined(__HIPCC__)
+__device__ inline int divide(int n, const Divisor& d) { return (int)((uint64_t)(uint32_t)n * d.m >> d.shift); }
+#endif
+
 // A packed tensor [tokens, heads, d]; strides in bytes.
 struct QkRows {
     uint64_t p;
@@ -27,6 +41,7 @@ struct KvpPages {
     int64_t        page_stride;   // bytes
     int32_t        pages, page, columns, n_seq, kv_heads;
     int32_t        capacity;      // columns * page
+    Divisor        by_page;
 };
 
 // ---- norm and rotation, with or without an append ----
@@ -71,6 +86,7 @@ struct KvpAttendParams {
     uint32_t least;    // units of a run at least
     int32_t  whole;    // segments are not cut, and there is no second launch
     float    scale_log2;
+    Divisor  by_group, by_kv_heads, by_heads;  // heads / kv_heads, kv_heads, heads
     KvpPages pages;
 };
 hipError_t launch_kvp_attend(const KvpAttendParams& p, hipStream_t stream);

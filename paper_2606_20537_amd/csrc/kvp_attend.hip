@@ -77,6 +77,23 @@ __device__ inline void read_k2(const uint32_t (&at)[2], u32x4 (&x)[4]) {
         : "v"(at[0]), "v"(at[1]), "i"(MORE)
         : "memory");
 }
+template <int MORE>
+__device__ inline void read_k8(const uint32_t (&at)[8], u32x4 (&x)[16]) {
+    asm volatile(
+        "ds_read_b128 %0, %16\n\tds_read_b128 %1, %16 offset:%24\n\t"
+        "ds_read_b128 %2, %17\n\tds_read_b128 %3, %17 offset:%24\n\t"
+        "ds_read_b128 %4, %18\n\tds_read_b128 %5, %18 offset:%24\n\t"
+        "ds_read_b128 %6, %19\n\tds_read_b128 %7, %19 offset:%24\n\t"
+        "ds_read_b128 %8, %20\n\tds_read_b128 %9, %20 offset:%24\n\t"
+        "ds_read_b128 %10, %21\n\tds_read_b128 %11, %21 offset:%24\n\t"
+        "ds_read_b128 %12, %22\n\tds_read_b128 %13, %22 offset:%24\n\t"
+        "ds_read_b128 %14, %23\n\tds_read_b128 %15, %23 offset:%24\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(x[8]), "=&v"(x[9]),
+          "=&v"(x[10]), "=&v"(x[11]), "=&v"(x[12]), "=&v"(x[13]), "=&v"(x[14]), "=&v"(x[15])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7]), "i"(MORE)
+        : "memory");
+}
 // Transposing reads of bf16 rows: lane n of 16 gets four rows of channel n, at `at` and `more` behind it.
 template <int MORE>
 __device__ inline void read_v4(const uint32_t (&at)[4], u32x2 (&x)[8]) {
@@ -88,6 +105,22 @@ __device__ inline void read_v4(const uint32_t (&at)[4], u32x2 (&x)[8]) {
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
         : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "i"(MORE)
+        : "memory");
+}
+template <int MORE>
+__device__ inline void read_v8(const uint32_t (&at)[8], u32x2 (&x)[16]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %2, %17\n\tds_read_b64_tr_b16 %3, %17 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %4, %18\n\tds_read_b64_tr_b16 %5, %18 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %6, %19\n\tds_read_b64_tr_b16 %7, %19 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %8, %20\n\tds_read_b64_tr_b16 %9, %20 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %10, %21\n\tds_read_b64_tr_b16 %11, %21 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %12, %22\n\tds_read_b64_tr_b16 %13, %22 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %14, %23\n\tds_read_b64_tr_b16 %15, %23 offset:%24\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(x[8]), "=&v"(x[9]), "=&v"(x[10]), "=&v"(x[11]), "=&v"(x[12]), "=&v"(x[13]), "=&v"(x[14]), "=&v"(x[15])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7]), "i"(MORE)
         : "memory");
 }
 // 1 KiB into LDS, 16 bytes from each lane's address.
@@ -106,6 +139,13 @@ __device__ inline T hidden(T x) {
     asm volatile("" : "+v"(x));
     return x;
 }
+// The kernel's arguments, to be read where they are used instead of being held from the kernel's beginning.
+template <class T>
+__device__ inline const T* hidden_arguments() {
+    auto at = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return (const T*)at;
+}
 // Until at most N loads of this wave are on their way (they come in order).
 template <int N>
 __device__ inline void wait_loads() {
@@ -122,14 +162,23 @@ __device__ inline void wait_lds() {
 __device__ inline float bits_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ inline uint32_t f32_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
 
+// x of the lanes in even rows of 16 and of those in odd ones, or of the lower and of the upper 32 lanes, each in both.
+__device__ inline f32x2 both16(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(f32_bits(x), f32_bits(x), false, false);
+    return (f32x2){bits_f32(r[0]), bits_f32(r[1])};
+}
+__device__ inline f32x2 both32(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(x), f32_bits(x), false, false);
+    return (f32x2){bits_f32(r[0]), bits_f32(r[1])};
+}
 // Maximum / sum over the four lanes that share lane % 16.
 __device__ inline float group_max(float x) {
-    x = __builtin_fmaxf(x, __shfl_xor(x, 16));
-    return __builtin_fmaxf(x, __shfl_xor(x, 32));
+    const f32x2 a = both16(x), b = both32(__builtin_fmaxf(a[0], a[1]));
+    return __builtin_fmaxf(b[0], b[1]);
 }
 __device__ inline float group_sum(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    const f32x2 a = both16(x), b = both32(a[0] + a[1]);
+    return b[0] + b[1];
 }
 // What scores are taken from, m the highest of them (-inf: none yet).
 __device__ inline float reference(float m) { return m == kNegInf ? 0.0f : m + kAbove; }
@@ -161,18 +210,17 @@ struct Seq {
 
 __device__ inline int clamp_token(const KvpAttendParams& p, int t) { return t < 0 ? 0 : t > p.tokens ? (int)p.tokens : t; }
 
-__device__ inline Seq load_seq(const KvpAttendParams& p, int s) {
+__device__ inline Seq load_seq(const KvpAttendParams& p, int group, int s) {
     const KvpPages& g = p.pages;
     Seq q = {};
     if (s >= g.n_seq) return q;
+    // (three loads on their way at once, whether there is a tok0 or not)
+    const int32_t* tok0 = g.tok0 ? g.tok0 : g.lens;
+    const int i = g.tok0 ? s : 0;
     q.n = g.lens[s];
-    if (g.tok0) {
-        q.t0 = clamp_token(p, g.tok0[s]);
-        q.T = clamp_token(p, g.tok0[s + 1]) - q.t0;
-    } else {
-        q.t0 = s;
-        q.T = s < p.tokens;
-    }
+    const int begin = tok0[i], end = tok0[g.tok0 ? i + 1 : 0];
+    q.t0 = g.tok0 ? clamp_token(p, begin) : s;
+    q.T = g.tok0 ? clamp_token(p, end) - q.t0 : s < p.tokens;
     if (q.n < 0) q.n = 0;
     if (q.T <= 0) {
         q.T = 0;
@@ -183,7 +231,7 @@ __device__ inline Seq load_seq(const KvpAttendParams& p, int s) {
     q.first = lo / kKvpUnit;
     q.units = (hi + kKvpUnit - 1) / kKvpUnit - q.first;
     if (q.units < 1) q.units = 1;
-    q.tiles = (int)(((int64_t)q.T * (p.heads / g.kv_heads) + 15) / 16);
+    q.tiles = (q.T * group + 15) / 16;  // (tokens * heads fits 31 bits)
     q.weight = (uint32_t)q.tiles * (uint32_t)g.kv_heads * (uint32_t)(q.units + kKvpBegin);
     return q;
 }
@@ -202,14 +250,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
     const KvpPages& g = p.pages;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const uint32_t w = blockIdx.x;
-    const int G = p.heads / g.kv_heads;
+    const int G = divide(p.heads, p.by_kv_heads);
 
     // the run [begin, end) of this workgroup
     const int chunks = (g.n_seq + 63) / 64;
-    Seq q = load_seq(p, (int)(threadIdx.x & 63));
+    Seq q = load_seq(p, G, (int)(threadIdx.x & 63));
     uint32_t scan = scan_lanes(q.weight), before = 0;
     uint32_t total = lane_u32(scan, 63);
-    for (int c = 1; c < chunks; ++c) total += lane_u32(scan_lanes(load_seq(p, 64 * c + (int)(threadIdx.x & 63)).weight), 63);
+    for (int c = 1; c < chunks; ++c) total += lane_u32(scan_lanes(load_seq(p, G, 64 * c + (int)(threadIdx.x & 63)).weight), 63);
     uint32_t per = (total + p.wgs - 1) / p.wgs;
     if (per < p.least) per = p.least;
     const uint32_t begin = w * per;
@@ -225,7 +273,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         while (at - before >= lane_u32(scan, 63)) {
             before += lane_u32(scan, 63);
             if (++chunk >= chunks) return;
-            q = load_seq(p, 64 * chunk + lane);
+            q = load_seq(p, G, 64 * chunk + lane);
             scan = scan_lanes(q.weight);
         }
         const int s = __builtin_popcountll(__ballot(scan <= at - before));
@@ -249,16 +297,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
             if (u1 <= 0) continue;
         }
         if (g.pages == 0) u1 = u0;  // there is nothing to read
-        const int tile = segment / g.kv_heads, h = segment - tile * g.kv_heads;
+        const int tile = divide(segment, p.by_kv_heads), h = segment - tile * g.kv_heads;
         const int first_unit = lane_int(q.first, s);
         const int seq = 64 * chunk + s;
 
         const int total_rows = T * G, r0 = tile * 16;
         const int rows = total_rows - r0 < 16 ? total_rows - r0 : 16;
         const int row = r0 + (li < rows ? li : rows - 1);  // rows past the last repeat it
-        const int my_t = (int)((uint32_t)row / (uint32_t)G);
+        const int my_t = divide(row, p.by_group);
         const int pos = n - T + my_t;
-        const int pos0 = n - T + (int)((uint32_t)r0 / (uint32_t)G), pos1 = n - T + (int)((uint32_t)(r0 + rows - 1) / (uint32_t)G);
+        const int pos0 = n - T + divide(r0, p.by_group), pos1 = n - T + divide(r0 + rows - 1, p.by_group);
         const int window = p.window > 0 ? p.window : 0x7fffffff;
         // keys above low are seen: pos - window, without passing 32 bits
         const int low = p.window > 0 ? (pos < 0 ? -1 : pos - window) : -1;
@@ -266,25 +314,28 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
 
         // Where a wave's next 64 units have their two groups of 16 rows in the pools, a lane each (unit u0 + wave
         // + 4 (step0 + lane)); -1: on no page.
-        int64_t off[2] = {-1, -1};
-        int step0 = 0;
-        bool whole_unit = false;  // on pages, and every row of the tile sees all of it
+        int64_t off[2];
+        uint64_t todo = 0, whole = 0;  // bits of the units that some row sees, and of those that every row sees all of
         const int32_t* table = g.table + (int64_t)seq * g.table_stride;
-        auto look_up = [&]() {
-            const int u = u0 + wave + 4 * (step0 + lane);
+        auto look_up = [&](int step0) {
+            const int u = u0 + wave + 4 * (step0 + lane), r = (first_unit + u) * kKvpUnit;
+            bool there[2];
+            int page[2], rest[2];
             #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const uint32_t r = (uint32_t)(first_unit + u) * kKvpUnit + 16 * t;
-                off[t] = -1;
-                if (u < u1 && r < (uint32_t)g.capacity && (int)r <= pos1) {
-                    const uint32_t column = r / (uint32_t)g.page;
-                    const int page = table[column];
-                    if ((uint32_t)page < (uint32_t)g.pages)
-                        off[t] = (int64_t)page * g.page_stride + (int64_t)(r - column * (uint32_t)g.page) * rowb;
-                }
+                const int rt = r + 16 * t;
+                there[t] = u < u1 && rt < g.capacity && rt <= pos1;
+                const int column = there[t] ? divide(rt, g.by_page) : 0;
+                rest[t] = rt - column * g.page;
+                page[t] = table[column];
             }
-            const int r = (first_unit + u) * kKvpUnit;
-            whole_unit = off[0] >= 0 && off[1] >= 0 && r + kKvpUnit - 1 <= pos0 && r > low1;
+            #pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                there[t] = there[t] && (uint32_t)page[t] < (uint32_t)g.pages;
+                off[t] = there[t] ? (int64_t)page[t] * g.page_stride + (int64_t)rest[t] * rowb : -1;
+            }
+            todo = __ballot((there[0] || there[1]) && r + kKvpUnit - 1 > low0);
+            whole = __ballot(there[0] && there[1] && r + kKvpUnit - 1 <= pos0 && r > low1);
         };
         auto lane_i64 = [&](int64_t x, int i) -> int64_t {
             return (int64_t)((uint64_t)lane_u32((uint32_t)(x >> 32), i) << 32 | lane_u32((uint32_t)x, i));
@@ -293,10 +344,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         // the query rows, while the table is on its way
         bf16x8 qf[NJ];
         {
-            const char* src = reinterpret_cast<const char*>(p.q.p) + (int64_t)(seq_t0 + my_t) * p.q.token +
-                              (int64_t)(h * G + (row - my_t * G)) * p.q.head + 16 * grp;
+            const global_bytes src = (global_bytes)p.q.p + (int64_t)(seq_t0 + my_t) * p.q.token +
+                                     (int64_t)(h * G + (row - my_t * G)) * p.q.head + 16 * grp;
             #pragma unroll
-            for (int j = 0; j < NJ; ++j) qf[j] = *reinterpret_cast<const bf16x8*>(src + 64 * j);
+            for (int j = 0; j < NJ; ++j) qf[j] = *(const bf16x8 __attribute__((address_space(1)))*)(src + 64 * j);
         }
 
         f32x4 acc[NC];  // channels 16 c + 4 grp ..
@@ -339,7 +390,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         auto scores = [&]() {
             const uint32_t from = hidden(kread);
             f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
-            constexpr int kAtOnce = NJ < 4 ? 2 : 4;
+            constexpr int kAtOnce = NJ;
             #pragma unroll
             for (int j0 = 0; j0 < NJ; j0 += kAtOnce) {
                 uint32_t at[kAtOnce];
@@ -347,7 +398,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
                 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) at[j] = from ^ (uint32_t)((j0 + j) << 6);
                 if constexpr (kAtOnce == 2) read_k2<16 * D * 2>(at, k);
-                else read_k4<16 * D * 2>(at, k);
+                else if constexpr (kAtOnce == 4) read_k4<16 * D * 2>(at, k);
+                else read_k8<16 * D * 2>(at, k);
                 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
                     s0 = dev::mma(__builtin_bit_cast(bf16x8, k[2 * j]), qf[j0 + j], s0);
@@ -394,15 +446,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         // f(c, the eight keys of a lane in channel 16 c + li), for all blocks of 16 channels.
         auto each_block = [&](auto&& f) {
             const uint32_t from = hidden(vread);
+            constexpr int kAtOnce = NC < 8 ? 4 : 8;
             #pragma unroll
-            for (int c0 = 0; c0 < NC; c0 += 4) {
-                uint32_t at[4];
-                u32x2 v[8];
+            for (int c0 = 0; c0 < NC; c0 += kAtOnce) {
+                uint32_t at[kAtOnce];
+                u32x2 v[2 * kAtOnce];
                 #pragma unroll
-                for (int c = 0; c < 4; ++c) at[c] = from ^ (uint32_t)((c0 + c) << 5);
-                read_v4<16 * D * 2>(at, v);
+                for (int c = 0; c < kAtOnce; ++c) at[c] = from ^ (uint32_t)((c0 + c) << 5);
+                if constexpr (kAtOnce == 4) read_v4<16 * D * 2>(at, v);
+                else read_v8<16 * D * 2>(at, v);
                 #pragma unroll
-                for (int c = 0; c < 4; ++c) f(c0 + c, (u32x4){v[2 * c][0], v[2 * c][1], v[2 * c + 1][0], v[2 * c + 1][1]});
+                for (int c = 0; c < kAtOnce; ++c) f(c0 + c, (u32x4){v[2 * c][0], v[2 * c][1], v[2 * c + 1][0], v[2 * c + 1][1]});
             }
         };
         auto add_values = [&](const bf16x8& hi, const bf16x8& lo) {
@@ -412,31 +466,22 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
             });
         };
 
-        // A unit that some row does not see in full, or that lies on no page in part.  A key that a row does not see has
-        // to leave the product, as its V may hold an infinity or NaN, of which no weight makes zero: keys that no row
-        // sees are cleared; where one that some rows see and others do not holds such a value, the
-        // rows of each position are taken by themselves.
-        auto edge_unit = [&](int r, const int64_t (&a)[2]) {
-            const int64_t there[2] = {a[0] < 0 ? 0 : a[0], a[1] < 0 ? 0 : a[1]};  // (rows of the first page, which count for nothing)
-            wait_lds();  // the last reads of both slots
-            load_k(there);
-            load_v(there);
-            wait_loads<0>();
-            scores();
-            auto seen = [&](int e, int first, int last) {  // key e lies on a page and in (first, last]
-                const int key = r + 4 * grp + (e < 4 ? e : 12 + e);
-                return a[e / 4] >= 0 && key <= last && key > first;
-            };
-            #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = seen(e, low, pos) ? x[e] : kNegInf;
-            bf16x8 hi, lo;
-            weigh(hi, lo);
+        // In a unit that some row does not see in full, or that lies on no page in part (there: the halves that are on
+        // one), a key that a row does not see has to leave the product, as its V may hold an infinity or NaN, of which
+        // no weight makes zero: keys that no row sees are cleared; where one that some rows see and
+        // others do not holds such a value, the rows of each position are taken by themselves.
+        auto seen = [&](int r, int there, int e, int first, int last) {  // key e lies on a page and in (first, last]
+            const int key = r + 4 * grp + (e < 4 ? e : 12 + e);
+            return (there >> (e / 4) & 1) && key <= last && key > first;
+        };
+        auto add_seen_values = [&](int r, int there, const bf16x8& hi, const bf16x8& lo) {
             int first = low0, last = pos1, at = pos1;
             bool each = false;
             for (bool look = pos0 != pos1; at <= pos1;) {
                 uint32_t keep[4];  // bits of keys 2i and 2i + 1
                 #pragma unroll
-                for (int i = 0; i < 4; ++i) keep[i] = (seen(2 * i, first, last) ? 0xFFFFu : 0u) | (seen(2 * i + 1, first, last) ? 0xFFFF0000u : 0u);
+                for (int i = 0; i < 4; ++i)
+                    keep[i] = (seen(r, there, 2 * i, first, last) ? 0xFFFFu : 0u) | (seen(r, there, 2 * i + 1, first, last) ? 0xFFFF0000u : 0u);
                 if (look) {
                     bool found = false;
                     each_block([&](int, const u32x4& v) {
@@ -467,54 +512,56 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         };
 
         const int steps = u1 - u0 > wave ? (u1 - u0 - wave + 3) / 4 : 0;
-        look_up();
-        for (int i = 0; i < steps;) {
-            if (i - step0 >= 64) {
-                step0 = i;
-                look_up();
-            }
-            // whole units from step i on, of those that lanes hold
-            const int at0 = i - step0;
-            const uint64_t gaps = ~__ballot(whole_unit) >> at0;
-            int count = gaps ? __builtin_ctzll(gaps) : 64;
-            if (count > 64 - at0) count = 64 - at0;
-            if (count == 0) {
-                const int r = (first_unit + u0 + wave + 4 * i) * kKvpUnit;
-                const int64_t a[2] = {lane_i64(off[0], at0), lane_i64(off[1], at0)};
-                if (r <= pos1 && r + kKvpUnit - 1 > low0 && (a[0] >= 0 || a[1] >= 0)) edge_unit(r, a);
-                ++i;
-                continue;
-            }
-            // The next K is on its way once its slot has been read, the next V likewise: loads come in
-            // order, so the ones behind those that are waited for tell how many may be outstanding.
-            auto step = [&](int j, auto more) {
-                bf16x8 hi, lo;
-                int64_t a[2];
+        for (int step0 = 0; step0 < steps; step0 += 64) {
+            look_up(step0);
+            if (todo == 0) continue;
+            // (of a half on no page, rows of the first one are read, and count for nothing)
+            int64_t a[2];
+            int there;
+            auto where = [&](int j) {
+                a[0] = lane_i64(off[0], j);
+                a[1] = lane_i64(off[1], j);
+                there = 0;
+                #pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if ((int)(a[t] >> 32) >= 0) there |= 1 << t;
+                    else a[t] = 0;
+                }
+            };
+            int j = __builtin_ctzll(todo);
+            where(j);
+            wait_lds();  // the last reads of both slots
+            load_k(a);
+            load_v(a);
+            for (;;) {
+                // The next K is on its way once its slot has been read, the next V likewise: loads come in order, so
+                // those behind the ones that are waited for tell how many may be outstanding.
+                todo &= todo - 1;
+                const bool more = todo != 0;
+                const int r = (first_unit + u0 + wave + 4 * (step0 + j)) * kKvpUnit, there_now = there;
+                const bool all = whole >> j & 1;
                 wait_loads<kLoads>();  // K: V's are behind it
                 scores();
-                if constexpr (decltype(more)::value) {
-                    a[0] = lane_i64(off[0], at0 + j + 1);
-                    a[1] = lane_i64(off[1], at0 + j + 1);
+                if (more) {
+                    j = __builtin_ctzll(todo);
+                    where(j);
                     wait_lds();
                     load_k(a);
                 }
-                weigh(hi, lo);
-                wait_loads<decltype(more)::value ? kLoads : 0>();  // V: the next K's are behind it
-                add_values(hi, lo);
-                if constexpr (decltype(more)::value) {
-                    wait_lds();
-                    load_v(a);
+                if (!all) {
+                    #pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = seen(r, there_now, e, low, pos) ? x[e] : kNegInf;
                 }
-            };
-            {
-                const int64_t a[2] = {lane_i64(off[0], at0), lane_i64(off[1], at0)};
-                wait_lds();  // the last reads of both slots
-                load_k(a);
+                bf16x8 hi, lo;
+                weigh(hi, lo);
+                if (more) wait_loads<kLoads>();  // V: the next K's are behind it
+                else wait_loads<0>();
+                if (all) add_values(hi, lo);
+                else add_seen_values(r, there_now, hi, lo);
+                if (!more) break;
+                wait_lds();
                 load_v(a);
             }
-            for (int j = 0; j + 1 < count; ++j) step(j, std::true_type{});
-            step(count - 1, std::false_type{});
-            i += count;
         }
 
         // join the waves
@@ -541,10 +588,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
             all_s[li][1] = sum;
         }
         __syncthreads();
-        // parts of the segment: the workgroups that have units of it
-        const uint32_t from_wg = p.whole ? w : unit0 / per, parts = p.whole ? 1 : (next - 1) / per - from_wg + 1;
-        const bool one = parts == 1;
-        const uint32_t slot = 2 * w + (from_wg == w ? 1 : 0);
+        // whether the segment's first unit is of this run, and all of them
+        const KvpAttendParams& late = *hidden_arguments<KvpAttendParams>();
+        const bool begins = late.whole || unit0 >= begin, one = late.whole || (begins && next <= end);
+        const uint32_t slot = 2 * w + (begins ? 1 : 0);
         constexpr int kPer = D / 4;  // threads of a row
         #pragma unroll
         for (int i = 0; i < 16 * kPer / kThreads; ++i) {
@@ -554,83 +601,92 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
             #pragma unroll
             for (int j = 1; j < 4; ++j) o += *reinterpret_cast<const f32x4*>(&o_s[j][rr][c]);
             if (!one) {
-                *reinterpret_cast<f32x4*>(p.part_o + ((int64_t)slot * 16 + rr) * D + c) = o;
+                *reinterpret_cast<f32x4*>(late.part_o + ((int64_t)slot * 16 + rr) * D + c) = o;
                 continue;
             }
             const float z = all_s[rr][1], inv = z > 0.0f || z != z ? 1.0f / z : 0.0f;
-            const int t = (int)((uint32_t)(r0 + rr) / (uint32_t)G);
-            const int64_t to = ((int64_t)(seq_t0 + t) * p.heads + h * G + (r0 + rr - t * G)) * D + c;
+            const int t = divide(r0 + rr, late.by_group);
+            const int64_t to = ((int64_t)(seq_t0 + t) * late.heads + h * G + (r0 + rr - t * G)) * D + c;
             const bf16x2 lo2 = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
             const bf16x2 hi2 = __builtin_convertvector((f32x2){o[2] * inv, o[3] * inv}, bf16x2);
-            *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + to) =
+            *reinterpret_cast<u32x2*>(static_cast<__bf16*>(late.o) + to) =
                 (u32x2){__builtin_bit_cast(uint32_t, lo2), __builtin_bit_cast(uint32_t, hi2)};
         }
         if (tid < rows) {
             const float mm = all_s[tid][0], z = all_s[tid][1];
-            const int t = (int)((uint32_t)(r0 + tid) / (uint32_t)G);
-            const int64_t to = (int64_t)(seq_t0 + t) * p.heads + h * G + (r0 + tid - t * G);
-            if (!one) *reinterpret_cast<f32x2*>(p.part_ml + ((int64_t)slot * 16 + tid) * 2) = (f32x2){mm, z};
-            else if (p.lse) p.lse[to] = (reference(mm) + __builtin_amdgcn_logf(z)) * kLn2;
-            if (!p.whole && from_wg == w) p.meta[to] = (uint64_t)tid << 48 | (uint64_t)parts << 24 | w;
+            const int t = divide(r0 + tid, late.by_group);
+            const int64_t to = (int64_t)(seq_t0 + t) * late.heads + h * G + (r0 + tid - t * G);
+            if (!one) *reinterpret_cast<f32x2*>(late.part_ml + ((int64_t)slot * 16 + tid) * 2) = (f32x2){mm, z};
+            else if (late.lse) late.lse[to] = (reference(mm) + __builtin_amdgcn_logf(z)) * kLn2;
+            if (!late.whole && begins) late.meta[to] = (uint64_t)tid << 48 | (uint64_t)((next - 1) / per - w + 1) << 24 | w;
         }
     }
 }
 
-// Joins the parts of a row: a workgroup has one output row, D / 4 threads to a part.
+// Joins the parts of a row: a workgroup has 64 channels of one output row, and 16 threads to a part.
 template <int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p) {
-    constexpr int kPer = D / 4, kWays = kThreads / kPer;
-    __shared__ __attribute__((aligned(16))) float o_s[kWays][D];
+    constexpr int kPer = 16, kWays = kThreads / kPer, kBlocks = D / 64;
+    constexpr int kAhead = 4;  // parts whose loads are on their way
+    __shared__ __attribute__((aligned(16))) float o_s[kWays][4 * kPer];
     __shared__ float ml_s[kWays][2];
     const KvpPages& g = p.pages;
-    const int64_t out = (int64_t)blockIdx.y * kFp8GridX + blockIdx.x;
+    const int64_t block = (int64_t)blockIdx.y * kFp8GridX + blockIdx.x, out = block / kBlocks;
     if (out >= p.tokens * p.heads) return;
-    const int tid = (int)threadIdx.x, way = tid / kPer, c = tid % kPer * 4;
+    const int tid = (int)threadIdx.x, way = tid / kPer, c = (int)(block % kBlocks) * 64 + tid % kPer * 4;
     const uint64_t meta = p.meta[out];
-    const int64_t token = out / p.heads;
+    const int64_t token = divide((int)out, p.by_heads);
     // a row that no sequence has: nothing was written for it
-    const int64_t first = g.tok0 ? clamp_token(p, g.tok0[0]) : 0, last = g.tok0 ? clamp_token(p, g.tok0[g.n_seq]) : g.n_seq;
-    if (token < first || token >= last) return;
+    const int32_t* tok0 = g.tok0 ? g.tok0 : g.lens;
+    const int t_first = tok0[0], t_last = tok0[g.tok0 ? g.n_seq : 0];
+    if (token < (g.tok0 ? clamp_token(p, t_first) : 0) || token >= (g.tok0 ? clamp_token(p, t_last) : g.n_seq)) return;
     const int rr = (int)(meta >> 48) & 15;
-    uint32_t parts = (uint32_t)(meta >> 24) & 0xFFFFFFu, w = (uint32_t)meta & 0xFFFFFFu;
+    const uint32_t parts = (uint32_t)(meta >> 24) & 0xFFFFFFu, w = (uint32_t)meta & 0xFFFFFFu;
     if (parts < 2 || w >= p.wgs || parts > p.wgs - w) return;
     float m = kNegInf, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t i = (uint32_t)way; i < parts; i += kWays) {
-        const int64_t slot = 2 * (int64_t)(w + i) + (i == 0 ? 1 : 0);
-        const f32x2 a = *reinterpret_cast<const f32x2*>(p.part_ml + (slot * 16 + rr) * 2);
-        const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + (slot * 16 + rr) * D + c);
-        const float top = __builtin_fmaxf(m, a[0]), from = reference(top);
-        const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m) - from);
-        const float e = a[0] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(a[0]) - from);
-        l = l * f + a[1] * e;
-        o = o * f + x * e;
-        m = top;
+    for (uint32_t i0 = (uint32_t)way; i0 < parts; i0 += kAhead * kWays) {
+        f32x2 a[kAhead];
+        f32x4 x[kAhead];
+        #pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const uint32_t i = i0 + k * kWays < parts ? i0 + k * kWays : i0;
+            const int64_t slot = 2 * (int64_t)(w + i) + (i == 0 ? 1 : 0);
+            a[k] = *(const f32x2 __attribute__((address_space(1)))*)(p.part_ml + (slot * 16 + rr) * 2);
+            x[k] = *(const f32x4 __attribute__((address_space(1)))*)(p.part_o + (slot * 16 + rr) * D + c);
+        }
+        #pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i0 + k * kWays >= parts) continue;
+            const float top = __builtin_fmaxf(m, a[k][0]), from = reference(top);
+            const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m) - from);
+            const float e = a[k][0] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(a[k][0]) - from);
+            l = l * f + a[k][1] * e;
+            o = o * f + x[k] * e;
+            m = top;
+        }
     }
     if (tid % kPer == 0) {
         ml_s[way][0] = m;
         ml_s[way][1] = l;
     }
-    *reinterpret_cast<f32x4*>(&o_s[way][c]) = o;
+    *reinterpret_cast<f32x4*>(&o_s[way][tid % kPer * 4]) = o;
     __syncthreads();
-    if (way) return;
-    m = kNegInf;
-    l = 0.0f;
-    o = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    if (tid >= 64) return;
+    // a thread to each channel
+    float top = kNegInf, sum = 0.0f, total = 0.0f;
     #pragma unroll
-    for (int i = 0; i < kWays; ++i) m = __builtin_fmaxf(m, ml_s[i][0]);
+    for (int i = 0; i < kWays; ++i) top = __builtin_fmaxf(top, ml_s[i][0]);
     #pragma unroll
     for (int i = 0; i < kWays; ++i) {
-        const float e = ml_s[i][0] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(ml_s[i][0]) - reference(m));
-        l += ml_s[i][1] * e;
-        o += *reinterpret_cast<const f32x4*>(&o_s[i][c]) * e;
+        const float e = ml_s[i][0] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(ml_s[i][0]) - reference(top));
+        total += ml_s[i][1] * e;
+        sum += o_s[i][tid] * e;
     }
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    const bf16x2 lo2 = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
-    const bf16x2 hi2 = __builtin_convertvector((f32x2){o[2] * inv, o[3] * inv}, bf16x2);
-    *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + out * D + c) =
-        (u32x2){__builtin_bit_cast(uint32_t, lo2), __builtin_bit_cast(uint32_t, hi2)};
-    if (c == 0 && p.lse) p.lse[out] = (reference(m) + __builtin_amdgcn_logf(l)) * kLn2;
+    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+    const int ch = (int)(block % kBlocks) * 64 + tid;
+    static_cast<__bf16*>(p.o)[out * D + ch] = (__bf16)(sum * inv);
+    if (ch == 0 && p.lse) p.lse[out] = (reference(top) + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 template <int D>
@@ -638,7 +694,7 @@ hipError_t launch(const KvpAttendParams& p, hipStream_t stream) {
     void* args[] = {const_cast<KvpAttendParams*>(&p)};
     const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&attend_kernel<D>), dim3(p.wgs), dim3(kThreads), args, 0, stream);
     if (e != hipSuccess || p.whole) return e;
-    return hipLaunchKernel(reinterpret_cast<const void*>(&join_kernel<D>), wide_grid((uint64_t)(p.tokens * p.heads)), dim3(kThreads), args, 0, stream);
+    return hipLaunchKernel(reinterpret_cast<const void*>(&join_kernel<D>), wide_grid((uint64_t)(p.tokens * p.heads) * (D / 64)), dim3(kThreads), args, 0, stream);
 }
 
 }  // namespace

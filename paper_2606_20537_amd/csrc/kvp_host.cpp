@@ -104,7 +104,7 @@ int check_cache(const kvp_cache* c, cap::KvpPages* g, Span (&span)[3]) {
     if (stride % 8 != 0 || ((addr(c->k) | addr(c->v)) & 15) || (addr(c->table) & 3)) return CAP_E_ALIGN;
     if (c->pages > 0 && (uint64_t)stride * 2 > UINT64_MAX / (uint64_t)c->pages) return CAP_E_SIZE;
     *g = {addr(c->k), addr(c->v), c->table, nullptr, nullptr, columns, stride * 2, (int32_t)c->pages, c->page, c->columns, c->n_seq,
-          c->kv_heads, (int32_t)capacity};
+          c->kv_heads, (int32_t)capacity, cap::divisor((uint32_t)c->page)};
     span[0] = {addr(c->k), (uint64_t)width * 2, (uint64_t)stride * 2, (uint64_t)c->pages};
     span[1] = {addr(c->v), (uint64_t)width * 2, (uint64_t)stride * 2, (uint64_t)c->pages};
     span[2] = {addr(c->table), (uint64_t)c->columns * 4, (uint64_t)columns * 4, (uint64_t)c->n_seq};
@@ -166,6 +166,9 @@ int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)
     p->heads = a->heads;
     p->d = c.d;
     p->window = a->window;
+    p->by_group = cap::divisor((uint32_t)(a->heads / c.kv_heads));
+    p->by_kv_heads = cap::divisor((uint32_t)c.kv_heads);
+    p->by_heads = cap::divisor((uint32_t)a->heads);
     p->whole = capacity <= kWholeRows;
     p->least = p->whole ? 1 : (uint32_t)kLeast;
     const int64_t most = p->whole ? segments : (segments * units + kLeast - 1) / kLeast;
