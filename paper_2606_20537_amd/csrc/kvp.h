@@ -65,14 +65,10 @@ hipError_t launch_qk(const QkParams& p, bool f32, bool append, hipStream_t strea
 // ---- attend ----
 // A segment is a KV head and 16 query rows of a sequence (row r: token r / G, query head
 // h G + r % G).  Its rows of the cache are cut into units of 32.  Units of all segments in a row, each
-// segment with kKvpBegin more before it for what a segment costs, are dealt out
+// segment with `begin` more before it for what a segment costs, are dealt out
 // to the workgroups in equal runs; a workgroup has at most two segments that it shares with others,
 // whose parts lie in its two slots of the workspace.
 constexpr int kKvpUnit = 32;
-#ifndef KBEGIN
-#define KBEGIN 4
-#endif
-constexpr int kKvpBegin = KBEGIN;
 struct KvpAttendParams {
     QkRows   q;
     void*    o;
@@ -83,10 +79,11 @@ struct KvpAttendParams {
     int64_t  tokens;
     int32_t  heads, d, window;
     uint32_t wgs;
+    int32_t  begin;    // units that the beginning of a segment counts for
     uint32_t least;    // units of a run at least
     int32_t  whole;    // segments are not cut, and there is no second launch
     float    scale_log2;
-    Divisor  by_group, by_kv_heads, by_heads;  // heads / kv_heads, kv_heads, heads
+    Divisor  by_group, by_kv_heads;  // heads / kv_heads, kv_heads
     KvpPages pages;
 };
 hipError_t launch_kvp_attend(const KvpAttendParams& p, hipStream_t stream);

@@ -30,6 +30,9 @@
 #include "device_util.h"
 #include "kvp.h"
 
+#ifndef KAUX
+#define KAUX 2
+#endif
 namespace cap {
 namespace {
 
@@ -125,7 +128,7 @@ __device__ inline void read_v8(const uint32_t (&at)[8], u32x2 (&x)[16]) {
 }
 // 1 KiB into LDS, 16 bytes from each lane's address.
 __device__ inline void load_lds(global_bytes from, lds_bytes to) {
-    __builtin_amdgcn_global_load_lds((lds_source)from, (lds_target)to, 16, 0, 2);  // (2: streamed)
+    __builtin_amdgcn_global_load_lds((lds_source)from, (lds_target)to, 16, 0, KAUX);  // (2: streamed)
 }
 // What a row's number changes in the places of its pieces: rows that lie over the same banks differ.
 template <int D>
@@ -232,7 +235,7 @@ __device__ inline Seq load_seq(const KvpAttendParams& p, int group, int s) {
     q.units = (hi + kKvpUnit - 1) / kKvpUnit - q.first;
     if (q.units < 1) q.units = 1;
     q.tiles = (q.T * group + 15) / 16;  // (tokens * heads fits 31 bits)
-    q.weight = (uint32_t)q.tiles * (uint32_t)g.kv_heads * (uint32_t)(q.units + kKvpBegin);
+    q.weight = (uint32_t)q.tiles * (uint32_t)g.kv_heads * (uint32_t)(q.units + p.begin);
     return q;
 }
 
@@ -280,12 +283,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         if (s > 63) return;
         const int n = lane_int(q.n, s), seq_t0 = lane_int(q.t0, s), T = lane_int(q.T, s), units = lane_int(q.units, s);
         const uint32_t weight = lane_u32(q.weight, s), base = before + lane_u32(scan, s) - weight;
-        const uint32_t size = (uint32_t)(units + kKvpBegin);
+        const uint32_t size = (uint32_t)(units + p.begin);
         if (at - base >= weight) return;
         const int segment = (int)((at - base) / size);
         const uint32_t seg0 = base + (uint32_t)segment * size;  // of the segment
         const uint32_t next = seg0 + size;
-        const uint32_t unit0 = seg0 + kKvpBegin;                // of its first unit
+        const uint32_t unit0 = seg0 + p.begin;                // of its first unit
         int u0 = 0, u1 = units;
         if (p.whole) {
             at = next;
@@ -297,26 +300,30 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
             if (u1 <= 0) continue;
         }
         if (g.pages == 0) u1 = u0;  // there is nothing to read
-        const int tile = divide(segment, p.by_kv_heads), h = segment - tile * g.kv_heads;
+        const KvpAttendParams& args = *hidden_arguments<KvpAttendParams>();
+        const KvpPages& gp = args.pages;
+        const float scale_log2 = args.scale_log2;
+        const bool windowed = args.window > 0;
+        const int tile = divide(segment, args.by_kv_heads), h = segment - tile * gp.kv_heads;
         const int first_unit = lane_int(q.first, s);
         const int seq = 64 * chunk + s;
 
         const int total_rows = T * G, r0 = tile * 16;
         const int rows = total_rows - r0 < 16 ? total_rows - r0 : 16;
         const int row = r0 + (li < rows ? li : rows - 1);  // rows past the last repeat it
-        const int my_t = divide(row, p.by_group);
+        const int my_t = divide(row, args.by_group);
         const int pos = n - T + my_t;
-        const int pos0 = n - T + divide(r0, p.by_group), pos1 = n - T + divide(r0 + rows - 1, p.by_group);
-        const int window = p.window > 0 ? p.window : 0x7fffffff;
+        const int pos0 = n - T + divide(r0, args.by_group), pos1 = n - T + divide(r0 + rows - 1, args.by_group);
+        const int window = args.window > 0 ? args.window : 0x7fffffff;
         // keys above low are seen: pos - window, without passing 32 bits
-        const int low = p.window > 0 ? (pos < 0 ? -1 : pos - window) : -1;
-        const int low0 = p.window > 0 ? (pos0 < 0 ? -1 : pos0 - window) : -1, low1 = p.window > 0 ? (pos1 < 0 ? -1 : pos1 - window) : -1;
+        const int low = args.window > 0 ? (pos < 0 ? -1 : pos - window) : -1;
+        const int low0 = args.window > 0 ? (pos0 < 0 ? -1 : pos0 - window) : -1, low1 = args.window > 0 ? (pos1 < 0 ? -1 : pos1 - window) : -1;
 
         // Where a wave's next 64 units have their two groups of 16 rows in the pools, a lane each (unit u0 + wave
         // + 4 (step0 + lane)); -1: on no page.
         int64_t off[2];
         uint64_t todo = 0, whole = 0;  // bits of the units that some row sees, and of those that every row sees all of
-        const int32_t* table = g.table + (int64_t)seq * g.table_stride;
+        const int32_t* table = gp.table + (int64_t)seq * gp.table_stride;
         auto look_up = [&](int step0) {
             const int u = u0 + wave + 4 * (step0 + lane), r = (first_unit + u) * kKvpUnit;
             bool there[2];
@@ -324,15 +331,15 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
             #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const int rt = r + 16 * t;
-                there[t] = u < u1 && rt < g.capacity && rt <= pos1;
-                const int column = there[t] ? divide(rt, g.by_page) : 0;
-                rest[t] = rt - column * g.page;
+                there[t] = u < u1 && rt < gp.capacity && rt <= pos1;
+                const int column = there[t] ? divide(rt, gp.by_page) : 0;
+                rest[t] = rt - column * gp.page;
                 page[t] = table[column];
             }
             #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                there[t] = there[t] && (uint32_t)page[t] < (uint32_t)g.pages;
-                off[t] = there[t] ? (int64_t)page[t] * g.page_stride + (int64_t)rest[t] * rowb : -1;
+                there[t] = there[t] && (uint32_t)page[t] < (uint32_t)gp.pages;
+                off[t] = there[t] ? (int64_t)page[t] * gp.page_stride + (int64_t)rest[t] * rowb : -1;
             }
             todo = __ballot((there[0] || there[1]) && r + kKvpUnit - 1 > low0);
             whole = __ballot(there[0] && there[1] && r + kKvpUnit - 1 <= pos0 && r > low1);
@@ -344,8 +351,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         // the query rows, while the table is on its way
         bf16x8 qf[NJ];
         {
-            const global_bytes src = (global_bytes)p.q.p + (int64_t)(seq_t0 + my_t) * p.q.token +
-                                     (int64_t)(h * G + (row - my_t * G)) * p.q.head + 16 * grp;
+            const global_bytes src = (global_bytes)args.q.p + (int64_t)(seq_t0 + my_t) * args.q.token +
+                                     (int64_t)(h * G + (row - my_t * G)) * args.q.head + 16 * grp;
             #pragma unroll
             for (int j = 0; j < NJ; ++j) qf[j] = *(const bf16x8 __attribute__((address_space(1)))*)(src + 64 * j);
         }
@@ -368,7 +375,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         const uint32_t kread = lds_at + (uint32_t)(wave * (2 * kSlot) + li * D * 2 + ((grp ^ fold_k<D>(li)) << 4));
         const int vrow = 4 * grp + (li >> 2);
         const uint32_t vread = lds_at + (uint32_t)(wave * (2 * kSlot) + kSlot + vrow * D * 2 + (fold_v<D>(vrow) << 5) + 8 * (li & 3));
-        const global_bytes kb = (global_bytes)g.k, vb = (global_bytes)g.v;
+        const global_bytes kb = (global_bytes)gp.k, vb = (global_bytes)gp.v;
         // (folds are linear: that of my_row + row is fold(my_row) ^ fold(row))
         auto load_k = [&](const int64_t (&a)[2]) {
             const uint32_t from = hidden(kvoff);
@@ -408,8 +415,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
             }
             #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[e] = s0[e] * p.scale_log2;
-                x[4 + e] = s1[e] * p.scale_log2;
+                x[e] = s0[e] * scale_log2;
+                x[4 + e] = s1[e] * scale_log2;
             }
         };
         // x becomes the weights.  hi is cut off, not rounded, and lo above zero, so that an infinity in V, times both, is
@@ -506,7 +513,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
                     });
                     ++at;
                 }
-                first = p.window > 0 ? (at < 0 ? -1 : at - window) : -1;
+                first = windowed ? (at < 0 ? -1 : at - window) : -1;
                 last = at;
             }
         };
@@ -623,78 +630,142 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
     }
 }
 
-// Joins the parts of a row: a workgroup has 64 channels of one output row, and 16 threads to a part.
-template <int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p) {
-    constexpr int kPer = 16, kWays = kThreads / kPer, kBlocks = D / 64;
-    constexpr int kAhead = 4;  // parts whose loads are on their way
-    __shared__ __attribute__((aligned(16))) float o_s[kWays][4 * kPer];
-    __shared__ float ml_s[kWays][2];
-    const KvpPages& g = p.pages;
-    const int64_t block = (int64_t)blockIdx.y * kFp8GridX + blockIdx.x, out = block / kBlocks;
-    if (out >= p.tokens * p.heads) return;
-    const int tid = (int)threadIdx.x, way = tid / kPer, c = (int)(block % kBlocks) * 64 + tid % kPer * 4;
-    const uint64_t meta = p.meta[out];
-    const int64_t token = divide((int)out, p.by_heads);
-    // a row that no sequence has: nothing was written for it
-    const int32_t* tok0 = g.tok0 ? g.tok0 : g.lens;
-    const int t_first = tok0[0], t_last = tok0[g.tok0 ? g.n_seq : 0];
-    if (token < (g.tok0 ? clamp_token(p, t_first) : 0) || token >= (g.tok0 ? clamp_token(p, t_last) : g.n_seq)) return;
-    const int rr = (int)(meta >> 48) & 15;
-    const uint32_t parts = (uint32_t)(meta >> 24) & 0xFFFFFFu, w = (uint32_t)meta & 0xFFFFFFu;
-    if (parts < 2 || w >= p.wgs || parts > p.wgs - w) return;
+// A running sum of parts: m the highest score, l the sum of weights, o that of weighted values.
+struct Joined {
     float m = kNegInf, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t i0 = (uint32_t)way; i0 < parts; i0 += kAhead * kWays) {
+    __device__ inline void add(float m1, float l1, const f32x4& o1) {
+        const float top = __builtin_fmaxf(m, m1), from = reference(top);
+        const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m) - from);
+        const float e = m1 == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m1) - from);
+        l = l * f + l1 * e;
+        o = o * f + o1 * e;
+        m = top;
+    }
+};
+
+// Parts `begin`, begin + step, .. of a row that begins in workgroup w's slots, the four channels from c on, with the loads
+// of four parts on their way.
+template <int D>
+__device__ inline Joined join_parts(const KvpAttendParams& p, uint32_t w, uint32_t parts, int row, uint32_t begin, uint32_t step, int c) {
+    constexpr int kAhead = 4;
+    Joined sum;
+    for (uint32_t i0 = begin; i0 < parts; i0 += kAhead * step) {
         f32x2 a[kAhead];
         f32x4 x[kAhead];
         #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const uint32_t i = i0 + k * kWays < parts ? i0 + k * kWays : i0;
+            const uint32_t i = i0 + k * step < parts ? i0 + k * step : i0;
             const int64_t slot = 2 * (int64_t)(w + i) + (i == 0 ? 1 : 0);
-            a[k] = *(const f32x2 __attribute__((address_space(1)))*)(p.part_ml + (slot * 16 + rr) * 2);
-            x[k] = *(const f32x4 __attribute__((address_space(1)))*)(p.part_o + (slot * 16 + rr) * D + c);
+            a[k] = *(const f32x2 __attribute__((address_space(1)))*)(p.part_ml + (slot * 16 + row) * 2);
+            x[k] = *(const f32x4 __attribute__((address_space(1)))*)(p.part_o + (slot * 16 + row) * D + c);
         }
         #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (i0 + k * kWays >= parts) continue;
-            const float top = __builtin_fmaxf(m, a[k][0]), from = reference(top);
-            const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m) - from);
-            const float e = a[k][0] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(a[k][0]) - from);
-            l = l * f + a[k][1] * e;
-            o = o * f + x[k] * e;
-            m = top;
+        for (int k = 0; k < kAhead; ++k)
+            if (i0 + k * step < parts) sum.add(a[k][0], a[k][1], x[k]);
+    }
+    return sum;
+}
+
+// Joins the parts of rows.  With FEW rows a workgroup has 64 channels of one, and 16 threads to a part, so that many parts
+// are read at once; else it has four rows, a wave each where they have few parts, and all of it one after another where
+// they have more.
+template <int D, bool FEW>
+__global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p) {
+    constexpr int kPer = FEW ? 16 : D / 4, kWays = kThreads / kPer, kBlocks = FEW ? D / 64 : 1, kRows = FEW ? 1 : 4;
+    constexpr int kWave = 64 / (D / 4);  // parts that a wave reads side by side
+    __shared__ __attribute__((aligned(16))) float o_s[kWays][4 * kPer];
+    __shared__ float m_s[kWays], l_s[kWays];
+    const KvpPages& g = p.pages;
+    const int64_t block = (int64_t)blockIdx.y * kFp8GridX + blockIdx.x, first = block / kBlocks * kRows, all = p.tokens * p.heads;
+    if (first >= all) return;
+    const int tid = (int)threadIdx.x, channel0 = (int)(block % kBlocks) * 64;
+    // rows that no sequence has: nothing was written for them
+    const int32_t* tok0 = g.tok0 ? g.tok0 : g.lens;
+    const int begin = tok0[0], end = tok0[g.tok0 ? g.n_seq : 0];
+    const int64_t low = (int64_t)(g.tok0 ? clamp_token(p, begin) : 0) * p.heads, high = (int64_t)(g.tok0 ? clamp_token(p, end) : g.n_seq) * p.heads;
+    uint64_t meta[kRows];
+    #pragma unroll
+    for (int i = 0; i < kRows; ++i) meta[i] = p.meta[first + i < all ? first + i : first];
+    auto parts_of = [&](int i) -> uint32_t {
+        const uint32_t parts = (uint32_t)(meta[i] >> 24) & 0xFFFFFFu, w = (uint32_t)meta[i] & 0xFFFFFFu;
+        return first + i >= low && first + i < high && first + i < all && w < p.wgs && parts <= p.wgs - w && parts >= 2 ? parts : 0;
+    };
+    auto write = [&](int64_t row, const Joined& x, int c) {
+        const float inv = x.l > 0.0f || x.l != x.l ? 1.0f / x.l : 0.0f;
+        const bf16x2 lo = __builtin_convertvector((f32x2){x.o[0] * inv, x.o[1] * inv}, bf16x2);
+        const bf16x2 hi = __builtin_convertvector((f32x2){x.o[2] * inv, x.o[3] * inv}, bf16x2);
+        *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + row * D + c) =
+            (u32x2){__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+        if (c == 0 && p.lse) p.lse[row] = (reference(x.m) + __builtin_amdgcn_logf(x.l)) * kLn2;
+    };
+    if constexpr (!FEW) {
+        const int wave = tid / 64, lane = tid % 64, c = lane % (D / 4) * 4;
+        uint64_t mine = meta[0];
+        uint32_t parts = parts_of(0);
+        #pragma unroll
+        for (int i = 1; i < kRows; ++i) {
+            if (wave == i) {
+                mine = meta[i];
+                parts = parts_of(i);
+            }
+        }
+        if (parts > 0 && parts <= 4 * kWave) {
+            Joined x = join_parts<D>(p, (uint32_t)mine & 0xFFFFFFu, parts, (int)(mine >> 48) & 15, (uint32_t)(lane / (D / 4)), kWave, c);
+            #pragma unroll
+            for (int step = D / 4; step < 64; step *= 2) {
+                Joined y;
+                y.m = __shfl_xor(x.m, step);
+                y.l = __shfl_xor(x.l, step);
+                #pragma unroll
+                for (int j = 0; j < 4; ++j) y.o[j] = __shfl_xor(x.o[j], step);
+                x.add(y.m, y.l, y.o);
+            }
+            if (lane < D / 4) write(first + wave, x, c);
         }
     }
-    if (tid % kPer == 0) {
-        ml_s[way][0] = m;
-        ml_s[way][1] = l;
-    }
-    *reinterpret_cast<f32x4*>(&o_s[way][tid % kPer * 4]) = o;
-    __syncthreads();
-    if (tid >= 64) return;
-    // a thread to each channel
-    float top = kNegInf, sum = 0.0f, total = 0.0f;
     #pragma unroll
-    for (int i = 0; i < kWays; ++i) top = __builtin_fmaxf(top, ml_s[i][0]);
-    #pragma unroll
-    for (int i = 0; i < kWays; ++i) {
-        const float e = ml_s[i][0] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(ml_s[i][0]) - reference(top));
-        total += ml_s[i][1] * e;
-        sum += o_s[i][tid] * e;
+    for (int i = 0; i < kRows; ++i) {
+        const uint32_t parts = parts_of(i);
+        if (parts == 0 || (!FEW && parts <= 4 * kWave)) continue;
+        const int way = tid / kPer, c = tid % kPer * 4;
+        Joined x = join_parts<D>(p, (uint32_t)meta[i] & 0xFFFFFFu, parts, (int)(meta[i] >> 48) & 15, (uint32_t)way, kWays, channel0 + c);
+        __syncthreads();
+        if (c == 0) m_s[way] = x.m;
+        __syncthreads();
+        float top = kNegInf;
+        #pragma unroll
+        for (int j = 0; j < kWays; ++j) top = __builtin_fmaxf(top, m_s[j]);
+        const float e = x.m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(x.m) - reference(top));
+        *reinterpret_cast<f32x4*>(&o_s[way][c]) = x.o * e;
+        if (c == 0) l_s[way] = x.l * e;
+        __syncthreads();
+        if (way) continue;
+        Joined y;
+        y.m = top;
+        #pragma unroll
+        for (int j = 0; j < kWays; ++j) {
+            y.l += l_s[j];
+            y.o += *reinterpret_cast<const f32x4*>(&o_s[j][c]);
+        }
+        write(first + i, y, channel0 + c);
     }
-    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-    const int ch = (int)(block % kBlocks) * 64 + tid;
-    static_cast<__bf16*>(p.o)[out * D + ch] = (__bf16)(sum * inv);
-    if (ch == 0 && p.lse) p.lse[out] = (reference(top) + __builtin_amdgcn_logf(total)) * kLn2;
 }
+
+#ifndef KFEW
+#define KFEW 1024
+#endif
+constexpr uint64_t kFewRows = KFEW;
 
 template <int D>
 hipError_t launch(const KvpAttendParams& p, hipStream_t stream) {
     void* args[] = {const_cast<KvpAttendParams*>(&p)};
     const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&attend_kernel<D>), dim3(p.wgs), dim3(kThreads), args, 0, stream);
     if (e != hipSuccess || p.whole) return e;
-    return hipLaunchKernel(reinterpret_cast<const void*>(&join_kernel<D>), wide_grid((uint64_t)(p.tokens * p.heads) * (D / 64)), dim3(kThreads), args, 0, stream);
+    const uint64_t rows = (uint64_t)p.tokens * (uint64_t)p.heads;
+    if (rows * (D / 64) <= kFewRows)
+        return hipLaunchKernel(reinterpret_cast<const void*>(&join_kernel<D, true>), wide_grid(rows * (D / 64)), dim3(kThreads), args, 0, stream);
+    return hipLaunchKernel(reinterpret_cast<const void*>(&join_kernel<D, false>), wide_grid((rows + 3) / 4), dim3(kThreads), args, 0, stream);
 }
 
 }  // namespace
