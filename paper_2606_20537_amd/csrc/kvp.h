@@ -73,14 +73,14 @@ struct KvpAttendParams {
     QkRows   q;
     void*    o;
     float*   lse;      // may be null
-    float*   part_o;   // [2 wgs][16][d], not divided by l
-    float*   part_ml;  // [2 wgs][16][2]: highest score (log2 units), sum
+    float*   part_o;   // [2 wgs][tile][d], not divided by l
+    float*   part_ml;  // [2 wgs][tile][2]: highest score (log2 units), sum
     uint64_t* meta;    // [tokens, heads]: first workgroup, parts, row of the segment
     int64_t  tokens;
     int32_t  heads, d, window;
     uint32_t wgs;
+    int32_t  tile;     // query rows of a segment: 16, 32 or 64
     int32_t  begin;    // units that the beginning of a segment counts for
-    uint32_t least;    // units of a run at least
     int32_t  whole;    // segments are not cut, and there is no second launch
     float    scale_log2;
     Divisor  by_group, by_kv_heads;  // heads / kv_heads, kv_heads

@@ -30,9 +30,6 @@
 #include "device_util.h"
 #include "kvp.h"
 
-#ifndef KAUX
-#define KAUX 2
-#endif
 namespace cap {
 namespace {
 
@@ -50,6 +47,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 // Weights are 2^-24 of what exp(x - m) gives, so that sums of 2^24 values, the most that a
 // sequence has, cannot overflow and means of finite values stay finite.
 constexpr float kAbove = 24.0f;
+// Parts of even cuts at least (a unit to each wave) and at most; with longer ones equal runs leave fewer workgroups idle.
+constexpr uint32_t kLeastCut = 4, kMostCut = 16;
 
 typedef const char __attribute__((address_space(1)))* global_bytes;
 typedef __attribute__((address_space(3))) char* lds_bytes;
@@ -128,7 +127,7 @@ __device__ inline void read_v8(const uint32_t (&at)[8], u32x2 (&x)[16]) {
 }
 // 1 KiB into LDS, 16 bytes from each lane's address.
 __device__ inline void load_lds(global_bytes from, lds_bytes to) {
-    __builtin_amdgcn_global_load_lds((lds_source)from, (lds_target)to, 16, 0, KAUX);  // (2: streamed)
+    __builtin_amdgcn_global_load_lds((lds_source)from, (lds_target)to, 16, 0, 2);  // (2: streamed)
 }
 // What a row's number changes in the places of its pieces: rows that lie over the same banks differ.
 template <int D>
@@ -207,12 +206,13 @@ __device__ inline uint32_t lane_u32(uint32_t x, int l) { return (uint32_t)__buil
 struct Seq {
     int n, t0, T;      // rows held, first packed token, tokens
     int first, units;  // first unit, number of units (1 at least where T > 0)
-    int tiles;         // of 16 query rows
-    uint32_t weight;   // units of all its segments, with their beginnings
+    int tiles;         // of 16 NT query rows
+    uint32_t segments; // tiles times KV heads
 };
 
 __device__ inline int clamp_token(const KvpAttendParams& p, int t) { return t < 0 ? 0 : t > p.tokens ? (int)p.tokens : t; }
 
+template <int NT>
 __device__ inline Seq load_seq(const KvpAttendParams& p, int group, int s) {
     const KvpPages& g = p.pages;
     Seq q = {};
@@ -234,13 +234,13 @@ __device__ inline Seq load_seq(const KvpAttendParams& p, int group, int s) {
     q.first = lo / kKvpUnit;
     q.units = (hi + kKvpUnit - 1) / kKvpUnit - q.first;
     if (q.units < 1) q.units = 1;
-    q.tiles = (q.T * group + 15) / 16;  // (tokens * heads fits 31 bits)
-    q.weight = (uint32_t)q.tiles * (uint32_t)g.kv_heads * (uint32_t)(q.units + p.begin);
+    q.tiles = (q.T * group + 16 * NT - 1) / (16 * NT);  // (tokens * heads fits 31 bits)
+    q.segments = (uint32_t)q.tiles * (uint32_t)g.kv_heads;
     return q;
 }
 
-template <int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void attend_kernel(const KvpAttendParams p) {
+template <int D, int NT>
+__global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void attend_kernel(const KvpAttendParams p) {
     constexpr int NJ = D / 32;                        // K: fragments of 32 channels
     constexpr int NC = D / 16;                        // V: blocks of 16 channels
     constexpr int kPitch = D + 4;
@@ -257,12 +257,30 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
 
     // the run [begin, end) of this workgroup
     const int chunks = (g.n_seq + 63) / 64;
-    Seq q = load_seq(p, G, (int)(threadIdx.x & 63));
-    uint32_t scan = scan_lanes(q.weight), before = 0;
-    uint32_t total = lane_u32(scan, 63);
-    for (int c = 1; c < chunks; ++c) total += lane_u32(scan_lanes(load_seq(p, G, 64 * c + (int)(threadIdx.x & 63)).weight), 63);
-    uint32_t per = (total + p.wgs - 1) / p.wgs;
-    if (per < p.least) per = p.least;
+    Seq q = load_seq<NT>(p, G, (int)(threadIdx.x & 63));
+    uint32_t segments = scan_lanes(q.segments), units_to = scan_lanes(q.segments * (uint32_t)q.units), before = 0;
+    uint32_t all_segments = lane_u32(segments, 63), all_units = lane_u32(units_to, 63);
+    for (int c = 1; c < chunks; ++c) {
+        const Seq r = load_seq<NT>(p, G, 64 * c + (int)(threadIdx.x & 63));
+        all_segments += lane_u32(scan_lanes(r.segments), 63);
+        all_units += lane_u32(scan_lanes(r.segments * (uint32_t)r.units), 63);
+    }
+    // Little work: segments are cut into even parts of `cut` units at most, a workgroup each (segments + units /
+    // cut are no more than there are workgroups).  More: units in a row, each segment's with `extra` before them
+    // for what its beginning costs, are dealt out in equal runs.
+    uint32_t cut = 0, by_cut = 0;
+    const uint32_t extra = (uint32_t)p.begin;
+    if (!p.whole && all_segments < p.wgs) {
+        cut = all_units / (p.wgs - all_segments) + 1;
+        if (cut < kLeastCut) cut = kLeastCut;
+        if (cut > kMostCut) cut = 0;
+        else by_cut = 0xFFFFFFFFu / cut + 1;
+    }
+    auto size_of = [&](uint32_t units) -> uint32_t {
+        return cut ? (uint32_t)((uint64_t)(units + cut - 1) * by_cut >> 32) : units + extra;
+    };
+    const uint32_t total = cut ? p.wgs : all_units + extra * all_segments, per = cut ? 1 : (total + p.wgs - 1) / p.wgs;
+    uint32_t scan = cut ? scan_lanes(q.segments * size_of((uint32_t)q.units)) : units_to + extra * segments;
     const uint32_t begin = w * per;
     if (begin >= total) return;
     const uint32_t end = begin + per < total ? begin + per : total;
@@ -276,23 +294,27 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         while (at - before >= lane_u32(scan, 63)) {
             before += lane_u32(scan, 63);
             if (++chunk >= chunks) return;
-            q = load_seq(p, G, 64 * chunk + lane);
-            scan = scan_lanes(q.weight);
+            q = load_seq<NT>(p, G, 64 * chunk + lane);
+            scan = scan_lanes(q.segments * size_of((uint32_t)q.units));
         }
         const int s = __builtin_popcountll(__ballot(scan <= at - before));
         if (s > 63) return;
         const int n = lane_int(q.n, s), seq_t0 = lane_int(q.t0, s), T = lane_int(q.T, s), units = lane_int(q.units, s);
-        const uint32_t weight = lane_u32(q.weight, s), base = before + lane_u32(scan, s) - weight;
-        const uint32_t size = (uint32_t)(units + p.begin);
+        const uint32_t size = size_of((uint32_t)units), weight = lane_u32(q.segments, s) * size, base = before + lane_u32(scan, s) - weight;
         if (at - base >= weight) return;
         const int segment = (int)((at - base) / size);
         const uint32_t seg0 = base + (uint32_t)segment * size;  // of the segment
         const uint32_t next = seg0 + size;
-        const uint32_t unit0 = seg0 + p.begin;                // of its first unit
+        const uint32_t unit0 = cut ? seg0 : seg0 + extra;                // of its first unit
         int u0 = 0, u1 = units;
         if (p.whole) {
             at = next;
             if (seg0 < begin) continue;  // its beginning was another workgroup's
+        } else if (cut) {
+            const int part = (int)(((uint32_t)units + size - 1) / size);
+            u0 = (int)(at - seg0) * part;
+            u1 = u0 + part < units ? u0 + part : units;
+            at = next;
         } else {
             u0 = at > unit0 ? (int)(at - unit0) : 0;
             u1 = end < next ? (int)(end - unit0) : units;
@@ -303,21 +325,22 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         const KvpAttendParams& args = *hidden_arguments<KvpAttendParams>();
         const KvpPages& gp = args.pages;
         const float scale_log2 = args.scale_log2;
-        const bool windowed = args.window > 0;
         const int tile = divide(segment, args.by_kv_heads), h = segment - tile * gp.kv_heads;
         const int first_unit = lane_int(q.first, s);
         const int seq = 64 * chunk + s;
 
-        const int total_rows = T * G, r0 = tile * 16;
-        const int rows = total_rows - r0 < 16 ? total_rows - r0 : 16;
-        const int row = r0 + (li < rows ? li : rows - 1);  // rows past the last repeat it
-        const int my_t = divide(row, args.by_group);
-        const int pos = n - T + my_t;
+        const int r0 = tile * (16 * NT), rows = T * G - r0 < 16 * NT ? T * G - r0 : 16 * NT;
+        // row 16 i + li of the tile (those past the last repeat it): its token; it sees the keys in (low, pos]
+        int row_t[NT], pos[NT], low[NT];
+        auto below = [&](int pos) { return args.window > 0 ? (pos < 0 ? -1 : pos - args.window) : -1; };
+        #pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            row_t[i] = divide(r0 + (16 * i + li < rows ? 16 * i + li : rows - 1), args.by_group);
+            pos[i] = n - T + row_t[i];
+            low[i] = below(pos[i]);
+        }
         const int pos0 = n - T + divide(r0, args.by_group), pos1 = n - T + divide(r0 + rows - 1, args.by_group);
-        const int window = args.window > 0 ? args.window : 0x7fffffff;
-        // keys above low are seen: pos - window, without passing 32 bits
-        const int low = args.window > 0 ? (pos < 0 ? -1 : pos - window) : -1;
-        const int low0 = args.window > 0 ? (pos0 < 0 ? -1 : pos0 - window) : -1, low1 = args.window > 0 ? (pos1 < 0 ? -1 : pos1 - window) : -1;
+        const int low0 = below(pos0), low1 = below(pos1);
 
         // Where a wave's next 64 units have their two groups of 16 rows in the pools, a lane each (unit u0 + wave
         // + 4 (step0 + lane)); -1: on no page.
@@ -349,18 +372,25 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
         };
 
         // the query rows, while the table is on its way
-        bf16x8 qf[NJ];
-        {
-            const global_bytes src = (global_bytes)args.q.p + (int64_t)(seq_t0 + my_t) * args.q.token +
-                                     (int64_t)(h * G + (row - my_t * G)) * args.q.head + 16 * grp;
+        bf16x8 qf[NT][NJ];
+        #pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int row = r0 + (16 * i + li < rows ? 16 * i + li : rows - 1);
+            const global_bytes src = (global_bytes)args.q.p + (int64_t)(seq_t0 + row_t[i]) * args.q.token +
+                                     (int64_t)(h * G + (row - row_t[i] * G)) * args.q.head + 16 * grp;
             #pragma unroll
-            for (int j = 0; j < NJ; ++j) qf[j] = *(const bf16x8 __attribute__((address_space(1)))*)(src + 64 * j);
+            for (int j = 0; j < NJ; ++j) qf[i][j] = *(const bf16x8 __attribute__((address_space(1)))*)(src + 64 * j);
         }
 
-        f32x4 acc[NC];  // channels 16 c + 4 grp ..
+        f32x4 acc[NT][NC];  // channels 16 c + 4 grp ..
+        float m[NT], l[NT];
         #pragma unroll
-        for (int c = 0; c < NC; ++c) acc[c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-        float m = kNegInf, l = 0.0f;
+        for (int i = 0; i < NT; ++i) {
+            m[i] = kNegInf;
+            l[i] = 0.0f;
+            #pragma unroll
+            for (int c = 0; c < NC; ++c) acc[i][c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+        }
 
         // Units in LDS, a slot for K and one for V to each wave: rows of D channels, in which 16 bytes (K: those of channels
         // 8 c .. at the place of c ^ fold_k(row)) or 32 (V: 16 c .., c ^ fold_v(row)) change places, so that reads of 16 rows
@@ -393,11 +423,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
                 load_lds(vb + a[i * kRows / 16] + row * rowb + (from ^ (uint32_t)(fold_v<D>(row) << 5)), v_slot + i * 1024);
             }
         };
-        float x[8];
+        float x[NT][8];
         auto scores = [&]() {
             const uint32_t from = hidden(kread);
-            f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
-            constexpr int kAtOnce = NJ;
+            f32x4 sums[NT][2];
+            #pragma unroll
+            for (int i = 0; i < NT; ++i) sums[i][0] = sums[i][1] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+            constexpr int kAtOnce = NT > 1 && NJ > 4 ? 2 : NJ;
             #pragma unroll
             for (int j0 = 0; j0 < NJ; j0 += kAtOnce) {
                 uint32_t at[kAtOnce];
@@ -408,52 +440,57 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
                 else if constexpr (kAtOnce == 4) read_k4<16 * D * 2>(at, k);
                 else read_k8<16 * D * 2>(at, k);
                 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) {
-                    s0 = dev::mma(__builtin_bit_cast(bf16x8, k[2 * j]), qf[j0 + j], s0);
-                    s1 = dev::mma(__builtin_bit_cast(bf16x8, k[2 * j + 1]), qf[j0 + j], s1);
-                }
+                for (int j = 0; j < kAtOnce; ++j)
+                    #pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        sums[i][0] = dev::mma(__builtin_bit_cast(bf16x8, k[2 * j]), qf[i][j0 + j], sums[i][0]);
+                        sums[i][1] = dev::mma(__builtin_bit_cast(bf16x8, k[2 * j + 1]), qf[i][j0 + j], sums[i][1]);
+                    }
             }
             #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = s0[e] * scale_log2;
-                x[4 + e] = s1[e] * scale_log2;
-            }
+            for (int i = 0; i < NT; ++i)
+                #pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] = sums[i][e / 4][e % 4] * scale_log2;
         };
         // x becomes the weights.  hi is cut off, not rounded, and lo above zero, so that an infinity in V, times both, is
         // one (lo: 2^-16 of the weight; 2^-20 at least).
-        auto weigh = [&](bf16x8& hi, bf16x8& lo) {
-            float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3])),
-                                        __builtin_fmaxf(__builtin_fmaxf(x[4], x[5]), __builtin_fmaxf(x[6], x[7])));
-            top = __builtin_fmaxf(m, group_max(top));
-            const float from = reference(top);
-            const float fade = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(reference(m) - from);
-            m = top;
-            float sum = 0.0f;
+        auto weigh = [&](bf16x8 (&hi)[NT], bf16x8 (&lo)[NT]) {
             #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = __builtin_amdgcn_exp2f(x[e] - from);
-                sum += x[e];
-            }
-            u32x4 h, low_part;
-            #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                h[e / 2] = __builtin_amdgcn_perm(f32_bits(x[e + 1]), f32_bits(x[e]), 0x07060302u);
-                const float h0 = bits_f32(h[e / 2] << 16), h1 = bits_f32(h[e / 2] & 0xFFFF0000u);
-                low_part[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
-                    (f32x2){__builtin_fmaxf(x[e] - h0, h0 * 0x1p-20f), __builtin_fmaxf(x[e + 1] - h1, h1 * 0x1p-20f)}, bf16x2));
-            }
-            hi = __builtin_bit_cast(bf16x8, h);
-            lo = __builtin_bit_cast(bf16x8, low_part);
-            l = l * fade + sum;
-            if (__any(fade != 1.0f)) {
+            for (int i = 0; i < NT; ++i) {
+                float top = x[i][0];
                 #pragma unroll
-                for (int c = 0; c < NC; ++c) acc[c] *= fade;
+                for (int e = 1; e < 8; ++e) top = __builtin_fmaxf(top, x[i][e]);
+                top = __builtin_fmaxf(m[i], group_max(top));
+                const float from = reference(top);
+                const float fade = m[i] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(reference(m[i]) - from);
+                m[i] = top;
+                float sum = 0.0f;
+                #pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[i][e] = __builtin_amdgcn_exp2f(x[i][e] - from);
+                    sum += x[i][e];
+                }
+                u32x4 h, low_part;
+                #pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    h[e / 2] = __builtin_amdgcn_perm(f32_bits(x[i][e + 1]), f32_bits(x[i][e]), 0x07060302u);
+                    const float h0 = bits_f32(h[e / 2] << 16), h1 = bits_f32(h[e / 2] & 0xFFFF0000u);
+                    low_part[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                        (f32x2){__builtin_fmaxf(x[i][e] - h0, h0 * 0x1p-20f), __builtin_fmaxf(x[i][e + 1] - h1, h1 * 0x1p-20f)}, bf16x2));
+                }
+                hi[i] = __builtin_bit_cast(bf16x8, h);
+                lo[i] = __builtin_bit_cast(bf16x8, low_part);
+                l[i] = l[i] * fade + sum;
+                if (__any(fade != 1.0f)) {
+                    #pragma unroll
+                    for (int c = 0; c < NC; ++c) acc[i][c] *= fade;
+                }
             }
         };
         // f(c, the eight keys of a lane in channel 16 c + li), for all blocks of 16 channels.
         auto each_block = [&](auto&& f) {
             const uint32_t from = hidden(vread);
-            constexpr int kAtOnce = NC < 8 ? 4 : 8;
+            constexpr int kAtOnce = NC < 8 || NT > 1 ? 4 : 8;
             #pragma unroll
             for (int c0 = 0; c0 < NC; c0 += kAtOnce) {
                 uint32_t at[kAtOnce];
@@ -466,55 +503,74 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
                 for (int c = 0; c < kAtOnce; ++c) f(c0 + c, (u32x4){v[2 * c][0], v[2 * c][1], v[2 * c + 1][0], v[2 * c + 1][1]});
             }
         };
-        auto add_values = [&](const bf16x8& hi, const bf16x8& lo) {
+        auto add_values = [&](const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT]) {
             each_block([&](int c, const u32x4& v) {
-                acc[c] = dev::mma(__builtin_bit_cast(bf16x8, v), hi, acc[c]);
-                acc[c] = dev::mma(__builtin_bit_cast(bf16x8, v), lo, acc[c]);
+                #pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    acc[i][c] = dev::mma(__builtin_bit_cast(bf16x8, v), hi[i], acc[i][c]);
+                    acc[i][c] = dev::mma(__builtin_bit_cast(bf16x8, v), lo[i], acc[i][c]);
+                }
             });
         };
 
         // In a unit that some row does not see in full, or that lies on no page in part (there: the halves that are on
         // one), a key that a row does not see has to leave the product, as its V may hold an infinity or NaN, of which
-        // no weight makes zero: keys that no row sees are cleared; where one that some rows see and
-        // others do not holds such a value, the rows of each position are taken by themselves.
+        // no weight makes zero.  Keys that no row sees are cleared, and where rows see different ones, such
+        // values of all keys are; they are put back, row by row, from memory (at: the unit's).
         auto seen = [&](int r, int there, int e, int first, int last) {  // key e lies on a page and in (first, last]
             const int key = r + 4 * grp + (e < 4 ? e : 12 + e);
             return (there >> (e / 4) & 1) && key <= last && key > first;
         };
-        auto add_seen_values = [&](int r, int there, const bf16x8& hi, const bf16x8& lo) {
-            int first = low0, last = pos1, at = pos1;
-            bool each = false;
-            for (bool look = pos0 != pos1; at <= pos1;) {
-                uint32_t keep[4];  // bits of keys 2i and 2i + 1
+        auto add_seen_values = [&](int r, int there, const int64_t (&at)[2], const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT]) {
+            uint32_t keep[4];  // bits of keys 2i and 2i + 1
+            #pragma unroll
+            for (int i = 0; i < 4; ++i)
+                keep[i] = (seen(r, there, 2 * i, low0, pos1) ? 0xFFFFu : 0u) | (seen(r, there, 2 * i + 1, low0, pos1) ? 0xFFFF0000u : 0u);
+            const bool mixed = pos0 != pos1;
+            bool found = false;
+            each_block([&](int c, u32x4 v) {
                 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    keep[i] = (seen(r, there, 2 * i, first, last) ? 0xFFFFu : 0u) | (seen(r, there, 2 * i + 1, first, last) ? 0xFFFF0000u : 0u);
-                if (look) {
-                    bool found = false;
-                    each_block([&](int, const u32x4& v) {
-                        #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t d = v[i] & keep[i] & 0x7F807F80u;
-                            found |= (d & 0xFFFFu) == 0x7F80u || (d >> 16) == 0x7F80u;
-                        }
-                    });
-                    look = false;
-                    each = __any(found);
-                    if (!each) continue;
-                    at = pos0;
-                } else {
-                    each_block([&](int c, u32x4 v) {
-                        #pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] &= keep[i];
-                        f32x4 sum = dev::mma(__builtin_bit_cast(bf16x8, v), hi, acc[c]);
-                        sum = dev::mma(__builtin_bit_cast(bf16x8, v), lo, sum);
-                        #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[c][j] = !each || pos == at ? sum[j] : acc[c][j];
-                    });
-                    ++at;
+                for (int i = 0; i < 4; ++i) {
+                    v[i] &= keep[i];
+                    const uint32_t out = ((v[i] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((v[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+                    if (mixed) {
+                        found |= out != 0;
+                        v[i] &= ~out;
+                    }
                 }
-                first = windowed ? (at < 0 ? -1 : at - window) : -1;
-                last = at;
+                #pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    acc[i][c] = dev::mma(__builtin_bit_cast(bf16x8, v), hi[i], acc[i][c]);
+                    acc[i][c] = dev::mma(__builtin_bit_cast(bf16x8, v), lo[i], acc[i][c]);
+                }
+            });
+            if (!__any(found)) return;
+            #pragma unroll 1
+            for (int t = 0; t < kKvpUnit; ++t) {
+                const int key = r + t, e = (t & 3) + (t >= 16 ? 4 : 0);
+                if (!(there >> (t / 16) & 1) || key > pos1 || key <= low0) continue;  // (uniform)
+                const global_bytes from = vb + at[t / 16] + (int64_t)(t % 16) * rowb + (uint32_t)(h * D * 2 + 8 * grp);
+                float weight[NT];
+                #pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    float mine = x[i][0];
+                    #pragma unroll
+                    for (int k = 1; k < 8; ++k) mine = e == k ? x[i][k] : mine;
+                    weight[i] = __shfl(mine, li + 16 * (t % 16 / 4));
+                }
+                #pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const u32x2 four = *(const u32x2 __attribute__((address_space(1)))*)(from + 32 * c);
+                    #pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float value = bits_f32(j & 1 ? four[j / 2] & 0xFFFF0000u : four[j / 2] << 16);
+                        const bool back = (f32_bits(value) & 0x7F800000u) == 0x7F800000u;
+                        #pragma unroll
+                        for (int i = 0; i < NT; ++i)
+                            if (back && key <= pos[i] && key > low[i]) acc[i][c][j] += weight[i] * value;
+                    }
+                }
             }
         };
 
@@ -546,6 +602,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
                 todo &= todo - 1;
                 const bool more = todo != 0;
                 const int r = (first_unit + u0 + wave + 4 * (step0 + j)) * kKvpUnit, there_now = there;
+                const int64_t now[2] = {a[0], a[1]};
                 const bool all = whole >> j & 1;
                 wait_loads<kLoads>();  // K: V's are behind it
                 scores();
@@ -557,75 +614,82 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 4) void att
                 }
                 if (!all) {
                     #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = seen(r, there_now, e, low, pos) ? x[e] : kNegInf;
+                    for (int i = 0; i < NT; ++i)
+                        #pragma unroll
+                        for (int e = 0; e < 8; ++e) x[i][e] = seen(r, there_now, e, low[i], pos[i]) ? x[i][e] : kNegInf;
                 }
-                bf16x8 hi, lo;
+                bf16x8 hi[NT], lo[NT];
                 weigh(hi, lo);
                 if (more) wait_loads<kLoads>();  // V: the next K's are behind it
                 else wait_loads<0>();
                 if (all) add_values(hi, lo);
-                else add_seen_values(r, there_now, hi, lo);
+                else add_seen_values(r, there_now, now, hi, lo);
                 if (!more) break;
                 wait_lds();
                 load_v(a);
             }
         }
 
-        // join the waves
-        l = group_sum(l);
-        __syncthreads();  // V, and the last segment's values, are done with
-        if (grp == 0) {
-            ml_s[wave][li][0] = m;
-            ml_s[wave][li][1] = l;
-        }
-        __syncthreads();
-        float top = kNegInf, sum = 0.0f;
-        #pragma unroll
-        for (int i = 0; i < 4; ++i) top = __builtin_fmaxf(top, ml_s[i][li][0]);
-        const float from = reference(top);
-        #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            sum += ml_s[i][li][0] == kNegInf ? ml_s[i][li][1] : ml_s[i][li][1] * __builtin_amdgcn_exp2f(reference(ml_s[i][li][0]) - from);
-        const float fade = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m) - from);
-        // (m is -inf where the wave saw nothing: zeros; or only NaN, which stays)
-        #pragma unroll
-        for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4*>(&o_s[wave][li][16 * c + 4 * grp]) = acc[c] * fade;
-        if (tid < 16) {  // wave 0: lane = row
-            all_s[li][0] = top;
-            all_s[li][1] = sum;
-        }
-        __syncthreads();
-        // whether the segment's first unit is of this run, and all of them
         const KvpAttendParams& late = *hidden_arguments<KvpAttendParams>();
+        // whether the segment's first unit is of this run, and all of them
         const bool begins = late.whole || unit0 >= begin, one = late.whole || (begins && next <= end);
-        const uint32_t slot = 2 * w + (begins ? 1 : 0);
-        constexpr int kPer = D / 4;  // threads of a row
-        #pragma unroll
-        for (int i = 0; i < 16 * kPer / kThreads; ++i) {
-            const int rr = (i * kThreads + hidden(tid)) / kPer, c = (tid % kPer) * 4;
-            if (rr >= rows) continue;
-            f32x4 o = *reinterpret_cast<const f32x4*>(&o_s[0][rr][c]);
-            #pragma unroll
-            for (int j = 1; j < 4; ++j) o += *reinterpret_cast<const f32x4*>(&o_s[j][rr][c]);
-            if (!one) {
-                *reinterpret_cast<f32x4*>(late.part_o + ((int64_t)slot * 16 + rr) * D + c) = o;
-                continue;
-            }
-            const float z = all_s[rr][1], inv = z > 0.0f || z != z ? 1.0f / z : 0.0f;
+        const int64_t part0 = (int64_t)(2 * w + (begins ? 1 : 0)) * (16 * NT);
+        auto out_row = [&](int rr) -> int64_t {
             const int t = divide(r0 + rr, late.by_group);
-            const int64_t to = ((int64_t)(seq_t0 + t) * late.heads + h * G + (r0 + rr - t * G)) * D + c;
-            const bf16x2 lo2 = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
-            const bf16x2 hi2 = __builtin_convertvector((f32x2){o[2] * inv, o[3] * inv}, bf16x2);
-            *reinterpret_cast<u32x2*>(static_cast<__bf16*>(late.o) + to) =
-                (u32x2){__builtin_bit_cast(uint32_t, lo2), __builtin_bit_cast(uint32_t, hi2)};
-        }
-        if (tid < rows) {
-            const float mm = all_s[tid][0], z = all_s[tid][1];
-            const int t = divide(r0 + tid, late.by_group);
-            const int64_t to = (int64_t)(seq_t0 + t) * late.heads + h * G + (r0 + tid - t * G);
-            if (!one) *reinterpret_cast<f32x2*>(late.part_ml + ((int64_t)slot * 16 + tid) * 2) = (f32x2){mm, z};
-            else if (late.lse) late.lse[to] = (reference(mm) + __builtin_amdgcn_logf(z)) * kLn2;
-            if (!late.whole && begins) late.meta[to] = (uint64_t)tid << 48 | (uint64_t)((next - 1) / per - w + 1) << 24 | w;
+            return (int64_t)(seq_t0 + t) * late.heads + h * G + (r0 + rr - t * G);
+        };
+        #pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            if (16 * i >= rows) break;
+            const float my_l = group_sum(l[i]);
+            __syncthreads();  // K and V, and the values before these, are done with
+            if (grp == 0) {
+                ml_s[wave][li][0] = m[i];
+                ml_s[wave][li][1] = my_l;
+            }
+            __syncthreads();
+            float top = kNegInf, sum = 0.0f;
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) top = __builtin_fmaxf(top, ml_s[k][li][0]);
+            const float from = reference(top);
+            #pragma unroll
+            for (int k = 0; k < 4; ++k)
+                sum += ml_s[k][li][0] == kNegInf ? ml_s[k][li][1] : ml_s[k][li][1] * __builtin_amdgcn_exp2f(reference(ml_s[k][li][0]) - from);
+            const float fade = m[i] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m[i]) - from);
+            // (m is -inf where the wave saw nothing: zeros; or only NaN, which stays)
+            #pragma unroll
+            for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4*>(&o_s[wave][li][16 * c + 4 * grp]) = acc[i][c] * fade;
+            if (tid < 16) {  // wave 0: lane = row
+                all_s[li][0] = top;
+                all_s[li][1] = sum;
+            }
+            __syncthreads();
+            constexpr int kPer = D / 4;  // threads of a row
+            #pragma unroll
+            for (int k = 0; k < 16 * kPer / kThreads; ++k) {
+                const int r16 = (k * kThreads + hidden(tid)) / kPer, rr = 16 * i + r16, c = (tid % kPer) * 4;
+                if (rr >= rows) continue;
+                f32x4 o = *reinterpret_cast<const f32x4*>(&o_s[0][r16][c]);
+                #pragma unroll
+                for (int j = 1; j < 4; ++j) o += *reinterpret_cast<const f32x4*>(&o_s[j][r16][c]);
+                if (!one) {
+                    *reinterpret_cast<f32x4*>(late.part_o + (part0 + rr) * D + c) = o;
+                    continue;
+                }
+                const float z = all_s[r16][1], inv = z > 0.0f || z != z ? 1.0f / z : 0.0f;
+                const bf16x2 lo2 = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
+                const bf16x2 hi2 = __builtin_convertvector((f32x2){o[2] * inv, o[3] * inv}, bf16x2);
+                *reinterpret_cast<u32x2*>(static_cast<__bf16*>(late.o) + out_row(rr) * D + c) =
+                    (u32x2){__builtin_bit_cast(uint32_t, lo2), __builtin_bit_cast(uint32_t, hi2)};
+            }
+            if (tid < 16 && 16 * i + tid < rows) {
+                const int rr = 16 * i + tid;
+                const int64_t to = out_row(rr);
+                const float mm = all_s[tid][0], z = all_s[tid][1];
+                if (!one) *reinterpret_cast<f32x2*>(late.part_ml + (part0 + rr) * 2) = (f32x2){mm, z};
+                else if (late.lse) late.lse[to] = (reference(mm) + __builtin_amdgcn_logf(z)) * kLn2;
+                if (!late.whole && begins) late.meta[to] = (uint64_t)rr << 48 | (uint64_t)((next - 1) / per - w + 1) << 24 | w;
+            }
         }
     }
 }
@@ -657,8 +721,8 @@ __device__ inline Joined join_parts(const KvpAttendParams& p, uint32_t w, uint32
         for (int k = 0; k < kAhead; ++k) {
             const uint32_t i = i0 + k * step < parts ? i0 + k * step : i0;
             const int64_t slot = 2 * (int64_t)(w + i) + (i == 0 ? 1 : 0);
-            a[k] = *(const f32x2 __attribute__((address_space(1)))*)(p.part_ml + (slot * 16 + row) * 2);
-            x[k] = *(const f32x4 __attribute__((address_space(1)))*)(p.part_o + (slot * 16 + row) * D + c);
+            a[k] = *(const f32x2 __attribute__((address_space(1)))*)(p.part_ml + (slot * p.tile + row) * 2);
+            x[k] = *(const f32x4 __attribute__((address_space(1)))*)(p.part_o + (slot * p.tile + row) * D + c);
         }
         #pragma unroll
         for (int k = 0; k < kAhead; ++k)
@@ -711,7 +775,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
             }
         }
         if (parts > 0 && parts <= 4 * kWave) {
-            Joined x = join_parts<D>(p, (uint32_t)mine & 0xFFFFFFu, parts, (int)(mine >> 48) & 15, (uint32_t)(lane / (D / 4)), kWave, c);
+            Joined x = join_parts<D>(p, (uint32_t)mine & 0xFFFFFFu, parts, (int)(mine >> 48) & (p.tile - 1), (uint32_t)(lane / (D / 4)), kWave, c);
             #pragma unroll
             for (int step = D / 4; step < 64; step *= 2) {
                 Joined y;
@@ -729,7 +793,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
         const uint32_t parts = parts_of(i);
         if (parts == 0 || (!FEW && parts <= 4 * kWave)) continue;
         const int way = tid / kPer, c = tid % kPer * 4;
-        Joined x = join_parts<D>(p, (uint32_t)meta[i] & 0xFFFFFFu, parts, (int)(meta[i] >> 48) & 15, (uint32_t)way, kWays, channel0 + c);
+        Joined x = join_parts<D>(p, (uint32_t)meta[i] & 0xFFFFFFu, parts, (int)(meta[i] >> 48) & (p.tile - 1), (uint32_t)way, kWays, channel0 + c);
         __syncthreads();
         if (c == 0) m_s[way] = x.m;
         __syncthreads();
@@ -752,15 +816,16 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
     }
 }
 
-#ifndef KFEW
-#define KFEW 1024
-#endif
-constexpr uint64_t kFewRows = KFEW;
+// Workgroups of the join at most with 16 threads to a part: 192 tokens x 16 heads of 128 channels, two parts each, took 8.1 us
+// so and 5.2 with four rows to a workgroup; 32 rows of 57 parts 4.0 and 7.8.
+constexpr uint64_t kFewRows = 1024;
 
 template <int D>
 hipError_t launch(const KvpAttendParams& p, hipStream_t stream) {
     void* args[] = {const_cast<KvpAttendParams*>(&p)};
-    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&attend_kernel<D>), dim3(p.wgs), dim3(kThreads), args, 0, stream);
+    const void* kernel = p.tile == 16 ? reinterpret_cast<const void*>(&attend_kernel<D, 1>)
+                                      : reinterpret_cast<const void*>(&attend_kernel<D, 2>);
+    const hipError_t e = hipLaunchKernel(kernel, dim3(p.wgs), dim3(kThreads), args, 0, stream);
     if (e != hipSuccess || p.whole) return e;
     const uint64_t rows = (uint64_t)p.tokens * (uint64_t)p.heads;
     if (rows * (D / 64) <= kFewRows)

@@ -145,13 +145,10 @@ int check_apart(const Span* out, const Span* const* own, int n_out, const Span* 
 // ---- attend: the launch ----
 // A run of units in whole mode is never cut; short capacities gain nothing from a second launch.
 constexpr int64_t kWholeRows = 512;
-#ifndef KB
-#define KB 1024
-#define KL 2
-#endif
-int64_t begin_of(int32_t d) { return KB / d; }
-// Workgroups: as many as fit the chip at once (LDS of two units to a wave).
-int64_t wgs_of(int32_t d) { return d == 256 ? 256 : d == 128 ? 512 : 1024; }
+int64_t wgs_of(int32_t d, int32_t tile) { return d == 64 && tile == 32 ? 768 : 65536 / d; }
+int64_t begin_of(int32_t d) { return d == 256 ? 6 : d == 128 ? 8 : 10; }
+int32_t tile_of(int64_t rows, int64_t n_seq, int64_t units, int64_t waves) { return rows <= 16 * n_seq || units < waves ? 16 : 32; }
+
 int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)[3], Span (&step)[2]) {
     int rc = check_cache(a->cache, &p->pages, cache);
     if (rc != CAP_OK) return rc;
@@ -160,8 +157,10 @@ int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)
     if (a->heads < 1 || a->heads % c.kv_heads != 0 || a->window < 0) return CAP_E_INVAL;
     const int64_t capacity = (int64_t)c.columns * c.page, rows = a->tokens * (a->heads / c.kv_heads);
     // segments at most, and units of all of them, which the kernel counts in 32 bits
-    const int64_t segments = (rows / 16 + c.n_seq) * c.kv_heads, begin = begin_of(c.d), least = begin + KL,
-                  units = (capacity + cap::kKvpUnit - 1) / cap::kKvpUnit + begin;
+    p->whole = capacity <= kWholeRows;
+    const int64_t seen = a->window > 0 && a->window < capacity ? a->window : capacity;
+    p->tile = tile_of(rows, c.n_seq, c.n_seq * c.kv_heads * (seen / cap::kKvpUnit), 4 * wgs_of(c.d, 32));
+    const int64_t segments = (rows / p->tile + c.n_seq) * c.kv_heads, begin = begin_of(c.d), units = (capacity + cap::kKvpUnit - 1) / cap::kKvpUnit + begin;
     if (segments > 0x7fffffff / units) return CAP_E_UNSUPPORTED;
     p->tokens = a->tokens;
     p->heads = a->heads;
@@ -169,15 +168,13 @@ int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)
     p->window = a->window;
     p->by_group = cap::divisor((uint32_t)(a->heads / c.kv_heads));
     p->by_kv_heads = cap::divisor((uint32_t)c.kv_heads);
-    p->whole = capacity <= kWholeRows;
     p->begin = (int32_t)begin;
-    p->least = p->whole ? 1 : (uint32_t)least;
-    const int64_t most = p->whole ? segments : (segments * units + least - 1) / least;
-    p->wgs = (uint32_t)std::min(most, wgs_of(c.d));
+    const int64_t most = p->whole ? segments : segments * units;
+    p->wgs = (uint32_t)std::min(most, wgs_of(c.d, p->tile));
     return CAP_OK;
 }
 
-uint64_t attend_parts(const cap::KvpAttendParams& p) { return p.whole ? 0 : (uint64_t)p.wgs * 2 * 16; }
+uint64_t attend_parts(const cap::KvpAttendParams& p) { return p.whole ? 0 : (uint64_t)p.wgs * 2 * (uint64_t)p.tile; }
 uint64_t attend_workspace(const cap::KvpAttendParams& p) {
     return p.whole || p.tokens == 0 ? 0 : attend_parts(p) * ((uint64_t)p.d + 2) * 4 + (uint64_t)p.tokens * (uint64_t)p.heads * 8;
 }

@@ -162,7 +162,7 @@ def sizes(c=None, **kw):
 def test_workspace():
     assert sizes(cache(columns=8)) == 0  # 512 rows: one launch
     assert sizes() > 0 and sizes() % 8 == 0
-    assert sizes(cache(columns=1 << 15)) <= (2 * 512 * 16 * 130 * 4) + 7 * 8 * 8
+    assert sizes(cache(columns=1 << 15)) <= (2 * 2048 * 16 * 130 * 4) + 7 * 8 * 8
     assert sizes(heads=6) == 0 and sizes(cache(d=80)) == 0 and sizes(tokens=0) == 0
     assert cap.load().kvp_attend_workspace_bytes(None) == 0
     for n in range(1, 70):  # as many tokens as any call of the kind may have
