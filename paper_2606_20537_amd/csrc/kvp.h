@@ -55,7 +55,8 @@ struct QkParams {
     int64_t        tokens;
     int32_t        heads, kv_heads, d, rot, axes;
     int32_t        tokens_wg;              // tokens of a workgroup, kQkTokens at most
-    float          eps, w_add;
+    float          eps, w_add, inv_d;
+    Divisor        by_rows;                // rows of a token
     bool           norm, pairs, w_f32;
     KvpPages       pages;
 };

@@ -80,9 +80,24 @@ void rule_spans(const qk_rule* r, const int32_t* pos, int64_t tokens, int32_t d,
     out[3] = plain(pos, r->rot ? (uint64_t)tokens * (uint64_t)r->axes * 4 : 0);
 }
 
+// Sizes of a call, all of whose tokens have `rows` rows.
+int32_t tokens_of_wg(int64_t tokens, int64_t rows, int32_t d);
+void enter_sizes(int64_t tokens, int32_t heads, int32_t kv_heads, int64_t rows, int32_t d, cap::QkParams* p) {
+    p->tokens = tokens;
+    p->heads = heads;
+    p->kv_heads = kv_heads;
+    p->d = d;
+    p->inv_d = 1.0f / (float)d;
+    p->by_rows = cap::divisor((uint32_t)rows);
+    p->tokens_wg = tokens_of_wg(tokens, rows, d);
+}
+
 // Tokens of a workgroup: heads of a token are 256 lanes or less where there are few, and one workgroup's
 // sines serve all of them; no more than leaves two workgroups for each CU.
 int32_t tokens_of_wg(int64_t tokens, int64_t rows, int32_t d) {
+#ifdef KTW
+    if (tokens >= 4096) return KTW;
+#endif
     int64_t n = 1;
     while (n < cap::kQkTokens && (n * 2) * 512 <= tokens && n * rows * (d / 16) < 2048) n *= 2;
     return (int32_t)n;
@@ -238,11 +253,7 @@ int qk_norm_rope(const qk_norm_rope_args* a, void* stream) {
     if ((rc = check_apart(out, own, 2, in, 2 + kRuleSpans)) != CAP_OK) return rc;
     enter_rule(a->rule, &p);
     p.pos = a->pos;
-    p.tokens = a->tokens;
-    p.heads = a->heads;
-    p.kv_heads = a->kv_heads;
-    p.d = a->d;
-    p.tokens_wg = tokens_of_wg(a->tokens, rows, a->d);
+    enter_sizes(a->tokens, a->heads, a->kv_heads, rows, a->d, &p);
     return launch_status(cap::launch_qk(p, a->dtype == CAP_DTYPE_F32, false, static_cast<hipStream_t>(stream)));
 }
 
@@ -278,11 +289,7 @@ int kvp_append(const kvp_append_args* a, void* stream) {
     if ((rc = check_apart(out, own, 3, in, 6 + kRuleSpans)) != CAP_OK) return rc;
     if (a->rule) enter_rule(a->rule, &p);
     p.pos = a->pos;
-    p.tokens = a->tokens;
-    p.heads = a->heads;
-    p.kv_heads = c.kv_heads;
-    p.d = c.d;
-    p.tokens_wg = tokens_of_wg(a->tokens, (int64_t)a->heads + 2 * c.kv_heads, c.d);
+    enter_sizes(a->tokens, a->heads, c.kv_heads, (int64_t)a->heads + 2 * c.kv_heads, c.d, &p);
     return launch_status(cap::launch_qk(p, false, true, static_cast<hipStream_t>(stream)));
 }
 

@@ -70,21 +70,25 @@ __device__ inline Vec<F32> narrow(const float* f) {
     return x;
 }
 
-// Sum over `lanes` (a power of two) neighbouring lanes, in all of them.
-__device__ inline float sum_lanes(float x, int lanes) {
-    for (int i = 1; i < lanes; i *= 2) x += __shfl_xor(x, i);
-    return x;
+// The factor of channel c.
+__device__ inline float weight(const void* w, int c, const QkParams& p) {
+    if (!w) return 1.0f;
+    return p.w_add + (p.w_f32 ? static_cast<const float*>(w)[c] : bits_f32((uint32_t)static_cast<const uint16_t*>(w)[c] << 16));
 }
 
-// The factors of channels c .. c + 7.
-__device__ inline void weights8(const void* w, int c, const QkParams& p, float* f) {
-    #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = 1.0f;
-    if (!p.norm || !w) return;
-    if (p.w_f32) widen<true>(load8<true>(static_cast<const char*>(w) + c * 4), f);
-    else widen<false>(load8<false>(static_cast<const char*>(w) + c * 2), f);
-    #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] += p.w_add;
+// Sum over `lanes` (a power of two, 32 at most) neighbouring lanes, in all of them: neighbours, pairs, and mirrored
+// quarters and halves of 16 lanes (whose values are equal by then) by cross-lane ALU operations.
+template <int CTRL>
+__device__ inline float moved(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ inline float sum_lanes(float x, int lanes) {
+    if (lanes > 1) x += moved<0xB1>(x);   // quad_perm 1 0 3 2
+    if (lanes > 2) x += moved<0x4E>(x);   // quad_perm 2 3 0 1
+    if (lanes > 4) x += moved<0x141>(x);  // row_half_mirror
+    if (lanes > 8) x += moved<0x140>(x);  // row_mirror
+    if (lanes > 16) x += __shfl_xor(x, 16);
+    return x;
 }
 
 // The sequence of packed token t: the last one that begins at or before it (-1: none).
@@ -107,65 +111,17 @@ __device__ inline int seq_of(const KvpPages& g, int t) {
 }
 
 template <bool F32, bool APPEND>
-__global__ __launch_bounds__(kThreads) void rotate_kernel(const QkParams p) {
+__global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void rotate_kernel(const QkParams p) {
     constexpr int kSize = F32 ? 4 : 2;
     __shared__ __attribute__((aligned(16))) float cs_s[kQkTokens * kMostPairs * 2];  // cosine, sine
-    __shared__ int64_t off_s[kQkTokens];  // bytes from a pool's begin to the token's row, -1: nowhere
+    __shared__ __attribute__((aligned(16))) float w_s[2][2 * kMostPairs];            // factors of q's channels and of k's
+    __shared__ int64_t off_s[kQkTokens];  // bytes from a pool's begin to the token's row; -1: on no page; -2: of no sequence
     __shared__ int row_s[kQkTokens];      // its number
     const int tid = (int)threadIdx.x;
     const int64_t t0 = ((int64_t)blockIdx.y * kFp8GridX + blockIdx.x) * p.tokens_wg;
     if (t0 >= p.tokens) return;
     const int here = (int)(p.tokens - t0 < p.tokens_wg ? p.tokens - t0 : p.tokens_wg);
     const int half = p.rot / 2;
-
-    if constexpr (APPEND) {
-        const KvpPages& g = p.pages;
-        for (int i = tid >> 6; i < here; i += kThreads / 64) {
-            const int t = (int)(t0 + i);
-            int64_t off = -1;
-            int row = 0;
-            if (g.tok0) {
-                const int s = __builtin_amdgcn_readfirstlane(seq_of(g, t));
-                if (s >= 0) {
-                    const int end = g.tok0[s + 1];
-                    row = (int)((int64_t)g.lens[s] - end + t);
-                    off = t < end && row >= 0 ? s : -1;
-                }
-            } else if (t < g.n_seq) {
-                row = g.lens[t] - 1;
-                off = row >= 0 ? t : -1;
-            }
-            const bool known = off >= 0;
-            if (known && row < g.capacity) {
-                const int column = (int)((uint32_t)row / (uint32_t)g.page);
-                const int page = g.table[off * g.table_stride + column];
-                off = (uint32_t)page < (uint32_t)g.pages
-                          ? (int64_t)page * g.page_stride + (int64_t)(row - column * g.page) * (g.kv_heads * p.d * 2) : -1;
-            } else {
-                off = -1;
-            }
-            if ((tid & 63) == 0) {
-                off_s[i] = off >= 0 ? off : known ? -1 : -2;  // -2: no sequence has the token
-                row_s[i] = row;
-            }
-        }
-        __syncthreads();
-    }
-
-    // sines and cosines of the workgroup's tokens
-    for (int i = tid; i < here * half; i += kThreads) {
-        const int t = (int)((uint32_t)i / (uint32_t)half), pair = i - t * half;
-        double turns = 0.0;
-        for (int a = 0; a < p.axes; ++a) {
-            const int at = APPEND && !p.pos ? row_s[t] : p.pos[(t0 + t) * p.axes + a];
-            turns += (double)at * p.freqs[(int64_t)a * half + pair];
-        }
-        turns *= 0.15915494309189533577;  // 1 / (2 pi)
-        turns -= __builtin_rint(turns);
-        float sine, cosine;
-        sincospif(2.0f * (float)turns, &sine, &cosine);
-        *reinterpret_cast<f32x2*>(&cs_s[2 * i]) = (f32x2){cosine, sine};
-    }
 
     // a lane's channels: 8 from `a` and 8 from `b`
     const int slots = p.d / 16;
@@ -184,42 +140,99 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const QkParams p) {
         a = p.rot + 8 * slot - half;
         b = a + (p.d - p.rot) / 2;
     }
-    float wq[16], wk[16];
-    weights8(p.wq, in ? a : 0, p, wq);
-    weights8(p.wq, in ? b : 0, p, wq + 8);
-    weights8(p.wk, in ? a : 0, p, wk);
-    weights8(p.wk, in ? b : 0, p, wk + 8);
-    __syncthreads();
-
+    // rows of the workgroup's tokens in order: q's heads, k's, and (append) v's
     const int of_q = p.heads, of_qk = p.heads + p.kv_heads, all = APPEND ? of_qk + p.kv_heads : of_qk;
-    const int per = kThreads / lanes;
-    for (int r = tid / lanes; r < here * all; r += per) {
-        const int t = (int)((uint32_t)r / (uint32_t)all), head = r - t * all;
+    const int rows = here * all, per = kThreads / lanes;
+    Vec<F32> va, vb;
+    auto load_row = [&](int t, int head) {
         const QkRows& src = head < of_q ? p.q : head < of_qk ? p.k : p.v;
         const int h = head < of_q ? head : head < of_qk ? head - of_q : head - of_qk;
         const char* from = reinterpret_cast<const char*>(src.p) + (t0 + t) * src.token + (int64_t)h * src.head;
+        va = load8<F32>(from + a * kSize);
+        vb = load8<F32>(from + b * kSize);
+    };
+    int r = tid / lanes, t = divide(r, p.by_rows), head = r - t * all;
+    if (in && r < rows) load_row(t, head);  // on its way while angles and pages are found
+
+    if (p.norm) {
+        for (int c = tid; c < p.d; c += kThreads) {
+            w_s[0][c] = weight(p.wq, c, p);
+            w_s[1][c] = weight(p.wk, c, p);
+        }
+    }
+    if constexpr (APPEND) {
+        const KvpPages& g = p.pages;
+        for (int i = tid >> 6; i < here; i += kThreads / 64) {
+            const int token = (int)(t0 + i);
+            int seq = -1, row = 0;
+            if (g.tok0) {
+                const int s = __builtin_amdgcn_readfirstlane(seq_of(g, token));
+                if (s >= 0) {
+                    const int end = g.tok0[s + 1];
+                    row = (int)((int64_t)g.lens[s] - end + token);
+                    if (token < end && row >= 0) seq = s;
+                }
+            } else if (token < g.n_seq) {
+                row = g.lens[token] - 1;
+                if (row >= 0) seq = token;
+            }
+            int64_t off = seq < 0 ? -2 : -1;
+            if (seq >= 0 && row < g.capacity) {
+                const int column = divide(row, g.by_page);
+                const int page = g.table[(int64_t)seq * g.table_stride + column];
+                if ((uint32_t)page < (uint32_t)g.pages)
+                    off = (int64_t)page * g.page_stride + (int64_t)(row - column * g.page) * (g.kv_heads * p.d * 2);
+            }
+            if ((tid & 63) == 0) {
+                off_s[i] = off;
+                row_s[i] = row;
+            }
+        }
+        __syncthreads();
+    }
+    // sines and cosines of the workgroup's tokens
+    for (int i = tid; i < here * half; i += kThreads) {
+        const int token = (int)((uint32_t)i / (uint32_t)half), pair = i - token * half;
+        double turns = 0.0;
+        for (int x = 0; x < p.axes; ++x) {
+            const int at = APPEND && !p.pos ? row_s[token] : p.pos[(t0 + token) * p.axes + x];
+            turns += (double)at * p.freqs[(int64_t)x * half + pair];
+        }
+        turns *= 0.15915494309189533577;  // 1 / (2 pi)
+        turns -= __builtin_rint(turns);
+        float sine, cosine;
+        sincospif(2.0f * (float)turns, &sine, &cosine);
+        *reinterpret_cast<f32x2*>(&cs_s[2 * i]) = (f32x2){cosine, sine};
+    }
+    __syncthreads();
+
+    while (r < rows) {
+        const int now_t = t, now_head = head;
+        const Vec<F32> ua = va, ub = vb;
+        r += per;
+        for (head += per; head >= all; head -= all) ++t;
+        if (in && r < rows) load_row(t, head);  // the next row
+
         char* to;
         bool write = in;
-        if (APPEND && head >= of_q) {
-            to = reinterpret_cast<char*>(head < of_qk ? p.pages.k : p.pages.v) + off_s[t] + (int64_t)h * p.d * 2;
-            write = in && off_s[t] >= 0;
+        if (APPEND && now_head >= of_q) {
+            const int h = now_head < of_qk ? now_head - of_q : now_head - of_qk;
+            to = reinterpret_cast<char*>(now_head < of_qk ? p.pages.k : p.pages.v) + off_s[now_t] + (int64_t)h * p.d * 2;
+            write = in && off_s[now_t] >= 0;
         } else {
-            const QkRows& dst = head < of_q ? p.q_out : p.k_out;
-            to = reinterpret_cast<char*>(dst.p) + (t0 + t) * dst.token + (int64_t)h * dst.head;
-            if (APPEND) write = in && off_s[t] != -2;
+            const QkRows& dst = now_head < of_q ? p.q_out : p.k_out;
+            const int h = now_head < of_q ? now_head : now_head - of_q;
+            to = reinterpret_cast<char*>(dst.p) + (t0 + now_t) * dst.token + (int64_t)h * dst.head;
+            if (APPEND) write = in && off_s[now_t] != -2;
         }
-        Vec<F32> va, vb;
-        if (in) {
-            va = load8<F32>(from + a * kSize);
-            vb = load8<F32>(from + b * kSize);
-        }
-        if (head < of_qk) {  // (uniform over a row's lanes)
+        Vec<F32> oa = ua, ob = ub;
+        if (now_head < of_qk) {  // (uniform over a row's lanes)
             float x[16];
             #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = 0.0f;
             if (in) {
-                widen<F32>(va, x);
-                widen<F32>(vb, x + 8);
+                widen<F32>(ua, x);
+                widen<F32>(ub, x + 8);
             }
             if (p.norm) {
                 float sum = 0.0f;
@@ -237,17 +250,21 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const QkParams p) {
                     sum = sum_lanes(sum, lanes);
                     eps = 0.0f;
                 }
-                const float f = 1.0f / __builtin_sqrtf(sum / (float)p.d + eps);
-                const bool q = head < of_q;
+                const float f = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, p.inv_d, eps));
+                const float* w = w_s[now_head < of_q ? 0 : 1];
                 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = x[e] * f * (q ? wq[e] : wk[e]);
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 four = *reinterpret_cast<const f32x4*>(&w[in ? (e < 8 ? a + e : b + e - 8) : 0]);
+                    #pragma unroll
+                    for (int i = 0; i < 4; ++i) x[e + i] = x[e + i] * f * four[i];
+                }
             }
             if (p.pairs) {
                 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
                     const int pair = ((e < 8 ? a + e : b + e - 8)) / 2;
                     if (in && pair < half) {
-                        const f32x2 cs = *reinterpret_cast<const f32x2*>(&cs_s[2 * (t * half + pair)]);
+                        const f32x2 cs = *reinterpret_cast<const f32x2*>(&cs_s[2 * (now_t * half + pair)]);
                         const float y0 = x[e], y1 = x[e + 1];
                         x[e] = y0 * cs[0] - y1 * cs[1];
                         x[e + 1] = y1 * cs[0] + y0 * cs[1];
@@ -256,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const QkParams p) {
             } else if (in && first >= 0) {
                 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const f32x4 cs = *reinterpret_cast<const f32x4*>(&cs_s[2 * (t * half + first + e)]);
+                    const f32x4 cs = *reinterpret_cast<const f32x4*>(&cs_s[2 * (now_t * half + first + e)]);
                     #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const float y0 = x[e + i], y1 = x[8 + e + i];
@@ -265,12 +282,12 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const QkParams p) {
                     }
                 }
             }
-            va = narrow<F32>(x);
-            vb = narrow<F32>(x + 8);
+            oa = narrow<F32>(x);
+            ob = narrow<F32>(x + 8);
         }
         if (write) {
-            store8<F32>(to + a * kSize, va);
-            store8<F32>(to + b * kSize, vb);
+            store8<F32>(to + a * kSize, oa);
+            store8<F32>(to + b * kSize, ob);
         }
     }
 }
