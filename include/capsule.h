@@ -826,8 +826,9 @@ typedef struct kvp_attend_args {
     int32_t          reserved;   /* 0 */
 } kvp_attend_args;
 
-/* Workspace of a call with these sizes (the cache's, tokens and heads); 0 where the call needs none
- * or is refused.  It holds nothing between calls; calls that may overlap need their own. */
+/* Workspace of a call with these sizes (the cache's, tokens, heads and window; that of window 0 does for
+ * any); 0 where the call needs none or is refused.  It holds nothing between calls; calls that may overlap need
+ * their own. */
 CAP_API uint64_t kvp_attend_workspace_bytes(const kvp_attend_args* args);
 CAP_API int kvp_attend(const kvp_attend_args* args, void* stream);
 

@@ -9,6 +9,7 @@ There is no fallback: if the library is missing, loading raises.
 """
 import ctypes as ct
 import os
+import struct
 
 from .build import LIB_PATH
 
@@ -176,10 +177,11 @@ SIGNATURES = [
     ("kvb_select_workspace_bytes", _u64, [ct.POINTER(kvb_select_args)]),
     ("kvb_select", ct.c_int, [ct.POINTER(kvb_select_args), _vp]),
     ("qk_fill_freqs", ct.c_int, [ct.c_double, _i32, _i32, ct.POINTER(_i32), _i32, ct.POINTER(ct.c_double)]),
-    ("qk_norm_rope", ct.c_int, [ct.POINTER(qk_norm_rope_args), _vp]),
-    ("kvp_append", ct.c_int, [ct.POINTER(kvp_append_args), _vp]),
-    ("kvp_attend_workspace_bytes", _u64, [ct.POINTER(kvp_attend_args)]),
-    ("kvp_attend", ct.c_int, [ct.POINTER(kvp_attend_args), _vp]),
+    # (the argument structs of these as pointers or as packed bytes)
+    ("qk_norm_rope", ct.c_int, [_vp, _vp]),
+    ("kvp_append", ct.c_int, [_vp, _vp]),
+    ("kvp_attend_workspace_bytes", _u64, [_vp]),
+    ("kvp_attend", ct.c_int, [_vp, _vp]),
 ]
 
 _lib = None
@@ -765,19 +767,26 @@ def qk_rule(freqs=None, *, wq=None, wk=None, eps=None, w_add=0.0, pairs=False):
     return QkRule(a, tensors, weights[0].shape[0] if weights else None, device)
 
 
+# The argument structs packed, which takes the host 0.5 us where filling ctypes structs takes 2.
+_pack_norm_rope = struct.Struct("<Q" + "Qqq" * 4 + "Qqiiii").pack
+_pack_append = struct.Struct("<QQQQ" + "Qqq" * 4 + "Qqii").pack
+_pack_attend = struct.Struct("<QQQ" + "Qqq" + "QQQQqiifi").pack
+_NO_ROWS = (0, 0, 0)
+
+
 def _qk_rows(fn, name, x, shape, dtype):
-    """qk_rows of a tensor [tokens, heads, d]."""
+    """The fields of qk_rows for a tensor [tokens, heads, d]."""
     if x.dtype != dtype or x.shape != shape:
         raise ValueError("%s: %s is a %s tensor of shape %s, not %s %s" % (fn, name, dtype, list(shape), x.dtype, list(x.shape)))
     if x.is_contiguous():
-        return qk_rows(x.data_ptr(), 0, 0)
+        return x.data_ptr(), 0, 0
     tokens, heads, d = shape
     st, sh, sd = x.stride()
     head = sh if heads > 1 else d
     # (strides of zero mean contiguous to the library, which would read past a broadcast row)
     if sd != 1 or head < d or (tokens > 1 and st < (heads - 1) * head + d):
         raise ValueError("%s: the channels of a head of %s follow each other, and heads and tokens do not overlap" % (fn, name))
-    return qk_rows(x.data_ptr(), st if tokens > 1 else 0, head)
+    return x.data_ptr(), st if tokens > 1 else 0, head
 
 
 def _qk_shape(fn, name, x):
@@ -820,21 +829,25 @@ def qk_norm_rope(rule, q, k, q_out=None, k_out=None, *, pos=None, stream=None):
     dtype = like.dtype
     if dtype != bf16 and dtype != f32:
         raise ValueError("qk_norm_rope: bfloat16 or float32 tensors, not %s" % dtype)
-    a = qk_norm_rope_args(rule=rule.address, tokens=tokens, d=d, dtype=CAP_DTYPE_F32 if dtype == f32 else CAP_DTYPE_BF16)
+    heads = kv_heads = 0
+    of_q = of_k = to_q = to_k = _NO_ROWS
     if q is not None:
         shape, q_out = q.shape, q if q_out is None else q_out
-        a.heads, a.q, a.q_out = shape[1], _qk_rows(fn, "q", q, shape, dtype), _qk_rows(fn, "q_out", q_out, shape, dtype)
+        heads, of_q = shape[1], _qk_rows(fn, "q", q, shape, dtype)
+        to_q = of_q if q_out is q else _qk_rows(fn, "q_out", q_out, shape, dtype)
     elif q_out is not None:
         raise ValueError("qk_norm_rope: q_out without q")
     if k is not None:
         shape, k_out = (tokens, _qk_shape(fn, "k", k)[1], d), k if k_out is None else k_out
-        a.kv_heads, a.k, a.k_out = shape[1], _qk_rows(fn, "k", k, shape, dtype), _qk_rows(fn, "k_out", k_out, shape, dtype)
+        kv_heads, of_k = shape[1], _qk_rows(fn, "k", k, shape, dtype)
+        to_k = of_k if k_out is k else _qk_rows(fn, "k_out", k_out, shape, dtype)
     elif k_out is not None:
         raise ValueError("qk_norm_rope: k_out without k")
-    a.pos = _qk_pos(fn, rule, pos, tokens)
+    at = _qk_pos(fn, rule, pos, tokens)
     _kvb_device(fn, like, q_out, k, k_out, pos)
     _qk_rule(fn, rule, d, like.get_device())
-    return _check(fn, load().qk_norm_rope(ct.byref(a), _stream(stream)))
+    a = _pack_norm_rope(rule.address, *of_q, *of_k, *to_q, *to_k, at, tokens, heads, kv_heads, d, CAP_DTYPE_F32 if dtype == f32 else CAP_DTYPE_BF16)
+    return _check(fn, load().qk_norm_rope(a, _stream(stream)))
 
 
 # ------------------------------------------------ paged bf16 KV cache ----
@@ -847,6 +860,7 @@ class KvpCache:
         self.tensors = tensors
         self.like = like  # a tensor on the cache's GPU
         self.n_seq, self.kv_heads, self.d = args.n_seq, args.kv_heads, args.d
+        self.device = like.get_device()
 
 
 def kvp_cache(k_pages, v_pages, table):
@@ -877,28 +891,32 @@ def kvp_append(cache, lens, k, v, *, tok0=None, rule=None, q=None, q_out=None, p
     bf16 = _kvb_torch()[1]
     shape = (_qk_shape(fn, "k", k)[0], cache.kv_heads, cache.d)
     tokens = shape[0]
-    a = kvp_append_args(cache=cache.address, lens=_qk_ints(fn, "lens", lens, (cache.n_seq,)),
-                        tok0=_qk_ints(fn, "tok0", tok0, (cache.n_seq + 1,)), k=_qk_rows(fn, "k", k, shape, bf16),
-                        v=_qk_rows(fn, "v", v, shape, bf16), tokens=tokens)
+    of_k, of_v = _qk_rows(fn, "k", k, shape, bf16), _qk_rows(fn, "v", v, shape, bf16)
+    heads = at = by = 0
+    of_q = to_q = _NO_ROWS
     if rule is None:
         if q is not None or q_out is not None or pos is not None:
             raise ValueError("kvp_append: q, q_out and pos go with a rule")
     else:
-        _qk_rule(fn, rule, cache.d, cache.like.get_device())
-        a.rule, a.pos = rule.address, _qk_pos(fn, rule, pos, tokens)
+        _qk_rule(fn, rule, cache.d, cache.device)
+        by, at = rule.address, _qk_pos(fn, rule, pos, tokens)
         if q is not None:
-            of_q, q_out = (tokens, _qk_shape(fn, "q", q)[1], cache.d), q if q_out is None else q_out
-            a.heads, a.q, a.q_out = of_q[1], _qk_rows(fn, "q", q, of_q, bf16), _qk_rows(fn, "q_out", q_out, of_q, bf16)
+            heads = _qk_shape(fn, "q", q)[1]
+            shape, q_out = (tokens, heads, cache.d), q if q_out is None else q_out
+            of_q = _qk_rows(fn, "q", q, shape, bf16)
+            to_q = of_q if q_out is q else _qk_rows(fn, "q_out", q_out, shape, bf16)
         elif q_out is not None:
             raise ValueError("kvp_append: q_out without q")
     _kvb_device(fn, cache.like, lens, k, v, tok0, q, q_out, pos)
-    return _check(fn, load().kvp_append(ct.byref(a), _stream(stream)))
+    a = _pack_append(cache.address, _qk_ints(fn, "lens", lens, (cache.n_seq,)), _qk_ints(fn, "tok0", tok0, (cache.n_seq + 1,)), by, *of_k, *of_v,
+                     *of_q, *to_q, at, tokens, heads, 0)
+    return _check(fn, load().kvp_append(a, _stream(stream)))
 
 
-def kvp_attend_workspace_bytes(cache, tokens, heads):
+def kvp_attend_workspace_bytes(cache, tokens, heads, window=0):
     """Bytes of workspace kvp_attend needs for this many packed tokens and query heads."""
-    a = kvp_attend_args(cache=cache.address, tokens=tokens, heads=heads)
-    return int(load().kvp_attend_workspace_bytes(ct.byref(a)))
+    a = _pack_attend(cache.address, 0, 0, 0, 0, 0, 0, 0, 0, 0, tokens, heads, window, 0.0, 0)
+    return int(load().kvp_attend_workspace_bytes(a))
 
 
 def kvp_attend(cache, lens, q, o, *, scale, tok0=None, window=0, lse=None, workspace=None, stream=None):
@@ -912,9 +930,15 @@ def kvp_attend(cache, lens, q, o, *, scale, tok0=None, window=0, lse=None, works
     _kvb_out(fn, "o", o, shape, bf16)
     _kvb_out(fn, "lse", lse, (tokens, heads), f32)
     _kvb_device(fn, cache.like, lens, q, o, tok0, lse, workspace)
-    a = kvp_attend_args(cache=cache.address, lens=_qk_ints(fn, "lens", lens, (cache.n_seq,)),
-                        tok0=_qk_ints(fn, "tok0", tok0, (cache.n_seq + 1,)), q=_qk_rows(fn, "q", q, shape, bf16), o=o.data_ptr(),
-                        lse=lse.data_ptr() if lse is not None else 0, tokens=tokens, heads=heads, window=window, scale=scale)
+    of_q, at = _qk_rows(fn, "q", q, shape, bf16), _qk_ints(fn, "lens", lens, (cache.n_seq,))
+    to, of_lse, first = o.data_ptr(), lse.data_ptr() if lse is not None else 0, _qk_ints(fn, "tok0", tok0, (cache.n_seq + 1,))
     lib, handle = load(), _stream(stream)
-    workspace = _kvb_workspace(fn, a, workspace, lib.kvp_attend_workspace_bytes, q, handle)
-    return _check(fn, lib.kvp_attend(ct.byref(a), handle))
+    if workspace is None:
+        need = kvp_attend_workspace_bytes(cache, tokens, heads, window)
+        if need:
+            workspace = _scratch(need, q.device, handle)
+    elif not workspace.is_contiguous():  # its elements are not the bytes behind its address
+        raise ValueError("kvp_attend: the workspace is a contiguous tensor")
+    space, size = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
+    a = _pack_attend(cache.address, at, first, *of_q, to, of_lse, space, size, tokens, heads, window, scale, 0)
+    return _check(fn, lib.kvp_attend(a, handle))

@@ -45,8 +45,8 @@ __device__ inline Vec<F32> load8(const char* at) {
 }
 template <bool F32>
 __device__ inline void store8(char* at, const Vec<F32>& x) {
-    *reinterpret_cast<u32x4*>(at) = x.w[0];
-    if constexpr (F32) *reinterpret_cast<u32x4*>(at + 16) = x.w[1];
+    __builtin_nontemporal_store(x.w[0], reinterpret_cast<u32x4*>(at));
+    if constexpr (F32) __builtin_nontemporal_store(x.w[1], reinterpret_cast<u32x4*>(at + 16));
 }
 template <bool F32>
 __device__ inline void widen(const Vec<F32>& x, float* f) {

@@ -165,8 +165,12 @@ def test_workspace():
     assert sizes(cache(columns=1 << 15)) <= (2 * 2048 * 16 * 130 * 4) + 7 * 8 * 8
     assert sizes(heads=6) == 0 and sizes(cache(d=80)) == 0 and sizes(tokens=0) == 0
     assert cap.load().kvp_attend_workspace_bytes(None) == 0
-    for n in range(1, 70):  # as many tokens as any call of the kind may have
-        assert sizes(tokens=n) >= sizes(tokens=1)
+    for d in (64, 128, 256):  # that of no window does for any
+        for columns in (9, 100, 5000):
+            for n_seq in (1, 3, 64):
+                for n in (1, 64, 500):
+                    c = cache(d=d, columns=columns, n_seq=n_seq)
+                    assert all(sizes(c, tokens=n, window=w) <= sizes(c, tokens=n) for w in (1, 100, 1000, 1 << 20))
 
 
 def test_frequencies():
