@@ -288,6 +288,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
     const int rowb = g.kv_heads * D * 2;
     uint32_t at = begin;  // where in the run we are
     int chunk = 0;
+    bool again = false;   // the waves have joined their sums in LDS
     while (at < end) {
         const int tid = hidden((int)threadIdx.x), lane = tid & 63, li = lane & 15, grp = lane >> 4;
         // the sequence that `at` is in (tok0 that does not ascend may make this fail: the run ends)
@@ -322,6 +323,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
             if (u1 <= 0) continue;
         }
         if (g.pages == 0) u1 = u0;  // there is nothing to read
+        if (again) __syncthreads();  // the other waves may still read the last segment's sums, which lie where K and V come
+        again = true;
         const KvpAttendParams& args = *hidden_arguments<KvpAttendParams>();
         const KvpPages& gp = args.pages;
         const float scale_log2 = args.scale_log2;

@@ -32,21 +32,25 @@ constexpr int kMostPairs = 256;  // rot <= 512
 
 __device__ inline float bits_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
 
-// Eight channels as they lie in memory.
+typedef char __attribute__((address_space(1)))* global_bytes;
+typedef u32x4 __attribute__((address_space(1)))* global_u32x4;
+
+// Eight channels as they lie in memory.  (Global addresses: an access by a generic one counts as one of LDS too, whose waits
+// it would then hold up.)
 template <bool F32>
 struct Vec { u32x4 w[F32 ? 2 : 1]; };
 
 template <bool F32>
-__device__ inline Vec<F32> load8(const char* at) {
+__device__ inline Vec<F32> load8(global_bytes at) {
     Vec<F32> x;
-    x.w[0] = *reinterpret_cast<const u32x4*>(at);
-    if constexpr (F32) x.w[1] = *reinterpret_cast<const u32x4*>(at + 16);
+    x.w[0] = *(const global_u32x4)at;
+    if constexpr (F32) x.w[1] = *(const global_u32x4)(at + 16);
     return x;
 }
 template <bool F32>
-__device__ inline void store8(char* at, const Vec<F32>& x) {
-    __builtin_nontemporal_store(x.w[0], reinterpret_cast<u32x4*>(at));
-    if constexpr (F32) __builtin_nontemporal_store(x.w[1], reinterpret_cast<u32x4*>(at + 16));
+__device__ inline void store8(global_bytes at, const Vec<F32>& x) {
+    __builtin_nontemporal_store(x.w[0], (global_u32x4)at);
+    if constexpr (F32) __builtin_nontemporal_store(x.w[1], (global_u32x4)(at + 16));
 }
 template <bool F32>
 __device__ inline void widen(const Vec<F32>& x, float* f) {
@@ -147,7 +151,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void rotate_kernel(const QkP
     auto load_row = [&](int t, int head) {
         const QkRows& src = head < of_q ? p.q : head < of_qk ? p.k : p.v;
         const int h = head < of_q ? head : head < of_qk ? head - of_q : head - of_qk;
-        const char* from = reinterpret_cast<const char*>(src.p) + (t0 + t) * src.token + (int64_t)h * src.head;
+        const global_bytes from = (global_bytes)src.p + (t0 + t) * src.token + (int64_t)h * src.head;
         va = load8<F32>(from + a * kSize);
         vb = load8<F32>(from + b * kSize);
     };
@@ -213,16 +217,16 @@ __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void rotate_kernel(const QkP
         for (head += per; head >= all; head -= all) ++t;
         if (in && r < rows) load_row(t, head);  // the next row
 
-        char* to;
+        global_bytes to;
         bool write = in;
         if (APPEND && now_head >= of_q) {
             const int h = now_head < of_qk ? now_head - of_q : now_head - of_qk;
-            to = reinterpret_cast<char*>(now_head < of_qk ? p.pages.k : p.pages.v) + off_s[now_t] + (int64_t)h * p.d * 2;
+            to = (global_bytes)(now_head < of_qk ? p.pages.k : p.pages.v) + off_s[now_t] + (int64_t)h * p.d * 2;
             write = in && off_s[now_t] >= 0;
         } else {
             const QkRows& dst = now_head < of_q ? p.q_out : p.k_out;
             const int h = now_head < of_q ? now_head : now_head - of_q;
-            to = reinterpret_cast<char*>(dst.p) + (t0 + now_t) * dst.token + (int64_t)h * dst.head;
+            to = (global_bytes)dst.p + (t0 + now_t) * dst.token + (int64_t)h * dst.head;
             if (APPEND) write = in && off_s[now_t] != -2;
         }
         Vec<F32> oa = ua, ob = ub;
