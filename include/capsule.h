@@ -805,9 +805,9 @@ CAP_API int kvp_append(const kvp_append_args* args, void* stream);
  * Precision: products and sums are fp32, weights enter the second product with 16 bits (two bf16),
  * o is rounded once.  Weights below 2^-100 of the largest may count as none.  Means of finite
  * values are finite.  A score beyond fp32 gives NaN.
- * Made for one token or a few drafts of each sequence: 16 query rows (tokens x heads / kv_heads)
- * read the cache once, so long runs of tokens are right but read it often.
- * Two launches; one where columns * page is 512 at most.  Results are reproducible for the same arguments and
+ * Made for one token or a few drafts of each sequence: 16 or 32 query rows (tokens x heads /
+ * kv_heads) read the cache once, so long runs of tokens are right but read it often.
+ * Two launches; one where columns * page, or the window and the tokens, are a few hundred rows (those that need no workspace).  Results are reproducible for the same arguments and
  * device data; a row's last bits depend on the other sequences of the call, over which work is
  * dealt out evenly. */
 typedef struct kvp_attend_args {

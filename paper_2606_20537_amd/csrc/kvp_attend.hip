@@ -48,7 +48,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // sequence has, cannot overflow and means of finite values stay finite.
 constexpr float kAbove = 24.0f;
 // Parts of even cuts at least (a unit to each wave) and at most; with longer ones equal runs leave fewer workgroups idle.
-constexpr uint32_t kLeastCut = 4, kMostCut = 16;
+constexpr uint32_t kLeastCut = 4, kMostCut = 32;
 
 typedef const char __attribute__((address_space(1)))* global_bytes;
 typedef __attribute__((address_space(3))) char* lds_bytes;

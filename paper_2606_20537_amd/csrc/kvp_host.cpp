@@ -157,10 +157,25 @@ int check_apart(const Span* out, const Span* const* own, int n_out, const Span* 
 }
 
 // ---- attend: the launch ----
-// A run of units in whole mode is never cut; short capacities gain nothing from a second launch.
-constexpr int64_t kWholeRows = 512;
+// Workgroups: as many as fit the chip at once, of which a CU has one, two or four: a unit of K and one of V to each of
+// four waves are 128 KiB of LDS with 256 channels, half of it with 128 (tiles of 32 rows of 64 channels: three, for their registers).
 int64_t wgs_of(int32_t d, int32_t tile) { return d == 64 && tile == 32 ? 768 : 65536 / d; }
+
+// Units that the beginning of a segment counts for: 4 to 6 us of lookups, first loads and sums, which are more units where
+// these are short.  Measured (us, for 2, 4, 6 and 8 units of 256 channels): one long sequence and 20 short ones, 401 MB, 104, 75, 77
+// and 76; 20 short sequences of up to six tokens, 8 KV heads, 372, 263, 211 and 191.
 int64_t begin_of(int32_t d) { return d == 256 ? 6 : d == 128 ? 8 : 10; }
+
+// Rows that a segment may have where no segment is cut, which spares the second launch: few, or more where there are
+// segments for every workgroup.  Measured (us, whole / cut; sequences x KV heads): 450 rows, 1 x 4 of 64 channels
+// 8.5 / 10.2, of 128 10.1 / 10.5, of 256 16.9 / 13.6; 700 rows, 1 x 4 of 64 9.6 / 10.2, of 128 12.4 / 10.5; 1000 rows of 256, 1 x 4
+// 26 / 14, 64 x 4 45 / 48.
+int64_t whole_rows(int32_t d, int64_t segments) { return segments >= wgs_of(d, 16) ? 1024 : d == 256 ? 256 : d == 128 ? 512 : 768; }
+
+// Query rows of a segment: 32 where sequences have more than 16 of a KV head on average and every wave has a unit of the
+// cache (else more segments are worth more than what they read twice).  Measured (us, 16 / 32; sequences of 16384 rows x tokens,
+// 32 heads on 4): 8 x 4 of 256 channels 172 / 107, of 128 70 / 64, of 64 53 / 33; 1 x 4 32 / 30, 21 / 18, 14.0 / 14.2; 8 x 4 behind 300
+// rows of 256 18 / 24.
 int32_t tile_of(int64_t rows, int64_t n_seq, int64_t units, int64_t waves) { return rows <= 16 * n_seq || units < waves ? 16 : 32; }
 
 int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)[3], Span (&step)[2]) {
@@ -171,8 +186,8 @@ int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)
     if (a->heads < 1 || a->heads % c.kv_heads != 0 || a->window < 0) return CAP_E_INVAL;
     const int64_t capacity = (int64_t)c.columns * c.page, rows = a->tokens * (a->heads / c.kv_heads);
     // segments at most, and units of all of them, which the kernel counts in 32 bits
-    p->whole = capacity <= kWholeRows;
-    const int64_t seen = a->window > 0 && a->window < capacity ? a->window : capacity;
+    const int64_t seen = a->window > 0 ? std::min(capacity, a->window + a->tokens) : capacity;  // rows of a segment at most
+    p->whole = seen <= whole_rows(c.d, (int64_t)c.n_seq * c.kv_heads);
     p->tile = tile_of(rows, c.n_seq, c.n_seq * c.kv_heads * (seen / cap::kKvpUnit), 4 * wgs_of(c.d, 32));
     const int64_t segments = (rows / p->tile + c.n_seq) * c.kv_heads, begin = begin_of(c.d), units = (capacity + cap::kKvpUnit - 1) / cap::kKvpUnit + begin;
     if (segments > 0x7fffffff / units) return CAP_E_UNSUPPORTED;

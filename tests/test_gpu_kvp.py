@@ -90,11 +90,40 @@ def test_lengths(d, page):
 
 
 @pytest.mark.parametrize("d", [64, 128, 256])
-@pytest.mark.parametrize("n", [1, 40, 511])
+@pytest.mark.parametrize("n", [1, 40, 255])
 def test_short_caches_in_one_launch(d, n):
-    s = Step([n, 0, 17], [1, 1, 1], 3, d, 16, seed=n, columns=32)
+    s = Step([n, 0, 17], [1, 1, 1], 3, d, 16, seed=n, columns=2048 // d if d > 64 else 48)
     assert cap.kvp_attend_workspace_bytes(s.cache, 3, 6) == 0
     s.check(*s.attend(2), d ** -0.5)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_short_windows_in_one_launch(d):
+    s = Step([5000, 3, 900], [1, 2, 1], 2, d, 64, seed=d)
+    assert cap.kvp_attend_workspace_bytes(s.cache, 4, 4, 200) == 0 < cap.kvp_attend_workspace_bytes(s.cache, 4, 4)
+    s.check(*s.attend(2, window=200), d ** -0.5, 200)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_segments_for_every_workgroup(d):
+    # whole segments of up to 1024 rows; the same cut, with one row more on the table
+    n = [1000, 7, 333, 0, 64] * (-(-65536 // d // 8 // 5))
+    s = Step(n, [1] * len(n), 8, d, 16, seed=d, columns=64)
+    assert cap.kvp_attend_workspace_bytes(s.cache, len(n), 8) == 0
+    q, o, lse = s.attend(1)
+    pick = [0, 1, 2, 3, 4, len(n) - 5]
+    host_q, host_o, host_l = host(q[pick]), host(o[pick]), host(lse[pick])
+    for j, i in enumerate(pick):
+        k, v = s.rows(i, s.k), s.rows(i, s.v)
+        for h in range(8):
+            want = plain.attend(host_q[j, h], k[:, h], v[:, h], d ** -0.5, np.arange(n[i]))
+            assert plain.attend_near(host_o[j, h], host_l[j, h], want, max(1, n[i]))
+    wide = torch.cat([s.dev_table, torch.full_like(s.dev_table[:, :1], -1)], 1)
+    o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    cap.kvp_attend(cap.kvp_cache(s.k, s.v, wide), s.lens, q, o2, scale=d ** -0.5, lse=lse2)
+    assert (o2.float() - o.float()).abs().max() <= 2.0 ** -7 * o.float().abs().max()
+    fine = lse.isfinite()
+    assert torch.equal(fine, lse2.isfinite()) and (lse2 - lse)[fine].abs().max() <= 1e-4
 
 
 @pytest.mark.parametrize("G, Hkv", [(1, 1), (1, 8), (3, 2), (8, 1), (16, 2), (17, 1), (40, 1)])
