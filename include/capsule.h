@@ -40,7 +40,7 @@
  *     gather of more than 64 environments, an append to more than 128
  *     buffers, a linear-attention prefill of many chunks, a delta-rule
  *     prefill, attention over an FP8 cache with long or many-rowed
- *     sequences, a block selection) the launches before it stay enqueued,
+ *     sequences, a block selection, attention over pages) the launches before it stay enqueued,
  *     and what they wrote of the outputs is not a result.
  *   - The library reads launch status from the launch calls themselves and
  *     never clears an error the caller left pending (the runtime's "last

@@ -64,11 +64,11 @@ constexpr int kQkTokens = 8;
 hipError_t launch_qk(const QkParams& p, bool f32, bool append, hipStream_t stream);
 
 // ---- attend ----
-// A segment is a KV head and 16 query rows of a sequence (row r: token r / G, query head
-// h G + r % G).  Its rows of the cache are cut into units of 32.  Units of all segments in a row, each
-// segment with `begin` more before it for what a segment costs, are dealt out
-// to the workgroups in equal runs; a workgroup has at most two segments that it shares with others,
-// whose parts lie in its two slots of the workspace.
+// A segment is a KV head and `tile` query rows of a sequence (row r: token r / G, query head
+// h G + r % G).  Its rows of the cache are cut into units of 32.  Either every segment is cut into even
+// parts, a workgroup each, or the units of all segments in a row, each segment with `begin` more
+// before it for what a segment costs, are dealt out in equal runs.  A workgroup has at most two segments that it
+// shares with others, whose parts lie in its two slots of the workspace.
 constexpr int kKvpUnit = 32;
 struct KvpAttendParams {
     QkRows   q;
@@ -80,7 +80,7 @@ struct KvpAttendParams {
     int64_t  tokens;
     int32_t  heads, d, window;
     uint32_t wgs;
-    int32_t  tile;     // query rows of a segment: 16, 32 or 64
+    int32_t  tile;     // query rows of a segment: 16 or 32
     int32_t  begin;    // units that the beginning of a segment counts for
     int32_t  whole;    // segments are not cut, and there is no second launch
     float    scale_log2;

@@ -5,24 +5,34 @@
 //   sees: max(0, pos - window + 1) <= j <= pos, on pages that are there
 //
 // in one pass over K and V with a running m and l.  The query rows of a KV head
-// (tokens x query heads of the group) share its K and V: 16 of them are the
+// (tokens x query heads of the group) share its K and V: 16 of them, or twice 16, are the
 // columns of the matrix instructions, keys and channels the rows.
 //  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 tiles, sums in fp32.
 //  * P goes in as two bf16 values, hi + lo, so that the weights keep 2^-16 and the
-//    output's own rounding is the only one to 8 bits: the matrix pipes have nothing
-//    else to do, as memory bounds the call.
+//    output's own rounding is the only one to 8 bits: the matrix pipes, 6 % busy, have
+//    the time, as memory bounds the call.
 // Both products leave a lane with one query row (lane % 16), so maximum, sum and
 // correction need no value of another row, and S^T's accumulators are P^T's
-// operand: lane group g holds keys 4g..4g+3 and 16+4g..16+4g+3 of 32, and loads
-// V's rows in that order.  A lane reads 16 bytes of each of eight rows and transposes them
-// in registers, two channels to a permute.  K and V go from memory to registers; LDS only
-// joins the four waves, which take units of 32 rows in turn.
+// operand: lane group g holds keys 4g..4g+3 and 16+4g..16+4g+3 of 32, in which order the
+// transposing reads of LDS give V's.
+//
+// A wave takes units of 32 rows.  K and V go from memory to LDS without registers, to a slot of
+// each that no other wave uses, so the waves wait for their own loads and never for each other;
+// the next K is on its way once a K has been read, the next V likewise.  That keeps 96 to 128 KiB on
+// their way to each CU.  With both in registers 64 to 128 KiB would fit, but the compiler,
+// which cannot tell the loads apart, waited for all of them at every step: 4.6 to 5.5 TB/s
+// over 1 GB, now 5.9 to 6.2 (and 6.8 over 4.3 GB).  Loads are streamed: cached ones read 1 GB 12 % slower, and
+// what fits the last cache 7 % faster, which a stack of layers does not.
 //
 // Lengths and the table are read on the device, so that a captured call goes on with the
 // sequences.  Every wave sums up the lengths for itself (a prefix sum over lanes) and
-// finds the run of units that its workgroup takes: equal runs over all sequences, heads and
-// tiles, so one long sequence beside many short ones spreads over the chip.  Segments that
-// several workgroups share are joined by a second launch.
+// finds the units that its workgroup takes: even parts of segments, or where there is more work equal
+// runs over all sequences, heads and tiles, so that one long sequence beside many short ones spreads
+// over the chip.  Segments that several workgroups share are joined by a second launch.
+//
+// What bounds it, one token, 8 query heads on each KV head of 256 channels: 131072 + 16449 + 2111 + 1 rows
+// x 4 heads, 613 MB, 100 us + 5 of the join (6.1 TB/s); 16385 rows x 4, 67 MB, 17 + 4, of which the data take
+// 10, the way to the first load 4 (lengths, table and 400 instructions behind each other) and the last sums 2.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -35,7 +45,6 @@ namespace {
 
 using dev::bf16x8;
 using dev::f32x4;
-using dev::rsrc_t;
 using dev::u32x4;
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
