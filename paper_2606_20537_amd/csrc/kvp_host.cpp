@@ -162,8 +162,8 @@ int check_apart(const Span* out, const Span* const* own, int n_out, const Span* 
 int64_t wgs_of(int32_t d, int32_t tile) { return d == 64 && tile == 32 ? 768 : 65536 / d; }
 
 // Units that the beginning of a segment counts for: 4 to 6 us of lookups, first loads and sums, which are more units where
-// these are short.  Measured (us, for 2, 4, 6 and 8 units of 256 channels): one long sequence and 20 short ones, 401 MB, 104, 75, 77
-// and 76; 20 short sequences of up to six tokens, 8 KV heads, 372, 263, 211 and 191.
+// these are short.  Measured (us, for 2, 4, 6 and 8 units of 256 channels): 35 sequences of up to 29300 rows, 401 MB,
+// 104, 75, 77 and 76; 50 of up to 12217 rows, six tokens and 8 KV heads, 372, 263, 211 and 191.
 int64_t begin_of(int32_t d) { return d == 256 ? 6 : d == 128 ? 8 : 10; }
 
 // Rows that a segment may have where no segment is cut, which spares the second launch: few, or more where there are
