@@ -211,6 +211,10 @@ __device__ inline uint32_t scan_lanes(uint32_t x) {
 __device__ inline int lane_int(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
 __device__ inline uint32_t lane_u32(uint32_t x, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); }
 
+// n / d rounded down, for quotients below 2^10 and d below 2^11 (by: the reciprocal of d, to the last place): (n + 1/2) / d is 2^-12
+// at least from every whole number, of which three roundings of 2^-24 lose less.
+__device__ inline uint32_t quotient(uint32_t n, float by) { return (uint32_t)(((float)n + 0.5f) * by); }
+
 // What a wave's lane knows of sequence 64 chunk + lane.
 struct Seq {
     int n, t0, T;      // rows held, first packed token, tokens
@@ -277,17 +281,16 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
     // Little work: segments are cut into even parts of `cut` units at most, a workgroup each (segments + units /
     // cut are no more than there are workgroups).  More: units in a row, each segment's with `extra` before them
     // for what its beginning costs, are dealt out in equal runs.
-    uint32_t cut = 0, by_cut = 0;
+    uint32_t cut = 0;
+    float by_cut = 0.0f;
     const uint32_t extra = (uint32_t)p.begin;
-    if (!p.whole && all_segments < p.wgs) {
-        cut = all_units / (p.wgs - all_segments) + 1;
+    if (!p.whole && all_segments < p.wgs && all_units < (kMostCut + 1) * p.wgs) {
+        cut = quotient(all_units, __builtin_amdgcn_rcpf((float)(p.wgs - all_segments))) + 1;
         if (cut < kLeastCut) cut = kLeastCut;
         if (cut > kMostCut) cut = 0;
-        else by_cut = 0xFFFFFFFFu / cut + 1;
+        else by_cut = __builtin_amdgcn_rcpf((float)cut);
     }
-    auto size_of = [&](uint32_t units) -> uint32_t {
-        return cut ? (uint32_t)((uint64_t)(units + cut - 1) * by_cut >> 32) : units + extra;
-    };
+    auto size_of = [&](uint32_t units) -> uint32_t { return cut ? quotient(units + cut - 1, by_cut) : units + extra; };
     const uint32_t total = cut ? p.wgs : all_units + extra * all_segments, per = cut ? 1 : (total + p.wgs - 1) / p.wgs;
     uint32_t scan = cut ? scan_lanes(q.segments * size_of((uint32_t)q.units)) : units_to + extra * segments;
     const uint32_t begin = w * per;
@@ -312,7 +315,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
         const int n = lane_int(q.n, s), seq_t0 = lane_int(q.t0, s), T = lane_int(q.T, s), units = lane_int(q.units, s);
         const uint32_t size = size_of((uint32_t)units), weight = lane_u32(q.segments, s) * size, base = before + lane_u32(scan, s) - weight;
         if (at - base >= weight) return;
-        const int segment = (int)((at - base) / size);
+        const float by_size = __builtin_amdgcn_rcpf((float)size);
+        const int segment = (int)(cut ? quotient(at - base, by_size) : (at - base) / size);
         const uint32_t seg0 = base + (uint32_t)segment * size;  // of the segment
         const uint32_t next = seg0 + size;
         const uint32_t unit0 = cut ? seg0 : seg0 + extra;                // of its first unit
@@ -321,7 +325,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
             at = next;
             if (seg0 < begin) continue;  // its beginning was another workgroup's
         } else if (cut) {
-            const int part = (int)(((uint32_t)units + size - 1) / size);
+            const int part = (int)quotient((uint32_t)units + size - 1, by_size);
             u0 = (int)(at - seg0) * part;
             u1 = u0 + part < units ? u0 + part : units;
             at = next;
