@@ -80,7 +80,7 @@ struct KvpAttendParams {
     int64_t  tokens;
     int32_t  heads, d, window;
     uint32_t wgs;
-    int32_t  tile;     // query rows of a segment: 16 or 32
+    int32_t  tile;     // query rows of a segment: 16, 32 or 128
     int32_t  begin;    // units that the beginning of a segment counts for
     int32_t  whole;    // segments are not cut, and there is no second launch
     float    scale_log2;

@@ -5,7 +5,7 @@
 //   sees: max(0, pos - window + 1) <= j <= pos, on pages that are there
 //
 // in one pass over K and V with a running m and l.  The query rows of a KV head
-// (tokens x query heads of the group) share its K and V: 16 of them, or twice 16, are the
+// (tokens x query heads of the group) share its K and V: 16 of them, twice 16 or eight times, are the
 // columns of the matrix instructions, keys and channels the rows.
 //  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 tiles, sums in fp32.
 //  * P goes in as two bf16 values, hi + lo, so that the weights keep 2^-16 and the
@@ -29,6 +29,12 @@
 // finds the units that its workgroup takes: even parts of segments, or where there is more work equal
 // runs over all sequences, heads and tiles, so that one long sequence beside many short ones spreads
 // over the chip.  Segments that several workgroups share are joined by a second launch.
+//
+// Long runs of tokens (prompts, resumed turns) have tiles of 128 query rows, where arithmetic counts: each wave
+// has its own rows and all of the units, which the waves load together into a ring of four, with
+// a barrier to each, so that K and V come from memory once for 128 rows and not for 32.  16384 tokens behind none, 32 heads on 4 of
+// 64, 128 and 256 channels: 3.2, 4.5 and 8.7 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.5 to 0.76 PFLOP/s
+// of matrix instructions with both parts of P, and between them the weights' exponentials.  Loads are kept by the caches here, as other tiles read the same.
 //
 // What bounds it, one token, 8 query heads on each KV head of 256 channels: 131072 + 16449 + 2111 + 1 rows
 // x 4 heads, 613 MB, 100 us + 5 of the join (6.1 TB/s); 16385 rows x 4, 67 MB, 17 + 4, of which the data take
@@ -134,9 +140,11 @@ __device__ inline void read_v8(const uint32_t (&at)[8], u32x2 (&x)[16]) {
         : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7]), "i"(MORE)
         : "memory");
 }
-// 1 KiB into LDS, 16 bytes from each lane's address.
+// 1 KiB into LDS, 16 bytes from each lane's address; streamed, or kept for the tiles that read it again.
+template <bool STREAM>
 __device__ inline void load_lds(global_bytes from, lds_bytes to) {
-    __builtin_amdgcn_global_load_lds((lds_source)from, (lds_target)to, 16, 0, 2);  // (2: streamed)
+    if constexpr (STREAM) __builtin_amdgcn_global_load_lds((lds_source)from, (lds_target)to, 16, 0, 2);
+    else __builtin_amdgcn_global_load_lds((lds_source)from, (lds_target)to, 16, 0, 0);
 }
 // What a row's number changes in the places of its pieces: rows that lie over the same banks differ.
 template <int D>
@@ -191,6 +199,18 @@ __device__ inline float group_sum(float x) {
     const f32x2 a = both16(x), b = both32(a[0] + a[1]);
     return b[0] + b[1];
 }
+// Four values times f, rounded to bf16.
+__device__ inline u32x2 bf16x4_of(const f32x4& o, float f) {
+    const bf16x2 lo = __builtin_convertvector((f32x2){o[0] * f, o[1] * f}, bf16x2);
+    const bf16x2 hi = __builtin_convertvector((f32x2){o[2] * f, o[3] * f}, bf16x2);
+    return (u32x2){__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+// A barrier of the workgroup that waits for no load.
+__device__ inline void meet_waves() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 // What scores are taken from, m the highest of them (-inf: none yet).
 __device__ inline float reference(float m) { return m == kNegInf ? 0.0f : m + kAbove; }
 
@@ -219,13 +239,13 @@ __device__ inline uint32_t quotient(uint32_t n, float by) { return (uint32_t)(((
 struct Seq {
     int n, t0, T;      // rows held, first packed token, tokens
     int first, units;  // first unit, number of units (1 at least where T > 0)
-    int tiles;         // of 16 NT query rows
+    int tiles;         // of TILE query rows
     uint32_t segments; // tiles times KV heads
 };
 
 __device__ inline int clamp_token(const KvpAttendParams& p, int t) { return t < 0 ? 0 : t > p.tokens ? (int)p.tokens : t; }
 
-template <int NT>
+template <int TILE>
 __device__ inline Seq load_seq(const KvpAttendParams& p, int group, int s) {
     const KvpPages& g = p.pages;
     Seq q = {};
@@ -247,13 +267,20 @@ __device__ inline Seq load_seq(const KvpAttendParams& p, int group, int s) {
     q.first = lo / kKvpUnit;
     q.units = (hi + kKvpUnit - 1) / kKvpUnit - q.first;
     if (q.units < 1) q.units = 1;
-    q.tiles = (q.T * group + 16 * NT - 1) / (16 * NT);  // (tokens * heads fits 31 bits)
+    q.tiles = (q.T * group + TILE - 1) / TILE;  // (tokens * heads fits 31 bits)
     q.segments = (uint32_t)q.tiles * (uint32_t)g.kv_heads;
     return q;
 }
 
-template <int D, int NT>
-__global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void attend_kernel(const KvpAttendParams p) {
+// Waves of a workgroup, and of a SIMD: as many as LDS and registers allow.
+constexpr int waves_of(int nt, bool wide) { return wide && nt == 1 ? 8 : 4; }
+constexpr int simd_waves(int d, int nt, bool wide) { return wide && nt == 1 ? 2 : d == 64 && nt == 2 ? 3 : 256 / d; }
+
+// Tiles of 16 NT query rows, whose units the four waves take in turn, each by itself; or (WIDE) of 128, of which
+// each wave has its share, and all of them every unit: a ring of four in LDS, which they fill together.
+template <int D, int NT, bool WIDE>
+__global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) void attend_kernel(const KvpAttendParams p) {
+    constexpr int WAVES = waves_of(NT, WIDE), kTile = WIDE ? 16 * NT * WAVES : 16 * NT;
     constexpr int NJ = D / 32;                        // K: fragments of 32 channels
     constexpr int NC = D / 16;                        // V: blocks of 16 channels
     constexpr int kPitch = D + 4;
@@ -270,11 +297,11 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
 
     // the run [begin, end) of this workgroup
     const int chunks = (g.n_seq + 63) / 64;
-    Seq q = load_seq<NT>(p, G, (int)(threadIdx.x & 63));
+    Seq q = load_seq<kTile>(p, G, (int)(threadIdx.x & 63));
     uint32_t segments = scan_lanes(q.segments), units_to = scan_lanes(q.segments * (uint32_t)q.units), before = 0;
     uint32_t all_segments = lane_u32(segments, 63), all_units = lane_u32(units_to, 63);
     for (int c = 1; c < chunks; ++c) {
-        const Seq r = load_seq<NT>(p, G, 64 * c + (int)(threadIdx.x & 63));
+        const Seq r = load_seq<kTile>(p, G, 64 * c + (int)(threadIdx.x & 63));
         all_segments += lane_u32(scan_lanes(r.segments), 63);
         all_units += lane_u32(scan_lanes(r.segments * (uint32_t)r.units), 63);
     }
@@ -307,7 +334,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
         while (at - before >= lane_u32(scan, 63)) {
             before += lane_u32(scan, 63);
             if (++chunk >= chunks) return;
-            q = load_seq<NT>(p, G, 64 * chunk + lane);
+            q = load_seq<kTile>(p, G, 64 * chunk + lane);
             scan = scan_lanes(q.segments * size_of((uint32_t)q.units));
         }
         const int s = __builtin_popcountll(__ballot(scan <= at - before));
@@ -341,36 +368,43 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
         const KvpAttendParams& args = *hidden_arguments<KvpAttendParams>();
         const KvpPages& gp = args.pages;
         const float scale_log2 = args.scale_log2;
-        const int tile = divide(segment, args.by_kv_heads), h = segment - tile * gp.kv_heads;
+        const int turn = divide(segment, args.by_kv_heads), h = segment - turn * gp.kv_heads;
+        // (a prefill's last tiles see most: first and last in turn, so that equal runs have equal work)
+        const int tile = WIDE && (turn & 1) ? lane_int(q.tiles, s) - 1 - turn / 2 : WIDE ? turn / 2 : turn;
         const int first_unit = lane_int(q.first, s);
         const int seq = 64 * chunk + s;
 
-        const int r0 = tile * (16 * NT), rows = T * G - r0 < 16 * NT ? T * G - r0 : 16 * NT;
-        // row 16 i + li of the tile (those past the last repeat it): its token; it sees the keys in (low, pos]
+        const int r0 = tile * kTile, rows = T * G - r0 < kTile ? T * G - r0 : kTile;
+        // the wave's rows: row w0 + 16 i + li of the tile (those past the last repeat it); it sees the keys in (low, pos]
+        const int w0 = WIDE ? wave * (16 * NT) : 0, my_rows = rows - w0 < 16 * NT ? rows - w0 : 16 * NT;
+        auto my_row = [&](int i) { return r0 + (w0 + 16 * i + li < rows ? w0 + 16 * i + li : rows - 1); };
         int row_t[NT], pos[NT], low[NT];
         auto below = [&](int pos) { return args.window > 0 ? (pos < 0 ? -1 : pos - args.window) : -1; };
         #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            row_t[i] = divide(r0 + (16 * i + li < rows ? 16 * i + li : rows - 1), args.by_group);
+            row_t[i] = divide(my_row(i), args.by_group);
             pos[i] = n - T + row_t[i];
             low[i] = below(pos[i]);
         }
-        const int pos0 = n - T + divide(r0, args.by_group), pos1 = n - T + divide(r0 + rows - 1, args.by_group);
-        const int low0 = below(pos0), low1 = below(pos1);
+        // positions of its first row and its last, and of the tile's
+        auto pos_of = [&](int row) { return n - T + divide(r0 + (row < rows ? row : rows - 1), args.by_group); };
+        const int pos0 = pos_of(w0), pos1 = pos_of(w0 + 16 * NT - 1), low0 = below(pos0), low1 = below(pos1);
+        const int tile_pos1 = WIDE ? pos_of(kTile - 1) : pos1, tile_low0 = WIDE ? below(pos_of(0)) : low0;
 
-        // Where a wave's next 64 units have their two groups of 16 rows in the pools, a lane each (unit u0 + wave
-        // + 4 (step0 + lane)); -1: on no page.
+        // Where a wave's next 64 units have their two groups of 16 rows in the pools, a lane each (a wave has every fourth
+        // unit from u0 + wave on, or (WIDE) every one); -1: on no page.
         int64_t off[2];
-        uint64_t todo = 0, whole = 0;  // bits of the units that some row sees, and of those that every row sees all of
+        uint64_t todo = 0, whole = 0;  // bits of the units that some row of the tile sees, and of those that every row of the wave sees all of
         const int32_t* table = gp.table + (int64_t)seq * gp.table_stride;
+        auto unit_of = [&](int step) { return WIDE ? u0 + step : u0 + wave + 4 * step; };
         auto look_up = [&](int step0) {
-            const int u = u0 + wave + 4 * (step0 + lane), r = (first_unit + u) * kKvpUnit;
+            const int u = unit_of(step0 + lane), r = (first_unit + u) * kKvpUnit;
             bool there[2];
             int page[2], rest[2];
             #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const int rt = r + 16 * t;
-                there[t] = u < u1 && rt < gp.capacity && rt <= pos1;
+                there[t] = u < u1 && rt < gp.capacity && rt <= tile_pos1;
                 const int column = there[t] ? divide(rt, gp.by_page) : 0;
                 rest[t] = rt - column * gp.page;
                 page[t] = table[column];
@@ -380,7 +414,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
                 there[t] = there[t] && (uint32_t)page[t] < (uint32_t)gp.pages;
                 off[t] = there[t] ? (int64_t)page[t] * gp.page_stride + (int64_t)rest[t] * rowb : -1;
             }
-            todo = __ballot((there[0] || there[1]) && r + kKvpUnit - 1 > low0);
+            todo = __ballot((there[0] || there[1]) && r + kKvpUnit - 1 > tile_low0);
             whole = __ballot(there[0] && there[1] && r + kKvpUnit - 1 <= pos0 && r > low1);
         };
         auto lane_i64 = [&](int64_t x, int i) -> int64_t {
@@ -391,7 +425,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
         bf16x8 qf[NT][NJ];
         #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            const int row = r0 + (16 * i + li < rows ? 16 * i + li : rows - 1);
+            const int row = my_row(i);
             const global_bytes src = (global_bytes)args.q.p + (int64_t)(seq_t0 + row_t[i]) * args.q.token +
                                      (int64_t)(h * G + (row - row_t[i] * G)) * args.q.head + 16 * grp;
             #pragma unroll
@@ -408,40 +442,55 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
             for (int c = 0; c < NC; ++c) acc[i][c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
         }
 
-        // Units in LDS, a slot for K and one for V to each wave: rows of D channels, in which 16 bytes (K: those of channels
-        // 8 c .. at the place of c ^ fold_k(row)) or 32 (V: 16 c .., c ^ fold_v(row)) change places, so that reads of 16 rows
-        // meet all banks.  An instruction brings 1 KiB: kRows rows, a lane 16 bytes.
+        // Units in LDS, a slot for K and one for V behind it to each wave (WIDE: to each place of the ring): rows of D channels, in
+        // which 16 bytes (K: those of channels 8 c .. at the place of c ^ fold_k(row)) or 32 (V: 16 c .., c ^ fold_v(row)) change
+        // places, so that reads of 16 rows meet all banks.  An instruction brings 1 KiB: kRows rows, a lane 16 bytes.
         constexpr int kRows = 512 / D, kLoads = kKvpUnit / kRows;
-        const int my_row = lane / (D / 8), chunk = lane % (D / 8);
-        const uint32_t lane_at = (uint32_t)(my_row * rowb + h * D * 2);
-        const uint32_t kvoff = lane_at + ((chunk ^ fold_k<D>(my_row)) << 4);
-        const uint32_t vvoff = lane_at + (((chunk >> 1) ^ fold_v<D>(my_row)) << 5) + ((chunk & 1) << 4);
-        lds_bytes k_slot = (lds_bytes)lds + wave * (2 * kSlot), v_slot = k_slot + kSlot;
+        const int lane_row = lane / (D / 8), piece = lane % (D / 8);
+        const uint32_t lane_at = (uint32_t)(lane_row * rowb + h * D * 2);
+        const uint32_t kvoff = lane_at + ((piece ^ fold_k<D>(lane_row)) << 4);
+        const uint32_t vvoff = lane_at + (((piece >> 1) ^ fold_v<D>(lane_row)) << 5) + ((piece & 1) << 4);
         const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_bytes)lds;  // (a multiple of the slots, which exchanges leave alone)
-        const uint32_t kread = lds_at + (uint32_t)(wave * (2 * kSlot) + li * D * 2 + ((grp ^ fold_k<D>(li)) << 4));
+        int place = WIDE ? 0 : wave;
+        const uint32_t kread = lds_at + (uint32_t)(li * D * 2 + ((grp ^ fold_k<D>(li)) << 4));
         const int vrow = 4 * grp + (li >> 2);
-        const uint32_t vread = lds_at + (uint32_t)(wave * (2 * kSlot) + kSlot + vrow * D * 2 + (fold_v<D>(vrow) << 5) + 8 * (li & 3));
+        const uint32_t vread = lds_at + (uint32_t)(kSlot + vrow * D * 2 + (fold_v<D>(vrow) << 5) + 8 * (li & 3));
         const global_bytes kb = (global_bytes)gp.k, vb = (global_bytes)gp.v;
-        // (folds are linear: that of my_row + row is fold(my_row) ^ fold(row))
+        // (folds are linear: that of lane_row + row is fold(lane_row) ^ fold(row))
         auto load_k = [&](const int64_t (&a)[2]) {
             const uint32_t from = hidden(kvoff);
+            const lds_bytes to = (lds_bytes)lds + place * (2 * kSlot);
             #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int row = i * kRows % 16;
-                load_lds(kb + a[i * kRows / 16] + row * rowb + (from ^ (uint32_t)(fold_k<D>(row) << 4)), k_slot + i * 1024);
+                load_lds<true>(kb + a[i * kRows / 16] + row * rowb + (from ^ (uint32_t)(fold_k<D>(row) << 4)), to + i * 1024);
             }
         };
         auto load_v = [&](const int64_t (&a)[2]) {
             const uint32_t from = hidden(vvoff);
+            const lds_bytes to = (lds_bytes)lds + place * (2 * kSlot) + kSlot;
             #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int row = i * kRows % 16;
-                load_lds(vb + a[i * kRows / 16] + row * rowb + (from ^ (uint32_t)(fold_v<D>(row) << 5)), v_slot + i * 1024);
+                load_lds<true>(vb + a[i * kRows / 16] + row * rowb + (from ^ (uint32_t)(fold_v<D>(row) << 5)), to + i * 1024);
+            }
+        };
+        // A wave's share of a unit of K and V, to a place of the ring.
+        constexpr int kShare = kLoads / WAVES;
+        auto load_share = [&](const int64_t (&a)[2], int to) {
+            const uint32_t k_from = hidden(kvoff), v_from = hidden(vvoff);
+            const int64_t at = a[wave * 2 / WAVES];
+            #pragma unroll
+            for (int i = 0; i < kShare; ++i) {
+                const int row = (wave * kShare + i) * kRows % 16;
+                const lds_bytes slot = (lds_bytes)lds + to * (2 * kSlot) + (wave * kShare + i) * 1024;
+                load_lds<!WIDE>(kb + at + row * rowb + (k_from ^ (uint32_t)(fold_k<D>(row) << 4)), slot);
+                load_lds<!WIDE>(vb + at + row * rowb + (v_from ^ (uint32_t)(fold_v<D>(row) << 5)), slot + kSlot);
             }
         };
         float x[NT][8];
         auto scores = [&]() {
-            const uint32_t from = hidden(kread);
+            const uint32_t from = hidden(kread) + (uint32_t)(place * (2 * kSlot));
             f32x4 sums[NT][2];
             #pragma unroll
             for (int i = 0; i < NT; ++i) sums[i][0] = sums[i][1] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
@@ -505,7 +554,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
         };
         // f(c, the eight keys of a lane in channel 16 c + li), for all blocks of 16 channels.
         auto each_block = [&](auto&& f) {
-            const uint32_t from = hidden(vread);
+            const uint32_t from = hidden(vread) + (uint32_t)(place * (2 * kSlot));
             constexpr int kAtOnce = NC < 8 || NT > 1 ? 4 : 8;
             #pragma unroll
             for (int c0 = 0; c0 < NC; c0 += kAtOnce) {
@@ -590,23 +639,68 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
             }
         };
 
-        const int steps = u1 - u0 > wave ? (u1 - u0 - wave + 3) / 4 : 0;
+        // (of a half on no page, rows of the first one are read, and count for nothing)
+        int64_t a[2];
+        int there;
+        auto where = [&](int j) {
+            a[0] = lane_i64(off[0], j);
+            a[1] = lane_i64(off[1], j);
+            there = 0;
+            #pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if ((int)(a[t] >> 32) >= 0) there |= 1 << t;
+                else a[t] = 0;
+            }
+        };
+        auto hide_unseen = [&](int r, int there) {
+            #pragma unroll
+            for (int i = 0; i < NT; ++i)
+                #pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] = seen(r, there, e, low[i], pos[i]) ? x[i][e] : kNegInf;
+        };
+        const int steps = WIDE ? u1 - u0 : u1 - u0 > wave ? (u1 - u0 - wave + 3) / 4 : 0;
         for (int step0 = 0; step0 < steps; step0 += 64) {
             look_up(step0);
             if (todo == 0) continue;
-            // (of a half on no page, rows of the first one are read, and count for nothing)
-            int64_t a[2];
-            int there;
-            auto where = [&](int j) {
-                a[0] = lane_i64(off[0], j);
-                a[1] = lane_i64(off[1], j);
-                there = 0;
+            if constexpr (WIDE) {
+                // Three units are on their way while one is in work.  A barrier for each: what the waves have loaded of it is
+                // there, and its predecessor's place is free.
+                uint64_t ahead = todo;
+                int to = 0;
+                auto load_next = [&]() {
+                    where(__builtin_ctzll(ahead));
+                    ahead &= ahead - 1;
+                    load_share(a, to);
+                    to = (to + 1) & 3;
+                };
+                meet_waves();  // the last 64 units' places are free
                 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if ((int)(a[t] >> 32) >= 0) there |= 1 << t;
-                    else a[t] = 0;
+                for (int i = 0; i < 3; ++i)
+                    if (ahead) load_next();
+                place = 0;
+                while (todo) {
+                    const int j = __builtin_ctzll(todo), left = __builtin_popcountll(todo);
+                    todo &= todo - 1;
+                    if (left > 2) wait_loads<4 * kShare>();
+                    else if (left > 1) wait_loads<2 * kShare>();
+                    else wait_loads<0>();
+                    meet_waves();
+                    if (ahead) load_next();
+                    const int r = (first_unit + unit_of(step0 + j)) * kKvpUnit;
+                    if (my_rows > 0 && r <= pos1 && r + kKvpUnit - 1 > low0) {
+                        const bool all = whole >> j & 1;
+                        where(j);
+                        scores();
+                        if (!all) hide_unseen(r, there);
+                        bf16x8 hi[NT], lo[NT];
+                        weigh(hi, lo);
+                        if (all) add_values(hi, lo);
+                        else add_seen_values(r, there, a, hi, lo);
+                    }
+                    place = (place + 1) & 3;
                 }
-            };
+                continue;
+            }
             int j = __builtin_ctzll(todo);
             where(j);
             wait_lds();  // the last reads of both slots
@@ -617,7 +711,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
                 // those behind the ones that are waited for tell how many may be outstanding.
                 todo &= todo - 1;
                 const bool more = todo != 0;
-                const int r = (first_unit + u0 + wave + 4 * (step0 + j)) * kKvpUnit, there_now = there;
+                const int r = (first_unit + unit_of(step0 + j)) * kKvpUnit, there_now = there;
                 const int64_t now[2] = {a[0], a[1]};
                 const bool all = whole >> j & 1;
                 wait_loads<kLoads>();  // K: V's are behind it
@@ -628,12 +722,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
                     wait_lds();
                     load_k(a);
                 }
-                if (!all) {
-                    #pragma unroll
-                    for (int i = 0; i < NT; ++i)
-                        #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[i][e] = seen(r, there_now, e, low[i], pos[i]) ? x[i][e] : kNegInf;
-                }
+                if (!all) hide_unseen(r, there_now);
                 bf16x8 hi[NT], lo[NT];
                 weigh(hi, lo);
                 if (more) wait_loads<kLoads>();  // V: the next K's are behind it
@@ -649,11 +738,35 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
         const KvpAttendParams& late = *hidden_arguments<KvpAttendParams>();
         // whether the segment's first unit is of this run, and all of them
         const bool begins = late.whole || unit0 >= begin, one = late.whole || (begins && next <= end);
-        const int64_t part0 = (int64_t)(2 * w + (begins ? 1 : 0)) * (16 * NT);
+        const int64_t part0 = (int64_t)(2 * w + (begins ? 1 : 0)) * kTile;
         auto out_row = [&](int rr) -> int64_t {
             const int t = divide(r0 + rr, late.by_group);
             return (int64_t)(seq_t0 + t) * late.heads + h * G + (r0 + rr - t * G);
         };
+        auto row_done = [&](int rr, float m, float l) {
+            const int64_t to = out_row(rr);
+            if (!one) *reinterpret_cast<f32x2*>(late.part_ml + (part0 + rr) * 2) = (f32x2){m, l};
+            else if (late.lse) late.lse[to] = (reference(m) + __builtin_amdgcn_logf(l)) * kLn2;
+            if (!late.whole && begins) late.meta[to] = (uint64_t)rr << 48 | (uint64_t)((next - 1) / per - w + 1) << 24 | w;
+        };
+        if constexpr (WIDE) {  // a row's values from the lanes that have them
+            #pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                const int rr = w0 + 16 * i + li;
+                const float my_l = group_sum(l[i]);
+                if (rr >= rows) continue;
+                const float inv = my_l > 0.0f || my_l != my_l ? 1.0f / my_l : 0.0f;
+                float* part = late.part_o + (part0 + rr) * D + 4 * grp;
+                __bf16* out = static_cast<__bf16*>(late.o) + out_row(rr) * D + 4 * grp;
+                #pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    if (one) *reinterpret_cast<u32x2*>(out + 16 * c) = bf16x4_of(acc[i][c], inv);
+                    else *reinterpret_cast<f32x4*>(part + 16 * c) = acc[i][c];
+                }
+                if (grp == 0) row_done(rr, m[i], my_l);
+            }
+            continue;
+        }
         #pragma unroll
         for (int i = 0; i < NT; ++i) {
             if (16 * i >= rows) break;
@@ -693,19 +806,9 @@ __global__ __launch_bounds__(kThreads, D == 64 && NT == 2 ? 3 : 256 / D) void at
                     continue;
                 }
                 const float z = all_s[r16][1], inv = z > 0.0f || z != z ? 1.0f / z : 0.0f;
-                const bf16x2 lo2 = __builtin_convertvector((f32x2){o[0] * inv, o[1] * inv}, bf16x2);
-                const bf16x2 hi2 = __builtin_convertvector((f32x2){o[2] * inv, o[3] * inv}, bf16x2);
-                *reinterpret_cast<u32x2*>(static_cast<__bf16*>(late.o) + out_row(rr) * D + c) =
-                    (u32x2){__builtin_bit_cast(uint32_t, lo2), __builtin_bit_cast(uint32_t, hi2)};
+                *reinterpret_cast<u32x2*>(static_cast<__bf16*>(late.o) + out_row(rr) * D + c) = bf16x4_of(o, inv);
             }
-            if (tid < 16 && 16 * i + tid < rows) {
-                const int rr = 16 * i + tid;
-                const int64_t to = out_row(rr);
-                const float mm = all_s[tid][0], z = all_s[tid][1];
-                if (!one) *reinterpret_cast<f32x2*>(late.part_ml + (part0 + rr) * 2) = (f32x2){mm, z};
-                else if (late.lse) late.lse[to] = (reference(mm) + __builtin_amdgcn_logf(z)) * kLn2;
-                if (!late.whole && begins) late.meta[to] = (uint64_t)rr << 48 | (uint64_t)((next - 1) / per - w + 1) << 24 | w;
-            }
+            if (tid < 16 && 16 * i + tid < rows) row_done(16 * i + tid, all_s[tid][0], all_s[tid][1]);
         }
     }
 }
@@ -773,10 +876,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
     };
     auto write = [&](int64_t row, const Joined& x, int c) {
         const float inv = x.l > 0.0f || x.l != x.l ? 1.0f / x.l : 0.0f;
-        const bf16x2 lo = __builtin_convertvector((f32x2){x.o[0] * inv, x.o[1] * inv}, bf16x2);
-        const bf16x2 hi = __builtin_convertvector((f32x2){x.o[2] * inv, x.o[3] * inv}, bf16x2);
-        *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + row * D + c) =
-            (u32x2){__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+        *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + row * D + c) = bf16x4_of(x.o, inv);
         if (c == 0 && p.lse) p.lse[row] = (reference(x.m) + __builtin_amdgcn_logf(x.l)) * kLn2;
     };
     if constexpr (!FEW) {
@@ -836,12 +936,18 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
 // so and 5.2 with four rows to a workgroup; 32 rows of 57 parts 4.0 and 7.8.
 constexpr uint64_t kFewRows = 1024;
 
+// Of 256 channels the sums of 16 rows to a wave leave registers for two waves on a SIMD.
+template <int D>
+constexpr int kWideTiles = D == 256 ? 1 : 2;
+
 template <int D>
 hipError_t launch(const KvpAttendParams& p, hipStream_t stream) {
     void* args[] = {const_cast<KvpAttendParams*>(&p)};
-    const void* kernel = p.tile == 16 ? reinterpret_cast<const void*>(&attend_kernel<D, 1>)
-                                      : reinterpret_cast<const void*>(&attend_kernel<D, 2>);
-    const hipError_t e = hipLaunchKernel(kernel, dim3(p.wgs), dim3(kThreads), args, 0, stream);
+    const void* kernel = p.tile == 16 ? reinterpret_cast<const void*>(&attend_kernel<D, 1, false>)
+                       : p.tile == 32 ? reinterpret_cast<const void*>(&attend_kernel<D, 2, false>)
+                                      : reinterpret_cast<const void*>(&attend_kernel<D, kWideTiles<D>, true>);
+    const uint32_t threads = p.tile == 128 ? 64 * (uint32_t)waves_of(kWideTiles<D>, true) : kThreads;
+    const hipError_t e = hipLaunchKernel(kernel, dim3(p.wgs), dim3(threads), args, 0, stream);
     if (e != hipSuccess || p.whole) return e;
     const uint64_t rows = (uint64_t)p.tokens * (uint64_t)p.heads;
     if (rows * (D / 64) <= kFewRows)

@@ -159,7 +159,7 @@ int check_apart(const Span* out, const Span* const* own, int n_out, const Span* 
 // ---- attend: the launch ----
 // Workgroups: as many as fit the chip at once, of which a CU has one, two or four: a unit of K and one of V to each of
 // four waves are 128 KiB of LDS with 256 channels, half of it with 128 (tiles of 32 rows of 64 channels: three, for their registers).
-int64_t wgs_of(int32_t d, int32_t tile) { return d == 64 && tile == 32 ? 768 : 65536 / d; }
+int64_t wgs_of(int32_t d, int32_t tile) { return d == 64 && tile > 16 ? 768 : 65536 / d; }
 
 // Units that the beginning of a segment counts for: 4 to 6 us of lookups, first loads and sums, which are more units where
 // these are short.  Measured (us, for 2, 4, 6 and 8 units of 256 channels): 35 sequences of up to 29300 rows, 401 MB,
@@ -172,11 +172,27 @@ int64_t begin_of(int32_t d) { return d == 256 ? 6 : d == 128 ? 8 : 10; }
 // 26 / 14, 64 x 4 45 / 48.
 int64_t whole_rows(int32_t d, int64_t segments) { return segments >= wgs_of(d, 16) ? 1024 : d == 256 ? 256 : d == 128 ? 512 : 768; }
 
-// Query rows of a segment: 32 where sequences have more than 16 of a KV head on average and every wave has a unit of the
-// cache (else more segments are worth more than what they read twice).  Measured (us, 16 / 32; sequences of 16384 rows x tokens,
-// 32 heads on 4): 8 x 4 of 256 channels 172 / 107, of 128 70 / 64, of 64 53 / 33; 1 x 4 32 / 30, 21 / 18, 14.0 / 14.2; 8 x 4 behind 300
-// rows of 256 18 / 24.
-int32_t tile_of(int64_t rows, int64_t n_seq, int64_t units, int64_t waves) { return rows <= 16 * n_seq || units < waves ? 16 : 32; }
+// Query rows of a segment.  16; 32 where sequences have more than 16 of a KV head on average, and 128 where they have more than
+// two tiles of 32 or so, if that leaves every workgroup a segment or some units (else more segments are worth more
+// than what they read again).  Measured (us, 16 / 32 / 128; sequences of so many rows x tokens, 32 heads on 4, for 64, 128 and 256 channels):
+//   8 of 16384 x 4    54 / 33 / 41    70 / 64 / 68      172 / 108 / 120
+//   32 of 2048 x 5    41 / 33 / 34    78 / 48 / 55      138 / 97 / 74
+//   32 of 2048 x 9    64 / 37 / 42    120 / 86 / 60     226 / 153 / 94
+//   32 of 2048 x 16   65 / 63 / 47    144 / 82 / 67     358 / 200 / 106
+//   1 of 16384 x 9    18 / 18 / 21    29 / 24 / 28      66 / 46 / 51
+//   8 of 300 x 6, G 16  8.5 / 10 / 18   12 / 14 / 23      20 / 24 / 26
+//   4 of 4000 x 16    21 / 20 / 27    49 / 31 / 33      72 / 61 / 44
+//   1 of 16384 x 161  - / 101 / 92    - / 217 / 117     - / 446 / 226
+// and prompts of 16 heads on 4: 1 x 512 9.5 / 11 / 25, 18 / 19 / 27, 40 / 31 / 37; 16 x 512 121 / 74 / 66, 310 / 201 / 128, 672 / 452 / 224;
+// 64 of 100 rows x 32 16 / 18 / 15, 32 / 25 / 21, 87 / 65 / 27.
+int32_t tile_of(const kvp_cache& c, int64_t rows, int64_t seen) {
+    auto fills = [&](int64_t tile, int64_t units) {
+        const int64_t segments = std::max<int64_t>(c.n_seq, rows / tile) * c.kv_heads, wgs = wgs_of(c.d, (int32_t)tile);
+        return segments >= wgs || segments * (seen / cap::kKvpUnit) >= units * wgs;
+    };
+    if (rows > (c.d == 256 ? 32 : c.d == 128 ? 64 : 96) * c.n_seq && fills(128, 6)) return 128;
+    return rows > 16 * c.n_seq && fills(32, 8) ? 32 : 16;
+}
 
 int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)[3], Span (&step)[2]) {
     int rc = check_cache(a->cache, &p->pages, cache);
@@ -188,7 +204,7 @@ int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)
     // segments at most, and units of all of them, which the kernel counts in 32 bits
     const int64_t seen = a->window > 0 ? std::min(capacity, a->window + a->tokens) : capacity;  // rows of a segment at most
     p->whole = seen <= whole_rows(c.d, (int64_t)c.n_seq * c.kv_heads);
-    p->tile = tile_of(rows, c.n_seq, c.n_seq * c.kv_heads * (seen / cap::kKvpUnit), 4 * wgs_of(c.d, 32));
+    p->tile = tile_of(c, rows, seen);
     const int64_t segments = (rows / p->tile + c.n_seq) * c.kv_heads, begin = begin_of(c.d), units = (capacity + cap::kKvpUnit - 1) / cap::kKvpUnit + begin;
     if (segments > 0x7fffffff / units) return CAP_E_UNSUPPORTED;
     p->tokens = a->tokens;

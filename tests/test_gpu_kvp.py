@@ -225,6 +225,102 @@ def test_values_that_some_tokens_do_not_see(T):
     assert torch.equal(o[same], o2[same]) and torch.equal(lse[:T], lse2[:T])
 
 
+def wide(s, G, window=0):
+    """That the call's segments have 128 query rows: its parts need more than those of fewer."""
+    return cap.kvp_attend_workspace_bytes(s.cache, s.tokens, s.Hkv * G, window) > 1 << 25
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 3, 50, 300])
+def test_runs_of_tokens(d, window):
+    n, T = [700, 130, 1000, 64, 0, 90, 129, 43], [300, 130, 1, 64, 0, 9, 129, 43]
+    s = Step(n, T, 2, d, 48, seed=window, columns=25000 if window else 1600)
+    assert window or wide(s, 3)
+    s.check(*s.attend(3, window=window), d ** -0.5, window)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G, window", [(3, 0), (17, 0), (40, 700)])
+def test_runs_behind_long_sequences(d, G, window):
+    # more units than even parts have, and fewer; the second sequence has one tile
+    s = Step([20011, 300, 4097], [320 // G, 1, 140 // G], 1, d, 64, seed=G, columns=2500)
+    if not window:
+        assert wide(s, G)
+    s.check(*s.attend(G, window=window), d ** -0.5, window)
+
+
+def test_runs_of_many_sequences():
+    rng = np.random.default_rng(5)
+    n = rng.integers(0, 200, 130).tolist()
+    T = [int(rng.integers(0, m + 1)) if i % 3 else 0 for i, m in enumerate(n)]
+    s = Step(n, T, 1, 128, 16, seed=5, columns=200)
+    assert wide(s, 5)
+    s.check(*s.attend(5), 128 ** -0.5)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_runs_in_one_launch(d):
+    n = [100, 7, 128, 0, 64, 99] * (-(-65536 // d // 8 // 6))
+    T = [40 if m else 0 for m in n]
+    T[1] = 7
+    s = Step(n, T, 8, d, 16, seed=d, columns=8)
+    assert cap.kvp_attend_workspace_bytes(s.cache, s.tokens, 32) == 0
+    q, o, lse = s.attend(4)
+    few = Step.__new__(Step)  # the first six
+    few.__dict__.update(s.__dict__, n=n[:6], T=T[:6])
+    few.check(q, o, lse, d ** -0.5)
+
+
+def test_runs_on_absent_pages_and_before_the_first_row():
+    # the first 150 tokens of sequence 0 see nothing, those of sequence 3 neither
+    s = Step([50, 400, 500, 90], [200, 150, 40, 30], 2, 64, 16, seed=2, columns=2600, absent=[(0, 1), (1, 0), (1, 7), (1, 12), (1, 24)] + [(3, c) for c in range(6)])
+    assert wide(s, 2)
+    q, o, lse = s.attend(2)
+    s.check(q, o, lse, 0.125)
+    assert not o[:150].any() and (lse[:150] == -float("inf")).all() and not o[390:].any()
+    # rows beyond the table, and packed tokens of no sequence
+    short = Step([700, 640], [90, 80], 2, 256, 16, seed=3, columns=40)
+    q, o, lse = short.normal(180, 8, 256), torch.full((180, 8, 256), 3.0, device="cuda").bfloat16(), torch.full((180, 8), 5.0, device="cuda")
+    cap.kvp_attend(short.cache, short.lens, q, o, scale=0.0625, tok0=short.tok0 + 6, lse=lse)
+    assert (o[:6] == 3).all() and (o[176:] == 3).all() and (lse[:6] == 5).all() and (lse[176:] == 5).all()
+    short.check(q[6:176], o[6:176], lse[6:176], 0.0625)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_values_that_some_tokens_of_a_run_do_not_see(d):
+    n, T, G = [270, 150], [200, 120], 2
+    make = lambda: Step(n, T, 2, d, 16, seed=d, columns=5000)
+    s, clean = make(), make()
+    put = [(0, 269, 0, 5, "v", float("inf")), (0, 200, 1, 33, "v", NAN), (0, 131, 0, 6, "v", -float("inf")), (1, 149, 1, 7, "k", NAN), (1, 64, 0, 8, "v", float("inf"))]
+    q, o2, lse2 = clean.attend(G)
+    want, want_lse = o2.clone(), lse2.clone()
+    t0 = [0, T[0]]
+    for i, row, h, c, what, value in put:
+        getattr(s, what)[int(s.table[i, row // 16]), row % 16, h, c] = value
+        first = t0[i] + row - (n[i] - T[i])  # the packed token at that row
+        mine = slice(h * G, h * G + G)
+        last = t0[i] + T[i]
+        if what == "v":
+            want[first:last, mine, c] = value
+        else:
+            want[first:last, mine], want_lse[first:last, mine] = NAN, NAN
+    _, o, lse = s.attend(G, q=q)
+    assert wide(s, G)
+    assert torch.equal(o.nan_to_num(9.0, 1e30, -1e30), want.nan_to_num(9.0, 1e30, -1e30))
+    assert torch.equal(o.isnan(), want.isnan()) and torch.equal(lse.nan_to_num(9.0), want_lse.nan_to_num(9.0))
+
+
+def test_a_run_out_of_strided_queries_is_reproducible():
+    s = Step([900, 333], [400, 200], 2, 128, 64, seed=11, columns=1500)
+    q = s.normal(600, 2, 8, 128)[:, 1]
+    assert wide(s, 4)
+    _, o, lse = s.attend(4, q=q)
+    s.check(q, o, lse, 128 ** -0.5)
+    for _ in range(3):
+        _, o2, lse2 = s.attend(4, q=q)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
 def test_large_and_small_values():
     for size in (3e38, 1e-30):
         s = Step([3000, 40], [1, 1], 1, 64, 16, seed=4)
