@@ -67,7 +67,7 @@ hipError_t launch_qk(const QkParams& p, bool f32, bool append, hipStream_t strea
 // A segment is a KV head and `tile` query rows of a sequence (row r: token r / G, query head
 // h G + r % G).  Its rows of the cache are cut into units of 32.  Either every segment is cut into even
 // parts, a workgroup each, or the units of all segments in a row, each segment with `begin` more
-// before it for what a segment costs, are dealt out in equal runs.  A workgroup has at most two segments that it
+// before it for what a segment costs, are dealt out in equal runs (tiles of 128: the units that each tile sees).  A workgroup has at most two segments that it
 // shares with others, whose parts lie in its two slots of the workspace.
 constexpr int kKvpUnit = 32;
 struct KvpAttendParams {
@@ -83,7 +83,7 @@ struct KvpAttendParams {
     int32_t  tile;     // query rows of a segment: 16, 32 or 128
     int32_t  begin;    // units that the beginning of a segment counts for
     int32_t  whole;    // segments are not cut, and there is no second launch
-    float    scale_log2;
+    float    scale_log2;  // not zero, so that scores that are masked by an infinity stay so
     Divisor  by_group, by_kv_heads;  // heads / kv_heads, kv_heads
     KvpPages pages;
 };

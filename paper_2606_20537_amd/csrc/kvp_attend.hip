@@ -33,7 +33,7 @@
 // Long runs of tokens (prompts, resumed turns) have tiles of 128 query rows, where arithmetic counts: each wave
 // has its own rows and all of the units, which the waves load together into a ring of four, with
 // a barrier to each, so that K and V come from memory once for 128 rows and not for 32.  16384 tokens behind none, 32 heads on 4 of
-// 64, 128 and 256 channels: 3.2, 4.5 and 8.7 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.5 to 0.76 PFLOP/s
+// 64, 128 and 256 channels: 2.7, 3.9 and 8.6 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.62 to 0.84 PFLOP/s
 // of matrix instructions with both parts of P, and between them the weights' exponentials.  Loads are kept by the caches here, as other tiles read the same.
 //
 // What bounds it, one token, 8 query heads on each KV head of 256 channels: 131072 + 16449 + 2111 + 1 rows
@@ -211,8 +211,8 @@ __device__ inline void meet_waves() {
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
-// What scores are taken from, m the highest of them (-inf: none yet).
-__device__ inline float reference(float m) { return m == kNegInf ? 0.0f : m + kAbove; }
+// What scores are taken from, m the highest of them (-inf: none yet; inf: NaN).
+__device__ inline float reference(float m) { return m == kNegInf ? 0.0f : m + (kAbove + (m - m)); }
 
 // Inclusive prefix sum over the lanes of a wave (as dev::wave_inclusive_sum).
 template <int CTRL, int ROW_MASK, bool BOUND_ZERO>
@@ -235,12 +235,19 @@ __device__ inline uint32_t lane_u32(uint32_t x, int l) { return (uint32_t)__buil
 // at least from every whole number, of which three roundings of 2^-24 lose less.
 __device__ inline uint32_t quotient(uint32_t n, float by) { return (uint32_t)(((float)n + 0.5f) * by); }
 
+// n / d rounded down, for quotients below 2^22: the reciprocal leaves less than one.
+__device__ inline uint32_t long_quotient(uint32_t n, uint32_t d) {
+    const uint32_t q = (uint32_t)((float)n * __builtin_amdgcn_rcpf((float)d));
+    return q * d > n ? q - 1 : n - q * d >= d ? q + 1 : q;
+}
+
 // What a wave's lane knows of sequence 64 chunk + lane.
 struct Seq {
     int n, t0, T;      // rows held, first packed token, tokens
     int first, units;  // first unit, number of units (1 at least where T > 0)
     int tiles;         // of TILE query rows
     uint32_t segments; // tiles times KV heads
+    uint32_t pair, head; // WIDE: units of two tiles, and of a KV head, with what beginnings count for
 };
 
 __device__ inline int clamp_token(const KvpAttendParams& p, int t) { return t < 0 ? 0 : t > p.tokens ? (int)p.tokens : t; }
@@ -272,6 +279,41 @@ __device__ inline Seq load_seq(const KvpAttendParams& p, int group, int s) {
     return q;
 }
 
+// The units that a tile of TILE rows sees, from the sequence's rows.
+struct Units {
+    int first, number;  // 1 at least
+};
+template <int TILE>
+__device__ inline Units units_of_tile(const KvpAttendParams& p, int n, int T, int group, int tile) {
+    const int last = (tile + 1) * TILE < T * group ? (tile + 1) * TILE : T * group;
+    const int pos0 = n - T + divide(tile * TILE, p.by_group), end = n - T + divide(last - 1, p.by_group) + 1;
+    const int lo = p.window > 0 && pos0 >= p.window ? pos0 - p.window + 1 : 0, hi = end < p.pages.capacity ? end : p.pages.capacity;
+    const int first = lo / kKvpUnit, number = (hi + kKvpUnit - 1) / kKvpUnit - first;
+    return {first, number < 1 ? 1 : number};
+}
+// What a KV head's tiles of TILE rows count for where runs are dealt out.  Later tiles see more: the first and the last of
+// all (of an odd number: of all but the last), the second and the last but one, .. are pairs, of which none has more
+// units than `pair`: tiles j and k, j + k = c, see 2 (n - T) + (TILE (c + 2) - 2) / group rows at most in all; with a window each sees
+// that and what its own rows are apart.  (Every tile counted as the last, first and last in turn: 2048 tokens, 16 heads on 4 of 64, 128 and 256
+// channels 69, 96 and 154 us, now 57, 70 and 111; 8192 of 64 522, now 417.)
+template <int TILE>
+__device__ inline void add_weights(const KvpAttendParams& p, Seq& q) {
+    const int pairs = q.tiles / 2, capacity = p.pages.capacity;
+    int one = q.units;
+    if (p.window > 0) {
+        const int most = (p.window < capacity ? p.window : capacity) + divide(TILE, p.by_group) + 3 * kKvpUnit;
+        one = most / kKvpUnit < one ? most / kKvpUnit : one;
+    }
+    int pair = 2 * one;
+    if (q.n >= q.T) {
+        const int before = q.n - q.T < capacity ? q.n - q.T : capacity;
+        const int both = (2 * before + divide(TILE * (2 * pairs + 1) - 2, p.by_group)) / kKvpUnit + 2;
+        pair = both < pair ? both : pair;
+    }
+    q.pair = (uint32_t)(pair + 2 * p.begin);
+    q.head = (uint32_t)pairs * q.pair + (q.tiles & 1 ? (uint32_t)(one + p.begin) : 0);
+}
+
 // Waves of a workgroup, and of a SIMD: as many as LDS and registers allow.
 constexpr int waves_of(int nt, bool wide) { return wide && nt == 1 ? 8 : 4; }
 constexpr int simd_waves(int d, int nt, bool wide) { return wide && nt == 1 ? 2 : d == 64 && nt == 2 ? 3 : 256 / d; }
@@ -292,25 +334,32 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
 
     const KvpPages& g = p.pages;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const uint32_t w = blockIdx.x;
     const int G = divide(p.heads, p.by_kv_heads);
 
     // the run [begin, end) of this workgroup
     const int chunks = (g.n_seq + 63) / 64;
-    Seq q = load_seq<kTile>(p, G, (int)(threadIdx.x & 63));
+    auto load = [&](int s) {
+        Seq q = load_seq<kTile>(p, G, s);
+        if (WIDE && q.T > 0) add_weights<kTile>(p, q);
+        return q;
+    };
+    const uint32_t extra = (uint32_t)p.begin;
+    auto run_of = [&](const Seq& q) -> uint32_t { return q.head * (uint32_t)g.kv_heads; };  // (WIDE)
+    Seq q = load((int)(threadIdx.x & 63));
     uint32_t segments = scan_lanes(q.segments), units_to = scan_lanes(q.segments * (uint32_t)q.units), before = 0;
     uint32_t all_segments = lane_u32(segments, 63), all_units = lane_u32(units_to, 63);
+    uint32_t run_to = WIDE ? scan_lanes(run_of(q)) : 0, all_runs = WIDE ? lane_u32(run_to, 63) : 0;
     for (int c = 1; c < chunks; ++c) {
-        const Seq r = load_seq<kTile>(p, G, 64 * c + (int)(threadIdx.x & 63));
+        const Seq r = load(64 * c + (int)(threadIdx.x & 63));
         all_segments += lane_u32(scan_lanes(r.segments), 63);
         all_units += lane_u32(scan_lanes(r.segments * (uint32_t)r.units), 63);
+        if (WIDE) all_runs += lane_u32(scan_lanes(run_of(r)), 63);
     }
     // Little work: segments are cut into even parts of `cut` units at most, a workgroup each (segments + units /
     // cut are no more than there are workgroups).  More: units in a row, each segment's with `extra` before them
     // for what its beginning costs, are dealt out in equal runs.
     uint32_t cut = 0;
     float by_cut = 0.0f;
-    const uint32_t extra = (uint32_t)p.begin;
     if (!p.whole && all_segments < p.wgs && all_units < (kMostCut + 1) * p.wgs) {
         cut = quotient(all_units, __builtin_amdgcn_rcpf((float)(p.wgs - all_segments))) + 1;
         if (cut < kLeastCut) cut = kLeastCut;
@@ -318,8 +367,17 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
         else by_cut = __builtin_amdgcn_rcpf((float)cut);
     }
     auto size_of = [&](uint32_t units) -> uint32_t { return cut ? quotient(units + cut - 1, by_cut) : units + extra; };
-    const uint32_t total = cut ? p.wgs : all_units + extra * all_segments, per = cut ? 1 : (total + p.wgs - 1) / p.wgs;
-    uint32_t scan = cut ? scan_lanes(q.segments * size_of((uint32_t)q.units)) : units_to + extra * segments;
+    const uint32_t total = cut ? p.wgs : WIDE ? all_runs : all_units + extra * all_segments, per = cut ? 1 : (total + p.wgs - 1) / p.wgs;
+    auto weight_of = [&](const Seq& q) -> uint32_t { return WIDE && !cut ? run_of(q) : q.segments * size_of((uint32_t)q.units); };
+    uint32_t scan = cut ? scan_lanes(weight_of(q)) : WIDE ? run_to : units_to + extra * segments;
+    uint32_t w = blockIdx.x;
+    // (runs behind each other to one XCD, w % 8 of the launch, whose L2 has what they share: 8192 tokens, 32 heads on 4 of 256 channels
+    // fetch 0.4 GB and not 6.9; 16384 of 128 channels 4314 -> 4176 us)
+    if (WIDE && !cut && !p.whole && p.wgs % 8 == 0) {
+        const uint32_t some = ((total + per - 1) / per + 7) / 8;
+        if (w / 8 >= some) return;
+        w = w % 8 * some + w / 8;
+    }
     const uint32_t begin = w * per;
     if (begin >= total) return;
     const uint32_t end = begin + per < total ? begin + per : total;
@@ -334,44 +392,75 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
         while (at - before >= lane_u32(scan, 63)) {
             before += lane_u32(scan, 63);
             if (++chunk >= chunks) return;
-            q = load_seq<kTile>(p, G, 64 * chunk + lane);
-            scan = scan_lanes(q.segments * size_of((uint32_t)q.units));
+            q = load(64 * chunk + lane);
+            scan = scan_lanes(weight_of(q));
         }
         const int s = __builtin_popcountll(__ballot(scan <= at - before));
         if (s > 63) return;
-        const int n = lane_int(q.n, s), seq_t0 = lane_int(q.t0, s), T = lane_int(q.T, s), units = lane_int(q.units, s);
-        const uint32_t size = size_of((uint32_t)units), weight = lane_u32(q.segments, s) * size, base = before + lane_u32(scan, s) - weight;
+        const int n = lane_int(q.n, s), seq_t0 = lane_int(q.t0, s), T = lane_int(q.T, s);
+        int units = lane_int(q.units, s), first_unit = lane_int(q.first, s);
+        const uint32_t weight = lane_u32(weight_of(q), s), base = before + lane_u32(scan, s) - weight;
         if (at - base >= weight) return;
-        const float by_size = __builtin_amdgcn_rcpf((float)size);
-        const int segment = (int)(cut ? quotient(at - base, by_size) : (at - base) / size);
-        const uint32_t seg0 = base + (uint32_t)segment * size;  // of the segment
-        const uint32_t next = seg0 + size;
-        const uint32_t unit0 = cut ? seg0 : seg0 + extra;                // of its first unit
+        // The segment that `at` is in, from seg0 to next: heads of a tile behind each other, as their rows lie in memory; or (WIDE,
+        // unless cut) pairs of tiles of a head, and the last of an odd number.
+        int segment, tile, h;
+        uint32_t seg0, next;
+        float by_size;
+        if (WIDE && !cut) {
+            const int tiles = lane_int(q.tiles, s), pairs = tiles / 2;
+            const uint32_t pair = lane_u32(q.pair, s), head = lane_u32(q.head, s);
+            h = (int)long_quotient(at - base, head);
+            seg0 = base + (uint32_t)h * head;
+            tile = (int)long_quotient(at - seg0, pair);
+            const bool alone = tile >= pairs;
+            if (alone) tile = pairs;
+            seg0 += (uint32_t)tile * pair;
+            next = alone ? base + (uint32_t)(h + 1) * head : seg0 + pair;
+            if (alone) tile = tiles - 1;
+            Units mine = units_of_tile<kTile>(p, n, T, G, tile);
+            const uint32_t second = seg0 + (uint32_t)mine.number + extra;
+            if (!alone && at >= second) {
+                seg0 = second;
+                tile = 2 * pairs - 1 - tile;
+                mine = units_of_tile<kTile>(p, n, T, G, tile);
+            } else if (!alone) {
+                next = second;
+            }
+            units = mine.number;
+            first_unit = mine.first;
+        } else {
+            const uint32_t size = size_of((uint32_t)units);
+            by_size = __builtin_amdgcn_rcpf((float)size);
+            segment = (int)(cut ? quotient(at - base, by_size) : (at - base) / size);
+            seg0 = base + (uint32_t)segment * size;
+            next = seg0 + size;
+        }
+        const uint32_t unit0 = cut ? seg0 : seg0 + extra, unit1 = cut ? next : unit0 + (uint32_t)units;  // of its first unit, behind its last
         int u0 = 0, u1 = units;
         if (p.whole) {
             at = next;
             if (seg0 < begin) continue;  // its beginning was another workgroup's
         } else if (cut) {
-            const int part = (int)quotient((uint32_t)units + size - 1, by_size);
+            const int part = (int)quotient((uint32_t)units + (next - seg0) - 1, by_size);
             u0 = (int)(at - seg0) * part;
             u1 = u0 + part < units ? u0 + part : units;
             at = next;
         } else {
             u0 = at > unit0 ? (int)(at - unit0) : 0;
-            u1 = end < next ? (int)(end - unit0) : units;
+            u1 = end < unit1 ? (int)(end - unit0) : units;
             at = next;
-            if (u1 <= 0) continue;
+            if (u1 <= 0 || (WIDE && u0 >= units)) continue;
         }
         if (g.pages == 0) u1 = u0;  // there is nothing to read
         if (again) __syncthreads();  // the other waves may still read the last segment's sums, which lie where K and V come
         again = true;
         const KvpAttendParams& args = *hidden_arguments<KvpAttendParams>();
         const KvpPages& gp = args.pages;
-        const float scale_log2 = args.scale_log2;
-        const int turn = divide(segment, args.by_kv_heads), h = segment - turn * gp.kv_heads;
-        // (a prefill's last tiles see most: first and last in turn, so that equal runs have equal work)
-        const int tile = WIDE && (turn & 1) ? lane_int(q.tiles, s) - 1 - turn / 2 : WIDE ? turn / 2 : turn;
-        const int first_unit = lane_int(q.first, s);
+        if (!WIDE || cut) {
+            tile = divide(segment, args.by_kv_heads);
+            h = segment - tile * gp.kv_heads;
+        }
+        const float scale = args.scale_log2, unseen = scale < 0.0f ? -kNegInf : kNegInf;
         const int seq = 64 * chunk + s;
 
         const int r0 = tile * kTile, rows = T * G - r0 < kTile ? T * G - r0 : kTile;
@@ -515,24 +604,30 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             #pragma unroll
             for (int i = 0; i < NT; ++i)
                 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] = sums[i][e / 4][e % 4] * scale_log2;
+                for (int e = 0; e < 8; ++e) x[i][e] = sums[i][e / 4][e % 4];
         };
-        // x becomes the weights.  hi is cut off, not rounded, and lo above zero, so that an infinity in V, times both, is
-        // one (lo: 2^-16 of the weight; 2^-20 at least).
+        // x, products not yet scaled, becomes the weights.  hi is cut off, not rounded, and lo (2^-16 of the weight) has 2^-20 of hi added,
+        // so that it is above zero, and an infinity in V, times both, is one.
         auto weigh = [&](bf16x8 (&hi)[NT], bf16x8 (&lo)[NT]) {
             #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 float top = x[i][0];
                 #pragma unroll
                 for (int e = 1; e < 8; ++e) top = __builtin_fmaxf(top, x[i][e]);
-                top = __builtin_fmaxf(m[i], group_max(top));
+                if (scale < 0.0f) {
+                    top = x[i][0];
+                    #pragma unroll
+                    for (int e = 1; e < 8; ++e) top = __builtin_fminf(top, x[i][e]);
+                    top = -top;
+                }
+                top = __builtin_fmaxf(m[i], group_max(top) * __builtin_fabsf(scale));
                 const float from = reference(top);
                 const float fade = m[i] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(reference(m[i]) - from);
                 m[i] = top;
                 float sum = 0.0f;
                 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[i][e] = __builtin_amdgcn_exp2f(x[i][e] - from);
+                    x[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][e], scale, -from));
                     sum += x[i][e];
                 }
                 u32x4 h, low_part;
@@ -541,7 +636,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                     h[e / 2] = __builtin_amdgcn_perm(f32_bits(x[i][e + 1]), f32_bits(x[i][e]), 0x07060302u);
                     const float h0 = bits_f32(h[e / 2] << 16), h1 = bits_f32(h[e / 2] & 0xFFFF0000u);
                     low_part[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
-                        (f32x2){__builtin_fmaxf(x[i][e] - h0, h0 * 0x1p-20f), __builtin_fmaxf(x[i][e + 1] - h1, h1 * 0x1p-20f)}, bf16x2));
+                        (f32x2){__builtin_fmaf(h0, 0x1p-20f - 1.0f, x[i][e]), __builtin_fmaf(h1, 0x1p-20f - 1.0f, x[i][e + 1])}, bf16x2));
                 }
                 hi[i] = __builtin_bit_cast(bf16x8, h);
                 lo[i] = __builtin_bit_cast(bf16x8, low_part);
@@ -656,7 +751,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             #pragma unroll
             for (int i = 0; i < NT; ++i)
                 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] = seen(r, there, e, low[i], pos[i]) ? x[i][e] : kNegInf;
+                for (int e = 0; e < 8; ++e) x[i][e] = seen(r, there, e, low[i], pos[i]) ? x[i][e] : unseen;
         };
         const int steps = WIDE ? u1 - u0 : u1 - u0 > wave ? (u1 - u0 - wave + 3) / 4 : 0;
         for (int step0 = 0; step0 < steps; step0 += 64) {
@@ -737,7 +832,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
 
         const KvpAttendParams& late = *hidden_arguments<KvpAttendParams>();
         // whether the segment's first unit is of this run, and all of them
-        const bool begins = late.whole || unit0 >= begin, one = late.whole || (begins && next <= end);
+        const bool begins = late.whole || unit0 >= begin, one = late.whole || (begins && unit1 <= end);
         const int64_t part0 = (int64_t)(2 * w + (begins ? 1 : 0)) * kTile;
         auto out_row = [&](int rr) -> int64_t {
             const int t = divide(r0 + rr, late.by_group);
@@ -747,7 +842,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             const int64_t to = out_row(rr);
             if (!one) *reinterpret_cast<f32x2*>(late.part_ml + (part0 + rr) * 2) = (f32x2){m, l};
             else if (late.lse) late.lse[to] = (reference(m) + __builtin_amdgcn_logf(l)) * kLn2;
-            if (!late.whole && begins) late.meta[to] = (uint64_t)rr << 48 | (uint64_t)((next - 1) / per - w + 1) << 24 | w;
+            if (!late.whole && begins) late.meta[to] = (uint64_t)rr << 48 | (uint64_t)((unit1 - 1) / per - w + 1) << 24 | w;
         };
         if constexpr (WIDE) {  // a row's values from the lanes that have them
             #pragma unroll

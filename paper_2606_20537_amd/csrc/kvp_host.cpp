@@ -178,13 +178,13 @@ int64_t whole_rows(int32_t d, int64_t segments) { return segments >= wgs_of(d, 1
 //   8 of 16384 x 4    54 / 33 / 41    70 / 64 / 68      172 / 108 / 120
 //   32 of 2048 x 5    41 / 33 / 34    78 / 48 / 55      138 / 97 / 74
 //   32 of 2048 x 9    64 / 37 / 42    120 / 86 / 60     226 / 153 / 94
-//   32 of 2048 x 16   65 / 63 / 47    144 / 82 / 67     358 / 200 / 106
+//   32 of 2048 x 16   65 / 63 / 45    144 / 82 / 64     358 / 200 / 101
 //   1 of 16384 x 9    18 / 18 / 21    29 / 24 / 28      66 / 46 / 51
 //   8 of 300 x 6, G 16  8.5 / 10 / 18   12 / 14 / 23      20 / 24 / 26
 //   4 of 4000 x 16    21 / 20 / 27    49 / 31 / 33      72 / 61 / 44
-//   1 of 16384 x 161  - / 101 / 92    - / 217 / 117     - / 446 / 226
-// and prompts of 16 heads on 4: 1 x 512 9.5 / 11 / 25, 18 / 19 / 27, 40 / 31 / 37; 16 x 512 121 / 74 / 66, 310 / 201 / 128, 672 / 452 / 224;
-// 64 of 100 rows x 32 16 / 18 / 15, 32 / 25 / 21, 87 / 65 / 27.
+//   1 of 16384 x 161  - / 101 / 78    - / 217 / 109     - / 446 / 211
+// and prompts of 16 heads on 4: 1 x 512 9.5 / 11 / 25, 18 / 19 / 27, 40 / 31 / 37; 16 x 512 121 / 74 / 48, 310 / 201 / 98, 672 / 452 / 163;
+// 64 of 100 rows x 32 16 / 18 / 15, 32 / 25 / 21, 87 / 65 / 28.
 int32_t tile_of(const kvp_cache& c, int64_t rows, int64_t seen) {
     auto fills = [&](int64_t tile, int64_t units) {
         const int64_t segments = std::max<int64_t>(c.n_seq, rows / tile) * c.kv_heads, wgs = wgs_of(c.d, (int32_t)tile);
@@ -338,6 +338,7 @@ int kvp_attend(const kvp_attend_args* a, void* stream) {
     cap::KvpAttendParams p{};
     p.scale_log2 = a->scale * 1.4426950408889634f;
     if (!std::isfinite(p.scale_log2)) return CAP_E_INVAL;
+    if (p.scale_log2 == 0.0f) p.scale_log2 = 0x1p-149f;
     Span cache[3], step[2];
     int rc = plan_attend(a, &p, cache, step);
     if (rc != CAP_OK) return rc;

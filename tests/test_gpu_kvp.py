@@ -271,6 +271,31 @@ def test_runs_in_one_launch(d):
     few.check(q, o, lse, d ** -0.5)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 1, 50, 333])
+def test_runs_of_windows(d, window):
+    # some with more tokens than rows, some with rows beyond the table, one to seven tiles each
+    rng = np.random.default_rng(window)
+    n = [1300, 20, 1120, 1160, 64, 500] + rng.integers(0, 400, 18).tolist()
+    T = [110, 70, 33, 222, 64, 32] + rng.integers(60, 130, 18).tolist()
+    s = Step(n, T, 2, d, 16, seed=d + window, columns=70)
+    assert wide(s, 4, window)
+    few = Step.__new__(Step)  # the first eight
+    few.__dict__.update(s.__dict__, n=n[:8], T=T[:8])
+    few.check(*s.attend(4, window=window), d ** -0.5, window)
+
+
+@pytest.mark.parametrize("window", [7, 90])
+def test_runs_of_windows_in_one_launch(window):
+    n = [1300, 20, 900, 40, 64, 500] * 4
+    T = [41, 30, 64, 40, 1, 33] * 4
+    s = Step(n, T, 16, 256, 16, seed=window)
+    assert cap.kvp_attend_workspace_bytes(s.cache, s.tokens, 64, window) == 0
+    few = Step.__new__(Step)
+    few.__dict__.update(s.__dict__, n=n[:6], T=T[:6])
+    few.check(*s.attend(4, window=window), 0.0625, window)
+
+
 def test_runs_on_absent_pages_and_before_the_first_row():
     # the first 150 tokens of sequence 0 see nothing, those of sequence 3 neither
     s = Step([50, 400, 500, 90], [200, 150, 40, 30], 2, 64, 16, seed=2, columns=2600, absent=[(0, 1), (1, 0), (1, 7), (1, 12), (1, 24)] + [(3, c) for c in range(6)])
@@ -334,6 +359,25 @@ def test_large_scores():
     s = Step([600, 3], [1, 2], 2, 64, 16, seed=6)
     for scale in (30.0, -30.0, 0.0):
         s.check(*s.attend(2, scale=scale), scale)
+    s = Step([300, 90], [150, 60], 2, 128, 16, seed=7, columns=6000)
+    assert wide(s, 2)
+    for scale in (5.0, -5.0, 0.0, 1e-44):
+        s.check(*s.attend(2, scale=scale), scale)
+
+
+@pytest.mark.parametrize("T", [1, 100])
+def test_scores_beyond_fp32(T):
+    # row 3's product with the first channel of a query is 2^100, times the scale 2^30 above the range; with -2^30 below it
+    s = Step([150, 40], [T, 1], 1, 64, 16, seed=7, columns=19300)
+    s.k[int(s.table[0, 0]), 3, 0] = 0
+    s.k[int(s.table[0, 0]), 3, 0, 0] = 2.0 ** 100
+    q = s.normal(s.tokens, 3, 64) * 1e-9
+    q[:, :, 0] = 1.0
+    assert T == 1 or wide(s, 3)
+    _, o, lse = s.attend(3, q=q, scale=2.0 ** 30)
+    assert o[:T].isnan().all() and lse[:T].isnan().all() and o[T:].isfinite().all() and lse[T:].isfinite().all()
+    _, o, lse = s.attend(3, q=q, scale=-2.0 ** 30)
+    assert o.isfinite().all() and lse.isfinite().all()
 
 
 def test_strided_queries_and_pools():
