@@ -807,9 +807,9 @@ CAP_API int kvp_append(const kvp_append_args* args, void* stream);
  * values are finite.  A score above fp32's range gives NaN, one below it counts as none.
  * Made for one token or a few drafts of each sequence, in tiles of 16 or 32 query rows (tokens x
  * heads / kv_heads), and for runs of tokens, in tiles of 128.
- * Two launches; one where columns * page, or the window and the tokens, are a few hundred rows (those that need no workspace).  Results are reproducible for the same arguments and
- * device data; a row's last bits depend on the other sequences of the call, over which work is
- * dealt out evenly. */
+ * Two launches; one where columns * page, or the window and the tokens, are a few hundred rows
+ * (those that need no workspace).  Results are reproducible for the same arguments and device data;
+ * a row's last bits depend on the other sequences of the call, over which work is dealt out evenly. */
 typedef struct kvp_attend_args {
     const kvp_cache* cache;      /* HOST */
     const int32_t*   lens;
@@ -827,8 +827,8 @@ typedef struct kvp_attend_args {
 } kvp_attend_args;
 
 /* Workspace of a call with these sizes (the cache's, tokens, heads and window; that of window 0 does for
- * any; 70 MB at most and 8 bytes for each query row); 0 where the call needs none or is refused.  It holds nothing between calls; calls that may overlap need
- * their own. */
+ * any; 70 MB at most and 8 bytes for each query row); 0 where the call needs none or is refused.
+ * It holds nothing between calls; calls that may overlap need their own. */
 CAP_API uint64_t kvp_attend_workspace_bytes(const kvp_attend_args* args);
 CAP_API int kvp_attend(const kvp_attend_args* args, void* stream);
 

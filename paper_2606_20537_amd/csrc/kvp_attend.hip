@@ -435,6 +435,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             seg0 = base + (uint32_t)segment * size;
             next = seg0 + size;
         }
+        if (next <= at) return;  // (sums past 32 bits, of tok0 that does not ascend)
         const uint32_t unit0 = cut ? seg0 : seg0 + extra, unit1 = cut ? next : unit0 + (uint32_t)units;  // of its first unit, behind its last
         int u0 = 0, u1 = units;
         if (p.whole) {

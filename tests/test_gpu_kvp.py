@@ -594,6 +594,32 @@ def test_decode_graph_goes_on_with_the_sequences():
         assert torch.equal(eager.k, graphed.k) and torch.equal(eager.v, graphed.v)
 
 
+def test_graph_of_a_run_goes_on_with_the_sequences():
+    s = Step([1500, 900, 700], [200, 60, 40], 2, 128, 16, seed=12, columns=1600)
+    assert wide(s, 4)
+    q, o, lse = s.normal(300, 8, 128), torch.zeros((300, 8, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((300, 8), device="cuda")
+    work = torch.empty(cap.kvp_attend_workspace_bytes(s.cache, 300, 8, 0), dtype=torch.uint8, device="cuda")
+    call = lambda o, lse, **kw: cap.kvp_attend(s.cache, s.lens, q, o, scale=0.1, tok0=s.tok0, lse=lse, **kw)
+    call(o, lse, workspace=work)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(o, lse, workspace=work)
+    for n, t in (([1500, 900, 700], [200, 60, 40]), ([1, 0, 600], [1, 0, 299]), ([0, 0, 0], [0, 0, 0]), ([300, 10, 0], [300, 0, 0]), ([1499, 5, 250], [10, 5, 250])):
+        s.lens.copy_(torch.tensor(n, dtype=torch.int32))
+        s.tok0.copy_(torch.tensor([sum(t[:i]) for i in range(4)], dtype=torch.int32))
+        work.fill_(0xFF)
+        eo, el = torch.full_like(o, 2.0), torch.full_like(lse, 2.0)
+        o.fill_(2.0)
+        lse.fill_(2.0)
+        g.replay()
+        call(eo, el)
+        torch.cuda.synchronize()
+        assert torch.equal(o, eo) and torch.equal(lse, el), n
+        s.n, s.T = n, t
+        s.check(q[:sum(t)], o[:sum(t)], lse[:sum(t)], 0.1)
+        assert (o[sum(t):] == 2).all() and (lse[sum(t):] == 2).all()
+
+
 def test_on_another_stream_with_its_own_workspace():
     s = Step([3000, 5], [1, 1], 2, 128, 16, seed=1)
     q, o, lse = s.attend(4)
