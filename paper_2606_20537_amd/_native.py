@@ -616,7 +616,7 @@ def _kvb_table(fn, seqs):
 
 
 def _kvb_device(fn, first, *rest):
-    """The tensors are on the current device, where the call launches."""
+    """The tensors are on the current device, where the call launches; its number."""
     index = first.get_device()
     ok = index >= 0
     for x in rest:
@@ -627,6 +627,7 @@ def _kvb_device(fn, first, *rest):
         ok = index == (raw[1]() if raw else _kvb_torch()[0].cuda.current_device())
     if not ok:
         raise ValueError("%s: every tensor is on the current GPU" % fn)
+    return index
 
 
 def _kvb_tokens(fn, name, x):
@@ -774,10 +775,16 @@ _pack_attend = struct.Struct("<QQQ" + "Qqq" + "QQQQqiifi").pack
 _NO_ROWS = (0, 0, 0)
 
 
-def _qk_rows(fn, name, x, shape, dtype):
-    """The fields of qk_rows for a tensor [tokens, heads, d]."""
-    if x.dtype != dtype or x.shape != shape:
-        raise ValueError("%s: %s is a %s tensor of shape %s, not %s %s" % (fn, name, dtype, list(shape), x.dtype, list(x.shape)))
+def _qk_shape(fn, name, x):
+    shape = x.shape
+    if len(shape) != 3:
+        raise ValueError("%s: %s is a tensor [tokens, heads, d]" % (fn, name))
+    return shape
+
+
+def _qk_strides(fn, name, x, shape):
+    """The fields of qk_rows for a tensor of this shape [tokens, heads, d].  (A look at a tensor takes the host 0.1 us, at its
+    shape 0.2: each is asked once.)"""
     if x.is_contiguous():
         return x.data_ptr(), 0, 0
     tokens, heads, d = shape
@@ -789,25 +796,29 @@ def _qk_rows(fn, name, x, shape, dtype):
     return x.data_ptr(), st if tokens > 1 else 0, head
 
 
-def _qk_shape(fn, name, x):
-    if x.ndim != 3:
-        raise ValueError("%s: %s is a tensor [tokens, heads, d]" % (fn, name))
-    return x.shape
+def _qk_rows(fn, name, x, shape, dtype, has=None):
+    """The fields of qk_rows for a tensor that has to have this shape and type (has: its shape, where that is known)."""
+    if x.dtype != dtype or (x.shape if has is None else has) != shape:
+        raise ValueError("%s: %s is a %s tensor of shape %s, not %s %s" % (fn, name, dtype, list(shape), x.dtype, list(x.shape)))
+    return _qk_strides(fn, name, x, shape)
 
 
 def _qk_ints(fn, name, x, shape):
     """Address of a contiguous int32 tensor of the GPU (None: 0)."""
     if x is None:
         return 0
-    if x.dtype != _kvb_torch()[3] or x.shape != shape or not x.is_contiguous():
+    if x.dtype != _torch[3] or x.shape != shape or not x.is_contiguous():
         raise ValueError("%s: %s is a contiguous int32 tensor of shape %s" % (fn, name, list(shape)))
     return x.data_ptr()
 
 
 def _qk_pos(fn, rule, pos, tokens):
-    if pos is not None and pos.ndim == 1 and rule.axes == 1:
-        return _qk_ints(fn, "pos", pos, (tokens,))
-    return _qk_ints(fn, "pos", pos, (tokens, rule.axes))
+    if pos is None:
+        return 0
+    shape, axes = pos.shape, rule.axes
+    if (shape != (tokens, axes) and (axes != 1 or shape != (tokens,))) or pos.dtype != _torch[3] or not pos.is_contiguous():
+        raise ValueError("%s: pos is a contiguous int32 tensor of shape %s" % (fn, [tokens, axes]))
+    return pos.data_ptr()
 
 
 def _qk_rule(fn, rule, d, device):
@@ -821,31 +832,40 @@ def qk_norm_rope(rule, q, k, q_out=None, k_out=None, *, pos=None, stream=None):
     """Norm and rotation of q [tokens, heads, d] and k [tokens, kv_heads, d] (either may be None), to q_out and
     k_out (None: in place).  pos: int32 [tokens, axes]."""
     fn = "qk_norm_rope"
-    _, bf16, f32, _ = _kvb_torch()
+    _, bf16, f32, _ = _torch or _kvb_torch()
     like = q if q is not None else k
     if like is None:
         raise ValueError("qk_norm_rope: neither q nor k")
-    tokens, _, d = _qk_shape(fn, "q" if q is not None else "k", like)
-    dtype = like.dtype
+    shape, dtype = _qk_shape(fn, "q" if q is not None else "k", like), like.dtype
+    tokens, _, d = shape
     if dtype != bf16 and dtype != f32:
         raise ValueError("qk_norm_rope: bfloat16 or float32 tensors, not %s" % dtype)
     heads = kv_heads = 0
     of_q = of_k = to_q = to_k = _NO_ROWS
     if q is not None:
-        shape, q_out = q.shape, q if q_out is None else q_out
-        heads, of_q = shape[1], _qk_rows(fn, "q", q, shape, dtype)
-        to_q = of_q if q_out is q else _qk_rows(fn, "q_out", q_out, shape, dtype)
+        heads, of_q = shape[1], _qk_strides(fn, "q", q, shape)
+        if q_out is None or q_out is q:
+            q_out, to_q = None, of_q
+        else:
+            to_q = _qk_rows(fn, "q_out", q_out, shape, dtype)
     elif q_out is not None:
         raise ValueError("qk_norm_rope: q_out without q")
     if k is not None:
-        shape, k_out = (tokens, _qk_shape(fn, "k", k)[1], d), k if k_out is None else k_out
-        kv_heads, of_k = shape[1], _qk_rows(fn, "k", k, shape, dtype)
-        to_k = of_k if k_out is k else _qk_rows(fn, "k_out", k_out, shape, dtype)
+        if k is not like:
+            has = _qk_shape(fn, "k", k)
+            shape = (tokens, has[1], d)
+            of_k = _qk_rows(fn, "k", k, shape, dtype, has)
+        else:
+            of_k = _qk_strides(fn, "k", k, shape)
+        kv_heads = shape[1]
+        if k_out is None or k_out is k:
+            k_out, to_k = None, of_k
+        else:
+            to_k = _qk_rows(fn, "k_out", k_out, shape, dtype)
     elif k_out is not None:
         raise ValueError("qk_norm_rope: k_out without k")
     at = _qk_pos(fn, rule, pos, tokens)
-    _kvb_device(fn, like, q_out, k, k_out, pos)
-    _qk_rule(fn, rule, d, like.get_device())
+    _qk_rule(fn, rule, d, _kvb_device(fn, like, q_out, k if k is not like else None, k_out, pos))
     a = _pack_norm_rope(rule.address, *of_q, *of_k, *to_q, *to_k, at, tokens, heads, kv_heads, d, CAP_DTYPE_F32 if dtype == f32 else CAP_DTYPE_BF16)
     return _check(fn, load().qk_norm_rope(a, _stream(stream)))
 
@@ -888,10 +908,11 @@ def kvp_append(cache, lens, k, v, *, tok0=None, rule=None, q=None, q_out=None, p
     the way, and q [tokens, heads, d] to q_out (None: in place).  lens [n_seq], tok0 [n_seq + 1] and pos [tokens, axes]
     are int32 tensors on the GPU."""
     fn = "kvp_append"
-    bf16 = _kvb_torch()[1]
-    shape = (_qk_shape(fn, "k", k)[0], cache.kv_heads, cache.d)
-    tokens = shape[0]
-    of_k, of_v = _qk_rows(fn, "k", k, shape, bf16), _qk_rows(fn, "v", v, shape, bf16)
+    bf16 = (_torch or _kvb_torch())[1]
+    has = _qk_shape(fn, "k", k)
+    tokens = has[0]
+    shape = (tokens, cache.kv_heads, cache.d)
+    of_k, of_v = _qk_rows(fn, "k", k, shape, bf16, has), _qk_rows(fn, "v", v, shape, bf16)
     heads = at = by = 0
     of_q = to_q = _NO_ROWS
     if rule is None:
@@ -901,13 +922,17 @@ def kvp_append(cache, lens, k, v, *, tok0=None, rule=None, q=None, q_out=None, p
         _qk_rule(fn, rule, cache.d, cache.device)
         by, at = rule.address, _qk_pos(fn, rule, pos, tokens)
         if q is not None:
-            heads = _qk_shape(fn, "q", q)[1]
-            shape, q_out = (tokens, heads, cache.d), q if q_out is None else q_out
-            of_q = _qk_rows(fn, "q", q, shape, bf16)
-            to_q = of_q if q_out is q else _qk_rows(fn, "q_out", q_out, shape, bf16)
+            has = _qk_shape(fn, "q", q)
+            heads = has[1]
+            shape = (tokens, heads, cache.d)
+            of_q = _qk_rows(fn, "q", q, shape, bf16, has)
+            if q_out is None or q_out is q:
+                q_out, to_q = None, of_q
+            else:
+                to_q = _qk_rows(fn, "q_out", q_out, shape, bf16)
         elif q_out is not None:
             raise ValueError("kvp_append: q_out without q")
-    _kvb_device(fn, cache.like, lens, k, v, tok0, q, q_out, pos)
+    _kvb_device(fn, k, lens, cache.like, v, tok0, q, q_out, pos)
     a = _pack_append(cache.address, _qk_ints(fn, "lens", lens, (cache.n_seq,)), _qk_ints(fn, "tok0", tok0, (cache.n_seq + 1,)), by, *of_k, *of_v,
                      *of_q, *to_q, at, tokens, heads, 0)
     return _check(fn, load().kvp_append(a, _stream(stream)))
@@ -924,13 +949,14 @@ def kvp_attend(cache, lens, q, o, *, scale, tok0=None, window=0, lse=None, works
     [tokens, heads] (float32).  lens [n_seq] and tok0 [n_seq + 1] are int32 tensors on the GPU.  With no workspace
     given, one is allocated as a torch tensor of the call's stream for the duration of the call."""
     fn = "kvp_attend"
-    _, bf16, f32, _ = _kvb_torch()
-    tokens, heads, _ = _qk_shape(fn, "q", q)
+    _, bf16, f32, _ = _torch or _kvb_torch()
+    has = _qk_shape(fn, "q", q)
+    tokens, heads, _ = has
     shape = (tokens, heads, cache.d)
     _kvb_out(fn, "o", o, shape, bf16)
     _kvb_out(fn, "lse", lse, (tokens, heads), f32)
     _kvb_device(fn, cache.like, lens, q, o, tok0, lse, workspace)
-    of_q, at = _qk_rows(fn, "q", q, shape, bf16), _qk_ints(fn, "lens", lens, (cache.n_seq,))
+    of_q, at = _qk_rows(fn, "q", q, shape, bf16, has), _qk_ints(fn, "lens", lens, (cache.n_seq,))
     to, of_lse, first = o.data_ptr(), lse.data_ptr() if lse is not None else 0, _qk_ints(fn, "tok0", tok0, (cache.n_seq + 1,))
     lib, handle = load(), _stream(stream)
     if workspace is None:
