@@ -803,7 +803,7 @@ CAP_API int kvp_append(const kvp_append_args* args, void* stream);
  * its result, infinities and NaN included; a row with such values that it sees makes those channels
  * infinite or NaN.
  * Precision: products and sums are fp32, weights enter the second product with 16 bits (two bf16),
- * o is rounded once.  Weights below 2^-100 of the largest may count as none.  Means of finite
+ * o is rounded once.  Weights below 2^-90 of the largest may count as none.  Means of finite
  * values are finite.  A score above fp32's range gives NaN, one below it counts as none.
  * Made for one token or a few drafts of each sequence, in tiles of 16 or 32 query rows (tokens x
  * heads / kv_heads), and for runs of tokens, in tiles of 128.

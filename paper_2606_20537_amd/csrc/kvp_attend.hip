@@ -4,7 +4,7 @@
 //   l = sum_j exp(x_j - m),  lse = m + log l,  over the rows j that the query
 //   sees: max(0, pos - window + 1) <= j <= pos, on pages that are there
 //
-// in one pass over K and V with a running m and l.  The query rows of a KV head
+// in one pass over K and V with a running m (or one a little below the maximum) and l.  The query rows of a KV head
 // (tokens x query heads of the group) share its K and V: 16 of them, twice 16 or eight times, are the
 // columns of the matrix instructions, keys and channels the rows.
 //  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 tiles, sums in fp32.
@@ -33,7 +33,7 @@
 // Long runs of tokens (prompts, resumed turns) have tiles of 128 query rows, where arithmetic counts: each wave
 // has its own rows and all of the units, which the waves load together into a ring of four, with
 // a barrier to each, so that K and V come from memory once for 128 rows and not for 32.  16384 tokens behind none, 32 heads on 4 of
-// 64, 128 and 256 channels: 2.7, 3.9 and 8.6 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.62 to 0.84 PFLOP/s
+// 64, 128 and 256 channels: 2.6, 3.9 and 8.4 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.62 to 0.84 PFLOP/s
 // of matrix instructions with both parts of P, and between them the weights' exponentials.  Loads are kept by the caches here, as other tiles read the same.
 //
 // What bounds it, one token, 8 query heads on each KV head of 256 channels: 131072 + 16449 + 2111 + 1 rows
@@ -59,9 +59,10 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int kThreads = 256;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
-// Weights are 2^-24 of what exp(x - m) gives, so that sums of 2^24 values, the most that a
-// sequence has, cannot overflow and means of finite values stay finite.
-constexpr float kAbove = 24.0f;
+// m may stay up to kBehind below the highest score so far (log2 units), as a new m has a row's sums multiplied: 512 tokens of 16 sequences, 16
+// heads on 4 of 256 channels 554 us with every new one, 531 so.  Weights are 2^-kAbove of what exp(x - m) gives, 2^-24 at most, so that
+// sums of 2^24 values, the most that a sequence has, cannot overflow and means of finite values stay finite.
+constexpr float kBehind = 8.0f, kAbove = 24.0f + kBehind;
 // Parts of even cuts at least (a unit to each wave) and at most; with longer ones equal runs leave fewer workgroups idle.
 constexpr uint32_t kLeastCut = 4, kMostCut = 32;
 
@@ -211,7 +212,7 @@ __device__ inline void meet_waves() {
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
-// What scores are taken from, m the highest of them (-inf: none yet; inf: NaN).
+// What scores are taken from, m as above (-inf: none yet; inf: NaN).
 __device__ inline float reference(float m) { return m == kNegInf ? 0.0f : m + (kAbove + (m - m)); }
 
 // Inclusive prefix sum over the lanes of a wave (as dev::wave_inclusive_sum).
@@ -621,7 +622,8 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                     for (int e = 1; e < 8; ++e) top = __builtin_fminf(top, x[i][e]);
                     top = -top;
                 }
-                top = __builtin_fmaxf(m[i], group_max(top) * __builtin_fabsf(scale));
+                top = group_max(top) * __builtin_fabsf(scale);
+                top = top > m[i] + kBehind ? top : m[i];
                 const float from = reference(top);
                 const float fade = m[i] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(reference(m[i]) - from);
                 m[i] = top;
@@ -909,7 +911,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
     }
 }
 
-// A running sum of parts: m the highest score, l the sum of weights, o that of weighted values.
+// A running sum of parts: m as above, l the sum of weights, o that of weighted values.
 struct Joined {
     float m = kNegInf, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};

@@ -60,13 +60,13 @@ def attend_near(o, lse, plain, n):
     """Whether a row's results are as near as the arithmetic allows.
 
     Scores: sums of d <= 256 products in fp32 (256 * 2^-24 of their magnitudes), times the scale; exponents in fp32
-    (2^-22 of score and reference).  A score's error dx changes a weight by the factor 1 +- 2 dx (weight and sum).
+    (2^-22 of score and reference, which stands 32 above a score).  A score's error dx changes a weight by the factor 1 +- 2 dx (weight and sum).
     Weights enter as hi + lo, two bf16 (2^-16), sums over n rows in fp32: 32 products to an instruction, then n / 32 of
     them and the joins (n / 32 + 96 roundings).  The output's rounding is half a step of bf16, 2^-8."""
     want, want_lse, mass, size = plain
     if not np.isfinite(want_lse):
         return np.isnan(o).all() and np.isnan(lse) if np.isnan(want_lse) else not o.any() and lse == want_lse
-    dx = 2.0 ** -16 * size + 2.0 ** -22 * (abs(want_lse) + size + 24)
+    dx = 2.0 ** -16 * size + 2.0 ** -22 * (abs(want_lse) + size + 32)
     steps = (n / 32 + 96) * 2.0 ** -24
     far = mass * (2.0 ** -16 + 2 * dx + 2 * steps) + 1e-37
     far = far + 2.0 ** -8 * (np.abs(want) + far)
