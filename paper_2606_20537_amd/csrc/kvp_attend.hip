@@ -33,7 +33,7 @@
 // Long runs of tokens (prompts, resumed turns) have tiles of 128 query rows, where arithmetic counts: each wave
 // has its own rows and all of the units, which the waves load together into a ring of four, with
 // a barrier to each, so that K and V come from memory once for 128 rows and not for 32.  16384 tokens behind none, 32 heads on 4 of
-// 64, 128 and 256 channels: 2.6, 3.9 and 8.4 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.62 to 0.84 PFLOP/s
+// 64, 128 and 256 channels: 2.5, 3.8 and 8.3 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.66 to 0.87 PFLOP/s
 // of matrix instructions with both parts of P, and between them the weights' exponentials.  Loads are kept by the caches here, as other tiles read the same.
 //
 // What bounds it, one token, 8 query heads on each KV head of 256 channels: 131072 + 16449 + 2111 + 1 rows
@@ -59,8 +59,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int kThreads = 256;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
-// m may stay up to kBehind below the highest score so far (log2 units), as a new m has a row's sums multiplied: 512 tokens of 16 sequences, 16
-// heads on 4 of 256 channels 554 us with every new one, 531 so.  Weights are 2^-kAbove of what exp(x - m) gives, 2^-24 at most, so that
+// m may stay up to kBehind below the highest score so far (log2 units), as a new m has all rows' sums multiplied, and comes
+// seldom so: 512 tokens of 16 sequences, 16 heads on 4 of 64 and 256 channels 211 and 554 us with every new one, 194 and 528 so.  Weights are 2^-kAbove of what exp(x - m) gives, 2^-24 at most, so that
 // sums of 2^24 values, the most that a sequence has, cannot overflow and means of finite values stay finite.
 constexpr float kBehind = 8.0f, kAbove = 24.0f + kBehind;
 // Parts of even cuts at least (a unit to each wave) and at most; with longer ones equal runs leave fewer workgroups idle.
@@ -524,10 +524,11 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
         }
 
         f32x4 acc[NT][NC];  // channels 16 c + 4 grp ..
-        float m[NT], l[NT];
+        float m[NT], from[NT], l[NT];  // from: reference(m)
         #pragma unroll
         for (int i = 0; i < NT; ++i) {
             m[i] = kNegInf;
+            from[i] = 0.0f;
             l[i] = 0.0f;
             #pragma unroll
             for (int c = 0; c < NC; ++c) acc[i][c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
@@ -611,28 +612,50 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
         // x, products not yet scaled, becomes the weights.  hi is cut off, not rounded, and lo (2^-16 of the weight) has 2^-20 of hi added,
         // so that it is above zero, and an infinity in V, times both, is one.
         auto weigh = [&](bf16x8 (&hi)[NT], bf16x8 (&lo)[NT]) {
+            float top[NT];
+            bool above = false;
+            if (scale < 0.0f) {
+                #pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    top[i] = x[i][0];
+                    #pragma unroll
+                    for (int e = 1; e < 8; ++e) top[i] = __builtin_fminf(top[i], x[i][e]);
+                    top[i] = -top[i];
+                }
+            } else {
+                #pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    top[i] = x[i][0];
+                    #pragma unroll
+                    for (int e = 1; e < 8; ++e) top[i] = __builtin_fmaxf(top[i], x[i][e]);
+                }
+            }
             #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                float top = x[i][0];
+                top[i] = group_max(top[i]) * __builtin_fabsf(scale);
+                above |= top[i] > m[i] + kBehind;
+            }
+            if (__any(above)) {
                 #pragma unroll
-                for (int e = 1; e < 8; ++e) top = __builtin_fmaxf(top, x[i][e]);
-                if (scale < 0.0f) {
-                    top = x[i][0];
+                for (int i = 0; i < NT; ++i) {
+                    top[i] = top[i] > m[i] + kBehind ? top[i] : m[i];
+                    const float fade = m[i] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(from[i] - reference(top[i]));
+                    m[i] = top[i];
+                    from[i] = reference(top[i]);
+                    l[i] *= fade;
                     #pragma unroll
-                    for (int e = 1; e < 8; ++e) top = __builtin_fminf(top, x[i][e]);
-                    top = -top;
+                    for (int c = 0; c < NC; ++c) acc[i][c] *= fade;
                 }
-                top = group_max(top) * __builtin_fabsf(scale);
-                top = top > m[i] + kBehind ? top : m[i];
-                const float from = reference(top);
-                const float fade = m[i] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(reference(m[i]) - from);
-                m[i] = top;
+            }
+            #pragma unroll
+            for (int i = 0; i < NT; ++i) {
                 float sum = 0.0f;
                 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][e], scale, -from));
+                    x[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][e], scale, -from[i]));
                     sum += x[i][e];
                 }
+                l[i] += sum;
                 u32x4 h, low_part;
                 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
@@ -643,11 +666,6 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                 }
                 hi[i] = __builtin_bit_cast(bf16x8, h);
                 lo[i] = __builtin_bit_cast(bf16x8, low_part);
-                l[i] = l[i] * fade + sum;
-                if (__any(fade != 1.0f)) {
-                    #pragma unroll
-                    for (int c = 0; c < NC; ++c) acc[i][c] *= fade;
-                }
             }
         };
         // f(c, the eight keys of a lane in channel 16 c + li), for all blocks of 16 channels.
