@@ -33,11 +33,11 @@
 // Long runs of tokens (prompts, resumed turns) have tiles of 128 query rows, where arithmetic counts: each wave
 // has its own rows and all of the units, which the waves load together into a ring of four, with
 // a barrier to each, so that K and V come from memory once for 128 rows and not for 32.  16384 tokens behind none, 32 heads on 4 of
-// 64, 128 and 256 channels: 2.5, 3.8 and 8.3 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.66 to 0.87 PFLOP/s
+// 64, 128 and 256 channels: 2.4, 3.7 and 8.0 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.67 to 0.89 PFLOP/s
 // of matrix instructions with both parts of P, and between them the weights' exponentials.  Loads are kept by the caches here, as other tiles read the same.
 //
 // What bounds it, one token, 8 query heads on each KV head of 256 channels: 131072 + 16449 + 2111 + 1 rows
-// x 4 heads, 613 MB, 100 us + 5 of the join (6.1 TB/s); 16385 rows x 4, 67 MB, 17 + 4, of which the data take
+// x 4 heads, 613 MB, 99 us + 5 of the join (6.2 TB/s); 16385 rows x 4, 67 MB, 17 + 4, of which the data take
 // 10, the way to the first load 4 (lengths, table and 400 instructions behind each other) and the last sums 2.
 #include <hip/hip_runtime.h>
 
@@ -668,32 +668,6 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                 lo[i] = __builtin_bit_cast(bf16x8, low_part);
             }
         };
-        // f(c, the eight keys of a lane in channel 16 c + li), for all blocks of 16 channels.
-        auto each_block = [&](auto&& f) {
-            const uint32_t from = hidden(vread) + (uint32_t)(place * (2 * kSlot));
-            constexpr int kAtOnce = NC < 8 || NT > 1 ? 4 : 8;
-            #pragma unroll
-            for (int c0 = 0; c0 < NC; c0 += kAtOnce) {
-                uint32_t at[kAtOnce];
-                u32x2 v[2 * kAtOnce];
-                #pragma unroll
-                for (int c = 0; c < kAtOnce; ++c) at[c] = from ^ (uint32_t)((c0 + c) << 5);
-                if constexpr (kAtOnce == 4) read_v4<16 * D * 2>(at, v);
-                else read_v8<16 * D * 2>(at, v);
-                #pragma unroll
-                for (int c = 0; c < kAtOnce; ++c) f(c0 + c, (u32x4){v[2 * c][0], v[2 * c][1], v[2 * c + 1][0], v[2 * c + 1][1]});
-            }
-        };
-        auto add_values = [&](const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT]) {
-            each_block([&](int c, const u32x4& v) {
-                #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    acc[i][c] = dev::mma(__builtin_bit_cast(bf16x8, v), hi[i], acc[i][c]);
-                    acc[i][c] = dev::mma(__builtin_bit_cast(bf16x8, v), lo[i], acc[i][c]);
-                }
-            });
-        };
-
         // In a unit that some row does not see in full, or that lies on no page in part (there: the halves that are on
         // one), a key that a row does not see has to leave the product, as its V may hold an infinity or NaN, of which
         // no weight makes zero.  Keys that no row sees are cleared, and where rows see different ones, such
@@ -702,29 +676,54 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             const int key = r + 4 * grp + (e < 4 ? e : 12 + e);
             return (there >> (e / 4) & 1) && key <= last && key > first;
         };
-        auto add_seen_values = [&](int r, int there, const int64_t (&at)[2], const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT]) {
-            uint32_t keep[4];  // bits of keys 2i and 2i + 1
-            #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                keep[i] = (seen(r, there, 2 * i, low0, pos1) ? 0xFFFFu : 0u) | (seen(r, there, 2 * i + 1, low0, pos1) ? 0xFFFF0000u : 0u);
+        // (all: every row sees all of the unit.  Products of their own for it had the compiler keep the sums in two places: 32 to 45
+        // registers more, and 16384 tokens of 128 and 256 channels 3.89 and 8.33 ms, now 3.72 and 8.01.)
+        auto add_values = [&](bool all, int r, int there, const int64_t (&at)[2], const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT]) {
+            uint32_t keep[4] = {};  // bits of keys 2i and 2i + 1
+            if (!all) {
+                #pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    keep[i] = (seen(r, there, 2 * i, low0, pos1) ? 0xFFFFu : 0u) | (seen(r, there, 2 * i + 1, low0, pos1) ? 0xFFFF0000u : 0u);
+            }
             const bool mixed = pos0 != pos1;
             bool found = false;
-            each_block([&](int c, u32x4 v) {
+            const uint32_t from_v = hidden(vread) + (uint32_t)(place * (2 * kSlot));
+            constexpr int kAtOnce = NC < 8 || NT > 1 ? 4 : 8;
+            #pragma unroll
+            for (int c0 = 0; c0 < NC; c0 += kAtOnce) {
+                uint32_t from[kAtOnce];
+                u32x2 pair[2 * kAtOnce];
+                u32x4 v[kAtOnce];  // the eight keys of a lane in channel 16 c + li
                 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[i] &= keep[i];
-                    const uint32_t out = ((v[i] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((v[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+                for (int c = 0; c < kAtOnce; ++c) from[c] = from_v ^ (uint32_t)((c0 + c) << 5);
+                if constexpr (kAtOnce == 4) read_v4<16 * D * 2>(from, pair);
+                else read_v8<16 * D * 2>(from, pair);
+                #pragma unroll
+                for (int c = 0; c < kAtOnce; ++c) v[c] = (u32x4){pair[2 * c][0], pair[2 * c][1], pair[2 * c + 1][0], pair[2 * c + 1][1]};
+                if (!all) {
+                    #pragma unroll
+                    for (int c = 0; c < kAtOnce; ++c)
+                        #pragma unroll
+                        for (int i = 0; i < 4; ++i) v[c][i] &= keep[i];
                     if (mixed) {
-                        found |= out != 0;
-                        v[i] &= ~out;
+                        #pragma unroll
+                        for (int c = 0; c < kAtOnce; ++c)
+                            #pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t out = ((v[c][i] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((v[c][i] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+                                found |= out != 0;
+                                v[c][i] &= ~out;
+                            }
                     }
                 }
                 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    acc[i][c] = dev::mma(__builtin_bit_cast(bf16x8, v), hi[i], acc[i][c]);
-                    acc[i][c] = dev::mma(__builtin_bit_cast(bf16x8, v), lo[i], acc[i][c]);
-                }
-            });
+                for (int c = 0; c < kAtOnce; ++c)
+                    #pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        acc[i][c0 + c] = dev::mma(__builtin_bit_cast(bf16x8, v[c]), hi[i], acc[i][c0 + c]);
+                        acc[i][c0 + c] = dev::mma(__builtin_bit_cast(bf16x8, v[c]), lo[i], acc[i][c0 + c]);
+                    }
+            }
             if (!__any(found)) return;
             #pragma unroll 1
             for (int t = 0; t < kKvpUnit; ++t) {
@@ -810,8 +809,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                         if (!all) hide_unseen(r, there);
                         bf16x8 hi[NT], lo[NT];
                         weigh(hi, lo);
-                        if (all) add_values(hi, lo);
-                        else add_seen_values(r, there, a, hi, lo);
+                        add_values(all, r, there, a, hi, lo);
                     }
                     place = (place + 1) & 3;
                 }
@@ -843,8 +841,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                 weigh(hi, lo);
                 if (more) wait_loads<kLoads>();  // V: the next K's are behind it
                 else wait_loads<0>();
-                if (all) add_values(hi, lo);
-                else add_seen_values(r, there_now, now, hi, lo);
+                add_values(all, r, there_now, now, hi, lo);
                 if (!more) break;
                 wait_lds();
                 load_v(a);
