@@ -74,7 +74,7 @@ struct KvpAttendParams {
     QkRows   q;
     void*    o;
     float*   lse;      // may be null
-    float*   part_o;   // [2 wgs][tile][d], not divided by l
+    float*   part_o;   // [2 wgs][tile][d], means
     float*   part_ml;  // [2 wgs][tile][2]: m (log2 units), sum
     uint64_t* meta;    // [tokens, heads]: first workgroup, parts, row of the segment
     int64_t  tokens;

@@ -60,8 +60,10 @@ constexpr int kThreads = 256;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
 // m may stay up to kBehind below the highest score so far (log2 units), as a new m has all rows' sums multiplied, and comes
-// seldom so: 512 tokens of 16 sequences, 16 heads on 4 of 64 and 256 channels 211 and 554 us with every new one, 194 and 528 so.  Weights are 2^-kAbove of what exp(x - m) gives, 2^-24 at most, so that
-// sums of 2^24 values, the most that a sequence has, cannot overflow and means of finite values stay finite.
+// seldom so: 512 tokens of 16 sequences, 16 heads on 4 of 64 and 256 channels 211 and 554 us with every new one, 194 and 528 so.
+// Sums of large values may leave fp32's range where their mean does not.  Such segments are taken a second time, with weights
+// of 2^-kAbove of what exp(x - m) gives, 2^-24 at most, so that sums of 2^24 values, the most that a sequence has, stay finite; and only
+// means that were not finite are replaced, as small values in other channels would lose bits to such weights.
 constexpr float kBehind = 8.0f, kAbove = 24.0f + kBehind;
 // Parts of even cuts at least (a unit to each wave) and at most; with longer ones equal runs leave fewer workgroups idle.
 constexpr uint32_t kLeastCut = 4, kMostCut = 32;
@@ -111,6 +113,12 @@ __device__ inline void read_k8(const uint32_t (&at)[8], u32x4 (&x)[16]) {
           "=&v"(x[10]), "=&v"(x[11]), "=&v"(x[12]), "=&v"(x[13]), "=&v"(x[14]), "=&v"(x[15])
         : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7]), "i"(MORE)
         : "memory");
+}
+// N words (4 or 8).
+template <int N>
+__device__ inline void read_words(uint32_t at, u32x4 (&x)[2]) {
+    if constexpr (N == 4) asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0]) : "v"(at) : "memory");
+    else asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:16\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0]), "=&v"(x[1]) : "v"(at) : "memory");
 }
 // Transposing reads of bf16 rows: lane n of 16 gets four rows of channel n, at `at` and `more` behind it.
 template <int MORE>
@@ -206,14 +214,47 @@ __device__ inline u32x2 bf16x4_of(const f32x4& o, float f) {
     const bf16x2 hi = __builtin_convertvector((f32x2){o[2] * f, o[3] * f}, bf16x2);
     return (u32x2){__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
+__device__ inline bool finite(float x) { return (f32_bits(x) & 0x7F800000u) != 0x7F800000u; }
+// Whether a sum is NaN, or so large that four of them may pass fp32's range.
+template <int N>
+__device__ inline bool too_large(const f32x4 (&o)[N]) {
+    float most = 0.0f;
+    #pragma unroll
+    for (int c = 0; c < N; ++c)
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) most = __builtin_elementwise_maximum(most, __builtin_fabsf(o[c][j]));  // (NaN is more than all)
+    return !(most < 0x1p125f);
+}
+// Four means, sums o times f, to bf16 or (a part) fp32; `second`: those that were not finite.
+__device__ inline void put(__bf16* to, const f32x4& o, float f, bool second) {
+    u32x2 x = bf16x4_of(o, f);
+    if (second) {
+        const u32x2 old = *reinterpret_cast<const u32x2*>(to);
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t lost = (finite(bits_f32(old[i] << 16)) ? 0u : 0xFFFFu) | (finite(bits_f32(old[i])) ? 0u : 0xFFFF0000u);
+            x[i] = (x[i] & lost) | (old[i] & ~lost);
+        }
+    }
+    *reinterpret_cast<u32x2*>(to) = x;
+}
+__device__ inline void put(float* to, const f32x4& o, float f, bool second) {
+    f32x4 x = o * f;
+    if (second) {
+        const f32x4 old = *reinterpret_cast<const f32x4*>(to);
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = finite(old[i]) ? old[i] : x[i];
+    }
+    *reinterpret_cast<f32x4*>(to) = x;
+}
 // A barrier of the workgroup that waits for no load.
 __device__ inline void meet_waves() {
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
-// What scores are taken from, m as above (-inf: none yet; inf: NaN).
-__device__ inline float reference(float m) { return m == kNegInf ? 0.0f : m + (kAbove + (m - m)); }
+// What scores are taken from, m as above (-inf: none yet; inf: NaN), or `lift` more.
+__device__ inline float reference(float m, float lift = 0.0f) { return m == kNegInf ? 0.0f : m + (lift + (m - m)); }
 
 // Inclusive prefix sum over the lanes of a wave (as dev::wave_inclusive_sum).
 template <int CTRL, int ROW_MASK, bool BOUND_ZERO>
@@ -331,6 +372,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
     __shared__ __attribute__((aligned(1024))) char lds[8 * kSlot];
     static_assert(8 * kSlot >= 4 * 16 * kPitch * 4, "o_s");
     __shared__ float ml_s[4][16][2], all_s[16][2];
+    __shared__ __attribute__((aligned(16))) uint32_t lost_s[2][WAVES];  // (WIDE) waves with sums that are too large, of this segment and the next
     float (*o_s)[16][kPitch] = reinterpret_cast<float (*)[16][kPitch]>(lds);  // once the waves are through with K and V
 
     const KvpPages& g = p.pages;
@@ -386,8 +428,11 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
     const int rowb = g.kv_heads * D * 2;
     uint32_t at = begin;  // where in the run we are
     int chunk = 0;
+    int turn = 0;         // of lost_s
     bool again = false;   // the waves have joined their sums in LDS
+    bool second = false;  // the segment is taken again, for means that were not finite
     while (at < end) {
+        const uint32_t start = at;
         const int tid = hidden((int)threadIdx.x), lane = tid & 63, li = lane & 15, grp = lane >> 4;
         // the sequence that `at` is in (tok0 that does not ascend may make this fail: the run ends)
         while (at - before >= lane_u32(scan, 63)) {
@@ -454,7 +499,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             if (u1 <= 0 || (WIDE && u0 >= units)) continue;
         }
         if (g.pages == 0) u1 = u0;  // there is nothing to read
-        if (again) __syncthreads();  // the other waves may still read the last segment's sums, which lie where K and V come
+        if (!WIDE && again) __syncthreads();  // the other waves may still read the last segment's sums, which lie where K and V come
         again = true;
         const KvpAttendParams& args = *hidden_arguments<KvpAttendParams>();
         const KvpPages& gp = args.pages;
@@ -463,6 +508,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             h = segment - tile * gp.kv_heads;
         }
         const float scale = args.scale_log2, unseen = scale < 0.0f ? -kNegInf : kNegInf;
+        const float lift = second ? kAbove : 0.0f;
         const int seq = 64 * chunk + s;
 
         const int r0 = tile * kTile, rows = T * G - r0 < kTile ? T * G - r0 : kTile;
@@ -524,7 +570,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
         }
 
         f32x4 acc[NT][NC];  // channels 16 c + 4 grp ..
-        float m[NT], from[NT], l[NT];  // from: reference(m)
+        float m[NT], from[NT], l[NT];  // from: reference(m, lift)
         #pragma unroll
         for (int i = 0; i < NT; ++i) {
             m[i] = kNegInf;
@@ -639,9 +685,9 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
                     top[i] = top[i] > m[i] + kBehind ? top[i] : m[i];
-                    const float fade = m[i] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(from[i] - reference(top[i]));
+                    const float fade = m[i] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(from[i] - reference(top[i], lift));
                     m[i] = top[i];
-                    from[i] = reference(top[i]);
+                    from[i] = reference(top[i], lift);
                     l[i] *= fade;
                     #pragma unroll
                     for (int c = 0; c < NC; ++c) acc[i][c] *= fade;
@@ -862,22 +908,34 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             else if (late.lse) late.lse[to] = (reference(m) + __builtin_amdgcn_logf(l)) * kLn2;
             if (!late.whole && begins) late.meta[to] = (uint64_t)rr << 48 | (uint64_t)((unit1 - 1) / per - w + 1) << 24 | w;
         };
+        bool lost = false;
         if constexpr (WIDE) {  // a row's values from the lanes that have them
             #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 const int rr = w0 + 16 * i + li;
                 const float my_l = group_sum(l[i]);
                 if (rr >= rows) continue;
+                lost |= too_large(acc[i]);
                 const float inv = my_l > 0.0f || my_l != my_l ? 1.0f / my_l : 0.0f;
                 float* part = late.part_o + (part0 + rr) * D + 4 * grp;
                 __bf16* out = static_cast<__bf16*>(late.o) + out_row(rr) * D + 4 * grp;
                 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    if (one) *reinterpret_cast<u32x2*>(out + 16 * c) = bf16x4_of(acc[i][c], inv);
-                    else *reinterpret_cast<f32x4*>(part + 16 * c) = acc[i][c];
+                    if (one) put(out + 16 * c, acc[i][c], inv, second);
+                    else put(part + 16 * c, acc[i][c], inv, second);
                 }
-                if (grp == 0) row_done(rr, m[i], my_l);
+                if (grp == 0 && !second) row_done(rr, m[i], my_l);
             }
+            const bool any = __any(lost);
+            if (lane == 0) lost_s[turn][wave] = any;
+            wait_lds();
+            meet_waves();
+            u32x4 x[2] = {};
+            read_words<WAVES>((uint32_t)(uintptr_t)(lds_bytes)&lost_s[turn][0], x);
+            const uint32_t all = x[0][0] | x[0][1] | x[0][2] | x[0][3] | x[1][0] | x[1][1] | x[1][2] | x[1][3];
+            turn ^= 1;
+            second = !second && __builtin_amdgcn_readfirstlane((int)all);
+            if (second) at = start;
             continue;
         }
         #pragma unroll
@@ -885,9 +943,10 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             if (16 * i >= rows) break;
             const float my_l = group_sum(l[i]);
             __syncthreads();  // K and V, and the values before these, are done with
+            const uint32_t sign = __any(too_large(acc[i])) ? 0x80000000u : 0u;  // goes with the sums of weights, which have none
             if (grp == 0) {
                 ml_s[wave][li][0] = m[i];
-                ml_s[wave][li][1] = my_l;
+                ml_s[wave][li][1] = bits_f32(f32_bits(my_l) | sign);
             }
             __syncthreads();
             float top = kNegInf, sum = 0.0f;
@@ -895,8 +954,11 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             for (int k = 0; k < 4; ++k) top = __builtin_fmaxf(top, ml_s[k][li][0]);
             const float from = reference(top);
             #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                sum += ml_s[k][li][0] == kNegInf ? ml_s[k][li][1] : ml_s[k][li][1] * __builtin_amdgcn_exp2f(reference(ml_s[k][li][0]) - from);
+            for (int k = 0; k < 4; ++k) {
+                const float weights = __builtin_fabsf(ml_s[k][li][1]);
+                lost |= (int)f32_bits(ml_s[k][li][1]) < 0;
+                sum += ml_s[k][li][0] == kNegInf ? weights : weights * __builtin_amdgcn_exp2f(reference(ml_s[k][li][0]) - from);
+            }
             const float fade = m[i] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m[i]) - from);
             // (m is -inf where the wave saw nothing: zeros; or only NaN, which stays)
             #pragma unroll
@@ -914,28 +976,37 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                 f32x4 o = *reinterpret_cast<const f32x4*>(&o_s[0][r16][c]);
                 #pragma unroll
                 for (int j = 1; j < 4; ++j) o += *reinterpret_cast<const f32x4*>(&o_s[j][r16][c]);
-                if (!one) {
-                    *reinterpret_cast<f32x4*>(late.part_o + (part0 + rr) * D + c) = o;
-                    continue;
-                }
                 const float z = all_s[r16][1], inv = z > 0.0f || z != z ? 1.0f / z : 0.0f;
-                *reinterpret_cast<u32x2*>(static_cast<__bf16*>(late.o) + out_row(rr) * D + c) = bf16x4_of(o, inv);
+                if (one) put(static_cast<__bf16*>(late.o) + out_row(rr) * D + c, o, inv, second);
+                else put(late.part_o + (part0 + rr) * D + c, o, inv, second);
             }
-            if (tid < 16 && 16 * i + tid < rows) row_done(16 * i + tid, all_s[tid][0], all_s[tid][1]);
+            if (!second && tid < 16 && 16 * i + tid < rows) row_done(16 * i + tid, all_s[tid][0], all_s[tid][1]);
         }
+        second = !second && __any(lost);  // (the same in every wave)
+        if (second) at = start;
     }
 }
 
-// A running sum of parts: m as above, l the sum of weights, o that of weighted values.
+// Parts put together: m as above, l the sum of weights, o the mean of the values, which stays in the range of the parts' means.
 struct Joined {
     float m = kNegInf, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    __device__ inline void add(float m1, float l1, const f32x4& o1) {
-        const float top = __builtin_fmaxf(m, m1), from = reference(top);
-        const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m) - from);
-        const float e = m1 == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m1) - from);
-        l = l * f + l1 * e;
-        o = o * f + o1 * e;
+    template <int N>
+    __device__ inline void add(const f32x2 (&ml)[N], const f32x4 (&mean)[N]) {
+        float top = m, e[N];
+        #pragma unroll
+        for (int k = 0; k < N; ++k) top = __builtin_fmaxf(top, ml[k][0]);
+        const float from = reference(top), f = l * (m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(m) - from));
+        l = f;
+        #pragma unroll
+        for (int k = 0; k < N; ++k) {
+            e[k] = ml[k][1] * (ml[k][0] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(ml[k][0]) - from));
+            l += e[k];
+        }
+        const float by = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
+        o *= f * by;
+        #pragma unroll
+        for (int k = 0; k < N; ++k) o += mean[k] * (e[k] * by);
         m = top;
     }
 };
@@ -957,8 +1028,12 @@ __device__ inline Joined join_parts(const KvpAttendParams& p, uint32_t w, uint32
             x[k] = *(const f32x4 __attribute__((address_space(1)))*)(p.part_o + (slot * p.tile + row) * D + c);
         }
         #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (i0 + k * step < parts) sum.add(a[k][0], a[k][1], x[k]);
+        for (int k = 1; k < kAhead; ++k)
+            if (i0 + k * step >= parts) {  // there is none
+                a[k] = (f32x2){kNegInf, 0.0f};
+                x[k] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+            }
+        sum.add(a, x);
     }
     return sum;
 }
@@ -988,8 +1063,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
         return first + i >= low && first + i < high && first + i < all && w < p.wgs && parts <= p.wgs - w && parts >= 2 ? parts : 0;
     };
     auto write = [&](int64_t row, const Joined& x, int c) {
-        const float inv = x.l > 0.0f || x.l != x.l ? 1.0f / x.l : 0.0f;
-        *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + row * D + c) = bf16x4_of(x.o, inv);
+        *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.o) + row * D + c) = bf16x4_of(x.o, 1.0f);
         if (c == 0 && p.lse) p.lse[row] = (reference(x.m) + __builtin_amdgcn_logf(x.l)) * kLn2;
     };
     if constexpr (!FEW) {
@@ -1007,12 +1081,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
             Joined x = join_parts<D>(p, (uint32_t)mine & 0xFFFFFFu, parts, (int)(mine >> 48) & (p.tile - 1), (uint32_t)(lane / (D / 4)), kWave, c);
             #pragma unroll
             for (int step = D / 4; step < 64; step *= 2) {
-                Joined y;
-                y.m = __shfl_xor(x.m, step);
-                y.l = __shfl_xor(x.l, step);
+                const f32x2 ml[1] = {(f32x2){__shfl_xor(x.m, step), __shfl_xor(x.l, step)}};
+                f32x4 mean[1];
                 #pragma unroll
-                for (int j = 0; j < 4; ++j) y.o[j] = __shfl_xor(x.o[j], step);
-                x.add(y.m, y.l, y.o);
+                for (int j = 0; j < 4; ++j) mean[0][j] = __shfl_xor(x.o[j], step);
+                x.add(ml, mean);
             }
             if (lane < D / 4) write(first + wave, x, c);
         }
@@ -1029,18 +1102,18 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
         float top = kNegInf;
         #pragma unroll
         for (int j = 0; j < kWays; ++j) top = __builtin_fmaxf(top, m_s[j]);
-        const float e = x.m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(x.m) - reference(top));
-        *reinterpret_cast<f32x4*>(&o_s[way][c]) = x.o * e;
-        if (c == 0) l_s[way] = x.l * e;
+        const float weight = x.l * (x.m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(reference(x.m) - reference(top)));
+        *reinterpret_cast<f32x4*>(&o_s[way][c]) = x.o;
+        if (c == 0) l_s[way] = weight;
         __syncthreads();
         if (way) continue;
         Joined y;
         y.m = top;
         #pragma unroll
-        for (int j = 0; j < kWays; ++j) {
-            y.l += l_s[j];
-            y.o += *reinterpret_cast<const f32x4*>(&o_s[j][c]);
-        }
+        for (int j = 0; j < kWays; ++j) y.l += l_s[j];
+        const float by = y.l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(y.l);
+        #pragma unroll
+        for (int j = 0; j < kWays; ++j) y.o += *reinterpret_cast<const f32x4*>(&o_s[j][c]) * (l_s[j] * by);
         write(first + i, y, channel0 + c);
     }
 }

@@ -1,0 +1,98 @@
+"""Attention over pages at the ends of the numbers' range, in tiles of each size, in one launch and in two."""
+import numpy as np
+import pytest
+import torch
+
+import kvp_plain as plain
+import paper_2606_20537_amd as cap
+from kvp_plan import plan_of
+from test_gpu_kvp import Step, host
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+
+# sequences' rows, tokens, query heads of a KV head and columns of 16 rows for tiles of 16, 32 and 128 rows, dealt out in parts, and whole ones
+CALLS = {"16": ([3000, 1, 40], [1, 1, 1], 2, 260), "32": ([3000, 40], [5, 5], 4, 4096), "128": ([900, 90], [150, 60], 2, 6000),
+         "whole": ([250, 1, 40], [1, 1, 2], 2, 16), "whole 128": ([128, 60], [100, 40], 4, 8)}
+
+
+def step(call, d, seed):
+    n, T, G, columns = CALLS[call]
+    many = call == "whole 128"  # enough segments for every workgroup
+    s = Step(n * (32 if many else 1), T * (32 if many else 1), 16 if many else 2, d, 16, seed=seed, columns=columns)
+    tile, mode = plan_of(s, G)[:2]
+    assert (mode == "whole") == call.startswith("whole") and (call == "whole" or tile == int(call.split()[-1]))
+    if many:
+        s.n, s.T = s.n[:2], s.T[:2]  # (those that are checked)
+    return s, G
+
+
+def near(o, want, mass, size, lse, n):
+    """As attend_near of the plain form, but small values have only what fp32's smallest step costs: each of the n products
+    with hi and lo, the n / 32 + 96 sums and the quotient is off by 2^-150 at most besides, and the sum of the weights is 1 at least; the output is off
+    by half a step of bf16, 2^-134 at least.  Scores are taken from a reference that is 8 below their maximum at most."""
+    dx = 2.0 ** -16 * size + 2.0 ** -22 * (abs(lse) + size + 8)
+    steps = (n / 32 + 96) * 2.0 ** -24
+    far = mass * (2.0 ** -16 + 2 * dx + 2 * steps) + (3 * n + 97) * 2.0 ** -150
+    far = far + np.maximum(2.0 ** -8 * (np.abs(want) + far), 2.0 ** -134)
+    return (np.abs(o - want) <= far).all()
+
+
+def check(s, q, o, G, scale, channels=slice(None)):
+    qh, oh = host(q), host(o)
+    for i, (n, T) in enumerate(zip(s.n, s.T)):
+        t0, k, v = sum(s.T[:i]), s.rows(i, s.k), s.rows(i, s.v)
+        for t in sorted({0, T // 2, T - 1}):
+            for h in range(0, q.shape[1], 3):
+                rows = np.arange(n - T + t + 1)
+                want, lse, mass, size = plain.attend(qh[t0 + t, h], k[:, h // G], v[:, h // G], scale, rows)
+                assert near(oh[t0 + t, h][channels], want[channels], mass[channels], size, lse, len(rows)), (i, t, h)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("size", [2.0 ** -96, 2.0 ** -112, 1e-36, 2.0 ** -126])
+def test_small_values(call, d, size):
+    s, G = step(call, d, 4)
+    s.v.copy_((s.v.float().clamp(-2, 2) * size).bfloat16())
+    q, o, _ = s.attend(G, scale=0.02)
+    check(s, q, o, G, 0.02)
+
+
+def test_one_row_is_its_value():
+    # the mean of one row is that row, of whatever size
+    s = Step([1] * 40, [1] * 40, 1, 64, 16, seed=1, columns=260)
+    size = 2.0 ** torch.arange(-125, 123, 6.35, device="cuda")[:40]
+    for i in range(40):
+        s.v[int(s.table[i, 0]), 0] = (s.v[int(s.table[i, 0]), 0].float().clamp(-1.9, 1.9) * size[i]).bfloat16()
+    q, o, _ = s.attend(2)
+    want = torch.stack([s.v[int(s.table[i, 0]), 0].expand(2, 64) for i in range(40)])
+    assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_small_values_beside_large_ones(call, d):
+    # sums of every other channel pass fp32's range, their means do not
+    s, G = step(call, d, 5)
+    size = torch.tensor([3e38, 1e-36], device="cuda").repeat(d // 2)
+    s.v.copy_(((1 - 0.3 * s.v.float().clamp(-1, 1).abs()) * size).bfloat16())
+    q, o, lse = s.attend(G, scale=0.02)
+    assert o[:sum(s.T)].isfinite().all() and lse[:sum(s.T)].isfinite().all()
+    check(s, q, o, G, 0.02)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_infinities_beside_small_values(call, d):
+    s, G = step(call, d, 6)
+    s.v.copy_((s.v.float().clamp(-2, 2) * 1e-36).bfloat16())
+    page = int(s.table[0, 0])
+    s.v[page, 0, 0, 5], s.v[page, 0, 0, 17], s.v[page, 0, 0, 40] = INF, -INF, NAN
+    q, o, lse = s.attend(G, scale=0.02)
+    mine = o[:s.T[0], :G]
+    assert (mine[..., 5] == INF).all() and (mine[..., 17] == -INF).all() and mine[..., 40].isnan().all()
+    assert mine.isfinite().sum() == mine.numel() - 3 * s.T[0] * G and o[:s.T[0], G:].isfinite().all() and o[s.T[0]:sum(s.T)].isfinite().all()
+    assert lse[:sum(s.T)].isfinite().all()
+    s.v[page, 0, 0, [5, 17, 40]] = 0
+    check(s, q, o, G, 0.02, [c for c in range(d) if c not in (5, 17, 40)])
