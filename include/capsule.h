@@ -802,8 +802,8 @@ CAP_API int kvp_append(const kvp_append_args* args, void* stream);
  * A token that sees nothing has o = 0 and lse = -inf.  Rows that a token does not see have no part in
  * its result, infinities and NaN included; a row with such values that it sees makes those channels
  * infinite or NaN.
- * Precision: products and sums are fp32, weights enter the second product with 16 bits (two bf16),
- * o is rounded once.  Weights below 2^-90 of the largest may count as none.  Means of finite
+ * Precision: products and sums are fp32, weights enter the second product with 24 bits (three bf16), or in
+ * tiles of 128 rows (below) with 16, o is rounded once.  Weights below 2^-90 of the largest may count as none.  Means of finite
  * values are finite, and small values keep their bits beside large ones (where sums pass fp32's range, or
  * V has infinities or NaN, that part of the call is computed twice).  A score above fp32's range gives NaN, one below it counts as none.
  * Made for one token or a few drafts of each sequence, in tiles of 16 or 32 query rows (tokens x

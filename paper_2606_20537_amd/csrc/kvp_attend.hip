@@ -8,9 +8,10 @@
 // (tokens x query heads of the group) share its K and V: 16 of them, twice 16 or eight times, are the
 // columns of the matrix instructions, keys and channels the rows.
 //  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 tiles, sums in fp32.
-//  * P goes in as two bf16 values, hi + lo, so that the weights keep 2^-16 and the
-//    output's own rounding is the only one to 8 bits: the matrix pipes, 6 % busy, have
-//    the time, as memory bounds the call.
+//  * P goes in as three bf16 values, in which the weights keep fp32's 24 bits: memory
+//    bounds the call, and the matrix pipes are 6 % busy with two.  In tiles of 128 rows, which arithmetic
+//    bounds, they are two, and the weights keep 2^-16, so that the output's own rounding stays the largest: 16384 tokens, 32 heads on 4
+//    of 64, 128 and 256 channels 2.43, 3.62 and 7.93 ms, with three 3.05, 4.46 and 9.30.
 // Both products leave a lane with one query row (lane % 16), so maximum, sum and
 // correction need no value of another row, and S^T's accumulators are P^T's
 // operand: lane group g holds keys 4g..4g+3 and 16+4g..16+4g+3 of 32, in which order the
@@ -247,6 +248,10 @@ __device__ inline void put(float* to, const f32x4& o, float f, bool second) {
     }
     *reinterpret_cast<f32x4*>(to) = x;
 }
+// The upper halves of two values, their bf16 cut off; and those two as fp32.
+__device__ inline uint32_t upper(float a, float b) { return __builtin_amdgcn_perm(f32_bits(b), f32_bits(a), 0x07060302u); }
+__device__ inline float first_of(uint32_t two) { return bits_f32(two << 16); }
+__device__ inline float second_of(uint32_t two) { return bits_f32(two & 0xFFFF0000u); }
 // A barrier of the workgroup that waits for no load.
 __device__ inline void meet_waves() {
     __builtin_amdgcn_sched_barrier(0);
@@ -367,6 +372,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
     constexpr int WAVES = waves_of(NT, WIDE), kTile = WIDE ? 16 * NT * WAVES : 16 * NT;
     constexpr int NJ = D / 32;                        // K: fragments of 32 channels
     constexpr int NC = D / 16;                        // V: blocks of 16 channels
+    constexpr int kParts = WIDE ? 2 : 3;              // bf16 parts of a weight
     constexpr int kPitch = D + 4;
     constexpr int kSlot = kKvpUnit * D * 2;           // a unit of K, or of V
     __shared__ __attribute__((aligned(1024))) char lds[8 * kSlot];
@@ -655,9 +661,9 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[i][e] = sums[i][e / 4][e % 4];
         };
-        // x, products not yet scaled, becomes the weights.  hi is cut off, not rounded, and lo (2^-16 of the weight) has 2^-20 of hi added,
-        // so that it is above zero, and an infinity in V, times both, is one.
-        auto weigh = [&](bf16x8 (&hi)[NT], bf16x8 (&lo)[NT]) {
+        // x, products not yet scaled, becomes the weights.  Their parts are cut off, not rounded, and what is left has 2^-24 of the first (2^-16 of the
+        // second, 2^-20 where there are two) added, so that it is above zero, and an infinity in V, times all parts, is one.
+        auto weigh = [&](bf16x8 (&w)[kParts][NT]) {
             float top[NT];
             bool above = false;
             if (scale < 0.0f) {
@@ -702,16 +708,22 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                     sum += x[i][e];
                 }
                 l[i] += sum;
-                u32x4 h, low_part;
+                u32x4 part[kParts];
                 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    h[e / 2] = __builtin_amdgcn_perm(f32_bits(x[i][e + 1]), f32_bits(x[i][e]), 0x07060302u);
-                    const float h0 = bits_f32(h[e / 2] << 16), h1 = bits_f32(h[e / 2] & 0xFFFF0000u);
-                    low_part[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
-                        (f32x2){__builtin_fmaf(h0, 0x1p-20f - 1.0f, x[i][e]), __builtin_fmaf(h1, 0x1p-20f - 1.0f, x[i][e + 1])}, bf16x2));
+                    // (what is left of the two values)
+                    float r0 = x[i][e], r1 = x[i][e + 1];
+                    #pragma unroll
+                    for (int k = 0; k + 1 < kParts; ++k) {
+                        const float less = (kParts == 2 ? 0x1p-20f : k == 0 ? 0x1p-24f : 0x1p-16f) - 1.0f;
+                        part[k][e / 2] = upper(r0, r1);
+                        r0 = __builtin_fmaf(first_of(part[k][e / 2]), less, r0);
+                        r1 = __builtin_fmaf(second_of(part[k][e / 2]), less, r1);
+                    }
+                    part[kParts - 1][e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){r0, r1}, bf16x2));
                 }
-                hi[i] = __builtin_bit_cast(bf16x8, h);
-                lo[i] = __builtin_bit_cast(bf16x8, low_part);
+                #pragma unroll
+                for (int k = 0; k < kParts; ++k) w[k][i] = __builtin_bit_cast(bf16x8, part[k]);
             }
         };
         // In a unit that some row does not see in full, or that lies on no page in part (there: the halves that are on
@@ -724,7 +736,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
         };
         // (all: every row sees all of the unit.  Products of their own for it had the compiler keep the sums in two places: 32 to 45
         // registers more, and 16384 tokens of 128 and 256 channels 3.89 and 8.33 ms, now 3.72 and 8.01.)
-        auto add_values = [&](bool all, int r, int there, const int64_t (&at)[2], const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT]) {
+        auto add_values = [&](bool all, int r, int there, const int64_t (&at)[2], const bf16x8 (&w)[kParts][NT]) {
             uint32_t keep[4] = {};  // bits of keys 2i and 2i + 1
             if (!all) {
                 #pragma unroll
@@ -765,10 +777,9 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                 #pragma unroll
                 for (int c = 0; c < kAtOnce; ++c)
                     #pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                        acc[i][c0 + c] = dev::mma(__builtin_bit_cast(bf16x8, v[c]), hi[i], acc[i][c0 + c]);
-                        acc[i][c0 + c] = dev::mma(__builtin_bit_cast(bf16x8, v[c]), lo[i], acc[i][c0 + c]);
-                    }
+                    for (int i = 0; i < NT; ++i)
+                        #pragma unroll
+                        for (int k = 0; k < kParts; ++k) acc[i][c0 + c] = dev::mma(__builtin_bit_cast(bf16x8, v[c]), w[k][i], acc[i][c0 + c]);
             }
             if (!__any(found)) return;
             #pragma unroll 1
@@ -853,9 +864,9 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                         where(j);
                         scores();
                         if (!all) hide_unseen(r, there);
-                        bf16x8 hi[NT], lo[NT];
-                        weigh(hi, lo);
-                        add_values(all, r, there, a, hi, lo);
+                        bf16x8 w[kParts][NT];
+                        weigh(w);
+                        add_values(all, r, there, a, w);
                     }
                     place = (place + 1) & 3;
                 }
@@ -883,11 +894,11 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
                     load_k(a);
                 }
                 if (!all) hide_unseen(r, there_now);
-                bf16x8 hi[NT], lo[NT];
-                weigh(hi, lo);
+                bf16x8 w[kParts][NT];
+                weigh(w);
                 if (more) wait_loads<kLoads>();  // V: the next K's are behind it
                 else wait_loads<0>();
-                add_values(all, r, there_now, now, hi, lo);
+                add_values(all, r, there_now, now, w);
                 if (!more) break;
                 wait_lds();
                 load_v(a);

@@ -96,3 +96,22 @@ def test_infinities_beside_small_values(call, d):
     assert lse[:sum(s.T)].isfinite().all()
     s.v[page, 0, 0, [5, 17, 40]] = 0
     check(s, q, o, G, 0.02, [c for c in range(d) if c not in (5, 17, 40)])
+
+
+@pytest.mark.parametrize("G, columns, tile", [(2, 4, 16), (2, 300, 16), (20, 4096, 32)])
+def test_weights_keep_24_bits(G, columns, tile):
+    # Two rows with scores 0 and -s, s of 8 bits, and values 1 and -1: o = tanh(s / 2), small beside the sum of weights.  Two's
+    # weight w is off by an exponential (2^-23) and its parts (2^-23), half of which reach o; six products' sums of 1 at most
+    # by 2^-23 each, halved by the quotient, and the sum of weights by 2^-24: below 12 * 2^-24.  Then the output's rounding.
+    n_seq = 128
+    s = Step([2] * n_seq, [1] * n_seq, 1, 64, 16, columns=columns)
+    assert plan_of(s, G)[0] == tile
+    at = s.table[:, 0].long().cuda()
+    s.k[at, :2], s.v[at, :2] = 0, 0
+    s.k[at, 1, 0, 0], s.v[at, 0, 0, :], s.v[at, 1, 0, :] = -1, 1, -1
+    x = (1 + torch.arange(n_seq, device="cuda") / 128) * 2.0 ** -13
+    q = torch.zeros((n_seq, G, 64), device="cuda")
+    q[:, :, 0] = x[:, None] * 2.0 ** torch.arange(-1, 1, device="cuda").repeat(G // 2)
+    q, o, _ = s.attend(G, scale=1.0, q=q.bfloat16())
+    want = np.tanh(host(q)[..., :1] / 2)
+    assert (np.abs(host(o) - want) <= 12 * 2.0 ** -24 + 2.0 ** -8 * want).all()
