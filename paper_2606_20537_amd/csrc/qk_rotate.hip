@@ -10,8 +10,8 @@
 // values that cross lanes are the sums of squares.  Sines and cosines are those
 // of the token: a workgroup takes all heads of its tokens, computes each once and
 // hands it round in LDS.  Everything between load and store is fp32, rounded once.
-// The angle is taken in 64 bits and in turns, of which the whole ones go before it is
-// rounded: at position 2^20 the products alone would be off by 2^-4 in 32 bits.
+// The angle is taken in 64 bits and in turns, of which the whole ones go before it becomes
+// two fp32 values: at position 2^20 the products alone would be off by 2^-4 in 32 bits.
 //
 // An append has the rows of v besides (copied), and k and v go to the row of the page
 // that the table names; sequence, length and page of a token are found while its first rows are on their way.
@@ -209,9 +209,11 @@ __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void rotate_kernel(const QkP
         }
         turns *= 0.15915494309189533577;  // 1 / (2 pi)
         turns -= __builtin_rint(turns);
+        // what fp32 leaves of the angle turns the pair once more
+        const float near = (float)turns, rest = 6.2831853f * (float)(turns - (double)near);
         float sine, cosine;
-        sincospif(2.0f * (float)turns, &sine, &cosine);
-        *reinterpret_cast<f32x2*>(&cs_s[2 * i]) = (f32x2){cosine, sine};
+        sincospif(2.0f * near, &sine, &cosine);
+        *reinterpret_cast<f32x2*>(&cs_s[2 * i]) = (f32x2){__builtin_fmaf(-rest, sine, cosine), __builtin_fmaf(rest, cosine, sine)};
     }
     __syncthreads();
 
