@@ -674,7 +674,7 @@ CAP_API int kvb_select(const kvb_select_args* args, void* stream);
  *   rotation pair i < rot / 2 turns by a_i = sum over axes of pos_axis freqs[axis][i]:
  *            (y_a, y_b) -> (y_a cos a_i - y_b sin a_i, y_b cos a_i + y_a sin a_i),
  *            (a, b) = (i, i + rot / 2), or (2 i, 2 i + 1) with QK_PAIRS;
- *            channels from rot on stay
+ *            channels from rot on stay, without a norm bit for bit
  * Angles are taken in 64 bits (within 2^-20 at any position), the rest in fp32, and
  * the result is rounded once.  Text has one axis; images and video give a patch a time, a
  * height and a width, each with a row of freqs that is zero for the pairs it does not turn. */
@@ -773,7 +773,7 @@ typedef struct kvp_cache {
     int32_t        reserved;      /* 0 */
 } kvp_cache;
 
-/* Append: the tokens' rows of k and v [tokens, kv_heads, d] to their pages, one launch.  With a
+/* Append: the tokens' rows of k and v [tokens, kv_heads, d] to their pages, bit for bit, one launch.  With a
  * rule, k is normed and rotated on the way, and so is q to q_out (both p NULL: there is no q);
  * positions are pos, or where that is NULL the row's own number on every axis.
  * No row of a page may be given to two tokens. */

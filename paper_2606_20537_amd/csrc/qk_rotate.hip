@@ -64,8 +64,9 @@ __device__ inline void widen(const Vec<F32>& x, float* f) {
         if constexpr (F32) f[e] = bits_f32(x.w[e / 4][e % 4]);
         else f[e] = bits_f32(e & 1 ? x.w[0][e / 2] & 0xFFFF0000u : x.w[0][e / 2] << 16);
 }
+// Rounded where values have changed (~0); else the bits that they came with, those of a NaN too.
 template <bool F32>
-__device__ inline Vec<F32> narrow(const float* f) {
+__device__ inline Vec<F32> narrow(const float* f, uint32_t changed) {
     Vec<F32> x;
     #pragma unroll
     for (int e = 0; e < 8; e += 2) {
@@ -73,7 +74,9 @@ __device__ inline Vec<F32> narrow(const float* f) {
             x.w[e / 4][e % 4] = __builtin_bit_cast(uint32_t, f[e]);
             x.w[e / 4][e % 4 + 1] = __builtin_bit_cast(uint32_t, f[e + 1]);
         } else {
-            x.w[0][e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){f[e], f[e + 1]}, bf16x2));
+            const uint32_t rounded = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){f[e], f[e + 1]}, bf16x2));
+            const uint32_t same = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, f[e + 1]), __builtin_bit_cast(uint32_t, f[e]), 0x07060302u);
+            x.w[0][e / 2] = (rounded & changed) | (same & ~changed);
         }
     }
     return x;
@@ -293,8 +296,8 @@ __global__ __launch_bounds__(kThreads, F32 ? 5 : 6) void rotate_kernel(const QkP
                     }
                 }
             }
-            oa = narrow<F32>(x);
-            ob = narrow<F32>(x + 8);
+            oa = narrow<F32>(x, p.norm || (p.pairs ? a < p.rot : first >= 0) ? ~0u : 0u);
+            ob = narrow<F32>(x + 8, p.norm || (p.pairs ? b < p.rot : first >= 0) ? ~0u : 0u);
         }
         if (write) {
             store8<F32>(to + a * kSize, oa);

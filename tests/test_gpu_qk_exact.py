@@ -31,3 +31,40 @@ def test_small_sines_and_cosines(quarter, pairs):
         for got, exact in ((c, np.cos(angle)), (s, np.sin(angle))):
             exact = exact.astype(np.float64)
             assert (np.abs(got - exact) <= 6 * 2.0 ** -24 * np.abs(exact) + 4 * 8 * 2.0 ** -53).all()
+
+
+def patterns(dtype, shape):
+    """Every bf16 pattern in turn, and fp32 ones whose upper halves are those."""
+    n = int(np.prod(shape))
+    i = torch.arange(n, dtype=torch.int64, device="cuda") % 65536
+    if dtype == torch.bfloat16:
+        return i.to(torch.int16).view(torch.bfloat16).view(shape)
+    return ((i << 16) + (i * 40503) % 65536).to(torch.int32).view(torch.float32).view(shape)
+
+
+def bits(x):
+    return x.contiguous().view(torch.int16)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 80, 256])
+@pytest.mark.parametrize("rot, pairs", [(0, False), (0, True), (32, False), (32, True), (48, True)])
+def test_channels_that_stay_keep_their_bits(dtype, d, rot, pairs):
+    # signalling NaN, infinities and denormals too; a call without norm and rotation is a copy
+    x = patterns(dtype, (65536 // 64, 3, d))
+    pos = torch.ones(len(x), dtype=torch.int32, device="cuda") if rot else None
+    out = torch.empty_like(x)
+    cap.qk_norm_rope(cap.qk_rule(cap.qk_freqs(1e4, rot).cuda() if rot else None, pairs=pairs), x, None, out, pos=pos)
+    assert torch.equal(bits(out[..., rot:]), bits(x[..., rot:]))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_rows_appended_without_a_rule_keep_their_bits(d):
+    tokens, page = 65536 * 2 // (2 * d), 16
+    k = patterns(torch.bfloat16, (tokens, 2, d))
+    v = k.flip(0)
+    pools = torch.zeros((2, tokens // page, page, 2, d), dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(tokens // page, dtype=torch.int32, device="cuda")[None]
+    cap.kvp_append(cap.kvp_cache(pools[0], pools[1], table), torch.tensor([tokens], dtype=torch.int32, device="cuda"), k, v,
+                   tok0=torch.tensor([0, tokens], dtype=torch.int32, device="cuda"))
+    assert torch.equal(bits(pools[0].flatten(0, 1)), bits(k)) and torch.equal(bits(pools[1].flatten(0, 1)), bits(v))
