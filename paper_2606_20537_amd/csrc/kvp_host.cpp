@@ -13,18 +13,23 @@ constexpr int64_t kMostStride = (int64_t)1 << 30;
 uint64_t addr(const void* p) { return (uint64_t)(uintptr_t)p; }
 
 // `count` pieces of `width` bytes, `step` bytes apart, from `a` on: the tokens of a packed tensor, the pages of a
-// pool, or (count 1) a plain array.
+// pool, or (count 1) a plain array.  A token's pieces are its heads, of `head` bytes, `head_step` apart.
 struct Span {
-    uint64_t a = 0, width = 0, step = 0, count = 0;
+    uint64_t a = 0, width = 0, step = 0, count = 0, head = 0, head_step = 0;
     bool empty() const { return a == 0 || width == 0 || count == 0; }
     uint64_t bytes() const { return empty() ? 0 : (count - 1) * step + width; }
     bool wraps() const { return a + bytes() < a; }
     bool same(const Span& x) const { return a == x.a && width == x.width && (step == x.step || count == 1) && count == x.count; }
 };
-Span plain(const void* p, uint64_t bytes) { return {addr(p), bytes, 0, 1}; }
+Span plain(const void* p, uint64_t bytes) { return {addr(p), bytes, 0, 1, 0, 0}; }
 
 bool meet(const Span& x, const Span& y) {
     if (x.empty() || y.empty() || x.a >= y.a + y.bytes() || y.a >= x.a + x.bytes()) return false;
+    // heads of one step, of which tokens are whole ones apart: heads of several tensors in turn
+    if (x.head && x.head_step == y.head_step && (x.count == 1 || x.step % x.head_step == 0) && (y.count == 1 || y.step % x.head_step == 0)) {
+        const uint64_t s = x.head_step, d = y.a >= x.a ? (y.a - x.a) % s : (s - (x.a - y.a) % s) % s;
+        if (d >= x.head && d + y.head <= s) return false;
+    }
     if (x.count == 1 || y.count == 1 || x.step != y.step) return true;
     // pieces of one step: slices of one larger tensor, beside each other in each of its tokens
     const uint64_t d = y.a >= x.a ? (y.a - x.a) % x.step : (x.step - (x.a - y.a) % x.step) % x.step;
@@ -43,7 +48,7 @@ int check_rows(const qk_rows& r, int64_t tokens, int32_t heads, int32_t d, int s
     if (token > kMostStride) return CAP_E_UNSUPPORTED;
     if ((head | token) % 8 != 0) return CAP_E_ALIGN;
     *out = {addr(r.p), token * size, head * size};
-    *span = {addr(r.p), (uint64_t)width * size, (uint64_t)token * size, (uint64_t)tokens};
+    *span = {addr(r.p), (uint64_t)width * size, (uint64_t)token * size, (uint64_t)tokens, (uint64_t)d * size, (uint64_t)head * size};
     return CAP_OK;
 }
 
@@ -119,9 +124,9 @@ int check_cache(const kvp_cache* c, cap::KvpPages* g, Span (&span)[3]) {
     if (c->pages > 0 && (uint64_t)stride * 2 > UINT64_MAX / (uint64_t)c->pages) return CAP_E_SIZE;
     *g = {addr(c->k), addr(c->v), c->table, nullptr, nullptr, columns, stride * 2, (int32_t)c->pages, c->page, c->columns, c->n_seq,
           c->kv_heads, (int32_t)capacity, cap::divisor((uint32_t)c->page)};
-    span[0] = {addr(c->k), (uint64_t)width * 2, (uint64_t)stride * 2, (uint64_t)c->pages};
-    span[1] = {addr(c->v), (uint64_t)width * 2, (uint64_t)stride * 2, (uint64_t)c->pages};
-    span[2] = {addr(c->table), (uint64_t)c->columns * 4, (uint64_t)columns * 4, (uint64_t)c->n_seq};
+    span[0] = {addr(c->k), (uint64_t)width * 2, (uint64_t)stride * 2, (uint64_t)c->pages, 0, 0};
+    span[1] = {addr(c->v), (uint64_t)width * 2, (uint64_t)stride * 2, (uint64_t)c->pages, 0, 0};
+    span[2] = {addr(c->table), (uint64_t)c->columns * 4, (uint64_t)columns * 4, (uint64_t)c->n_seq, 0, 0};
     for (const Span& x : span)
         if (x.wraps()) return CAP_E_SIZE;
     return CAP_OK;

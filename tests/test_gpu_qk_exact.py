@@ -68,3 +68,26 @@ def test_rows_appended_without_a_rule_keep_their_bits(d):
     cap.kvp_append(cap.kvp_cache(pools[0], pools[1], table), torch.tensor([tokens], dtype=torch.int32, device="cuda"), k, v,
                    tok0=torch.tensor([0, tokens], dtype=torch.int32, device="cuda"))
     assert torch.equal(bits(pools[0].flatten(0, 1)), bits(k)) and torch.equal(bits(pools[1].flatten(0, 1)), bits(v))
+
+
+@pytest.mark.parametrize("tokens", [1, 37])
+def test_heads_of_q_k_and_v_in_turn(tokens):
+    # a projection [tokens, heads, (q, k, v), d] in place
+    heads, d = 4, 64
+    x = torch.randn((tokens, heads, 3, d), generator=torch.Generator("cuda").manual_seed(1), device="cuda").bfloat16()
+    before = x.clone()
+    q, k, v = (x[:, :, i] for i in range(3))
+    pos = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    rule = cap.qk_rule(cap.qk_freqs(1e4, d).cuda(), eps=1e-6)
+    qo, ko = torch.empty((2, tokens, heads, d), dtype=torch.bfloat16, device="cuda")
+    cap.qk_norm_rope(rule, q, k, qo, ko, pos=pos)
+    assert torch.equal(x, before)
+    cap.qk_norm_rope(rule, q, k, pos=pos)
+    assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(v, before[:, :, 2])
+    x.copy_(before)
+    pools = torch.zeros((2, 3, 16, heads, d), dtype=torch.bfloat16, device="cuda")
+    cache = cap.kvp_cache(pools[0], pools[1], torch.arange(3, dtype=torch.int32, device="cuda")[None])
+    lens, tok0 = (torch.tensor(i, dtype=torch.int32, device="cuda") for i in ([tokens], [0, tokens]))
+    cap.kvp_append(cache, lens, k, v, tok0=tok0, rule=rule, q=q, pos=pos)
+    assert torch.equal(q, qo) and torch.equal(x[:, :, 1:], before[:, :, 1:])
+    assert torch.equal(pools[0].flatten(0, 1)[:tokens], ko) and torch.equal(pools[1].flatten(0, 1)[:tokens], v)
