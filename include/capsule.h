@@ -754,8 +754,13 @@ CAP_API int qk_norm_rope(const qk_norm_rope_args* args, void* stream);
  * address: a table or lengths that break these rules give wrong results, not accesses out of bounds.
  *
  * Supported: d in {64, 128, 256}, heads a multiple of kv_heads, bf16, page a multiple
- * of 16, n_seq <= KVP_MAX_SEQ, columns * page <= 2^24, 16 * kv_heads * d * 2 < 2^31.
- * Errors: as for qk_norm_rope. */
+ * of 16, n_seq <= KVP_MAX_SEQ, columns * page <= 2^24, 16 * kv_heads * d * 2 < 2^31; tokens * heads and
+ * tokens * kv_heads up to (2^31 - 1) / 3.  kvp_attend counts units of 32 rows that its segments (KV heads of a sequence, a tile
+ * of 16, 32 or 128 query rows each) may see in 32 bits: (tokens * (heads / kv_heads) / tile + n_seq) * kv_heads * (rows / 32 + 12) < 2^31,
+ * rows = columns * page, or window + tokens if that is less.  (1024 sequences of 8 KV heads: 2^22 rows; one sequence of
+ * 8 KV heads, 8 heads on each, 131072 tokens: 2^19.)  Columns that no sequence has reached can be left out: the table may be the first
+ * columns of a wider one.
+ * Errors: as for qk_norm_rope; CAP_E_UNSUPPORTED where sizes are above these. */
 #define KVP_MAX_SEQ 1024
 
 typedef struct kvp_cache {

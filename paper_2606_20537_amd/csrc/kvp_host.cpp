@@ -206,11 +206,12 @@ int plan_attend(const kvp_attend_args* a, cap::KvpAttendParams* p, Span (&cache)
     const kvp_cache& c = *a->cache;
     if (a->heads < 1 || a->heads % c.kv_heads != 0 || a->window < 0) return CAP_E_INVAL;
     const int64_t capacity = (int64_t)c.columns * c.page, rows = a->tokens * (a->heads / c.kv_heads);
-    // segments at most, and units of all of them, which the kernel counts in 32 bits
     const int64_t seen = a->window > 0 ? std::min(capacity, a->window + a->tokens) : capacity;  // rows of a segment at most
     p->whole = seen <= whole_rows(c.d, (int64_t)c.n_seq * c.kv_heads);
     p->tile = tile_of(c, rows, seen);
-    const int64_t segments = (rows / p->tile + c.n_seq) * c.kv_heads, begin = begin_of(c.d), units = (capacity + cap::kKvpUnit - 1) / cap::kKvpUnit + begin;
+    // segments at most, and units of all of them (a window's rows may begin and end inside one), which the kernel counts in 32 bits
+    const int64_t segments = (rows / p->tile + c.n_seq) * c.kv_heads, begin = begin_of(c.d);
+    const int64_t units = std::min((capacity + cap::kKvpUnit - 1) / cap::kKvpUnit, seen / cap::kKvpUnit + 2) + begin;
     if (segments > 0x7fffffff / units) return CAP_E_UNSUPPORTED;
     p->tokens = a->tokens;
     p->heads = a->heads;

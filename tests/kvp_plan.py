@@ -22,7 +22,7 @@ def plan(d, Hkv, G, page, columns, n, T, window=0):
         return segments >= places(d, tile) or segments * (seen // UNIT) >= units * places(d, tile)
 
     tile = 128 if rows > {64: 96, 128: 64, 256: 32}[d] * n_seq and fills(128, 6) else 32 if rows > 16 * n_seq and fills(32, 8) else 16
-    units = -(-capacity // UNIT) + BEGIN[d]
+    units = min(-(-capacity // UNIT), seen // UNIT + 2) + BEGIN[d]
     most = (rows // tile + n_seq) * Hkv * (1 if whole else units)
     wgs = min(most, places(d, tile))
     if whole:

@@ -115,3 +115,25 @@ def test_weights_keep_24_bits(G, columns, tile):
     q, o, _ = s.attend(G, scale=1.0, q=q.bfloat16())
     want = np.tanh(host(q)[..., :1] / 2)
     assert (np.abs(host(o) - want) <= 12 * 2.0 ** -24 + 2.0 ** -8 * want).all()
+
+
+@pytest.mark.parametrize("n", [90, (1 << 24) - 5, 1 << 24])
+def test_a_window_over_the_widest_table(n):
+    # 1024 sequences of 8 KV heads and 2^24 rows: a window's units are few, however many the table has
+    n_seq, Hkv, d, page, window = 1024, 8, 64, 1 << 14, 100
+    gen = torch.Generator("cuda").manual_seed(3)
+    k, v = (torch.randn((3, page, Hkv, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    table = torch.full((n_seq, 1024), -1, dtype=torch.int32, device="cuda")
+    at = torch.arange(n_seq, device="cuda") % 3
+    table[:, (n - 1) // page] = at.int()  # (the window lies on one page)
+    cache = cap.kvp_cache(k, v, table)
+    q = torch.randn((n_seq, Hkv, d), generator=gen, device="cuda").bfloat16()
+    o, lse = torch.empty_like(q), torch.empty((n_seq, Hkv), device="cuda")
+    lens = torch.full((n_seq,), n, dtype=torch.int32, device="cuda")
+    cap.kvp_attend(cache, lens, q, o, scale=0.125, window=window, lse=lse)
+    rows = np.arange(max(0, n - window), n) % page
+    kh, vh, qh, oh, lh = host(k), host(v), host(q), host(o), host(lse)
+    for i in (0, 1, 500, 1023):
+        for h in range(Hkv):
+            want = plain.attend(qh[i, h], kh[i % 3, :, h], vh[i % 3, :, h], 0.125, rows)
+            assert plain.attend_near(oh[i, h], lh[i, h], want, len(rows)), (i, h)

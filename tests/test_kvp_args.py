@@ -185,6 +185,18 @@ def test_workspace():
                     assert all(sizes(c, tokens=n, window=w) <= sizes(c, tokens=n) for w in (1, 100, 1000, 1 << 20))
 
 
+def test_largest_sizes():
+    # units that segments may see: below 2^31, by the table's width, or a window's
+    wide = lambda columns: cache(n_seq=1024, kv_heads=8, d=64, columns=columns)
+    assert sizes(wide(1 << 16), tokens=1024) > 0 == sizes(wide(1 << 18), tokens=1024)
+    assert sizes(wide(1 << 18), tokens=1024, window=4000) > 0
+    one = lambda columns: cache(n_seq=1, kv_heads=8, columns=columns)
+    assert sizes(one(1 << 13), tokens=131072, heads=64) > 0 == sizes(one(1 << 15), tokens=131072, heads=64)
+    most = (2 ** 31 - 1) // 3 // 8
+    assert sizes(tokens=most) > 0 == sizes(tokens=most + 1)
+    assert call("kvp_append", tokens=most + 1) == UNSUP
+
+
 def test_frequencies():
     f = cap.qk_freqs(1e6, 64)
     assert f.shape == (1, 32) and f.dtype == torch.float64
