@@ -810,7 +810,8 @@ CAP_API int kvp_append(const kvp_append_args* args, void* stream);
  * Precision: products and sums are fp32, weights enter the second product with 24 bits (three bf16), or in
  * tiles of 128 rows (below) with 16, o is rounded once.  Weights below 2^-90 of the largest may count as none.  Means of finite
  * values are finite, and small values keep their bits beside large ones (where sums pass fp32's range, or
- * V has infinities or NaN, that part of the call is computed twice).  A score above fp32's range gives NaN, one below it counts as none.
+ * V has infinities or NaN, that part of the call is computed twice).  A score above fp32's range gives NaN, one below it counts as
+ * none; so do products q . k beyond that range, whatever the scale.
  * Made for one token or a few drafts of each sequence, in tiles of 16 or 32 query rows (tokens x
  * heads / kv_heads), and for runs of tokens, in tiles of 128.
  * Two launches; one where columns * page, or the window and the tokens, are a few hundred rows

@@ -137,3 +137,26 @@ def test_a_window_over_the_widest_table(n):
         for h in range(Hkv):
             want = plain.attend(qh[i, h], kh[i % 3, :, h], vh[i % 3, :, h], 0.125, rows)
             assert plain.attend_near(oh[i, h], lh[i, h], want, len(rows)), (i, h)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("scale", [2.0 ** -130, -2.0 ** -130])
+def test_products_beyond_fp32(call, scale):
+    # q . k of row 2 is +-2^140, which the small scale comes after: above the range the row is NaN, below it row 2 counts as none
+    s, G = step(call, 64, 8)
+    page = int(s.table[0, 0])
+    s.k[page, 2] = 0
+    s.k[page, 2, :, 0] = 2.0 ** 70
+    q = s.normal(s.tokens, s.Hkv * G, 64)
+    for sign in (1.0, -1.0):
+        q[:, :, 0] = sign * 2.0 ** 70
+        _, o, lse = s.attend(G, q=q, scale=scale)
+        first = s.T[0]
+        if sign * scale > 0:
+            assert o[:first].isnan().all() and lse[:first].isnan().all()
+        else:
+            assert o[:first].isfinite().all() and lse[:first].isfinite().all()
+            n, T = s.n[0], s.T[0]
+            v = s.rows(0, s.v)[:, 0]
+            want = np.delete(v, 2, 0)[:n - 1].mean(0)  # the last token sees all other rows alike
+            assert np.abs(host(o)[T - 1, 0] - want).max() <= 2.0 ** -7 * np.abs(v).max()
