@@ -889,8 +889,9 @@ def kvp_cache(k_pages, v_pages, table):
     program goes on writing the table in place; the handle is made once."""
     _, bf16, _, i32 = _kvb_torch()
     for x in (k_pages, v_pages):
-        if x.ndim != 4 or x.dtype != bf16 or x.shape != k_pages.shape or x.stride()[1:] != (x.shape[2] * x.shape[3], x.shape[3], 1) \
-                or x.stride(0) != k_pages.stride(0) or (x.shape[0] > 1 and x.stride(0) < x.shape[1] * x.shape[2] * x.shape[3]):
+        # (a dimension of one has no stride; pools of one page need not be alike)
+        if x.ndim != 4 or x.dtype != bf16 or x.shape != k_pages.shape or (x.shape[0] > 0 and not x[0].is_contiguous()) \
+                or (x.shape[0] > 1 and (x.stride(0) != k_pages.stride(0) or x.stride(0) < x.shape[1] * x.shape[2] * x.shape[3])):
             raise ValueError("kvp_cache: k_pages and v_pages are bfloat16 tensors [pages, page, kv_heads, d] whose pages are contiguous")
     if table.ndim != 2 or table.dtype != i32 or (table.shape[1] > 1 and table.stride(1) != 1) or (table.shape[0] > 1 and table.stride(0) < table.shape[1]):
         raise ValueError("kvp_cache: table is an int32 tensor [n_seq, columns] whose rows are contiguous")

@@ -160,3 +160,20 @@ def test_products_beyond_fp32(call, scale):
             v = s.rows(0, s.v)[:, 0]
             want = np.delete(v, 2, 0)[:n - 1].mean(0)  # the last token sees all other rows alike
             assert np.abs(host(o)[T - 1, 0] - want).max() <= 2.0 ** -7 * np.abs(v).max()
+
+
+def test_pools_with_dimensions_of_one():
+    s = Step([90, 7], [1, 1], 1, 64, 16, seed=9)
+    q, o, lse = s.attend(4)
+    k = s.k.transpose(1, 2).contiguous().transpose(1, 2)  # [pages, head, rows, channels] of one head
+    o2 = torch.empty_like(o)
+    cap.kvp_attend(cap.kvp_cache(k, s.v, s.dev_table), s.lens, q, o2, scale=0.125, tok0=s.tok0)
+    assert torch.equal(o, o2)
+    both = torch.stack([s.k[:1], s.k[1:2], s.v[:1]], 1)  # one page, apart from others
+    table = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    lens = torch.tensor([5], dtype=torch.int32, device="cuda")
+    both[:, :, :5] = s.normal(1, 3, 5, 1, 64)
+    o3, o4 = torch.empty_like(o[:1]), torch.empty_like(o[:1])
+    cap.kvp_attend(cap.kvp_cache(both[:, 0], both[:, 2].clone(), table), lens, q[:1], o3, scale=0.125)
+    cap.kvp_attend(cap.kvp_cache(both[:, 0].clone(), both[:, 2].clone(), table), lens, q[:1], o4, scale=0.125)
+    assert torch.equal(o3, o4) and o3.isfinite().all()

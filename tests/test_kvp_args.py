@@ -214,6 +214,16 @@ def test_frequencies():
             cap.qk_freqs(**kw)
 
 
+def test_dimensions_of_one_have_no_stride():
+    # pages [kv_heads, page, d] of one head, and pools of one page out of different tensors, are refused only for not being on a GPU
+    table = torch.zeros(1, 2, dtype=torch.int32)
+    heads_first = torch.zeros(3, 1, 16, 64, dtype=torch.bfloat16).transpose(1, 2)
+    one, other = torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)[:1], torch.zeros(2, 3, 16, 2, 64, dtype=torch.bfloat16)[:1, 1]
+    for k, v in ((heads_first, heads_first), (heads_first, torch.zeros(3, 16, 1, 64, dtype=torch.bfloat16)), (one, other)):
+        with pytest.raises(ValueError, match="on one GPU"):
+            cap.kvp_cache(k, v, table)
+
+
 def test_binding_refuses():
     bf16, i32 = torch.bfloat16, torch.int32
     with pytest.raises(ValueError, match="on one GPU"):
