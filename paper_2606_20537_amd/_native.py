@@ -813,7 +813,7 @@ def _qk_ints(fn, name, x, shape):
 
 
 def _qk_pos(fn, rule, pos, tokens):
-    if pos is None:
+    if pos is None or rule.rot == 0:  # (without a rotation no positions are read)
         return 0
     shape, axes = pos.shape, rule.axes
     if (shape != (tokens, axes) and (axes != 1 or shape != (tokens,))) or pos.dtype != _torch[3] or not pos.is_contiguous():
@@ -830,7 +830,7 @@ def _qk_rule(fn, rule, d, device):
 
 def qk_norm_rope(rule, q, k, q_out=None, k_out=None, *, pos=None, stream=None):
     """Norm and rotation of q [tokens, heads, d] and k [tokens, kv_heads, d] (either may be None), to q_out and
-    k_out (None: in place).  pos: int32 [tokens, axes]."""
+    k_out (None: in place).  pos: int32 [tokens, axes]; a rule without a rotation does not look at it."""
     fn = "qk_norm_rope"
     _, bf16, f32, _ = _torch or _kvb_torch()
     like = q if q is not None else k

@@ -70,6 +70,22 @@ def test_rows_appended_without_a_rule_keep_their_bits(d):
     assert torch.equal(bits(pools[0].flatten(0, 1)), bits(k)) and torch.equal(bits(pools[1].flatten(0, 1)), bits(v))
 
 
+def test_positions_beside_a_rule_without_rotation():
+    # a layer that only norms, called as those that rotate
+    x = patterns(torch.bfloat16, (5, 3, 64)).nan_to_num(1.0, 1.0, 1.0)
+    rule, pos = cap.qk_rule(eps=1e-6), torch.arange(5, dtype=torch.int32, device="cuda")
+    want, got = torch.empty_like(x), torch.empty_like(x)
+    cap.qk_norm_rope(rule, x, None, want)
+    for p in (pos, pos[:, None], pos[:, None].repeat(1, 3)):
+        cap.qk_norm_rope(rule, x, None, got.zero_(), pos=p)
+        assert torch.equal(got, want)
+    pools = torch.zeros((2, 1, 16, 3, 64), dtype=torch.bfloat16, device="cuda")
+    cache = cap.kvp_cache(pools[0], pools[1], torch.zeros((1, 1), dtype=torch.int32, device="cuda"))
+    lens, tok0 = (torch.tensor(i, dtype=torch.int32, device="cuda") for i in ([5], [0, 5]))
+    cap.kvp_append(cache, lens, x, x, tok0=tok0, rule=rule, pos=pos)
+    assert torch.equal(pools[0, 0, :5], want) and torch.equal(pools[1, 0, :5], x)
+
+
 @pytest.mark.parametrize("tokens", [1, 37])
 def test_heads_of_q_k_and_v_in_turn(tokens):
     # a projection [tokens, heads, (q, k, v), d] in place
