@@ -775,6 +775,10 @@ _pack_attend = struct.Struct("<QQQ" + "Qqq" + "QQQQqiifi").pack
 _NO_ROWS = (0, 0, 0)
 
 
+_UNPACKED = struct.error, OverflowError  # numbers that a caller gives, not tensors' own
+_NO_FIELD = "kvp_attend: tokens, heads, window or scale is not a number that its field holds"
+
+
 def _qk_shape(fn, name, x):
     shape = x.shape
     if len(shape) != 3:
@@ -941,7 +945,10 @@ def kvp_append(cache, lens, k, v, *, tok0=None, rule=None, q=None, q_out=None, p
 
 def kvp_attend_workspace_bytes(cache, tokens, heads, window=0):
     """Bytes of workspace kvp_attend needs for this many packed tokens and query heads."""
-    a = _pack_attend(cache.address, 0, 0, 0, 0, 0, 0, 0, 0, 0, tokens, heads, window, 0.0, 0)
+    try:
+        a = _pack_attend(cache.address, 0, 0, 0, 0, 0, 0, 0, 0, 0, tokens, heads, window, 0.0, 0)
+    except _UNPACKED:
+        raise ValueError(_NO_FIELD) from None
     return int(load().kvp_attend_workspace_bytes(a))
 
 
@@ -967,5 +974,8 @@ def kvp_attend(cache, lens, q, o, *, scale, tok0=None, window=0, lse=None, works
     elif not workspace.is_contiguous():  # its elements are not the bytes behind its address
         raise ValueError("kvp_attend: the workspace is a contiguous tensor")
     space, size = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
-    a = _pack_attend(cache.address, at, first, *of_q, to, of_lse, space, size, tokens, heads, window, scale, 0)
+    try:
+        a = _pack_attend(cache.address, at, first, *of_q, to, of_lse, space, size, tokens, heads, window, scale, 0)
+    except _UNPACKED:
+        raise ValueError(_NO_FIELD) from None
     return _check(fn, lib.kvp_attend(a, handle))

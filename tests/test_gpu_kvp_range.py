@@ -177,3 +177,12 @@ def test_pools_with_dimensions_of_one():
     cap.kvp_attend(cap.kvp_cache(both[:, 0], both[:, 2].clone(), table), lens, q[:1], o3, scale=0.125)
     cap.kvp_attend(cap.kvp_cache(both[:, 0].clone(), both[:, 2].clone(), table), lens, q[:1], o4, scale=0.125)
     assert torch.equal(o3, o4) and o3.isfinite().all()
+
+
+def test_a_scale_that_no_field_holds():
+    s = Step([30], [1], 1, 64, 16)
+    for scale in (1e39, -1e39, "1"):
+        with pytest.raises(ValueError, match="scale"):
+            s.attend(2, scale=scale)
+    with pytest.raises(cap.CapsuleError):
+        s.attend(2, scale=INF)

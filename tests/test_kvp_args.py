@@ -214,6 +214,15 @@ def test_frequencies():
             cap.qk_freqs(**kw)
 
 
+def test_numbers_that_no_field_holds():
+    held = cache()
+    handle = N.KvpCache(held, (), torch.zeros(1))
+    for tokens, heads, window in ((7, 8, 1 << 31), (7, 1 << 31, 0), (1 << 63, 8, 0), (7, 8, 1.5), (7, 8, None)):
+        with pytest.raises(ValueError, match="kvp_attend: .*window"):
+            cap.kvp_attend_workspace_bytes(handle, tokens, heads, window)
+    assert cap.kvp_attend_workspace_bytes(handle, 7, 8, (1 << 31) - 1) > 0
+
+
 def test_dimensions_of_one_have_no_stride():
     # pages [kv_heads, page, d] of one head, and pools of one page out of different tensors, are refused only for not being on a GPU
     table = torch.zeros(1, 2, dtype=torch.int32)
