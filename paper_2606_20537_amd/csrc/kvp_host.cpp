@@ -98,12 +98,17 @@ void enter_sizes(int64_t tokens, int32_t heads, int32_t kv_heads, int64_t rows, 
 }
 
 // Tokens of a workgroup: one lot of sines serves all heads of a token, so a workgroup has whole tokens, up to five rounds
-// of its 256 threads, and there are two workgroups for each place on the chip.  Measured (us): 16384 tokens
-// x 36 heads of 256, 1, 2, 4 and 8 tokens 125, 123, 126 and 137; 4159 x 20 of 128 14.8, 13.9, 12.9 and 14.2.
+// of its 256 threads, and more of them as long as half of the places on the chip (six workgroups to a CU, 1536) have one.
+// Measured (us; 1, 2, 4 and 8 tokens), 9 heads of 256: 1500 tokens 6.1, 6.1, 6.9 and 8.5; 2000 7.4, 6.5, 7.0 and 8.5; 3000 9.0, 7.5, 7.5 and
+// 9.2; 4000 10.8, 9.2, 8.1 and 9.3; 6000 15.5, 12.4, 10.4 and 11.1; 8000 21.7, 18.2, 16.4 and 15.1.  40 heads of 128: 1500 7.6, 7.8, 9.6
+// and 14; 2000 9.3, 8.5, 9.6 and 16; 3000 12.9, 11.7, 12.3 and 17; 4000 19.3, 17.4, 16.0 and 18.  36 heads of 256, 16384 tokens: 111, 105, 109
+// and 125.  (Over 99 calls of 1000 to 16384 tokens 2.6 % behind the best of the four in the mean; for 1024 workgroups in place
+// of 768 4.9 %.)
+constexpr int64_t kHalfOfPlaces = 768;
 int32_t tokens_of_wg(int64_t tokens, int64_t rows, int32_t d) {
     int64_t n = 1, lanes = 1;
     while (lanes < d / 16) lanes *= 2;
-    while (n < cap::kQkTokens && 2 * n * rows * lanes <= 1280 && 2 * n * 1024 <= tokens) n *= 2;
+    while (n < cap::kQkTokens && 2 * n * rows * lanes <= 1280 && 2 * n * kHalfOfPlaces <= tokens) n *= 2;
     return (int32_t)n;
 }
 
