@@ -814,9 +814,13 @@ CAP_API int kvp_append(const kvp_append_args* args, void* stream);
  * none; so do products q . k beyond that range, whatever the scale.
  * Made for one token or a few drafts of each sequence, in tiles of 16 or 32 query rows (tokens x
  * heads / kv_heads), and for runs of tokens, in tiles of 128.
- * Two launches; one where columns * page, or the window and the tokens, are a few hundred rows
- * (those that need no workspace).  Results are reproducible for the same arguments and device data;
- * a row's last bits depend on the other sequences of the call, over which work is dealt out evenly. */
+ * Two launches; one where columns * page, or the window and the tokens, are up to 256 rows of 256 channels, 512 of 128 or 768 of
+ * 64, or up to 1024 where n_seq * kv_heads is 65536 / d or more (these calls need no workspace).  As lengths are on the device, launches
+ * and tiles go by what the table has room for: short sequences behind a table for long ones take up to 3 us more, and six
+ * drafts of each up to half as much again, which a handle over the table's first columns saves.
+ * Results are reproducible for the same arguments and device data;
+ * a row's last bits depend on the other tokens and sequences of the call and on the table's width, by which work is dealt out; so the rows
+ * of a prompt in one call and in two differ in them. */
 typedef struct kvp_attend_args {
     const kvp_cache* cache;      /* HOST */
     const int32_t*   lens;

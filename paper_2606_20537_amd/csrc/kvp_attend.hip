@@ -9,7 +9,7 @@
 // columns of the matrix instructions, keys and channels the rows.
 //  * S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 tiles, sums in fp32.
 //  * P goes in as three bf16 values, in which the weights keep fp32's 24 bits: memory
-//    bounds the call, and the matrix pipes are 6 % busy with two.  In tiles of 128 rows, which arithmetic
+//    bounds the call, and the matrix pipes are 9 % busy.  In tiles of 128 rows, which arithmetic
 //    bounds, they are two, and the weights keep 2^-16, so that the output's own rounding stays the largest: 16384 tokens, 32 heads on 4
 //    of 64, 128 and 256 channels 2.43, 3.62 and 7.93 ms, with three 3.05, 4.46 and 9.30.
 // Both products leave a lane with one query row (lane % 16), so maximum, sum and
@@ -34,11 +34,11 @@
 // Long runs of tokens (prompts, resumed turns) have tiles of 128 query rows, where arithmetic counts: each wave
 // has its own rows and all of the units, which the waves load together into a ring of four, with
 // a barrier to each, so that K and V come from memory once for 128 rows and not for 32.  16384 tokens behind none, 32 heads on 4 of
-// 64, 128 and 256 channels: 2.4, 3.7 and 8.0 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.7): 0.67 to 0.89 PFLOP/s
+// 64, 128 and 256 channels: 2.4, 3.6 and 8.0 ms (floor 0.9, 1.8, 3.6; in tiles of 32 rows 5.8, 11.3, 26.1): 0.67 to 0.91 PFLOP/s
 // of matrix instructions with both parts of P, and between them the weights' exponentials.  Loads are kept by the caches here, as other tiles read the same.
 //
 // What bounds it, one token, 8 query heads on each KV head of 256 channels: 131072 + 16449 + 2111 + 1 rows
-// x 4 heads, 613 MB, 99 us + 5 of the join (6.2 TB/s); 16385 rows x 4, 67 MB, 17 + 4, of which the data take
+// x 4 heads, 613 MB, 100 us + 5 of the join (6.1 TB/s); 16385 rows x 4, 67 MB, 18 + 4, of which the data take
 // 10, the way to the first load 4 (lengths, table and 400 instructions behind each other) and the last sums 2.
 #include <hip/hip_runtime.h>
 
@@ -61,7 +61,7 @@ constexpr int kThreads = 256;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
 // m may stay up to kBehind below the highest score so far (log2 units), as a new m has all rows' sums multiplied, and comes
-// seldom so: 512 tokens of 16 sequences, 16 heads on 4 of 64 and 256 channels 211 and 554 us with every new one, 194 and 528 so.
+// seldom so: 512 tokens of 16 sequences, 16 heads on 4 of 64 and 256 channels 209 and 556 us with every new one, 193 and 512 so.
 // Sums of large values may leave fp32's range where their mean does not.  Such segments are taken a second time, with weights
 // of 2^-kAbove of what exp(x - m) gives, 2^-24 at most, so that sums of 2^24 values, the most that a sequence has, stay finite; and only
 // means that were not finite are replaced, as small values in other channels would lose bits to such weights.
@@ -341,8 +341,8 @@ __device__ inline Units units_of_tile(const KvpAttendParams& p, int n, int T, in
 // What a KV head's tiles of TILE rows count for where runs are dealt out.  Later tiles see more: the first and the last of
 // all (of an odd number: of all but the last), the second and the last but one, .. are pairs, of which none has more
 // units than `pair`: tiles j and k, j + k = c, see 2 (n - T) + (TILE (c + 2) - 2) / group rows at most in all; with a window each sees
-// that and what its own rows are apart.  (Every tile counted as the last, first and last in turn: 2048 tokens, 16 heads on 4 of 64, 128 and 256
-// channels 69, 96 and 154 us, now 57, 70 and 111; 8192 of 64 522, now 417.)
+// that and what its own rows are apart.  (2048 tokens, 16 heads on 4 of 64, 128 and 256 channels, every tile counted as the last, first and last in
+// turn: 69, 96 and 154 us; so 57, 70 and 111, when other parts took longer than now.)
 template <int TILE>
 __device__ inline void add_weights(const KvpAttendParams& p, Seq& q) {
     const int pairs = q.tiles / 2, capacity = p.pages.capacity;
@@ -564,7 +564,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             return (int64_t)((uint64_t)lane_u32((uint32_t)(x >> 32), i) << 32 | lane_u32((uint32_t)x, i));
         };
 
-        // the query rows, while the table is on its way
+        // the query rows, before the table is asked
         bf16x8 qf[NT][NJ];
         #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -735,7 +735,7 @@ __global__ __launch_bounds__(64 * waves_of(NT, WIDE), simd_waves(D, NT, WIDE)) v
             return (there >> (e / 4) & 1) && key <= last && key > first;
         };
         // (all: every row sees all of the unit.  Products of their own for it had the compiler keep the sums in two places: 32 to 45
-        // registers more, and 16384 tokens of 128 and 256 channels 3.89 and 8.33 ms, now 3.72 and 8.01.)
+        // registers more, and 16384 tokens of 128 and 256 channels 3.89 and 8.33 ms, so 3.72 and 8.01.)
         auto add_values = [&](bool all, int r, int there, const int64_t (&at)[2], const bf16x8 (&w)[kParts][NT]) {
             uint32_t keep[4] = {};  // bits of keys 2i and 2i + 1
             if (!all) {
@@ -1129,8 +1129,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const KvpAttendParams p)
     }
 }
 
-// Workgroups of the join at most with 16 threads to a part: 192 tokens x 16 heads of 128 channels, two parts each, took 8.1 us
-// so and 5.2 with four rows to a workgroup; 32 rows of 57 parts 4.0 and 7.8.
+// Workgroups of the join at most with 16 threads to a part: 192 tokens x 16 heads of 128 channels, two parts each, took 32.6 us
+// so (the whole call) and 30.1 with four rows to a workgroup; 32 rows of 57 parts of 256 channels 21.2 and 31.7.
 constexpr uint64_t kFewRows = 1024;
 
 // Of 256 channels the sums of 16 rows to a wave leave registers for two waves on a SIMD.

@@ -172,29 +172,32 @@ int check_apart(const Span* out, const Span* const* own, int n_out, const Span* 
 int64_t wgs_of(int32_t d, int32_t tile) { return d == 64 && tile > 16 ? 768 : 65536 / d; }
 
 // Units that the beginning of a segment counts for: 4 to 6 us of lookups, first loads and sums, which are more units where
-// these are short.  Measured (us, for 2, 4, 6 and 8 units of 256 channels): 35 sequences of up to 29300 rows, 401 MB,
-// 104, 75, 77 and 76; 50 of up to 12217 rows, six tokens and 8 KV heads, 372, 263, 211 and 191.
+// these are short.  Measured (us, for 2, 4, 6, 8 and 10 units): 35 sequences of 29300^(i / 34) rows x 4 KV heads, 256 channels 142, 97,
+// 86, 85 and 85, 128 channels 65, 53, 50, 50 and 50; 50 of 12200^(i / 49) rows, six tokens, 8 KV heads, 256 channels 260, 177, 154, 159
+// and 162, 128 channels 218, 154, 131, 125 and 125, 64 channels 122, 87, 75, 73 and 70.
 int64_t begin_of(int32_t d) { return d == 256 ? 6 : d == 128 ? 8 : 10; }
 
 // Rows that a segment may have where no segment is cut, which spares the second launch: few, or more where there are
-// segments for every workgroup.  Measured (us, whole / cut; sequences x KV heads): 450 rows, 1 x 4 of 64 channels
-// 8.5 / 10.2, of 128 10.1 / 10.5, of 256 16.9 / 13.6; 700 rows, 1 x 4 of 64 9.6 / 10.2, of 128 12.4 / 10.5; 1000 rows of 256, 1 x 4
-// 26 / 14, 64 x 4 45 / 48.
+// segments for every workgroup.  Lengths are on the device: these are the rows that the table has room for.  Measured (us, whole / cut;
+// sequences x KV heads): 1 x 4 of 64 channels, 450 rows 8.2 / 9.2, 700 9.8 / 9.7, 800 10.1 / 9.5; of 128, 450 rows 10.0 / 9.9, 600 11.1 / 10.2, 700
+// 12.1 / 10.2; of 256, 240 rows 12.0 / 13.0, 450 15.9 / 12.8; 1000 rows, 64 x 4 of 256 45 / 48, 128 x 4 of 128 43 / 47, 256 x 4 of 64 47 / 52.
 int64_t whole_rows(int32_t d, int64_t segments) { return segments >= wgs_of(d, 16) ? 1024 : d == 256 ? 256 : d == 128 ? 512 : 768; }
 
 // Query rows of a segment.  16; 32 where sequences have more than 16 of a KV head on average, and 128 where they have more than
 // two tiles of 32 or so, if that leaves every workgroup a segment or some units (else more segments are worth more
 // than what they read again).  Measured (us, 16 / 32 / 128; sequences of so many rows x tokens, 32 heads on 4, for 64, 128 and 256 channels):
-//   8 of 16384 x 4    54 / 33 / 41    70 / 64 / 68      172 / 108 / 120
-//   32 of 2048 x 5    41 / 33 / 34    78 / 48 / 55      138 / 97 / 74
-//   32 of 2048 x 9    64 / 37 / 42    120 / 86 / 60     226 / 153 / 94
-//   32 of 2048 x 16   65 / 63 / 45    144 / 82 / 64     358 / 200 / 101
-//   1 of 16384 x 9    18 / 18 / 21    29 / 24 / 28      66 / 46 / 51
-//   8 of 300 x 6, G 16  8.5 / 10 / 18   12 / 14 / 23      20 / 24 / 26
-//   4 of 4000 x 16    21 / 20 / 27    49 / 31 / 33      72 / 61 / 44
-//   1 of 16384 x 161  - / 101 / 78    - / 217 / 109     - / 446 / 211
-// and prompts of 16 heads on 4: 1 x 512 9.5 / 11 / 25, 18 / 19 / 27, 40 / 31 / 37; 16 x 512 121 / 74 / 48, 310 / 201 / 98, 672 / 452 / 163;
-// 64 of 100 rows x 32 16 / 18 / 15, 32 / 25 / 21, 87 / 65 / 28.
+//   8 of 16384 x 4    54 / 34 / 38    72 / 63 / 61      170 / 103 / 120
+//   32 of 2048 x 5    42 / 34 / 31    79 / 49 / 49      135 / 94 / 75
+//   32 of 2048 x 9    66 / 39 / 37    121 / 87 / 52     219 / 147 / 88
+//   32 of 2048 x 16   65 / 64 / 42    140 / 82 / 58     357 / 197 / 94
+//   1 of 16384 x 9    19 / 19 / 20    30 / 25 / 27      64 / 42 / 44
+//   8 of 300 x 6, G 16  8.1 / 11 / 17   11 / 14 / 22      18 / 24 / 25
+//   4 of 4000 x 16    22 / 22 / 23    49 / 32 / 30      72 / 59 / 41
+//   1 of 16384 x 161  136 / 102 / 70  398 / 220 / 100   809 / 437 / 195
+// and prompts of 16 heads on 4: 1 x 512 9.8 / 11 / 29, 14 / 15 / 37, 39 / 29 / 37; 16 x 512 121 / 77 / 43, 261 / 155 / 56, 677 / 438 / 157;
+// 64 of 100 rows x 32 16 / 18 / 15, 34 / 26 / 21, 93 / 68 / 27.  The rule takes the best of the three or one within 5 %, but for 64 of 100 x 32 of 64 and 128
+// channels (32, 26 % behind), 32 of 2048 x 5 of 64 (32, 9 %) and 1 x 512 of 128 (32, 8 %).  What it does not know is the rows held: with a
+// table for 16384 rows 8 of 300 x 6 take 14, 18 and 25 us.
 int32_t tile_of(const kvp_cache& c, int64_t rows, int64_t seen) {
     auto fills = [&](int64_t tile, int64_t units) {
         const int64_t segments = std::max<int64_t>(c.n_seq, rows / tile) * c.kv_heads, wgs = wgs_of(c.d, (int32_t)tile);

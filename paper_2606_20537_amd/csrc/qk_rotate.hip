@@ -16,8 +16,8 @@
 // An append has the rows of v besides (copied), and k and v go to the row of the page
 // that the table names; sequence, length and page of a token are found while its first rows are on their way.
 //
-// Bound by memory: 16384 tokens x 36 heads of 256 channels, 604 MB read and written, 113 us (5.3 TB/s, a
-// copy of 1 GiB 5.2; without the arithmetic 111); the append of 40 heads, 671 MB, 127 us.  Stores are streamed
+// Bound by memory: 16384 tokens x 36 heads of 256 channels, 604 MB read and written, 114 us (5.3 TB/s, a
+// copy of 1 GiB 5.2; without the arithmetic 111), in fp32, 1208 MB, 240 (5.0); the append of 40 heads, 671 MB, 127 us.  Stores are streamed
 // (cached ones 123 us; 43 MB, which the last cache holds, 14 us against 11).  One row ahead of the one in work is
 // on its way; with two the registers spill (132 us).
 #include <hip/hip_runtime.h>
