@@ -837,7 +837,7 @@ typedef struct kvp_attend_args {
     int32_t          reserved;   /* 0 */
 } kvp_attend_args;
 
-/* Workspace of a call with these sizes (the cache's, tokens, heads and window; that of window 0 does for
+/* Workspace of a call with these sizes (the cache's, tokens, heads and window; that of window 0, where it is not refused, does for
  * any; 70 MB at most and 8 bytes for each query row); 0 where the call needs none or is refused.
  * It holds nothing between calls; calls that may overlap need their own. */
 CAP_API uint64_t kvp_attend_workspace_bytes(const kvp_attend_args* args);

@@ -84,6 +84,23 @@ def test_small_values_beside_large_ones(call, d):
 
 @pytest.mark.parametrize("call", list(CALLS))
 @pytest.mark.parametrize("d", [64, 128, 256])
+def test_large_values_of_both_signs(call, d):
+    # sums that pass the range upwards and downwards (NaN, not an infinity), and scores that grow by the row, so that weights stand above 1 for a while
+    s, G = step(call, d, 7)
+    s.v.copy_(((1 - 0.3 * s.v.float().clamp(-1, 1).abs()) * 3.3e38 * s.v.float().sign()).bfloat16())
+    for i, n in enumerate(s.n):
+        r = torch.arange(min(n, s.table.shape[1] * s.page))
+        at = s.table[i, r // s.page].long().cuda(), (r % s.page).cuda()
+        s.k[at[0], at[1], :, 0] = (0.01 * r.cuda()).bfloat16()[:, None]
+    q = s.normal(s.tokens, s.Hkv * G, d)
+    q[:, :, 0] = 1.0
+    q, o, lse = s.attend(G, scale=0.5, q=q)
+    assert o[:sum(s.T)].isfinite().all() and lse[:sum(s.T)].isfinite().all()
+    check(s, q, o, G, 0.5)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("d", [64, 128, 256])
 def test_infinities_beside_small_values(call, d):
     s, G = step(call, d, 6)
     s.v.copy_((s.v.float().clamp(-2, 2) * 1e-36).bfloat16())

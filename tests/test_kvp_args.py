@@ -154,15 +154,15 @@ def test_overlaps():
 
 
 def test_heads_in_turn_that_overlap():
-    # q and k of a projection [tokens, heads, (q, k, v), d], in place; k begins inside q's heads, or q's inside k's
-    def heads(i, at_channel, token=8 * 384, head=384):
+    # q and k of a projection [tokens, heads, (q, k, v, 16 more), d], in place; k begins inside q's heads, or q's inside k's
+    def heads(i, at_channel, token=8 * 400, head=400):
         return N.qk_rows(at(i) + 2 * at_channel, token, head)
 
-    for first, second in ((0, 120), (0, 272), (136, 16), (128, 8)):
+    for first, second in ((0, 120), (0, 288), (136, 16), (128, 8)):
         q, k = heads(1, first), heads(1, second)
         assert call("qk_norm_rope", q=q, q_out=q, k=k, k_out=k, kv_heads=8) == INVAL, (first, second)
     q = heads(1, 0)
-    assert call("qk_norm_rope", q=q, q_out=q, k=heads(1, 128, 3072, 256), k_out=rows(4)) == INVAL   # other steps
+    assert call("qk_norm_rope", q=q, q_out=q, k=heads(1, 128, 8 * 400, 256), k_out=rows(4)) == INVAL   # other steps
 
 
 def sizes(c=None, **kw):
